@@ -19,3 +19,14 @@ def sage_attention(Q, K, V, causal: bool = True, k_smooth: bool = True, q_smooth
     (Algorithm 2 takes them as inputs); costs that workspace's memory between the two calls."""
     O, L = binding._host().attention(Q, K, V, causal, k_smooth, q_smooth, sm_scale, token_major, share_quantized)
     return (O, L) if return_lse else O
+
+
+def sage_rotary(Q, K, positions, inv_freq, sections=None, adjacent: bool = False, token_major: bool = True, inverse: bool = False):
+    """Q and K (or Q alone, K = None) turned by their tokens' positions, differentiable in both.
+
+    Q, K: bf16 [tokens, heads, d], [B, N, heads, d] or, without `token_major`, [B, heads, N, d]; any strides (those whose rows do not
+    begin on 16 bytes are copied).  inv_freq: float32, one for every pair of channels that turns; the channels behind them pass.
+    sections: how many of the frequencies go by each axis of `positions`, int32 or int64 [axes, tokens] (video: time, height, width);
+    with one axis (the default) [tokens].  [axes, N] serves every batch.  adjacent: channel 2i turns with 2i + 1, else i with
+    i + len(inv_freq).  inverse: by the negative angles.  Returns (Q, K) as new dense tensors."""
+    return binding._host().rotary(Q, K, positions, inv_freq, sections, adjacent, token_major, inverse)

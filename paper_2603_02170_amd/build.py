@@ -4,11 +4,14 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libsagebwd.so")
 HOST = os.path.join(HERE, "_sage_host.so")
+SOURCES = ("sagebwd_api", "serve_api")
 
 
 def hipcc_path() -> str:
@@ -31,19 +34,21 @@ def _run(cmd, verbose: bool) -> None:
 
 
 def build(verbose: bool = True) -> str:
-    """Compile csrc/sagebwd_api.hip (which includes every kernel) into libsagebwd.so, and csrc/torch_host.cpp
+    """Compile csrc/sagebwd_api.hip and csrc/serve_api.hip (which include every kernel) into libsagebwd.so, and csrc/torch_host.cpp
     (host code only: what stands between Python's tensors and that library) into _sage_host.so."""
-    src = os.path.join(HERE, "csrc", "sagebwd_api.hip")
-    cmd = [
-        hipcc_path(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC",
+    common = [
+        hipcc_path(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
         # packed FP32 instructions are kept out of the generated code on purpose
         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
         "-Wno-unused-command-line-argument",
         "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"),
-        src, "-o", LIB,
     ]
-    cmd[1:1] = os.environ.get("SAGEBWD_EXTRA_CFLAGS", "").split()   # e.g. -DNAME for kernel experiments
-    _run(cmd, verbose)
+    common[1:1] = os.environ.get("SAGEBWD_EXTRA_CFLAGS", "").split()   # e.g. -DNAME for kernel experiments
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, name + ".o") for name in SOURCES]
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
+            list(pool.map(lambda s, o: _run(common + ["-c", os.path.join(HERE, "csrc", s + ".hip"), "-o", o], verbose), SOURCES, objects))
+        _run([common[0], "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", LIB], verbose)
     build_host(verbose)
     return LIB
 

@@ -1,0 +1,102 @@
+// Rotary positions of Q and K in one launch (gfx950 only).
+#pragma once
+
+#include "common.h"
+
+namespace sage {
+
+struct RotaryArgs {
+  const __bf16* x[2];       // Q, K
+  __bf16* y[2];
+  int64_t xs[2][3], ys[2][3];   // batch, row, head strides in elements
+  const void* positions;
+  const float* inv_freq;
+  int N, tokens, d, half;   // half = rotary_dim / 2 frequencies
+  int heads[2];
+  int axes, end[4];         // end[a]: first frequency behind axis a
+  int pieces;               // threads a token and group of heads takes: ceil(d / 16)
+  int heads_per_thread, head_groups[2];
+  float sign;
+};
+
+// cos and sin of 2 pi t, |t| <= 1/2, as floats.
+__device__ __forceinline__ void turn_of(double turns, float sign, float& c, float& s) {
+  // (the product position * frequency is exact in float64: 24 and 31 bits; of it only the fraction of a turn counts, good to 1e-10 at
+  // 2^20 turns, which float32 holds to 3e-8)
+  const float t = (float)(turns - __builtin_rint(turns));
+  float sv, cv;
+  sv = sinpif(2.f * t);
+  cv = cospif(2.f * t);
+  c = cv;
+  s = sign * sv;
+}
+
+// A thread has 16 channels of a token (8 frequencies, or 16 channels that are copied) and up to heads_per_thread heads, for which it
+// forms sine and cosine once: y1 = x1 cos - x2 sin, y2 = x2 cos + x1 sin.  The bytes of x and y are what bounds it; the angles cost
+// about 50 instructions a frequency, which several heads share.
+template <bool ADJACENT, typename POS>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
+  const unsigned per_token = a.pieces;
+  const unsigned id = blockIdx.x * 256u + threadIdx.x;
+  const unsigned token = id / per_token, piece = id % per_token;
+  if (token >= (unsigned)a.tokens) return;
+  int group = blockIdx.y;
+  const int which = group >= a.head_groups[0];
+  if (which) group -= a.head_groups[0];
+  const int h0 = group * a.heads_per_thread;
+  const int h1 = min(h0 + a.heads_per_thread, a.heads[which]);
+  const unsigned b = token / (unsigned)a.N, n = token % (unsigned)a.N;
+  const __bf16* x = a.x[which] + b * a.xs[which][0] + n * a.xs[which][1];
+  __bf16* y = a.y[which] + b * a.ys[which][0] + n * a.ys[which][1];
+  const int64_t xh = a.xs[which][2], yh = a.ys[which][2];
+
+  const int f0 = piece * 8;          // first frequency, or (f0 >= half) channels 2 f0 ..  that pass through
+  if (f0 >= a.half) {
+    const int c = 2 * f0;
+    for (int h = h0; h < h1; h++) {
+      const v4i u = *(const v4i*)(x + h * xh + c), w = *(const v4i*)(x + h * xh + c + 8);
+      *(v4i*)(y + h * yh + c) = u;
+      *(v4i*)(y + h * yh + c + 8) = w;
+    }
+    return;
+  }
+  float cs[8], sn[8];
+  {
+    const POS* pos = (const POS*)a.positions + token;
+    double p[4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) p[k] = k < a.axes ? (double)pos[(size_t)k * a.tokens] : 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int f = f0 + i;
+      const double at = f < a.end[0] ? p[0] : f < a.end[1] ? p[1] : f < a.end[2] ? p[2] : p[3];
+      turn_of(at * (double)a.inv_freq[f] * 0.15915494309189533577, a.sign, cs[i], sn[i]);
+    }
+  }
+  // halves: 8 channels from f0 and 8 from half + f0; adjacent: 16 channels from 2 f0
+  const int c0 = ADJACENT ? 2 * f0 : f0, c1 = ADJACENT ? 2 * f0 + 8 : a.half + f0;
+  for (int h = h0; h < h1; h++) {
+    const v8bf u = *(const v8bf*)(x + h * xh + c0), w = *(const v8bf*)(x + h * xh + c1);
+    v8bf r, t;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const float x1 = ADJACENT ? (float)(i < 4 ? u[2 * (i & 3)] : w[2 * (i & 3)]) : (float)u[i];
+      const float x2 = ADJACENT ? (float)(i < 4 ? u[2 * (i & 3) + 1] : w[2 * (i & 3) + 1]) : (float)w[i];
+      const __bf16 y1 = (__bf16)(x1 * cs[i] - x2 * sn[i]), y2 = (__bf16)(x2 * cs[i] + x1 * sn[i]);
+      if (!ADJACENT) {
+        r[i] = y1;
+        t[i] = y2;
+      } else if (i < 4) {
+        r[2 * i] = y1;
+        r[2 * i + 1] = y2;
+      } else {
+        t[2 * (i - 4)] = y1;
+        t[2 * (i - 4) + 1] = y2;
+      }
+    }
+    *(v8bf*)(y + h * yh + c0) = r;
+    *(v8bf*)(y + h * yh + c1) = t;
+  }
+}
+
+}  // namespace sage

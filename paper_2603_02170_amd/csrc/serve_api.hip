@@ -1,0 +1,308 @@
+// C-ABI host side of the operators around the attention: argument checks, workspace layout, launches.
+// See include/sagebwd_serve.h for the contract of every entry point.
+#include "sagebwd_serve.h"
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <type_traits>
+
+#include "cache_attend_kernel.h"
+#include "cache_kernels.h"
+#include "rotary_kernel.h"
+
+namespace {
+
+using namespace sage;
+
+#define SERVE_LAUNCH_CHECK() do { if (hipGetLastError() != hipSuccess) return SAGEBWD_HIP_ERROR; } while (0)
+
+constexpr int64_t kMostElements = (int64_t)1 << 40;
+
+inline bool aligned(const void* p, size_t to = 16) { return ((uintptr_t)p & (to - 1)) == 0; }
+inline bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s <= kMostElements; }
+
+int page_shift_of(int page) {
+  for (int s = 5; s <= 8; s++)
+    if (page == 1 << s) return s;
+  return -1;
+}
+
+int check_cache(const sagebwd_cache_params* p, bool pool) {
+  if (p == nullptr || p->reserved != 0 || p->H < 1 || (pool && p->pages < 1)) return SAGEBWD_INVALID_ARG;
+  if ((p->d != 64 && p->d != 128) || (p->group != 32 && p->group != 64) || page_shift_of(p->page) < 0 || p->H > 1024)
+    return SAGEBWD_UNSUPPORTED_SHAPE;
+  return SAGEBWD_OK;
+}
+CacheGeometry geometry(const sagebwd_cache_params& p) { return CacheGeometry{p.H, p.d, page_shift_of(p.page), p.group, p.pages}; }
+
+int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c) {
+  const int rc = check_cache(p, true);
+  if (rc != SAGEBWD_OK) return rc;
+  if (c == nullptr || c->R < 0 || c->T < 0 || c->Hq < 1 || c->columns < 1 || c->max_new < 1 || c->max_length < 0 ||
+      (c->causal != 0 && c->causal != 1) || !(c->sm_scale >= 0.f) || !isfinite(c->sm_scale) || !stride_ok(c->q_token_stride) ||
+      !stride_ok(c->q_head_stride))
+    return SAGEBWD_INVALID_ARG;
+  if (c->Hq % p->H != 0 || c->Hq / p->H > 64 || (int64_t)c->T * c->Hq * p->d >= kMostElements || c->R > 1 << 20 ||
+      (int64_t)c->columns * p->page > INT32_MAX / 2 || (int64_t)c->T * (c->Hq / p->H) > INT32_MAX / 2)
+    return SAGEBWD_UNSUPPORTED_SHAPE;
+  return SAGEBWD_OK;
+}
+
+constexpr int kSlots = 1024;      // workgroups of the attention that the machine takes at a time, at most
+
+// How a call is laid out: row tiles, workgroups, workspace.
+struct AttendPlan {
+  int nq, row_tiles, workgroups, max_length;
+  size_t prefix, sums, stats, total;
+};
+inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
+
+AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
+  AttendPlan w;
+  const int G = c.Hq / p.H;
+  const int64_t all = (int64_t)c.columns * p.page;
+  w.max_length = (int)(c.max_length > 0 && c.max_length < all ? c.max_length : all);
+  const int64_t most = (int64_t)(c.max_new < c.T ? c.max_new : c.T) * G;      // query rows of a request and head
+  const int64_t rows = most > 0 ? most : 1;
+  w.nq = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  w.row_tiles = (int)((rows + 16 * w.nq - 1) / (16 * w.nq));
+  const int64_t units = (int64_t)c.R * p.H * ((w.max_length + kUnit - 1) / kUnit);
+  const int64_t slots = kSlots / w.row_tiles > 8 ? kSlots / w.row_tiles : 8;
+  w.workgroups = (int)(units < slots ? (units > 0 ? units : 1) : slots);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
+  w.prefix = take((size_t)w.row_tiles * (c.R + 1) * 4);
+  const size_t parts = (size_t)w.row_tiles * w.workgroups * 2 * 16 * w.nq;
+  w.sums = take(parts * p.d * 4);
+  w.stats = take(parts * 8);
+  w.total = off;
+  return w;
+}
+
+template <int D, int GROUP, int NQ>
+int launch_attend(const AttendArgs& a, const AttendPlan& w, hipStream_t st) {
+  cache_attend_kernel<D, GROUP, NQ><<<dim3(w.workgroups, w.row_tiles), 256, 0, st>>>(a);
+  SERVE_LAUNCH_CHECK();
+  if (w.workgroups > 1) {
+    cache_join_kernel<D, NQ><<<dim3(w.workgroups - 1, 4 * NQ, w.row_tiles), 256, 0, st>>>(a);
+    SERVE_LAUNCH_CHECK();
+  }
+  return SAGEBWD_OK;
+}
+template <int D, int GROUP>
+int launch_attend(const AttendArgs& a, const AttendPlan& w, hipStream_t st) {
+  switch (w.nq) {
+    case 1: return launch_attend<D, GROUP, 1>(a, w, st);
+    case 2: return launch_attend<D, GROUP, 2>(a, w, st);
+    default: return launch_attend<D, GROUP, 4>(a, w, st);
+  }
+}
+
+template <typename F>
+int with_format(const sagebwd_cache_params& p, F f) {
+  if (p.d == 64) return p.group == 32 ? f(std::integral_constant<int, 64>(), std::integral_constant<int, 32>())
+                                      : f(std::integral_constant<int, 64>(), std::integral_constant<int, 64>());
+  return p.group == 32 ? f(std::integral_constant<int, 128>(), std::integral_constant<int, 32>())
+                       : f(std::integral_constant<int, 128>(), std::integral_constant<int, 64>());
+}
+
+}  // namespace
+
+extern "C" {
+
+int sagebwd_cache_page_bytes(const sagebwd_cache_params* params, size_t* bytes) {
+  const int rc = check_cache(params, false);
+  if (rc != SAGEBWD_OK) return rc;
+  if (bytes == nullptr) return SAGEBWD_INVALID_ARG;
+  *bytes = geometry(*params).page_bytes();
+  return SAGEBWD_OK;
+}
+
+int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block_table, const int32_t* free_pages, const int32_t* free_count,
+                       int32_t R, int32_t columns, int32_t page, int32_t capacity, int32_t rows, int64_t* slots, int32_t* positions,
+                       int32_t* cu_new, int32_t* lengths, int32_t* granted, int32_t* free_left, void* stream) {
+  if (R < 0 || rows < 0 || columns < 1 || capacity < 0) return SAGEBWD_INVALID_ARG;
+  if ((R > 0 && (held == nullptr || added == nullptr || block_table == nullptr || lengths == nullptr || granted == nullptr)) ||
+      (capacity > 0 && free_pages == nullptr) || free_count == nullptr || cu_new == nullptr || free_left == nullptr ||
+      (rows > 0 && (slots == nullptr || positions == nullptr)))
+    return SAGEBWD_INVALID_ARG;
+  if (page_shift_of(page) < 0 || (int64_t)columns * page > INT32_MAX / 2 || R > 1 << 20) return SAGEBWD_UNSUPPORTED_SHAPE;
+  const PlanArgs a{held, added, free_pages, free_count, block_table, slots, positions, cu_new, lengths, granted, free_left,
+                   R, columns, page_shift_of(page), capacity, rows};
+  hipStream_t st = (hipStream_t)stream;
+  if (rows <= 2048) {
+    cache_plan_kernel<true><<<1, 1024, 0, st>>>(a);
+    SERVE_LAUNCH_CHECK();
+    return SAGEBWD_OK;
+  }
+  cache_plan_kernel<false><<<1, 1024, 0, st>>>(a);
+  SERVE_LAUNCH_CHECK();
+  cache_plan_rows_kernel<<<(rows + 255) / 256, 256, 0, st>>>(a);
+  SERVE_LAUNCH_CHECK();
+  return SAGEBWD_OK;
+}
+
+int sagebwd_cache_trim(const int32_t* keep, int32_t* lengths, int32_t* block_table, int32_t* free_pages, int32_t* free_count, int32_t R,
+                       int32_t columns, int32_t page, int32_t capacity, void* stream) {
+  if (R < 0 || columns < 1 || capacity < 0 || free_count == nullptr || (capacity > 0 && free_pages == nullptr) ||
+      (R > 0 && (keep == nullptr || lengths == nullptr || block_table == nullptr)))
+    return SAGEBWD_INVALID_ARG;
+  if (page_shift_of(page) < 0 || (int64_t)columns * page > INT32_MAX / 2 || R > 1 << 20) return SAGEBWD_UNSUPPORTED_SHAPE;
+  if (R == 0) return SAGEBWD_OK;
+  cache_trim_kernel<<<1, 1024, 0, (hipStream_t)stream>>>(
+      TrimArgs{keep, lengths, block_table, free_pages, free_count, R, columns, page_shift_of(page), capacity});
+  SERVE_LAUNCH_CHECK();
+  return SAGEBWD_OK;
+}
+
+int sagebwd_cache_append(const void* K, const void* V, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                         int64_t v_head_stride, const int64_t* slots, int32_t T, const float* k_mean, const float* v_mean,
+                         const sagebwd_cache_params* params, void* pool, void* stream) {
+  const int rc = check_cache(params, true);
+  if (rc != SAGEBWD_OK) return rc;
+  if (T < 0 || !stride_ok(k_token_stride) || !stride_ok(k_head_stride) || !stride_ok(v_token_stride) || !stride_ok(v_head_stride))
+    return SAGEBWD_INVALID_ARG;
+  if (T == 0) return SAGEBWD_OK;
+  if (K == nullptr || V == nullptr || slots == nullptr || pool == nullptr || !aligned(K) || !aligned(V) || !aligned(pool)) return SAGEBWD_INVALID_ARG;
+  const int64_t rows = (int64_t)T * params->H, per = 256 / (params->d / 8);
+  if ((rows + per - 1) / per > INT32_MAX) return SAGEBWD_UNSUPPORTED_SHAPE;
+  const StoreArgs a{(const __bf16*)K, (const __bf16*)V, {k_token_stride, k_head_stride}, {v_token_stride, v_head_stride}, slots, k_mean, v_mean,
+                    (unsigned char*)pool, nullptr, nullptr, T, geometry(*params)};
+  return with_format(*params, [&](auto d, auto group) -> int {
+    cache_append_kernel<decltype(d)::value, decltype(group)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, (hipStream_t)stream>>>(a);
+    SERVE_LAUNCH_CHECK();
+    return SAGEBWD_OK;
+  });
+}
+
+int sagebwd_cache_read(const int64_t* slots, int32_t T, const float* k_mean, const float* v_mean, const sagebwd_cache_params* params,
+                       const void* pool, void* K, void* V, void* stream) {
+  const int rc = check_cache(params, true);
+  if (rc != SAGEBWD_OK) return rc;
+  if (T < 0) return SAGEBWD_INVALID_ARG;
+  if (T == 0) return SAGEBWD_OK;
+  if (K == nullptr || V == nullptr || slots == nullptr || pool == nullptr || !aligned(K) || !aligned(V) || !aligned(pool)) return SAGEBWD_INVALID_ARG;
+  const int64_t rows = (int64_t)T * params->H, per = 256 / (params->d / 8);
+  if ((rows + per - 1) / per > INT32_MAX) return SAGEBWD_UNSUPPORTED_SHAPE;
+  const StoreArgs a{nullptr, nullptr, {0, 0}, {0, 0}, slots, k_mean, v_mean, (unsigned char*)pool, (__bf16*)K, (__bf16*)V, T, geometry(*params)};
+  return with_format(*params, [&](auto d, auto group) -> int {
+    cache_read_kernel<decltype(d)::value, decltype(group)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, (hipStream_t)stream>>>(a);
+    SERVE_LAUNCH_CHECK();
+    return SAGEBWD_OK;
+  });
+}
+
+int sagebwd_cache_workspace_bytes(const sagebwd_cache_params* params, const sagebwd_cache_call* call, size_t* bytes) {
+  const int rc = check_call(params, call);
+  if (rc != SAGEBWD_OK) return rc;
+  if (bytes == nullptr) return SAGEBWD_INVALID_ARG;
+  *bytes = attend_plan(*params, *call).total;
+  return SAGEBWD_OK;
+}
+
+int sagebwd_cache_attention(const void* Q, const void* pool, const int32_t* block_table, const int32_t* lengths, const int32_t* cu,
+                            const float* v_mean, const sagebwd_cache_params* params, const sagebwd_cache_call* call, void* O, float* LSE,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_call(params, call);
+  if (rc != SAGEBWD_OK) return rc;
+  if (call->R == 0 || call->T == 0) return SAGEBWD_OK;
+  if (Q == nullptr || pool == nullptr || block_table == nullptr || lengths == nullptr || cu == nullptr || O == nullptr || workspace == nullptr ||
+      !aligned(Q) || !aligned(pool) || !aligned(O) || !aligned(workspace, 256))
+    return SAGEBWD_INVALID_ARG;
+  const AttendPlan w = attend_plan(*params, *call);
+  if (workspace_bytes < w.total) return SAGEBWD_WORKSPACE_TOO_SMALL;
+  char* ws = (char*)workspace;
+  AttendArgs a;
+  a.Q = (const __bf16*)Q;
+  a.pool = (const unsigned char*)pool;
+  a.table = block_table;
+  a.lengths = lengths;
+  a.cu = cu;
+  a.v_mean = v_mean;
+  a.O = (__bf16*)O;
+  a.LSE = LSE;
+  a.prefix = (int32_t*)(ws + w.prefix);
+  a.sums = (float*)(ws + w.sums);
+  a.stats = (float2*)(ws + w.stats);
+  a.g = geometry(*params);
+  a.R = call->R;
+  a.T = call->T;
+  a.Hq = call->Hq;
+  a.G = call->Hq / params->H;
+  a.columns = call->columns;
+  a.max_new = call->max_new;
+  a.max_length = w.max_length;
+  a.causal = call->causal;
+  a.scale_log2 = (call->sm_scale > 0.f ? call->sm_scale : 1.f / sqrtf((float)params->d)) * 1.4426950408889634f;
+  a.q_token = call->q_token_stride;
+  a.q_head = call->q_head_stride;
+  a.workgroups = w.workgroups;
+  return with_format(*params, [&](auto d, auto group) { return launch_attend<decltype(d)::value, decltype(group)::value>(a, w, (hipStream_t)stream); });
+}
+
+int sagebwd_rotary(const void* Q, const void* K, void* Qo, void* Ko, const void* positions, const float* inv_freq,
+                   const sagebwd_rotary_params* p, void* stream) {
+  if (p == nullptr || p->B < 0 || p->N < 0 || p->Hq < 1 || p->Hk < 0 || p->axes < 1 || p->axes > 4 || (p->adjacent != 0 && p->adjacent != 1) ||
+      (p->inverse != 0 && p->inverse != 1) || (p->positions64 != 0 && p->positions64 != 1))
+    return SAGEBWD_INVALID_ARG;
+  if (p->d < 16 || p->d > 512 || p->d % 16 != 0 || p->rotary_dim < 16 || p->rotary_dim > p->d || p->rotary_dim % 16 != 0 ||
+      (int64_t)p->B * p->N > INT32_MAX / 64 || p->Hq > 65535 || p->Hk > 65535)
+    return SAGEBWD_UNSUPPORTED_SHAPE;
+  int64_t sum = 0;
+  for (int k = 0; k < p->axes; k++) {
+    if (p->sections[k] < 0) return SAGEBWD_INVALID_ARG;
+    sum += p->sections[k];
+  }
+  if (sum != p->rotary_dim / 2) return SAGEBWD_INVALID_ARG;
+  for (int k = 0; k < 3; k++)
+    if (!stride_ok(p->q_strides[k]) || !stride_ok(p->qo_strides[k]) || (p->Hk > 0 && (!stride_ok(p->k_strides[k]) || !stride_ok(p->ko_strides[k]))))
+      return SAGEBWD_INVALID_ARG;
+  if (p->B == 0 || p->N == 0) return SAGEBWD_OK;
+  if (Q == nullptr || Qo == nullptr || positions == nullptr || inv_freq == nullptr || !aligned(Q) || !aligned(Qo) ||
+      (p->Hk > 0 && (K == nullptr || Ko == nullptr || !aligned(K) || !aligned(Ko))))
+    return SAGEBWD_INVALID_ARG;
+  RotaryArgs a;
+  a.x[0] = (const __bf16*)Q;
+  a.x[1] = (const __bf16*)K;
+  a.y[0] = (__bf16*)Qo;
+  a.y[1] = (__bf16*)Ko;
+  for (int k = 0; k < 3; k++) {
+    a.xs[0][k] = p->q_strides[k];
+    a.xs[1][k] = p->k_strides[k];
+    a.ys[0][k] = p->qo_strides[k];
+    a.ys[1][k] = p->ko_strides[k];
+  }
+  a.positions = positions;
+  a.inv_freq = inv_freq;
+  a.N = p->N;
+  a.tokens = p->B * p->N;
+  a.d = p->d;
+  a.half = p->rotary_dim / 2;
+  a.heads[0] = p->Hq;
+  a.heads[1] = p->Hk;
+  a.axes = p->axes;
+  int at = 0;
+  for (int k = 0; k < 4; k++) {
+    if (k < p->axes) at += p->sections[k];
+    a.end[k] = at;
+  }
+  a.pieces = p->d / 16;
+  a.sign = p->inverse ? -1.f : 1.f;
+  const int64_t threads = (int64_t)a.tokens * a.pieces;
+  a.heads_per_thread = threads >= 65536 ? 8 : 1;
+  for (int k = 0; k < 2; k++) a.head_groups[k] = (a.heads[k] + a.heads_per_thread - 1) / a.heads_per_thread;
+  const dim3 grid((unsigned)((threads + 255) / 256), a.head_groups[0] + a.head_groups[1]);
+  hipStream_t st = (hipStream_t)stream;
+  if (p->adjacent) {
+    if (p->positions64) rotary_kernel<true, int64_t><<<grid, 256, 0, st>>>(a);
+    else rotary_kernel<true, int32_t><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (p->positions64) rotary_kernel<false, int64_t><<<grid, 256, 0, st>>>(a);
+    else rotary_kernel<false, int32_t><<<grid, 256, 0, st>>>(a);
+  }
+  SERVE_LAUNCH_CHECK();
+  return SAGEBWD_OK;
+}
+
+}  // extern "C"

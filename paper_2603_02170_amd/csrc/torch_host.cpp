@@ -10,9 +10,11 @@
 #include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/saved_variable.h>
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 
 #include "sagebwd.h"
+#include "sagebwd_serve.h"
 
 namespace {
 
@@ -434,11 +436,20 @@ PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+#include "torch_serve.h"
+
 PyMethodDef g_methods[] = {
     {"fwd", (PyCFunction)(void (*)(void))py_fwd, METH_FASTCALL, nullptr},
     {"fwd_static", (PyCFunction)(void (*)(void))py_fwd_static, METH_FASTCALL, nullptr},
     {"bwd", (PyCFunction)(void (*)(void))py_bwd, METH_FASTCALL, nullptr},
     {"attention", (PyCFunction)(void (*)(void))py_attention, METH_FASTCALL, nullptr},
+    {"cache_plan", (PyCFunction)(void (*)(void))py_cache_plan, METH_FASTCALL, nullptr},
+    {"cache_trim", (PyCFunction)(void (*)(void))py_cache_trim, METH_FASTCALL, nullptr},
+    {"cache_append", (PyCFunction)(void (*)(void))py_cache_append, METH_FASTCALL, nullptr},
+    {"cache_read", (PyCFunction)(void (*)(void))py_cache_read, METH_FASTCALL, nullptr},
+    {"cache_attention", (PyCFunction)(void (*)(void))py_cache_attention, METH_FASTCALL, nullptr},
+    {"cache_workspace_bytes", (PyCFunction)(void (*)(void))py_cache_workspace_bytes, METH_FASTCALL, nullptr},
+    {"rotary", (PyCFunction)(void (*)(void))py_rotary, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_sage_host", "Host side of the SageBwd entry points", -1, g_methods,

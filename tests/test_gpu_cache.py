@@ -1,0 +1,459 @@
+"""The 4-bit cache against plain implementations: storing, reading, the bookkeeping of pages, and attention over it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import serve_ref as ref
+from paper_2603_02170_amd import binding, cache
+from paper_2603_02170_amd.cache import CacheParams
+
+pytestmark = pytest.mark.gpu
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy()
+
+
+def _randn(shape, g, scale=1.0):
+    return (scale * torch.randn(shape, generator=g)).to(torch.bfloat16)
+
+
+# ---- storing and reading ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d,group,page,H,T", [(64, 32, 32, 1, 1), (64, 64, 64, 3, 37), (128, 32, 128, 2, 100), (128, 64, 256, 8, 300), (128, 64, 64, 5, 9)])
+@pytest.mark.parametrize("mean", [False, True])
+def test_what_is_stored_is_read_back_as_the_quantiser_says(d, group, page, H, T, mean):
+    g = torch.Generator().manual_seed(d + T)
+    p = CacheParams(H=H, d=d, page=page, group=group)
+    pages = -(-T // page) + 2
+    pool = torch.randint(0, 256, tuple(cache.alloc_cache(p, pages).shape), generator=g, dtype=torch.uint8).cuda()
+    before = pool.clone()
+    qkv = _randn((T, 2 * H + 1, d), g).cuda()          # K and V as slices of one tensor
+    K, V = qkv[:, 1:1 + H], qkv[:, 1 + H:]
+    slots = torch.randperm(pages * page, generator=g)[:T].cuda()
+    km, vm = (torch.randn((H, d), generator=g).cuda(), torch.randn((H, d), generator=g).cuda()) if mean else (None, None)
+    cache.sagebwd_cache_append(K, V, slots, pool, p, k_mean=km, v_mean=vm)
+    Kr, Vr = cache.sagebwd_cache_read(slots, pool, p)
+    for got, x, m in ((Kr, K, km), (Vr, V, vm)):
+        x = _np(x) - (_np(m) if mean else np.float32(0))
+        _, _, want = ref.quantise(x, group)
+        assert np.array_equal(_np(got), want)          # bf16 holds the values exactly
+        # and they are the nearest of their grid: half a step, and a step is at most 17/16 of a seventh of the group's maximum
+        a = np.abs(x).reshape(T, H, -1, group).max(-1).repeat(group, -1).reshape(T, H, d)
+        assert (np.abs(want - x) <= a / 7 * 17 / 32 * (1 + 2e-6)).all()
+    if mean:
+        Km, Vm = cache.sagebwd_cache_read(slots, pool, p, k_mean=km, v_mean=vm)
+        assert np.array_equal(_np(Km), ref.bf16_round(_np(Kr) + _np(km))) and np.array_equal(_np(Vm), ref.bf16_round(_np(Vr) + _np(vm)))
+    # the bytes are where the header says, and every other token's are as they were
+    stored = {int(s) for s in slots}
+    Kr, Vr = _np(Kr), _np(Vr)
+    at = {int(s): t for t, s in enumerate(slots)}
+    for n in range(pages):
+        for h in range(H) if n < 2 else [0]:
+            K1, V1 = ref.decode_page(pool[n, h].cpu().numpy(), d, page, group)
+            K0, V0 = ref.decode_page(before[n, h].cpu().numpy(), d, page, group)
+            for t in range(page):
+                s = n * page + t
+                want = (Kr[at[s], h], Vr[at[s], h]) if s in stored else (K0[t], V0[t])
+                assert np.array_equal(K1[t], want[0], equal_nan=True) and np.array_equal(V1[t], want[1], equal_nan=True)
+
+
+def test_groups_of_every_magnitude():
+    """Zeros, ties, the ends of the range, infinities and NaN; a group does not touch its neighbours."""
+    p = CacheParams(H=1, d=64, page=32, group=32)
+    rows = []
+    for e in (-133, -101, -100, -99, -60, -1, 0, 3, 60, 126, 127):
+        rows.append(np.linspace(-1, 1, 64, dtype=np.float32) * np.float32(2.0 ** e))
+    rows.append(np.zeros(64))
+    rows.append(np.full(64, 3.5))
+    rows.append(np.where(np.arange(64) % 2 == 0, 7.0, np.arange(64) % 15 / 2 - 3.5))      # scale 1: halves are ties
+    for bad in (np.inf, -np.inf, np.nan):
+        r = np.linspace(-2, 2, 64)
+        r[40] = bad
+        rows.append(r)
+    K = torch.tensor(np.array(rows, np.float32)).to(torch.bfloat16).reshape(-1, 1, 64).cuda()
+    T = K.shape[0]
+    V = K.flip(-1).contiguous()
+    pool = cache.alloc_cache(p, 1)
+    slots = torch.arange(T, device="cuda")
+    cache.sagebwd_cache_append(K, V, slots, pool, p)
+    Kr, Vr = cache.sagebwd_cache_read(slots, pool, p)
+    for got, x in ((Kr, K), (Vr, V)):
+        _, _, want = ref.quantise(_np(x), 32)
+        assert np.array_equal(_np(got), want, equal_nan=True)
+    assert torch.isnan(Kr[-3:, 0, 32:]).all() and torch.isfinite(Kr[-3:, 0, :32]).all()
+
+
+def test_slots_outside_the_pool_are_skipped_and_read_as_zeros():
+    p = CacheParams(H=2, d=128, page=32)
+    g = torch.Generator().manual_seed(3)
+    pool = torch.full(tuple(cache.alloc_cache(p, 2).shape), 0x77, dtype=torch.uint8, device="cuda")
+    K = _randn((6, 2, 128), g).cuda()
+    slots = torch.tensor([-1, 64, 1 << 40, -(1 << 50), 5, 64 + 5], device="cuda")
+    before = pool.clone()
+    cache.sagebwd_cache_append(K, K, slots, pool, p)
+    Kr, Vr = cache.sagebwd_cache_read(slots, pool, p)
+    assert (Kr[[0, 1, 2, 3, 5]] == 0).all() and (Vr[[0, 1, 2, 3, 5]] == 0).all() and (Kr[4] != 0).any()
+    assert torch.equal(pool[1], before[1])
+    changed = (pool[0] != before[0]).sum().item()
+    assert 0 < changed <= 2 * (128 + 8)
+
+
+# ---- bookkeeping ------------------------------------------------------------------------------------------------
+
+def _check_plan(held, added, columns, page, count, rows, seed=0, capacity=None):
+    R = len(held)
+    g = np.random.default_rng(seed)
+    capacity = capacity or count + 5
+    stack = [int(x) for x in g.permutation(capacity)]
+    table = [[int(x) for x in g.integers(0, 1000, columns)] for _ in range(R)]
+    t, h = _i32(table).reshape(R, columns), _i32(held)
+    got = cache.sagebwd_cache_plan(h, _i32(added), t, _i32(stack), _i32([count]), CacheParams(1, 64, page=page), rows)
+    want_table = [list(r) for r in table]
+    want = ref.plan(held, added, want_table, stack, count, page, rows)
+    for name, x in got._asdict().items():
+        assert x.tolist() == want[name], name
+    assert t.tolist() == want_table
+    # called again on the same tensors: the same
+    again = cache.sagebwd_cache_plan(h, _i32(added), t, _i32(stack), _i32([count]), CacheParams(1, 64, page=page), rows, out=got)
+    assert again.slots.tolist() == want["slots"] and t.tolist() == want_table
+    return got
+
+
+@pytest.mark.parametrize("R,page,most,rows_of", [(1, 32, 1, 1), (7, 64, 3, 1), (64, 32, 40, 1), (1024, 64, 2, 1), (1500, 32, 9, 1), (2100, 256, 600, 2),
+                                                 (40, 128, 200, 0.6), (5, 32, 2000, 1.01)])
+def test_plan_against_the_plain_one(R, page, most, rows_of):
+    g = np.random.default_rng(R)
+    held, added = g.integers(0, 500, R).tolist(), g.integers(0, most + 1, R).tolist()
+    columns = -(-(500 + most) // page)
+    need = sum(-(-(a + n) // page) - -(-a // page) for a, n in zip(held, added))
+    rows = int(sum(added) * rows_of)
+    _check_plan(held, added, columns, page, need, rows, seed=R)
+    _check_plan(held, added, columns, page, need // 2, rows, seed=R + 1)         # not enough pages
+
+
+def test_plan_of_sizes_that_are_not_valid():
+    _check_plan([5, -1, 60, 0, 64, 2 ** 30, 10], [1, 3, 10, -4, 0, 2 ** 30, 2], columns=2, page=32, count=9, rows=20)
+    _check_plan([0, 0], [0, 0], columns=1, page=32, count=0, rows=0)
+    got = _check_plan([0], [64], columns=2, page=32, count=2, rows=64, capacity=2)
+    assert got.free_left.item() == 0
+    # a count beyond the stack is read as the stack's size
+    t = _i32([[0, 0]])
+    got = cache.sagebwd_cache_plan(_i32([0]), _i32([40]), t, _i32([7, 8]), _i32([99]), CacheParams(1, 64, page=32), 40)
+    assert t.tolist() == [[8, 7]] and got.free_left.item() == 0
+
+
+def test_plan_in_place_and_trim_takes_it_back():
+    g = np.random.default_rng(5)
+    R, page, columns = 70, 32, 20
+    held = g.integers(0, 300, R)
+    order = g.permutation(3000)
+    table = np.full((R, columns), -1)
+    used = 0
+    for r in range(R):
+        n = -(-int(held[r]) // page)
+        table[r, :n] = order[used:used + n]
+        used += n
+    stack = np.concatenate([order[used:][::-1], np.zeros(used, int)])        # room for every page
+    count0 = 3000 - used
+    h, t, f, c = _i32(held.tolist()), _i32(table.tolist()), _i32(stack.tolist()), _i32([count0])
+    p = CacheParams(1, 64, page=page)
+    added = g.integers(0, 200, R).tolist()
+    rows = sum(added)
+    new = torch.empty(R, dtype=torch.int32, device="cuda")
+    out = cache.CachePlan(torch.empty(rows, dtype=torch.int64, device="cuda"), *(torch.empty(n, dtype=torch.int32, device="cuda") for n in (rows, R + 1)),
+                          h, new, c)
+    got = cache.sagebwd_cache_plan(h, _i32(added), t, f, c, p, rows, out=out)
+    want_table = table.tolist()
+    want = ref.plan(held.tolist(), added, want_table, stack.tolist(), count0, page, rows)
+    assert h.tolist() == want["lengths"] and c.tolist() == want["free_left"] and got.slots.tolist() == want["slots"] and t.tolist() == want_table
+    cache.sagebwd_cache_trim(_i32(held.tolist()), h, t, f, c, p)
+    assert h.tolist() == held.tolist() and c.item() == count0 and t.tolist() == table.tolist() and f.tolist()[:count0] == stack.tolist()[:count0]
+    # some requests end, some lose their last tokens, some name a length that they do not have
+    keep = [0 if r % 3 == 0 else max(0, int(held[r]) - 40) if r % 3 == 1 else [int(held[r]) + 1, -1][r % 2] for r in range(R)]
+    cache.sagebwd_cache_trim(_i32(keep), h, t, f, c, p)
+    freed, left = [], t.tolist()
+    for r in range(R):
+        k = keep[r] if r % 3 < 2 else int(held[r])
+        first, end = -(-k // page), -(-int(held[r]) // page)
+        freed += table[r, first:end].tolist()
+        assert left[r] == table[r, :first].tolist() + [-1] * (columns - first)
+        assert h[r].item() == k
+    assert c.item() == count0 + len(freed) and f.tolist()[count0:c.item()] == freed[::-1]
+
+
+def test_trim_of_many_requests():
+    R, page = 2300, 32
+    lengths = [(7 * r) % 100 for r in range(R)]
+    table = [[4 * r + k if k * page < lengths[r] else -1 for k in range(4)] for r in range(R)]
+    h, t, f, c = _i32(lengths), _i32(table), torch.zeros(4 * R, dtype=torch.int32, device="cuda"), _i32([3])
+    cache.sagebwd_cache_trim(_i32([0] * R), h, t, f, c, CacheParams(1, 64, page=page))
+    freed = [x for row in table for x in row if x >= 0]
+    assert c.item() == 3 + len(freed) and f.tolist()[3:c.item()] == freed[::-1] and h.sum().item() == 0 and (t == -1).all()
+    # a stack that is too small keeps what fits and writes nothing behind it
+    h, t, f, c = _i32([64, 64]), _i32([[1, 2], [3, 4]]), _i32([9, 9, 9, 9])[:3], _i32([1])
+    cache.sagebwd_cache_trim(_i32([0, 0]), h, t, f, c, CacheParams(1, 64, page=page))
+    assert f.tolist() == [9, 4, 3] and c.item() == 3
+
+
+# ---- attention --------------------------------------------------------------------------------------------------
+
+class Filled:
+    """A cache of random tokens for requests of given lengths: pages in random order, everything else in the pool NaN."""
+
+    def __init__(self, lens, p, g, extra=3, sigma=1.0, spare_columns=1):
+        self.p, self.lens = p, lens
+        used = [-(-n // p.page) for n in lens]
+        columns = max(used + [1]) + spare_columns
+        order = torch.randperm(sum(used) + extra, generator=g).tolist()
+        self.pool = torch.full(tuple(cache.alloc_cache(p, sum(used) + extra).shape), 0xFF, dtype=torch.uint8, device="cuda")
+        table, slots = [], []
+        for n, u in zip(lens, used):
+            pages = [order.pop() for _ in range(u)]
+            table.append(pages + [-1] * (columns - u))
+            slots += [pages[t // p.page] * p.page + t % p.page for t in range(n)]
+        self.table, self.lengths = _i32(table).reshape(len(lens), columns), _i32(lens)
+        T = len(slots)
+        self.K, self.V = _randn((T, p.H, p.d), g, sigma), _randn((T, p.H, p.d), g)
+        self.slots = torch.tensor(slots, dtype=torch.int64, device="cuda")
+        self.store()
+
+    def store(self):
+        if self.slots.numel():
+            cache.sagebwd_cache_append(self.K.cuda(), self.V.cuda(), self.slots, self.pool, self.p)
+        k, v = (ref.quantise(_np(x), self.p.group)[2] for x in (self.K, self.V))
+        self.k, self.v = k.astype(np.float64), v.astype(np.float64)
+        self.at = np.concatenate([[0], np.cumsum(self.lens)]).astype(int)
+
+
+def _attend(f, news, Hq, g, causal=True, sm_scale=0.0, v_mean=None, q=None, **kw):
+    T = sum(news)
+    q = _randn((T, Hq, f.p.d), g) if q is None else q
+    cu = np.concatenate([[0], np.cumsum(news)]).astype(int).tolist()
+    O, lse = cache.sagebwd_cache_attention(q.cuda(), f.pool, f.table, f.lengths, _i32(cu), f.p, max(news + [1]), causal=causal, sm_scale=sm_scale,
+                                           v_mean=v_mean, **kw)
+    return q, cu, O, lse
+
+
+def _check(f, q, cu, O, lse, causal, sm_scale=0.0, v_mean=None, requests=None):
+    """Tolerances, from the roundings: O is rounded to bf16 (2^-8 of it), every probability times its scale too (2^-8 of sum p |v|); a logit
+    is a chain of four products' sums in FP32 of magnitude 32 s sum |q| (eight roundings of 2^-24 of it counted), which moves a
+    probability by as much; hardware exp2, log2 and sums: 2^-18.  V's chains hold up to 32 s, rounded twice a tile."""
+    scale = sm_scale or f.p.d ** -0.5
+    O, lse = O.float().cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64)
+    for r in range(len(f.lens)) if requests is None else requests:
+        a, b = cu[r], cu[r + 1]
+        qs = _np(q[a:b]).astype(np.float64)
+        k, v = f.k[f.at[r]:f.at[r + 1]], f.v[f.at[r]:f.at[r + 1]]
+        want, wlse, A = ref.attention(qs, k, v, b - a, causal, scale, None if v_mean is None else _np(v_mean))
+        s_k = np.abs(k).max() / 7 * 17 / 16 if k.size else 0.0
+        s_v = np.abs(v).max() / 7 * 17 / 16 if v.size else 0.0
+        e = scale * 8 * 2.0 ** -24 * 32 * s_k * np.abs(qs).sum(-1) + 2.0 ** -18
+        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2 * e[..., None]) * A + 32 * s_v * 2 * 2.0 ** -24 * (f.lens[r] / 32 + 1) + 1e-30
+        err = np.abs(O[a:b] - want)
+        assert (err <= tol).all(), (r, f.lens[r], b - a, float((err / tol).max()), np.argwhere(err > tol)[:4].tolist())
+        none = np.isinf(wlse)
+        assert np.array_equal(lse[:, a:b][none], wlse[none]) and (O[a:b].transpose(1, 0, 2)[none] == 0).all()
+        le = np.abs(lse[:, a:b] - wlse)[~none]
+        assert (le <= (e.T + 2.0 ** -22 * (1 + np.abs(wlse)))[~none]).all(), (r, float(le.max()))
+
+
+LENGTHS = [
+    ([1], [1]), ([0], [1]), ([33], [1]), ([500, 1, 130, 31], [1, 1, 1, 1]),
+    ([3, 0, 40, 700, 64, 128], [2, 3, 5, 1, 4, 0]),       # a request shorter than its new tokens, an empty one, one without new tokens
+    ([260, 90], [17, 3]), ([200, 1000], [1, 70]), ([300], [300]), ([70, 1, 513, 129], [70, 1, 200, 129]),
+]
+
+
+@pytest.mark.parametrize("lens,news", LENGTHS)
+@pytest.mark.parametrize("d,group,page,Hq,H", [(64, 32, 32, 1, 1), (64, 64, 128, 6, 2), (128, 32, 64, 8, 1), (128, 64, 256, 10, 5), (128, 64, 32, 17, 1)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_against_64_bits(lens, news, d, group, page, Hq, H, causal):
+    g = torch.Generator().manual_seed(sum(lens) + d + Hq)
+    p = CacheParams(H=H, d=d, page=page, group=group)
+    f = Filled(lens, p, g)
+    v_mean = torch.randn((H, d), generator=g).cuda() if page == 64 else None
+    sm = 0.3 if page == 32 else 0.0
+    q, cu, O, lse = _attend(f, news, Hq, g, causal=causal, sm_scale=sm, v_mean=v_mean)
+    _check(f, q, cu, O, lse, causal, sm, v_mean)
+
+
+@pytest.mark.parametrize("d,group,page,Hq,H,n,L", [(64, 32, 32, 4, 4, 1, 777), (128, 64, 64, 4, 1, 1, 1025), (128, 32, 64, 32, 2, 3, 300), (64, 64, 256, 16, 2, 40, 333),
+                                                   (128, 64, 128, 8, 2, 150, 400)])
+def test_every_token_is_weighed_alone(d, group, page, Hq, H, n, L):
+    """One query row in turn points at one key so sharply that its value alone comes out: a token left out, read twice or given another's
+    scale shows whole."""
+    g = torch.Generator().manual_seed(L)
+    p = CacheParams(H=H, d=d, page=page, group=group)
+    f = Filled([L], p, g)
+    G = Hq // H
+    for start in range(0, L, n * G):
+        q = torch.zeros((n, Hq, d))
+        target = np.zeros((n, Hq), int)
+        for i in range(n):
+            for h in range(Hq):
+                t = (start + i * G + h % G) % L
+                target[i, h] = t
+                q[i, h] = torch.tensor(f.k[t, h // G] * 8)
+        _, _, O, lse = _attend(f, [n], Hq, g, causal=False, sm_scale=1.0, q=q.to(torch.bfloat16))
+        O = _np(O)
+        for h in range(Hq):
+            want = f.v[target[:, h], h // G]
+            # (another key's logit is 8 |k|^2 less 8 k.k' below: hundreds; P times the scale and O are rounded to bf16)
+            assert np.abs(O[:, h] - want).max() <= 2.0 ** -7 * np.abs(want).max()
+        if start > 6 * n * G:
+            break
+
+
+def test_the_mask_hides_infinities_and_nan():
+    """Keys and values that are NaN are seen by the rows whose mask lets them, and by no other."""
+    g = torch.Generator().manual_seed(8)
+    for d, n, Hq in ((128, 9, 2), (64, 40, 4)):
+        p = CacheParams(H=2, d=d, page=32)
+        f = Filled([100], p, g)
+        f.K[97, 0, 3], f.V[96, 1, 5] = math.nan, math.inf
+        f.store()
+        q, cu, O, lse = _attend(f, [n], Hq, g)
+        k, v = f.k.copy(), f.v.copy()
+        O = O.float().cpu().numpy()
+        G = Hq // 2
+        for i in range(n):
+            sees = 100 - n + i + 1
+            assert np.isnan(O[i, :G]).all() == (sees > 97) and np.isfinite(O[i, :G]).all() == (sees <= 97)
+            bad = np.isnan(O[i, G:]).reshape(G, d)
+            assert bad[:, :64].all() == (sees > 96) if d == 64 else bad.any() == (sees > 96)
+            if sees <= 96:
+                assert np.isfinite(O[i]).all()
+
+
+def test_pages_that_do_not_exist_are_not_attended_to():
+    g = torch.Generator().manual_seed(9)
+    p = CacheParams(H=2, d=128, page=32)
+    f = Filled([320, 96], p, g)
+    q, cu, O, lse = _attend(f, [1, 1], 4, g, causal=False)
+    table = f.table.clone()
+    f.table[0, 3], f.table[0, 7], f.table[1, :3] = -1, f.pool.shape[0], _i32([-7, 1 << 30, -(1 << 31)])
+    keep = np.array([t for t in range(320) if t // 32 not in (3, 7)])
+    _, _, O2, lse2 = _attend(f, [1, 1], 4, g, causal=False, q=q)
+    whole = f.k, f.v, f.at
+    f.k, f.v, f.at = np.concatenate([f.k[keep], f.k[320:]]), np.concatenate([f.v[keep], f.v[320:]]), np.array([0, 256, 352])
+    _check(f, q, cu, O2, lse2, False, requests=[0])
+    assert (O2[1] == 0).all() and torch.isinf(lse2[:, 1]).all()
+    f.k, f.v, f.at = whole
+    f.table.copy_(table)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_batches(seed):
+    rng = np.random.default_rng(seed)
+    g = torch.Generator().manual_seed(seed)
+    d, group, page = int(rng.choice([64, 128])), int(rng.choice([32, 64])), int(rng.choice([32, 64, 128, 256]))
+    H = int(rng.integers(1, 6))
+    Hq = H * int(rng.choice([1, 2, 3, 4, 7, 8, 16, 33, 64]))
+    R = int(rng.integers(1, 40))
+    lens = [int(x) for x in np.exp(rng.uniform(0, math.log(1500), R))]
+    kind = rng.choice(["decode", "few", "mixed"])
+    news = [1 if kind == "decode" or (kind == "mixed" and rng.random() < 0.8) else int(rng.integers(0, 7 if kind == "few" else 200)) for _ in range(R)]
+    if Hq * sum(n * a for n, a in zip(news, lens)) > 4e7:
+        news = [min(n, 2) for n in news]
+    if sum(news) == 0:
+        news[0] = 1
+    p = CacheParams(H=H, d=d, page=page, group=group)
+    f = Filled(lens, p, g, sigma=float(rng.choice([0.1, 1.0, 4.0])))
+    causal = bool(rng.integers(2))
+    v_mean = torch.randn((H, d), generator=g).cuda() if rng.integers(2) else None
+    q, cu, O, lse = _attend(f, news, Hq, g, causal=causal, v_mean=v_mean)
+    check = rng.permutation(R)[:6].tolist()
+    _check(f, q, cu, O, lse, causal, 0.0, v_mean, requests=check)
+
+
+def test_more_requests_than_threads():
+    g = torch.Generator().manual_seed(4)
+    lens = [(37 * r) % 90 for r in range(700)]
+    f = Filled(lens, CacheParams(H=1, d=64, page=32), g)
+    q, cu, O, lse = _attend(f, [r % 3 for r in range(700)], 2, g)
+    _check(f, q, cu, O, lse, True, requests=list(range(0, 700, 13)) + [698, 699])
+
+
+def test_strided_queries_rows_behind_the_last_request_and_a_dirty_workspace():
+    g = torch.Generator().manual_seed(6)
+    p = CacheParams(H=2, d=128, page=64)
+    for lens, news in (([200, 1500, 64], [1, 1, 1]), ([200, 900, 64], [30, 1, 64])):
+        f = Filled(lens, p, g)
+        T = sum(news)
+        qkv = _randn((T + 5, 4 + 4, 128), g).cuda()
+        q = qkv[:, 2:6]
+        q[T:] = math.nan
+        cu = _i32(np.concatenate([[0], np.cumsum(news)]).tolist())
+        O, lse = torch.full((T + 5, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((4, T + 5), 7.0, device="cuda")
+        n = cache.cache_workspace_bytes(p, 3, T + 5, 4, f.table.shape[1], max(news))
+        for fill in (0xFF, 0x00):
+            ws = torch.full((n,), fill, dtype=torch.uint8, device="cuda")
+            O.fill_(7.0), lse.fill_(7.0)
+            cache.sagebwd_cache_attention(q, f.pool, f.table, f.lengths, cu, p, max(news), O=O, LSE=lse, workspace=ws)
+            assert (O[T:] == 7).all() and (lse[:, T:] == 7).all()
+            _check(f, q[:T].cpu(), cu.tolist(), O[:T], lse[:, :T], True)
+        dense = cache.sagebwd_cache_attention(q[:T].contiguous(), f.pool, f.table, f.lengths, cu, p, max(news))
+        _check(f, q[:T].cpu(), cu.tolist(), *dense, True)
+        with pytest.raises(binding.SageError) as e:
+            cache.sagebwd_cache_attention(q, f.pool, f.table, f.lengths, cu, p, max(news), workspace=ws[:-256])
+        assert e.value.status == -3
+
+
+def test_the_bounds_of_the_call_hold_whatever_device_memory_says():
+    """Lengths and offsets that contradict the call's bounds are read as those bounds."""
+    g = torch.Generator().manual_seed(7)
+    p = CacheParams(H=1, d=64, page=32)
+    f = Filled([64, 64], p, g, spare_columns=0)
+    q = _randn((4, 2, 64), g)
+    O, lse = cache.sagebwd_cache_attention(q.cuda(), f.pool, f.table, _i32([1 << 30, -5]), _i32([0, 2, 1 << 30]), p, 2)
+    want, wl = cache.sagebwd_cache_attention(q.cuda(), f.pool, f.table, _i32([64, 0]), _i32([0, 2, 4]), p, 2)
+    assert torch.equal(O, want) and torch.equal(lse, wl)
+    O, lse = cache.sagebwd_cache_attention(q.cuda(), f.pool, f.table, _i32([64, 64]), _i32([0, 2, 4]), p, 2, max_length=40)
+    want, wl = cache.sagebwd_cache_attention(q.cuda(), f.pool, f.table, _i32([40, 40]), _i32([0, 2, 4]), p, 2)
+    assert torch.equal(O, want) and torch.equal(lse, wl)
+
+
+def test_offsets_beyond_32_bits():
+    p = CacheParams(H=8, d=128, page=64, group=32)
+    page_bytes = cache.cache_page_bytes(p)
+    pages = (5 << 30) // page_bytes
+    g = torch.Generator().manual_seed(2)
+    small = Filled([300, 40], p, g)
+    big = torch.empty((pages, p.H, page_bytes // p.H), dtype=torch.uint8, device="cuda")
+    shift = pages - small.pool.shape[0]
+    big[shift:] = 0xFF
+    table = torch.where(small.table >= 0, small.table + shift, small.table)
+    slots = small.slots + shift * p.page
+    cache.sagebwd_cache_append(small.K.cuda(), small.V.cuda(), slots, big, p)
+    assert torch.equal(big[shift:], small.pool)
+    a, b = cache.sagebwd_cache_read(slots, big, p), cache.sagebwd_cache_read(small.slots, small.pool, p)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    for news in ([1, 1], [100, 3]):
+        q, cu, O, lse = _attend(small, news, 16, g)
+        O2, lse2 = cache.sagebwd_cache_attention(q.cuda(), big, table, small.lengths, _i32(cu), p, max(news))
+        assert torch.equal(O, O2) and torch.equal(lse, lse2)
+
+
+def test_streams_repeats_and_two_calls_at_once():
+    g = torch.Generator().manual_seed(12)
+    p = CacheParams(H=2, d=128)
+    f1, f2 = Filled([900, 3000, 20], p, g), Filled([2500], p, g)
+    q1, cu1, O1, l1 = _attend(f1, [1, 2, 1], 8, g)
+    q2, cu2, O2, l2 = _attend(f2, [70], 8, g)
+    d1, d2, c1, c2 = q1.cuda(), q2.cuda(), _i32(cu1), _i32(cu2)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(4):
+        with torch.cuda.stream(s1):
+            a = cache.sagebwd_cache_attention(d1, f1.pool, f1.table, f1.lengths, c1, p, 2)
+        with torch.cuda.stream(s2):
+            b = cache.sagebwd_cache_attention(d2, f2.pool, f2.table, f2.lengths, c2, p, 70)
+        torch.cuda.synchronize()
+        assert torch.equal(a[0], O1) and torch.equal(a[1], l1) and torch.equal(b[0], O2) and torch.equal(b[1], l2)
