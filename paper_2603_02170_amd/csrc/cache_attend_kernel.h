@@ -61,16 +61,41 @@ __device__ __forceinline__ int attend_units(const AttendArgs& a, int r, int row0
   return max(1, (attend_visible(a, q, row0, count) + kUnit - 1) / kUnit);     // (rows without a key are an item too: zeros)
 }
 
-// Items are (request, key/value head), request after request, of attend_units units each; workgroup w of n has units
-// [w total / n, (w + 1) total / n).
-__device__ __forceinline__ int64_t attend_share(int64_t total, int n, int w) { return total * w / n; }
-
-// Two bf16 numbers 16 + n from nibble E of a word's half-words.
-template <int E>
-__device__ __forceinline__ int nibble_pair(int w) {
-  const unsigned u = (unsigned)w;
-  return (int)(((E == 0 ? u << 3 : u >> (4 * E - 3)) & 0x00780078u) | 0x41804180u);
+// Items are (request, key/value head), request after request, of attend_units units each; the units are dealt to the workgroups in
+// order, total / n each and one more to the first total % n.  (The host bounds the total by 2^30.)
+struct AttendShares {
+  int each, more, n;
+  __device__ __forceinline__ AttendShares(int total, int workgroups) {
+    n = min(workgroups, total);
+    each = n > 0 ? total / n : 0;
+    more = total - each * n;
+  }
+  __device__ __forceinline__ int begin(int w) const { return each * w + min(w, more); }
+  // the workgroup that has a unit
+  __device__ __forceinline__ int owner(int unit) const {
+    const int big = (each + 1) * more;
+    return unit < big ? unit / (each + 1) : more + (unit - big) / each;
+  }
+};
+__device__ __forceinline__ float wave_max_f32(float v) {
+  for (int k = 1; k < 64; k <<= 1) v = fmaxf(v, __shfl_xor(v, k));
+  return v;
 }
+
+// Two bf16 numbers 16 + n from nibble E of a word's half-words.  The AND and the OR are one instruction if the compiler does not see that
+// their constants are constants (two literals fit none), hence a register of each kind that it knows nothing about.
+struct Unpack {
+  int mask, sixteens;
+  __device__ __forceinline__ Unpack() : mask(0x00780078), sixteens(0x41804180) {
+    asm("" : "+s"(mask));
+    asm("" : "+v"(sixteens));
+  }
+  template <int E>
+  __device__ __forceinline__ int pair(int w) const {
+    const unsigned u = (unsigned)w;
+    return (int)((E == 0 ? u << 3 : u >> (4 * E - 3)) & (unsigned)mask) | sixteens;
+  }
+};
 __device__ __forceinline__ v8bf as_bf16(const v4i& x) {
   v8bf r;
   __builtin_memcpy(&r, &x, 16);
@@ -95,36 +120,57 @@ __device__ __forceinline__ float column_sum(float v) {
   return half_swap_sum_f32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-// 32 tokens of a head as a lane (column m, g) takes them.
+// 32 tokens of a head.  They come past the registers into a ring of the wave's own in LDS (K's codes, V's, the scales, as they lie in
+// the page), two to three tiles ahead; a lane (column m, g) then takes its operands.  (In registers one tile ahead was all that fitted, and
+// the 16 lanes of a group each fetched the same scales: 61 us for 64 requests that now take RINGUS.)
 template <int D, int GROUP>
 struct CacheTile {
-  int k[2][D / 32];       // token 8 (m / 4) + m % 4 (+ 4), channels of quarter g
-  v4i v[D / 64];          // octet g, channels m + 16 j of each half
-  v4i ks[D / GROUP], vs[D / GROUP];   // octet g
-  bool exists;
+  static constexpr int NG = D / GROUP, CODES = 16 * D, SCALES = 64 * NG, SLOT = 2 * CODES + (2 * SCALES > 256 ? 2 * SCALES : 256);
+  static constexpr int COPIES = 2 * CODES / 1024 + (NG == 4 ? 2 : 1);
 
-  __device__ __forceinline__ void load(const AttendArgs& a, const int32_t* table, int head, int t0) {
-    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-    const int entry = __builtin_amdgcn_readfirstlane(table[t0 >> a.g.page_shift]);
-    exists = (unsigned)entry < (unsigned)a.g.pages;
-    const unsigned char* p = a.pool + (size_t)(exists ? entry : 0) * a.g.page_bytes() + (size_t)head * a.g.head_bytes();
-    const int at = t0 & (a.g.page() - 1), octet = (at >> 3) + g;
-    const unsigned char* pk = p + (at + 8 * (m >> 2) + (m & 3)) * (D / 2) + g * (D / 8);
-    if (D == 128) {
-      const v4i x = *(const v4i*)pk, y = *(const v4i*)(pk + 4 * (D / 2));
+  v4i v[D / 64];          // octet g, channels m + 16 j of each half
+  int k[2][D / 32];       // token 8 (m / 4) + m % 4 (+ 4), channels of quarter g
+  v4i ks[NG], vs[NG];     // octet g
+
+  // Starts the copies of the 32 tokens from `at` of a page; `p` is the head's part of it.
+  static __device__ __forceinline__ void fetch(const CacheGeometry& geo, const unsigned char* p, int at, char* slot) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-      for (int j = 0; j < D / 32; j++) { k[0][j] = x[j]; k[1][j] = y[j]; }
+    for (int c = 0; c < CODES / 1024; c++) {
+      copy_16(uniform(p + at * (D / 2) + c * 1024) + lane * 16, slot + c * 1024);
+      copy_16(uniform(p + geo.v_codes() + at * (D / 2) + c * 1024) + lane * 16, slot + CODES + c * 1024);
+    }
+    const gbytes_t ps = uniform(p + geo.k_scales() + at * (2 * NG));
+    const int apart = geo.v_scales() - geo.k_scales();
+    if (NG == 4) {
+      copy_4(ps + lane * 4, slot + 2 * CODES);
+      copy_4(ps + (unsigned)(apart + lane * 4), slot + 2 * CODES + SCALES);
     } else {
-      const v2i x = *(const v2i*)pk, y = *(const v2i*)(pk + 4 * (D / 2));
+      const int l = lane % (32 * NG);        // (with one group the upper half of the lanes copies the same to where nothing is read)
+      copy_4(ps + (unsigned)(l < 16 * NG ? 4 * l : apart + 4 * l - SCALES), slot + 2 * CODES);
+    }
+  }
+  __device__ __forceinline__ void take(const char* slot) {
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const char* pk = slot + (8 * (m >> 2) + (m & 3)) * (D / 2) + g * (D / 8);
 #pragma unroll
-      for (int j = 0; j < D / 32; j++) { k[0][j] = x[j]; k[1][j] = y[j]; }
+    for (int b = 0; b < 2; b++) {
+      if (D == 128) {
+        const v4i x = *(const v4i*)(pk + b * 4 * (D / 2));
+#pragma unroll
+        for (int j = 0; j < D / 32; j++) k[b][j] = x[j];
+      } else {
+        const v2i x = *(const v2i*)(pk + b * 4 * (D / 2));
+#pragma unroll
+        for (int j = 0; j < D / 32; j++) k[b][j] = x[j];
+      }
     }
 #pragma unroll
-    for (int f = 0; f < D / 64; f++) v[f] = *(const v4i*)(p + a.g.v_codes() + octet * (4 * D) + f * 256 + m * 16);
+    for (int f = 0; f < D / 64; f++) v[f] = *(const v4i*)(slot + CODES + g * (4 * D) + f * 256 + m * 16);
 #pragma unroll
-    for (int s = 0; s < D / GROUP; s++) {
-      ks[s] = *(const v4i*)(p + a.g.k_scales() + (octet * (D / GROUP) + s) * 16);
-      vs[s] = *(const v4i*)(p + a.g.v_scales() + (octet * (D / GROUP) + s) * 16);
+    for (int s = 0; s < NG; s++) {
+      ks[s] = *(const v4i*)(slot + 2 * CODES + (g * NG + s) * 16);
+      vs[s] = *(const v4i*)(slot + 2 * CODES + SCALES + (g * NG + s) * 16);
     }
   }
 };
@@ -139,16 +185,20 @@ struct AttendRows {
   float m, l;           // reference (log2), this lane's part of the sum
   int sees;             // keys that the query sees
 
-  __device__ __forceinline__ void begin(const AttendArgs& a, const AttendRequest& rq, int head, int row0) {
+  __device__ __forceinline__ void fetch(const AttendArgs& a, const AttendRequest& rq, int head, int row0) {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int row = row0 + n, i = row / a.G;
     const bool exists = row < rq.rows;
     const __bf16* p = a.Q + (int64_t)(rq.begin + (exists ? i : 0)) * a.q_token + (int64_t)(head * a.G + (exists ? row - i * a.G : 0)) * a.q_head + 8 * g;
 #pragma unroll
+    for (int j = 0; j < NJ; j++) q[j] = exists ? *(const v4i*)(p + 32 * j) : v4i{0, 0, 0, 0};
+    sees = exists && a.causal ? min(rq.len, rq.first_sees + i) : rq.len;
+  }
+  __device__ __forceinline__ void begin() {
+#pragma unroll
     for (int s = 0; s < NG; s++) start[s] = 0.f;
 #pragma unroll
     for (int j = 0; j < NJ; j++) {
-      q[j] = exists ? *(const v4i*)(p + 32 * j) : v4i{0, 0, 0, 0};
       float t = 0.f;
 #pragma unroll
       for (int e = 0; e < 4; e++) t += low_bf16(q[j][e]) + high_bf16(q[j][e]);
@@ -160,84 +210,99 @@ struct AttendRows {
     for (int v = 0; v < NV; v++) o[v] = v4f{0.f, 0.f, 0.f, 0.f};
     m = -INFINITY;
     l = 0.f;
-    sees = a.causal ? min(rq.len, rq.first_sees + i) : rq.len;
-    if (!exists) sees = rq.len;
   }
+};
 
-  template <bool MASKED>
-  __device__ __forceinline__ void add(const CacheTile<D, GROUP>& t, int t0, float scale_log2) {
-    const int g = (threadIdx.x & 63) >> 4;
-    float s[8];
+// 32 tokens into NQ tiles of queries.  `masked`: some row does not see all of them.
+template <int D, int GROUP, int NQ>
+__device__ __forceinline__ void attend_tile(AttendRows<D, GROUP> (&rows)[NQ], CacheTile<D, GROUP>& t, int t0, bool masked, float scale_log2, const Unpack& un) {
+  constexpr int NG = D / GROUP;
+  const int g = (threadIdx.x & 63) >> 4;
+  float s[NQ][8];
 #pragma unroll
-    for (int b = 0; b < 2; b++) {
+  for (int b = 0; b < 2; b++) {
 #pragma unroll
-      for (int gr = 0; gr < NG; gr++) {
-        v4f c = {start[gr], start[gr], start[gr], start[gr]};
+    for (int gr = 0; gr < NG; gr++) {
+      v4f c[NQ];
 #pragma unroll
-        for (int j = gr * GROUP / 32; j < (gr + 1) * GROUP / 32; j++) {
-          const int w = t.k[b][j];
-          const v4i k = {nibble_pair<0>(w), nibble_pair<1>(w), nibble_pair<2>(w), nibble_pair<3>(w)};
-          c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(k), as_bf16(q[j]), c, 0, 0, 0);
-        }
+      for (int q = 0; q < NQ; q++) c[q] = v4f{rows[q].start[gr], rows[q].start[gr], rows[q].start[gr], rows[q].start[gr]};
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const int w = t.ks[gr][2 * b + i / 2];
-          const float x = i % 2 == 0 ? low_bf16(w) : high_bf16(w);
-          s[4 * b + i] = gr == 0 ? x * c[i] : __builtin_fmaf(x, c[i], s[4 * b + i]);
-        }
+      for (int j = gr * GROUP / 32; j < (gr + 1) * GROUP / 32; j++) {
+        const int w = t.k[b][j];
+        const v8bf k = as_bf16(v4i{un.pair<0>(w), un.pair<1>(w), un.pair<2>(w), un.pair<3>(w)});
+#pragma unroll
+        for (int q = 0; q < NQ; q++) c[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, as_bf16(rows[q].q[j]), c[q], 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const int w = t.ks[gr][2 * b + i / 2];
+        const float x = i % 2 == 0 ? low_bf16(w) : high_bf16(w);
+#pragma unroll
+        for (int q = 0; q < NQ; q++) s[q][4 * b + i] = gr == 0 ? x * c[q][i] : __builtin_fmaf(x, c[q][i], s[q][4 * b + i]);
       }
     }
-    const int behind = sees - t0 - 8 * g;        // tokens of the octet that the query sees
+  }
+  __builtin_amdgcn_sched_barrier(0);           // (left to itself the compiler unpacks everything first, which the registers do not hold)
+  v8bf pt[NQ][NG];
+#pragma unroll
+  for (int q = 0; q < NQ; q++) {
+    AttendRows<D, GROUP>& R = rows[q];
+    int seen[4] = {-1, -1, -1, -1};              // of the octet's scales of V: one that is not seen may be anything
+    if (masked) {
+      const int behind = R.sees - t0 - 8 * g;    // tokens of the octet that the query sees
+#pragma unroll
+      for (int i = 0; i < 8; i++) s[q][i] = i < behind ? s[q][i] : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; i++) seen[i] = (2 * i < behind ? 0xFFFF : 0) | (2 * i + 1 < behind ? (int)0xFFFF0000 : 0);
+    }
     float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      if (MASKED) s[i] = i < behind ? s[i] : -INFINITY;
-      top = fmaxf(top, s[i]);
-    }
+    for (int i = 0; i < 8; i++) top = fmaxf(top, s[q][i]);
     // The reference only has to be near the maximum: it is raised where a logit is 2^8 above it (O / l and m + log l do not depend on it).
-    if (__any(top * scale_log2 > m + 8.f)) {
-      const float to = fmaxf(m, column_max(top) * scale_log2);
-      const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+    if (__any(top * scale_log2 > R.m + 8.f)) {
+      const float to = fmaxf(R.m, column_max(top) * scale_log2);
+      const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(R.m - to);
 #pragma unroll
-      for (int v = 0; v < NV; v++) o[v] *= f;
-      l *= f;
-      m = to;
+      for (int v = 0; v < D / 16; v++) R.o[v] *= f;
+      R.l *= f;
+      R.m = to;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
+    const float ref = R.m == -INFINITY ? 0.f : R.m;
     float p[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale_log2, -ref));
-      l += p[i];
+      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][i], scale_log2, -ref));
+      R.l += p[i];
     }
-    const int minus24 = (int)0xC1C0C1C0;
-    const v8bf less = as_bf16(v4i{minus24, minus24, minus24, minus24});
 #pragma unroll
     for (int gr = 0; gr < NG; gr++) {
       v4i pb;
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        const int w = t.vs[gr][i];
-        float x = p[2 * i] * low_bf16(w), y = p[2 * i + 1] * high_bf16(w);
-        if (MASKED) {              // (the scale of a token that is not seen may be anything)
-          x = 2 * i < behind ? x : 0.f;
-          y = 2 * i + 1 < behind ? y : 0.f;
-        }
-        pb[i] = pack_bf16(x, y);
+        const int w = t.vs[gr][i] & seen[i];
+        pb[i] = pack_bf16(p[2 * i] * low_bf16(w), p[2 * i + 1] * high_bf16(w));
       }
-      const v8bf pt = as_bf16(pb);
-#pragma unroll
-      for (int v = gr * GROUP / 16; v < (gr + 1) * GROUP / 16; v++) {
-        const v4i& w = t.v[v / 4];
-        v4i x;
-#pragma unroll
-        for (int i = 0; i < 4; i++) x[i] = v % 4 == 0 ? nibble_pair<0>(w[i]) : v % 4 == 1 ? nibble_pair<1>(w[i]) : v % 4 == 2 ? nibble_pair<2>(w[i]) : nibble_pair<3>(w[i]);
-        o[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(less, pt, o[v], 0, 0, 0);
-        o[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(x), pt, o[v], 0, 0, 0);
-      }
+      pt[q][gr] = as_bf16(pb);
     }
   }
-};
+  __builtin_amdgcn_sched_barrier(0);
+  const int minus24 = (int)0xC1C0C1C0;
+  const v8bf less = as_bf16(v4i{minus24, minus24, minus24, minus24});
+#pragma unroll
+  for (int v = 0; v < D / 16; v++) {
+    const v4i& w = t.v[v / 4];
+    v4i x;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      x[i] = v % 4 == 0 ? un.pair<0>(w[i]) : v % 4 == 1 ? un.pair<1>(w[i]) : v % 4 == 2 ? un.pair<2>(w[i]) : un.pair<3>(w[i]);
+#pragma unroll
+    for (int q = 0; q < NQ; q++) {
+      rows[q].o[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(less, pt[q][16 * v / GROUP], rows[q].o[v], 0, 0, 0);
+      rows[q].o[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(x), pt[q][16 * v / GROUP], rows[q].o[v], 0, 0, 0);
+    }
+    if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+  }
+}
 
 // Writes channels c .. c + N - 1 of a finished row.
 template <int N>
@@ -255,103 +320,121 @@ __device__ __forceinline__ void attend_store(const AttendArgs& a, const AttendRe
   if (c == 0 && a.LSE != nullptr) a.LSE[(int64_t)hq * a.T + token] = any ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
 }
 
+constexpr int kStages = 4;          // tiles of a wave's ring
+
 template <int D, int GROUP, int NQ>
 __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(AttendArgs a) {
-  constexpr int ROWS = 16 * NQ, PITCH = D + 4, NC = D / 16;
-  __shared__ float stage[4][16][PITCH];
+  typedef CacheTile<D, GROUP> Tile;
+  constexpr int ROWS = 16 * NQ, PITCH = D + 4, NC = D / 16, RING = kStages * Tile::SLOT;
+  // the ring of every wave, then, when an item's keys are through, their sums of 16 rows each
+  __shared__ __attribute__((aligned(16))) char lds[4 * RING > 4 * 16 * PITCH * 4 ? 4 * RING : 4 * 16 * PITCH * 4];
+  float (*stage)[16][PITCH] = (float (*)[16][PITCH])lds;
   __shared__ float wave_m[4][ROWS], wave_l[4][ROWS];
-  __shared__ int64_t wave_units[4];
-  __shared__ int found_request;
-  __shared__ int64_t found_prefix;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ int wave_units[4], found[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int H = a.g.H, row0 = blockIdx.y * ROWS;
+  char* ring = lds + wave * RING;
+  const Unpack un;
 
   // units up to every thread's requests (R / 256 each)
   const int per = (a.R + 255) / 256, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
-  int64_t mine = 0;
+  int mine = 0;
   for (int r = r0; r < r1; r++) mine += attend_units(a, r, row0, ROWS);
-  int64_t upto = mine;
+  int upto = mine;
   for (int k = 1; k < 64; k <<= 1) {
-    const int64_t u = __shfl_up(upto, k);
+    const int u = __shfl_up(upto, k);
     if (lane >= k) upto += u;
   }
   if (lane == 63) wave_units[wave] = upto;
   __syncthreads();
-  int64_t units = 0;
+  int units = 0;
 #pragma unroll
   for (int k = 0; k < 4; k++) {
     if (k < wave) upto += wave_units[k];
     units += wave_units[k];
   }
-  const int64_t total = units * H;
-  const int n = (int)min((int64_t)a.workgroups, total);
   if (blockIdx.x == 0) {           // for the launch that joins
     int32_t* prefix = a.prefix + (size_t)blockIdx.y * (a.R + 1);
-    int64_t at = upto - mine;
+    int at = upto - mine;
     for (int r = r0; r < r1; r++) {
-      prefix[r] = (int)at;
+      prefix[r] = at;
       at += attend_units(a, r, row0, ROWS);
     }
-    if (tid == 0) prefix[a.R] = (int)units;
+    if (tid == 0) prefix[a.R] = units;
   }
-  if ((int)blockIdx.x >= n) return;
-  int64_t x = attend_share(total, n, blockIdx.x);
-  const int64_t end = attend_share(total, n, blockIdx.x + 1);
+  const AttendShares shares(__builtin_amdgcn_readfirstlane(units) * H, a.workgroups);
+  if ((int)blockIdx.x >= shares.n) return;
+  int x = shares.begin(blockIdx.x);
+  const int end = shares.begin(blockIdx.x + 1);
   if ((upto - mine) * H <= x && x < upto * H) {
-    int64_t at = upto - mine;
+    int at = upto - mine;
     for (int r = r0; r < r1; r++) {
       const int u = attend_units(a, r, row0, ROWS);
       if (x < (at + u) * H) {
-        found_request = r;
-        found_prefix = at;
+        found[0] = r;
+        found[1] = at;
         break;
       }
       at += u;
     }
   }
   __syncthreads();
-  int r = __builtin_amdgcn_readfirstlane(found_request);
-  int64_t prefix = found_prefix;
+  int r = __builtin_amdgcn_readfirstlane(found[0]), prefix = __builtin_amdgcn_readfirstlane(found[1]);
 
   while (x < end) {
-    const int u = __builtin_amdgcn_readfirstlane(attend_units(a, r, row0, ROWS));
-    const int64_t rel = x - prefix * H;
-    if (rel >= (int64_t)u * H) {    // the next request
+    const AttendRequest rq = attend_request(a, r);
+    const int visible = __builtin_amdgcn_readfirstlane(attend_visible(a, rq, row0, ROWS));
+    const int u = __builtin_amdgcn_readfirstlane(rq.rows > row0 ? max(1, (visible + kUnit - 1) / kUnit) : 0);
+    const int rel = x - prefix * H;
+    if (rel >= u * H) {    // the next request
       prefix += u;
       r++;
       continue;
     }
-    const AttendRequest rq = attend_request(a, r);
-    const int head = __builtin_amdgcn_readfirstlane((int)(rel / u)), j0 = __builtin_amdgcn_readfirstlane((int)(rel % u));
-    const int j1 = __builtin_amdgcn_readfirstlane((int)min((int64_t)u, j0 + (end - x)));
+    const int head = rel / u, j0 = rel - head * u, j1 = min(u, j0 + (end - x));
     x += j1 - j0;
     AttendRows<D, GROUP> rows[NQ];
 #pragma unroll
-    for (int q = 0; q < NQ; q++) rows[q].begin(a, rq, head, row0 + 16 * q);
-    const int visible = attend_visible(a, rq, row0, ROWS);
-    const int all_see = a.causal ? rq.first_sees + row0 / a.G : rq.len;       // keys that every row of the tile sees
+    for (int q = 0; q < NQ; q++) rows[q].fetch(a, rq, head, row0 + 16 * q);
+    const int all_see = __builtin_amdgcn_readfirstlane(a.causal ? rq.first_sees + row0 / a.G : rq.len);       // keys that every row of the tile sees
     const int32_t* table = a.table + (size_t)r * a.columns;
-    CacheTile<D, GROUP> tile;
-    int t0 = j0 * kUnit + wave * 32;
-    if (t0 < visible) tile.load(a, table, head, t0);
-    for (int j = j0; j < j1 && t0 < visible; j++, t0 += kUnit) {
-      CacheTile<D, GROUP> next;
-      const bool more = j + 1 < j1 && t0 + kUnit < visible;
-      if (more) next.load(a, table, head, t0 + kUnit);
-      if (tile.exists) {
-        if (t0 + 32 > all_see) {
+    const int first = j0 * kUnit + wave * 32;                              // the wave's tiles: every 128 tokens from here
+    const int count = max(0, min(j1 - j0, (visible - first + kUnit - 1) / kUnit));
+    // A lane has the page of one of the wave's next 64 tiles: a tile's address then waits for no load.
+    const auto pages_from = [&](int k) { return table[min(first + (k + lane) * kUnit, max(visible - 1, 0)) >> a.g.page_shift]; };
+    int pages = pages_from(0);
+    unsigned exists = 0;                                                   // of the tiles in the ring
+    const auto fetch = [&](int k) {
+      if (k % 64 == 0 && k != 0) pages = pages_from(k);
+      const int entry = __builtin_amdgcn_readlane(pages, k % 64);
+      const bool ok = (unsigned)entry < (unsigned)a.g.pages;
+      const unsigned bit = 1u << (k % kStages);
+      exists = ok ? exists | bit : exists & ~bit;
+      const unsigned char* p = a.pool + (size_t)(ok ? entry : 0) * a.g.page_bytes() + (size_t)(head * a.g.head_bytes());
+      Tile::fetch(a.g, p, (first + k * kUnit) & (a.g.page() - 1), ring + k % kStages * Tile::SLOT);
+    };
+    for (int k = 0; k < kStages - 1 && k < count; k++) fetch(k);
 #pragma unroll
-          for (int q = 0; q < NQ; q++) rows[q].template add<true>(tile, t0, a.scale_log2);
-        } else {
-#pragma unroll
-          for (int q = 0; q < NQ; q++) rows[q].template add<false>(tile, t0, a.scale_log2);
-        }
-      }
-      if (more) tile = next;
+    for (int q = 0; q < NQ; q++) rows[q].begin();
+    for (int k = 0; k < count; k++) {
+      compiler_fence();
+      if (k + kStages - 1 < count) fetch(k + kStages - 1);
+      compiler_fence();
+      const int behind = min(count - 1 - k, kStages - 1);                  // tiles on their way behind this one
+      if (behind >= 3) __builtin_amdgcn_s_waitcnt(vmcnt_only(3 * Tile::COPIES));
+      else if (behind == 2) __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * Tile::COPIES));
+      else if (behind == 1) __builtin_amdgcn_s_waitcnt(vmcnt_only(Tile::COPIES));
+      else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+      compiler_fence();
+      if ((exists >> (k % kStages) & 1) == 0) continue;
+      const int t0 = first + k * kUnit;
+      Tile tile;
+      tile.take(ring + k % kStages * Tile::SLOT);
+      attend_tile<D, GROUP, NQ>(rows, tile, t0, t0 + 32 > all_see, a.scale_log2, un);
     }
     // join the waves
     const bool whole = j0 == 0 && j1 == u;
-    const int64_t slot = ((int64_t)blockIdx.y * a.workgroups + blockIdx.x) * 2 + (j0 == 0 ? 1 : 0);
+    const size_t slot = ((size_t)blockIdx.y * a.workgroups + blockIdx.x) * 2 + (j0 == 0 ? 1 : 0);
 #pragma unroll
     for (int q = 0; q < NQ; q++) {
       const float l = column_sum(rows[q].l);
@@ -393,46 +476,69 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
   }
 }
 
-// Items that several workgroups had parts of.  Workgroup (w, rows) looks at the border in front of workgroup w's share and joins the item
-// that it divides, if it is the first border to do so: the parts in the order of the keys.  A wave has a row.
+// Items that several workgroups had parts of.  Workgroup (w, row) looks at the border in front of workgroup w's share and joins the item
+// that it divides, if it is the first border to do so.  Every lane weighs a part; then the four waves take every fourth part, several
+// loads in flight (one wave a row and one part after the other: 97 us for the 128 parts of a request alone, now JOINUS), and meet in LDS:
+// the order of the sums does not depend on timing.
 template <int D, int NQ>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
-  constexpr int ROWS = 16 * NQ, NC = D / 64;
+  constexpr int ROWS = 16 * NQ, NC = D / 64, MOST = 256;
+  __shared__ float weight[MOST], meet[4][D + 2];
   const int32_t* prefix = a.prefix + (size_t)blockIdx.z * (a.R + 1);
   const int H = a.g.H;
-  const int64_t total = (int64_t)prefix[a.R] * H;
-  const int n = (int)min((int64_t)a.workgroups, total), w = blockIdx.x + 1;
-  if (w >= n) return;
-  const int64_t border = attend_share(total, n, w);
+  const AttendShares shares(prefix[a.R] * H, a.workgroups);
+  const int w = blockIdx.x + 1;
+  if (w >= shares.n) return;
+  const int border = shares.begin(w);
   int r = 0;
   for (int hi = a.R; hi - r > 1;) {
     const int mid = (r + hi) >> 1;
-    if ((int64_t)prefix[mid] * H <= border) r = mid;
+    if (prefix[mid] * H <= border) r = mid;
     else hi = mid;
   }
-  const int u = prefix[r + 1] - prefix[r];
-  const int64_t rel = border - (int64_t)prefix[r] * H;
-  const int head = (int)(rel / u);
-  const int64_t first = border - rel % u, last = first + u;
-  if (first == border || attend_share(total, n, w - 1) > first) return;
+  const int u = prefix[r + 1] - prefix[r], rel = border - prefix[r] * H, head = rel / u;
+  const int first = border - (rel - head * u), last = first + u;
+  if (first == border || shares.begin(w - 1) > first) return;
   const AttendRequest rq = attend_request(a, r);
-  const int lane = threadIdx.x & 63, k = blockIdx.y * 4 + (threadIdx.x >> 6), row = blockIdx.z * ROWS + k;
+  const int k = blockIdx.y, row = blockIdx.z * ROWS + k;
   if (row >= rq.rows) return;
-  const int64_t slot0 = ((int64_t)blockIdx.z * a.workgroups + w) * 2;
-  float M = a.stats[(slot0 - 1) * ROWS + k].x;
-  int parts = 1;
-  for (; attend_share(total, n, w + parts - 1) < last; parts++) M = fmaxf(M, a.stats[(slot0 + 2 * (parts - 1)) * ROWS + k].x);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const size_t slot0 = ((size_t)blockIdx.z * a.workgroups + w) * 2;
+  const int parts = shares.owner(last - 1) - w + 2;        // of workgroups w - 1 .. the one that has the last unit
+  const auto at = [&](int p) { return (p == 0 ? slot0 - 1 : slot0 + 2 * (p - 1)) * ROWS + k; };
+  float M = -INFINITY;
+  for (int p = lane; p < parts; p += 64) M = fmaxf(M, a.stats[at(p)].x);
+  M = wave_max_f32(M);
   float o[NC], l = 0.f;
 #pragma unroll
   for (int i = 0; i < NC; i++) o[i] = 0.f;
-  for (int p = 0; p < parts; p++) {
-    const int64_t at = (p == 0 ? slot0 - 1 : slot0 + 2 * (p - 1)) * ROWS + k;
-    const float2 s = a.stats[at];
-    const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - M);
-    l += s.y * f;
+  for (int p0 = 0; p0 < parts; p0 += MOST) {
+    const int here = min(parts - p0, MOST);
+    __syncthreads();
+    if (tid < here) {
+      const float2 s = a.stats[at(p0 + tid)];
+      const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - M);
+      weight[tid] = f;
+      l += s.y * f;
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int p = wave; p < here; p += 4) {
+      const float f = weight[p];
+      const float* x = a.sums + at(p0 + p) * D + NC * lane;
 #pragma unroll
-    for (int i = 0; i < NC; i++) o[i] += a.sums[at * D + NC * lane + i] * f;
+      for (int i = 0; i < NC; i++) o[i] += x[i] * f;
+    }
   }
+#pragma unroll
+  for (int i = 0; i < NC; i++) meet[wave][NC * lane + i] = o[i];
+  for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
+  if (lane == 0) meet[wave][D] = l;
+  __syncthreads();
+  if (wave != 0) return;
+  l = (meet[0][D] + meet[1][D]) + (meet[2][D] + meet[3][D]);
+#pragma unroll
+  for (int i = 0; i < NC; i++) o[i] = (meet[0][NC * lane + i] + meet[1][NC * lane + i]) + (meet[2][NC * lane + i] + meet[3][NC * lane + i]);
   attend_store<NC>(a, rq, head, row, D, NC * lane, M, l, o);
 }
 

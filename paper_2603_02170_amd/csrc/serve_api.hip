@@ -44,16 +44,17 @@ int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c) {
       !stride_ok(c->q_head_stride))
     return SAGEBWD_INVALID_ARG;
   if (c->Hq % p->H != 0 || c->Hq / p->H > 64 || (int64_t)c->T * c->Hq * p->d >= kMostElements || c->R > 1 << 20 ||
-      (int64_t)c->columns * p->page > INT32_MAX / 2 || (int64_t)c->T * (c->Hq / p->H) > INT32_MAX / 2)
+      (int64_t)c->columns * p->page > INT32_MAX / 2 || (int64_t)c->R * p->H * (c->columns * (int64_t)p->page / kUnit + 1) > 1 << 30 || (int64_t)c->T * (c->Hq / p->H) > INT32_MAX / 2)
     return SAGEBWD_UNSUPPORTED_SHAPE;
   return SAGEBWD_OK;
 }
 
-constexpr int kSlots = 1024;      // workgroups of the attention that the machine takes at a time, at most
+constexpr int kSlots = 512;      // workgroups of the attention that the machine takes at a time, at most
 
 // How a call is laid out: row tiles, workgroups, workspace.
 struct AttendPlan {
   int nq, row_tiles, workgroups, max_length;
+  int join_rows;      // of a tile, that any request has
   size_t prefix, sums, stats, total;
 };
 inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
@@ -67,6 +68,7 @@ AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& 
   const int64_t rows = most > 0 ? most : 1;
   w.nq = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   w.row_tiles = (int)((rows + 16 * w.nq - 1) / (16 * w.nq));
+  w.join_rows = (int)(rows < 16 * w.nq ? rows : 16 * w.nq);
   const int64_t units = (int64_t)c.R * p.H * ((w.max_length + kUnit - 1) / kUnit);
   const int64_t slots = kSlots / w.row_tiles > 8 ? kSlots / w.row_tiles : 8;
   w.workgroups = (int)(units < slots ? (units > 0 ? units : 1) : slots);
@@ -85,7 +87,7 @@ int launch_attend(const AttendArgs& a, const AttendPlan& w, hipStream_t st) {
   cache_attend_kernel<D, GROUP, NQ><<<dim3(w.workgroups, w.row_tiles), 256, 0, st>>>(a);
   SERVE_LAUNCH_CHECK();
   if (w.workgroups > 1) {
-    cache_join_kernel<D, NQ><<<dim3(w.workgroups - 1, 4 * NQ, w.row_tiles), 256, 0, st>>>(a);
+    cache_join_kernel<D, NQ><<<dim3(w.workgroups - 1, w.join_rows, w.row_tiles), 256, 0, st>>>(a);
     SERVE_LAUNCH_CHECK();
   }
   return SAGEBWD_OK;
