@@ -32,6 +32,7 @@ struct AttendArgs {
   float scale_log2;     // sm_scale * log2(e)
   int64_t q_token, q_head;
   int workgroups;
+  int split;            // 1: an item's units may go to several workgroups
 };
 
 constexpr int kUnit = 128;          // tokens that a workgroup of four waves takes at a time
@@ -121,7 +122,7 @@ __device__ __forceinline__ float column_sum(float v) {
 }
 
 // 32 tokens of a head.  They come past the registers into a ring of the wave's own in LDS (K's codes, V's, the scales, as they lie in
-// the page), two to three tiles ahead; a lane (column m, g) then takes its operands.  (In registers one tile ahead was all that fitted, and
+// the page), two tiles ahead; a lane (column m, g) then takes its operands.  (In registers one tile ahead was all that fitted, and
 // the 16 lanes of a group each fetched the same scales: 61 us for 64 requests that now take RINGUS.)
 template <int D, int GROUP>
 struct CacheTile {
@@ -185,14 +186,21 @@ struct AttendRows {
   float m, l;           // reference (log2), this lane's part of the sum
   int sees;             // keys that the query sees
 
-  __device__ __forceinline__ void fetch(const AttendArgs& a, const AttendRequest& rq, int head, int row0) {
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int row = row0 + n, i = row / a.G;
-    const bool exists = row < rq.rows;
-    const __bf16* p = a.Q + (int64_t)(rq.begin + (exists ? i : 0)) * a.q_token + (int64_t)(head * a.G + (exists ? row - i * a.G : 0)) * a.q_head + 8 * g;
+  int row, token, head_of;   // the lane's query row: new token, head of the group
+
+  __device__ __forceinline__ void place(const AttendArgs& a, int row0) {
+    row = row0 + (threadIdx.x & 15);
+    token = row / a.G;
+    head_of = row - token * a.G;
+  }
+  template <typename Piece>
+  __device__ __forceinline__ void fetch(const AttendArgs& a, const Piece& p) {
+    const int g = (threadIdx.x & 63) >> 4;
+    const bool exists = row < p.n_rows;
+    const __bf16* x = a.Q + (int64_t)(p.begin + (exists ? token : 0)) * a.q_token + (int64_t)(p.head * a.G + (exists ? head_of : 0)) * a.q_head + 8 * g;
 #pragma unroll
-    for (int j = 0; j < NJ; j++) q[j] = exists ? *(const v4i*)(p + 32 * j) : v4i{0, 0, 0, 0};
-    sees = exists && a.causal ? min(rq.len, rq.first_sees + i) : rq.len;
+    for (int j = 0; j < NJ; j++) q[j] = exists ? *(const v4i*)(x + 32 * j) : v4i{0, 0, 0, 0};
+    sees = exists && a.causal ? min(p.len, p.first_sees + token) : p.len;
   }
   __device__ __forceinline__ void begin() {
 #pragma unroll
@@ -249,6 +257,7 @@ __device__ __forceinline__ void attend_tile(AttendRows<D, GROUP> (&rows)[NQ], Ca
     AttendRows<D, GROUP>& R = rows[q];
     int seen[4] = {-1, -1, -1, -1};              // of the octet's scales of V: one that is not seen may be anything
     if (masked) {
+      asm volatile("");                          // (stays a branch: as selects it is a tenth of the tile's instructions)
       const int behind = R.sees - t0 - 8 * g;    // tokens of the octet that the query sees
 #pragma unroll
       for (int i = 0; i < 8; i++) s[q][i] = i < behind ? s[q][i] : -INFINITY;
@@ -306,9 +315,9 @@ __device__ __forceinline__ void attend_tile(AttendRows<D, GROUP> (&rows)[NQ], Ca
 
 // Writes channels c .. c + N - 1 of a finished row.
 template <int N>
-__device__ __forceinline__ void attend_store(const AttendArgs& a, const AttendRequest& rq, int head, int row, int D, int c, float m, float l, const float* o) {
+__device__ __forceinline__ void attend_store(const AttendArgs& a, int begin, int head, int row, int D, int c, float m, float l, const float* o) {
   const int i = row / a.G, hq = head * a.G + row - i * a.G;
-  const int64_t token = rq.begin + i;
+  const int64_t token = begin + i;
   const bool any = !(l == 0.f);
   const float r = any ? 1.f / l : 0.f;
   __bf16* p = a.O + (token * a.Hq + hq) * D + c;
@@ -320,26 +329,84 @@ __device__ __forceinline__ void attend_store(const AttendArgs& a, const AttendRe
   if (c == 0 && a.LSE != nullptr) a.LSE[(int64_t)hq * a.T + token] = any ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-constexpr int kStages = 4;          // tiles of a wave's ring
+constexpr int kStages = 3;          // tiles of a wave's ring
+
+// What a workgroup does with one item: units j0 .. j1 - 1 of the u of (request, head).  All of it is the same in every lane.
+struct AttendPiece {
+  int r, head, j0, j1, u;
+  int begin, n_rows, len, first_sees, visible;
+};
+
+// 64 requests at a time, one a lane: where one ends the next one's sizes are at hand.
+struct AttendCursor {
+  int base;                                                // request of lane 0
+  int begin, n_rows, len, first_sees, visible, units;      // of request base + lane
+  int r, head, j;                                          // the next piece begins here
+  int x, end;                                              // units taken, and to take
+
+  __device__ __forceinline__ void look(const AttendArgs& a, int from, int row0, int count) {
+    base = from;
+    const AttendRequest q = attend_request(a, min(from + (int)(threadIdx.x & 63), a.R - 1));
+    begin = q.begin;
+    n_rows = q.rows;
+    len = q.len;
+    first_sees = q.first_sees;
+    visible = q.rows > row0 ? attend_visible(a, q, row0, count) : 0;
+    units = q.rows > row0 ? max(1, (visible + kUnit - 1) / kUnit) : 0;
+  }
+  // (x < end)
+  __device__ __forceinline__ AttendPiece next(const AttendArgs& a, int row0, int count) {
+    AttendPiece p;
+    int at;
+    do {
+      if (r >= base + 64) look(a, r, row0, count);
+      at = r - base;
+      p.u = __builtin_amdgcn_readlane(units, at);
+      if (p.u == 0) r++;
+    } while (p.u == 0);
+    p.r = r;
+    p.head = head;
+    p.begin = __builtin_amdgcn_readlane(begin, at);
+    p.n_rows = __builtin_amdgcn_readlane(n_rows, at);
+    p.len = __builtin_amdgcn_readlane(len, at);
+    p.first_sees = __builtin_amdgcn_readlane(first_sees, at);
+    p.visible = __builtin_amdgcn_readlane(visible, at);
+    p.j0 = j;
+    p.j1 = a.split ? min(p.u, j + (end - x)) : p.u;
+    x += a.split ? p.j1 - p.j0 : 1;
+    j = p.j1;
+    if (j == p.u) {
+      j = 0;
+      if (++head == a.g.H) {
+        head = 0;
+        r++;
+      }
+    }
+    return p;
+  }
+};
 
 template <int D, int GROUP, int NQ>
 __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(AttendArgs a) {
   typedef CacheTile<D, GROUP> Tile;
-  constexpr int ROWS = 16 * NQ, PITCH = D + 4, NC = D / 16, RING = kStages * Tile::SLOT;
-  // the ring of every wave, then, when an item's keys are through, their sums of 16 rows each
-  __shared__ __attribute__((aligned(16))) char lds[4 * RING > 4 * 16 * PITCH * 4 ? 4 * RING : 4 * 16 * PITCH * 4];
-  float (*stage)[16][PITCH] = (float (*)[16][PITCH])lds;
+  constexpr int ROWS = 16 * NQ, PITCH = 64 + 4, RING = kStages * Tile::SLOT;
+  __shared__ __attribute__((aligned(16))) char lds[4 * RING];          // the ring of every wave
+  __shared__ __attribute__((aligned(16))) float stage[4][16][PITCH];   // their sums for 16 rows and 64 channels
   __shared__ float wave_m[4][ROWS], wave_l[4][ROWS];
   __shared__ int wave_units[4], found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int H = a.g.H, row0 = blockIdx.y * ROWS;
   char* ring = lds + wave * RING;
   const Unpack un;
+  const auto shared_units = [&](int r) {           // what is dealt out of a request and head: its units, or all of it
+    const int u = attend_units(a, r, row0, ROWS);
+    return a.split ? u : min(u, 1);
+  };
 
   // units up to every thread's requests (R / 256 each)
   const int per = (a.R + 255) / 256, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
   int mine = 0;
-  for (int r = r0; r < r1; r++) mine += attend_units(a, r, row0, ROWS);
+  for (int r = r0; r < r1; r++) mine += shared_units(r);
   int upto = mine;
   for (int k = 1; k < 64; k <<= 1) {
     const int u = __shfl_up(upto, k);
@@ -353,7 +420,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
     if (k < wave) upto += wave_units[k];
     units += wave_units[k];
   }
-  if (blockIdx.x == 0) {           // for the launch that joins
+  if (blockIdx.x == 0 && a.split) {           // for the launch that joins
     int32_t* prefix = a.prefix + (size_t)blockIdx.y * (a.R + 1);
     int at = upto - mine;
     for (int r = r0; r < r1; r++) {
@@ -364,77 +431,95 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
   }
   const AttendShares shares(__builtin_amdgcn_readfirstlane(units) * H, a.workgroups);
   if ((int)blockIdx.x >= shares.n) return;
-  int x = shares.begin(blockIdx.x);
-  const int end = shares.begin(blockIdx.x + 1);
-  if ((upto - mine) * H <= x && x < upto * H) {
+  AttendCursor cursor;
+  cursor.x = shares.begin(blockIdx.x);
+  cursor.end = shares.begin(blockIdx.x + 1);
+  if ((upto - mine) * H <= cursor.x && cursor.x < upto * H) {
     int at = upto - mine;
     for (int r = r0; r < r1; r++) {
-      const int u = attend_units(a, r, row0, ROWS);
-      if (x < (at + u) * H) {
+      const int u = shared_units(r);
+      if (cursor.x < (at + u) * H) {
         found[0] = r;
-        found[1] = at;
+        found[1] = cursor.x - at * H;
         break;
       }
       at += u;
     }
   }
   __syncthreads();
-  int r = __builtin_amdgcn_readfirstlane(found[0]), prefix = __builtin_amdgcn_readfirstlane(found[1]);
+  cursor.r = __builtin_amdgcn_readfirstlane(found[0]);
+  cursor.look(a, cursor.r, row0, ROWS);
+  {
+    const int rel = __builtin_amdgcn_readfirstlane(found[1]), u = a.split ? __builtin_amdgcn_readlane(cursor.units, 0) : 1;
+    cursor.head = rel / u;
+    cursor.j = a.split ? rel - cursor.head * u : 0;
+  }
 
-  while (x < end) {
-    const AttendRequest rq = attend_request(a, r);
-    const int visible = __builtin_amdgcn_readfirstlane(attend_visible(a, rq, row0, ROWS));
-    const int u = __builtin_amdgcn_readfirstlane(rq.rows > row0 ? max(1, (visible + kUnit - 1) / kUnit) : 0);
-    const int rel = x - prefix * H;
-    if (rel >= u * H) {    // the next request
-      prefix += u;
-      r++;
-      continue;
-    }
-    const int head = rel / u, j0 = rel - head * u, j1 = min(u, j0 + (end - x));
-    x += j1 - j0;
-    AttendRows<D, GROUP> rows[NQ];
+  AttendRows<D, GROUP> rows[NQ];
 #pragma unroll
-    for (int q = 0; q < NQ; q++) rows[q].fetch(a, rq, head, row0 + 16 * q);
-    const int all_see = __builtin_amdgcn_readfirstlane(a.causal ? rq.first_sees + row0 / a.G : rq.len);       // keys that every row of the tile sees
-    const int32_t* table = a.table + (size_t)r * a.columns;
-    const int first = j0 * kUnit + wave * 32;                              // the wave's tiles: every 128 tokens from here
-    const int count = max(0, min(j1 - j0, (visible - first + kUnit - 1) / kUnit));
-    // A lane has the page of one of the wave's next 64 tiles: a tile's address then waits for no load.
-    const auto pages_from = [&](int k) { return table[min(first + (k + lane) * kUnit, max(visible - 1, 0)) >> a.g.page_shift]; };
-    int pages = pages_from(0);
-    unsigned exists = 0;                                                   // of the tiles in the ring
-    const auto fetch = [&](int k) {
-      if (k % 64 == 0 && k != 0) pages = pages_from(k);
-      const int entry = __builtin_amdgcn_readlane(pages, k % 64);
-      const bool ok = (unsigned)entry < (unsigned)a.g.pages;
-      const unsigned bit = 1u << (k % kStages);
-      exists = ok ? exists | bit : exists & ~bit;
-      const unsigned char* p = a.pool + (size_t)(ok ? entry : 0) * a.g.page_bytes() + (size_t)(head * a.g.head_bytes());
-      Tile::fetch(a.g, p, (first + k * kUnit) & (a.g.page() - 1), ring + k % kStages * Tile::SLOT);
-    };
+  for (int q = 0; q < NQ; q++) rows[q].place(a, row0 + 16 * q);
+  AttendPiece piece = cursor.next(a, row0, ROWS);
+  int first, count;           // the wave's tiles: `count`, every 128 tokens from `first`
+  int pages;                  // a lane has the page of one of the wave's next 64 tiles: a tile's address then waits for no load
+  unsigned exists;            // of the tiles in the ring
+  const auto pages_from = [&](int k) {
+    return a.table[(size_t)piece.r * a.columns + (min(first + (k + lane) * kUnit, max(piece.visible - 1, 0)) >> a.g.page_shift)];
+  };
+  const auto look = [&] {      // loads what the piece's copies wait for, and its queries
+    first = piece.j0 * kUnit + wave * 32;
+    count = max(0, min(piece.j1 - piece.j0, (piece.visible - first + kUnit - 1) / kUnit));
+    pages = pages_from(0);
+#pragma unroll
+    for (int q = 0; q < NQ; q++) rows[q].fetch(a, piece);
+  };
+  const auto fetch = [&](int k) {
+    if (k % 64 == 0 && k != 0) pages = pages_from(k);
+    const int entry = __builtin_amdgcn_readlane(pages, k % 64);
+    const bool ok = (unsigned)entry < (unsigned)a.g.pages;
+    const int at = k % kStages;
+    exists = ok ? exists | 1u << at : exists & ~(1u << at);
+    const unsigned char* p = a.pool + (size_t)(ok ? entry : 0) * a.g.page_bytes() + (size_t)(piece.head * a.g.head_bytes());
+    Tile::fetch(a.g, p, (first + k * kUnit) & (a.g.page() - 1), ring + at * Tile::SLOT);
+  };
+  const auto start = [&] {
+    exists = 0;
     for (int k = 0; k < kStages - 1 && k < count; k++) fetch(k);
+  };
+  look();
+  start();
+
+  for (;;) {
+    const int all_see = a.causal ? piece.first_sees + row0 / a.G : piece.len;       // keys that every row of the tile sees
 #pragma unroll
     for (int q = 0; q < NQ; q++) rows[q].begin();
+    int slot = 0;
     for (int k = 0; k < count; k++) {
       compiler_fence();
       if (k + kStages - 1 < count) fetch(k + kStages - 1);
       compiler_fence();
       const int behind = min(count - 1 - k, kStages - 1);                  // tiles on their way behind this one
-      if (behind >= 3) __builtin_amdgcn_s_waitcnt(vmcnt_only(3 * Tile::COPIES));
-      else if (behind == 2) __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * Tile::COPIES));
+      if (behind >= 2) __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * Tile::COPIES));
       else if (behind == 1) __builtin_amdgcn_s_waitcnt(vmcnt_only(Tile::COPIES));
       else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
       compiler_fence();
-      if ((exists >> (k % kStages) & 1) == 0) continue;
-      const int t0 = first + k * kUnit;
-      Tile tile;
-      tile.take(ring + k % kStages * Tile::SLOT);
-      attend_tile<D, GROUP, NQ>(rows, tile, t0, t0 + 32 > all_see, a.scale_log2, un);
+      if ((exists >> slot & 1) != 0) {
+        Tile tile;
+        tile.take(ring + slot * Tile::SLOT);
+        const int t0 = first + k * kUnit;
+        attend_tile<D, GROUP, NQ>(rows, tile, t0, t0 + 32 > all_see, a.scale_log2, un);
+      }
+      slot = slot == kStages - 1 ? 0 : slot + 1;
     }
-    // join the waves
-    const bool whole = j0 == 0 && j1 == u;
-    const size_t slot = ((size_t)blockIdx.y * a.workgroups + blockIdx.x) * 2 + (j0 == 0 ? 1 : 0);
+    // Join the waves; the next piece's loads and first copies are on their way meanwhile.
+    const AttendPiece done = piece;
+    const bool more = cursor.x < cursor.end;
+    if (more) {
+      piece = cursor.next(a, row0, ROWS);
+      look();
+    }
+    const bool whole = done.j0 == 0 && done.j1 == done.u;
+    const size_t part = ((size_t)blockIdx.y * a.workgroups + blockIdx.x) * 2 + (done.j0 == 0 ? 1 : 0);
+    barrier_lds_only();           // (the sums of the piece before are read)
 #pragma unroll
     for (int q = 0; q < NQ; q++) {
       const float l = column_sum(rows[q].l);
@@ -443,36 +528,40 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
         wave_l[wave][16 * q + lane] = l;
       }
     }
-    __syncthreads();
 #pragma unroll
     for (int q = 0; q < NQ; q++) {
-      {
-        const int k = 16 * q + (lane & 15);
-        const float M = fmaxf(fmaxf(wave_m[0][k], wave_m[1][k]), fmaxf(wave_m[2][k], wave_m[3][k]));
-        const float f = rows[q].m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rows[q].m - M);
+      const int row = tid / 16, c = tid % 16 * 4, k = 16 * q + row;
+      float M = 0.f, f[4], l = 0.f;
 #pragma unroll
-        for (int v = 0; v < D / 16; v++) *(v4f*)&stage[wave][lane & 15][16 * v + 4 * (lane >> 4)] = rows[q].o[v] * f;
-      }
-      __syncthreads();
-      const int row = tid / 16, c = (tid % 16) * NC, k = 16 * q + row;
-      const float M = fmaxf(fmaxf(wave_m[0][k], wave_m[1][k]), fmaxf(wave_m[2][k], wave_m[3][k]));
-      float o[NC], l = 0.f;
+      for (int half = 0; half < D / 64; half++) {
+        if (q + half > 0) barrier_lds_only();
 #pragma unroll
-      for (int i = 0; i < NC; i++) o[i] = (stage[0][row][c + i] + stage[1][row][c + i]) + (stage[2][row][c + i] + stage[3][row][c + i]);
+        for (int v = 0; v < 4; v++) *(v4f*)&stage[wave][lane & 15][16 * v + 4 * (lane >> 4)] = rows[q].o[4 * half + v];
+        if (q + half == 0 && more) start();
+        barrier_lds_only();
+        if (half == 0) {
+          M = fmaxf(fmaxf(wave_m[0][k], wave_m[1][k]), fmaxf(wave_m[2][k], wave_m[3][k]));
 #pragma unroll
-      for (int w = 0; w < 4; w++) l += wave_m[w][k] == -INFINITY ? 0.f : wave_l[w][k] * __builtin_amdgcn_exp2f(wave_m[w][k] - M);
-      if (row0 + k < rq.rows) {
-        if (whole) {
-          attend_store<NC>(a, rq, head, row0 + k, D, c, M, l, o);
-        } else {
-          float* p = a.sums + (slot * ROWS + k) * D + c;
+          for (int w = 0; w < 4; w++) {
+            f[w] = wave_m[w][k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(wave_m[w][k] - M);
+            l += wave_l[w][k] * f[w];
+          }
+        }
+        v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < NC; i++) p[i] = o[i];
-          if (c == 0) a.stats[slot * ROWS + k] = float2{M, l};
+        for (int w = 0; w < 4; w++) o += *(const v4f*)&stage[w][row][c] * f[w];
+        if (row0 + k < done.n_rows) {
+          const int channel = 64 * half + c;
+          if (whole) {
+            attend_store<4>(a, done.begin, done.head, row0 + k, D, channel, M, l, (const float*)&o);
+          } else {
+            *(v4f*)(a.sums + (part * ROWS + k) * D + channel) = o;
+            if (channel == 0) a.stats[part * ROWS + k] = float2{M, l};
+          }
         }
       }
-      __syncthreads();
     }
+    if (!more) break;
   }
 }
 
@@ -539,7 +628,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
   l = (meet[0][D] + meet[1][D]) + (meet[2][D] + meet[3][D]);
 #pragma unroll
   for (int i = 0; i < NC; i++) o[i] = (meet[0][NC * lane + i] + meet[1][NC * lane + i]) + (meet[2][NC * lane + i] + meet[3][NC * lane + i]);
-  attend_store<NC>(a, rq, head, row, D, NC * lane, M, l, o);
+  attend_store<NC>(a, rq.begin, head, row, D, NC * lane, M, l, o);
 }
 
 }  // namespace sage

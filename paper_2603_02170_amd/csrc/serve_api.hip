@@ -51,9 +51,15 @@ int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c) {
 
 constexpr int kSlots = 512;      // workgroups of the attention that the machine takes at a time, at most
 
+#ifndef KWU
+#define KWU 8
+#endif
+constexpr int kWholeUnits = KWU;    // keys of a request up to this many units are not divided
+
 // How a call is laid out: row tiles, workgroups, workspace.
 struct AttendPlan {
   int nq, row_tiles, workgroups, max_length;
+  bool split;         // keys of a request over several workgroups
   int join_rows;      // of a tile, that any request has
   size_t prefix, sums, stats, total;
 };
@@ -69,13 +75,15 @@ AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& 
   w.nq = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   w.row_tiles = (int)((rows + 16 * w.nq - 1) / (16 * w.nq));
   w.join_rows = (int)(rows < 16 * w.nq ? rows : 16 * w.nq);
-  const int64_t units = (int64_t)c.R * p.H * ((w.max_length + kUnit - 1) / kUnit);
+  const int most_units = (w.max_length + kUnit - 1) / kUnit;
+  w.split = most_units > kWholeUnits;
+  const int64_t units = (int64_t)c.R * p.H * (w.split ? most_units : 1);
   const int64_t slots = kSlots / w.row_tiles > 8 ? kSlots / w.row_tiles : 8;
   w.workgroups = (int)(units < slots ? (units > 0 ? units : 1) : slots);
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
   w.prefix = take((size_t)w.row_tiles * (c.R + 1) * 4);
-  const size_t parts = (size_t)w.row_tiles * w.workgroups * 2 * 16 * w.nq;
+  const size_t parts = !w.split ? 0 : (size_t)w.row_tiles * w.workgroups * 2 * 16 * w.nq;
   w.sums = take(parts * p.d * 4);
   w.stats = take(parts * 8);
   w.total = off;
@@ -86,7 +94,7 @@ template <int D, int GROUP, int NQ>
 int launch_attend(const AttendArgs& a, const AttendPlan& w, hipStream_t st) {
   cache_attend_kernel<D, GROUP, NQ><<<dim3(w.workgroups, w.row_tiles), 256, 0, st>>>(a);
   SERVE_LAUNCH_CHECK();
-  if (w.workgroups > 1) {
+  if (w.split && w.workgroups > 1) {
     cache_join_kernel<D, NQ><<<dim3(w.workgroups - 1, w.join_rows, w.row_tiles), 256, 0, st>>>(a);
     SERVE_LAUNCH_CHECK();
   }
@@ -209,11 +217,12 @@ int sagebwd_cache_attention(const void* Q, const void* pool, const int32_t* bloc
   const int rc = check_call(params, call);
   if (rc != SAGEBWD_OK) return rc;
   if (call->R == 0 || call->T == 0) return SAGEBWD_OK;
-  if (Q == nullptr || pool == nullptr || block_table == nullptr || lengths == nullptr || cu == nullptr || O == nullptr || workspace == nullptr ||
-      !aligned(Q) || !aligned(pool) || !aligned(O) || !aligned(workspace, 256))
+  if (Q == nullptr || pool == nullptr || block_table == nullptr || lengths == nullptr || cu == nullptr || O == nullptr || !aligned(Q) ||
+      !aligned(pool) || !aligned(O))
     return SAGEBWD_INVALID_ARG;
   const AttendPlan w = attend_plan(*params, *call);
   if (workspace_bytes < w.total) return SAGEBWD_WORKSPACE_TOO_SMALL;
+  if (workspace == nullptr || !aligned(workspace, 256)) return SAGEBWD_INVALID_ARG;
   char* ws = (char*)workspace;
   AttendArgs a;
   a.Q = (const __bf16*)Q;
@@ -240,6 +249,7 @@ int sagebwd_cache_attention(const void* Q, const void* pool, const int32_t* bloc
   a.q_token = call->q_token_stride;
   a.q_head = call->q_head_stride;
   a.workgroups = w.workgroups;
+  a.split = w.split;
   return with_format(*params, [&](auto d, auto group) { return launch_attend<decltype(d)::value, decltype(group)::value>(a, w, (hipStream_t)stream); });
 }
 
