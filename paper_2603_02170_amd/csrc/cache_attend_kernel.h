@@ -36,6 +36,10 @@ struct AttendArgs {
 };
 
 constexpr int kUnit = 128;          // tokens that a workgroup of four waves takes at a time
+// What an item costs beside its units, in units: its queries, the joining of its waves, its stores.  (Without it a workgroup with many
+// short items ends last: 64 ragged requests 62.7 us, with 1, 2, 3: 58.0, 56.6, 54.0; 32 equal ones of 4 drafted tokens, whose items
+// came out whole by chance, 48.2 and 52.6, 49.4, 51.7.)
+constexpr int kItemCost = 2;
 
 struct AttendRequest {
   int begin, n, rows, len;          // first row, new tokens, query rows computed of each head, keys
@@ -62,8 +66,10 @@ __device__ __forceinline__ int attend_units(const AttendArgs& a, int r, int row0
   return max(1, (attend_visible(a, q, row0, count) + kUnit - 1) / kUnit);     // (rows without a key are an item too: zeros)
 }
 
-// Items are (request, key/value head), request after request, of attend_units units each; the units are dealt to the workgroups in
-// order, total / n each and one more to the first total % n.  (The host bounds the total by 2^30.)
+// Items are (request, key/value head), request after request, of attend_units units each and kItemCost in front of them; those are dealt to
+// the workgroups in order, total / n each and one more to the first total % n.  (The host bounds the total by 2^30.)  A border inside
+// an item's first kItemCost (or before it) cuts nothing off: attend_cut.
+__device__ __forceinline__ int attend_cut(int offset) { return max(0, offset - kItemCost); }
 struct AttendShares {
   int each, more, n;
   __device__ __forceinline__ AttendShares(int total, int workgroups) {
@@ -341,8 +347,9 @@ struct AttendPiece {
 struct AttendCursor {
   int base;                                                // request of lane 0
   int begin, n_rows, len, first_sees, visible, units;      // of request base + lane
-  int r, head, j;                                          // the next piece begins here
-  int x, end;                                              // units taken, and to take
+  int r, head, j;                                          // the next piece begins here: request, head, unit
+  int x, end;                                              // where its item begins in what is dealt out, and where the share ends
+  __device__ __forceinline__ bool more(const AttendArgs& a) const { return a.split ? attend_cut(end - x) > j : x < end; }
 
   __device__ __forceinline__ void look(const AttendArgs& a, int from, int row0, int count) {
     base = from;
@@ -354,7 +361,7 @@ struct AttendCursor {
     visible = q.rows > row0 ? attend_visible(a, q, row0, count) : 0;
     units = q.rows > row0 ? max(1, (visible + kUnit - 1) / kUnit) : 0;
   }
-  // (x < end)
+  // (more)
   __device__ __forceinline__ AttendPiece next(const AttendArgs& a, int row0, int count) {
     AttendPiece p;
     int at;
@@ -372,10 +379,10 @@ struct AttendCursor {
     p.first_sees = __builtin_amdgcn_readlane(first_sees, at);
     p.visible = __builtin_amdgcn_readlane(visible, at);
     p.j0 = j;
-    p.j1 = a.split ? min(p.u, j + (end - x)) : p.u;
-    x += a.split ? p.j1 - p.j0 : 1;
+    p.j1 = a.split ? min(p.u, attend_cut(end - x)) : p.u;
     j = p.j1;
     if (j == p.u) {
+      x += a.split ? p.u + kItemCost : 1;
       j = 0;
       if (++head == a.g.H) {
         head = 0;
@@ -400,7 +407,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
   const Unpack un;
   const auto shared_units = [&](int r) {           // what is dealt out of a request and head: its units, or all of it
     const int u = attend_units(a, r, row0, ROWS);
-    return a.split ? u : min(u, 1);
+    return u == 0 ? 0 : a.split ? u + kItemCost : 1;
   };
 
   // units up to every thread's requests (R / 256 each)
@@ -425,35 +432,37 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
     int at = upto - mine;
     for (int r = r0; r < r1; r++) {
       prefix[r] = at;
-      at += attend_units(a, r, row0, ROWS);
+      at += shared_units(r);
     }
     if (tid == 0) prefix[a.R] = units;
   }
   const AttendShares shares(__builtin_amdgcn_readfirstlane(units) * H, a.workgroups);
   if ((int)blockIdx.x >= shares.n) return;
-  AttendCursor cursor;
-  cursor.x = shares.begin(blockIdx.x);
-  cursor.end = shares.begin(blockIdx.x + 1);
-  if ((upto - mine) * H <= cursor.x && cursor.x < upto * H) {
+  const int begin = shares.begin(blockIdx.x);
+  if ((upto - mine) * H <= begin && begin < upto * H) {
     int at = upto - mine;
     for (int r = r0; r < r1; r++) {
       const int u = shared_units(r);
-      if (cursor.x < (at + u) * H) {
+      if (begin < (at + u) * H) {
         found[0] = r;
-        found[1] = cursor.x - at * H;
+        found[1] = begin - at * H;
         break;
       }
       at += u;
     }
   }
   __syncthreads();
+  AttendCursor cursor;
   cursor.r = __builtin_amdgcn_readfirstlane(found[0]);
   cursor.look(a, cursor.r, row0, ROWS);
   {
-    const int rel = __builtin_amdgcn_readfirstlane(found[1]), u = a.split ? __builtin_amdgcn_readlane(cursor.units, 0) : 1;
+    const int rel = __builtin_amdgcn_readfirstlane(found[1]), u = a.split ? __builtin_amdgcn_readlane(cursor.units, 0) + kItemCost : 1;
     cursor.head = rel / u;
-    cursor.j = a.split ? rel - cursor.head * u : 0;
+    cursor.j = attend_cut(rel - cursor.head * u);
+    cursor.x = begin - (rel - cursor.head * u);
+    cursor.end = shares.begin(blockIdx.x + 1);
   }
+  if (!cursor.more(a)) return;
 
   AttendRows<D, GROUP> rows[NQ];
 #pragma unroll
@@ -512,7 +521,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
     }
     // Join the waves; the next piece's loads and first copies are on their way meanwhile.
     const AttendPiece done = piece;
-    const bool more = cursor.x < cursor.end;
+    const bool more = cursor.more(a);
     if (more) {
       piece = cursor.next(a, row0, ROWS);
       look();
@@ -587,7 +596,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
   }
   const int u = prefix[r + 1] - prefix[r], rel = border - prefix[r] * H, head = rel / u;
   const int first = border - (rel - head * u), last = first + u;
-  if (first == border || shares.begin(w - 1) > first) return;
+  if (attend_cut(border - first) == 0 || attend_cut(shares.begin(w - 1) - first) > 0) return;
   const AttendRequest rq = attend_request(a, r);
   const int k = blockIdx.y, row = blockIdx.z * ROWS + k;
   if (row >= rq.rows) return;
