@@ -24,8 +24,8 @@ struct AttendArgs {
   const float* v_mean;
   __bf16* O;
   float* LSE;
-  int32_t* prefix;      // [row tiles, R + 1] units up to a request
-  float* sums;          // [row tiles, 2 slots of every workgroup, rows, D]: parts of items that workgroups share
+  int4* joins;          // of every workgroup: parts (or 0), request, head, first row of the item that its first unit divides
+  float* sums;          // [2 slots of every workgroup, rows, D]: parts of items that workgroups share
   float2* stats;        // their maximum (log2) and sum
   CacheGeometry g;
   int R, T, Hq, G, columns, max_new, max_length, causal;
@@ -33,6 +33,7 @@ struct AttendArgs {
   int64_t q_token, q_head;
   int workgroups;
   int split;            // 1: an item's units may go to several workgroups
+  int rows_from, rows_to;   // the launch has the requests of rows_from < rows (new tokens times G) <= rows_to
 };
 
 constexpr int kUnit = 128;          // tokens that a workgroup of four waves takes at a time
@@ -50,6 +51,7 @@ __device__ __forceinline__ AttendRequest attend_request(const AttendArgs& a, int
   q.begin = min(max(a.cu[r], 0), a.T);
   q.n = min(max(a.cu[r + 1], q.begin), a.T) - q.begin;
   q.rows = min(q.n, a.max_new) * a.G;
+  if (q.rows <= a.rows_from || q.rows > a.rows_to) q.rows = 0;
   q.len = min(max(a.lengths[r], 0), a.max_length);
   q.first_sees = a.causal ? q.len - q.n + 1 : q.len;
   return q;
@@ -60,10 +62,9 @@ __device__ __forceinline__ int attend_visible(const AttendArgs& a, const AttendR
   const int last = (min(q.rows, row0 + count) - 1) / a.G;
   return max(0, min(q.len, q.first_sees + last));
 }
-__device__ __forceinline__ int attend_units(const AttendArgs& a, int r, int row0, int count) {
+__device__ __forceinline__ int attend_units(const AttendArgs& a, int r) {
   const AttendRequest q = attend_request(a, r);
-  if (q.rows <= row0) return 0;
-  return max(1, (attend_visible(a, q, row0, count) + kUnit - 1) / kUnit);     // (rows without a key are an item too: zeros)
+  return q.rows == 0 ? 0 : max(1, (attend_visible(a, q, 0, q.rows) + kUnit - 1) / kUnit);     // (rows without a key are an item too: zeros)
 }
 
 // Items are (request, key/value head), request after request, of attend_units units each and kItemCost in front of them; those are dealt to
@@ -351,22 +352,22 @@ struct AttendCursor {
   int x, end;                                              // where its item begins in what is dealt out, and where the share ends
   __device__ __forceinline__ bool more(const AttendArgs& a) const { return a.split ? attend_cut(end - x) > j : x < end; }
 
-  __device__ __forceinline__ void look(const AttendArgs& a, int from, int row0, int count) {
+  __device__ __forceinline__ void look(const AttendArgs& a, int from) {
     base = from;
     const AttendRequest q = attend_request(a, min(from + (int)(threadIdx.x & 63), a.R - 1));
     begin = q.begin;
     n_rows = q.rows;
     len = q.len;
     first_sees = q.first_sees;
-    visible = q.rows > row0 ? attend_visible(a, q, row0, count) : 0;
-    units = q.rows > row0 ? max(1, (visible + kUnit - 1) / kUnit) : 0;
+    visible = q.rows > 0 ? attend_visible(a, q, 0, q.rows) : 0;
+    units = q.rows > 0 ? max(1, (visible + kUnit - 1) / kUnit) : 0;
   }
   // (more)
-  __device__ __forceinline__ AttendPiece next(const AttendArgs& a, int row0, int count) {
+  __device__ __forceinline__ AttendPiece next(const AttendArgs& a) {
     AttendPiece p;
     int at;
     do {
-      if (r >= base + 64) look(a, r, row0, count);
+      if (r >= base + 64) look(a, r);
       at = r - base;
       p.u = __builtin_amdgcn_readlane(units, at);
       if (p.u == 0) r++;
@@ -402,11 +403,11 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
   __shared__ float wave_m[4][ROWS], wave_l[4][ROWS];
   __shared__ int wave_units[4], found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int H = a.g.H, row0 = blockIdx.y * ROWS;
+  const int H = a.g.H;
   char* ring = lds + wave * RING;
   const Unpack un;
   const auto shared_units = [&](int r) {           // what is dealt out of a request and head: its units, or all of it
-    const int u = attend_units(a, r, row0, ROWS);
+    const int u = attend_units(a, r);
     return u == 0 ? 0 : a.split ? u + kItemCost : 1;
   };
 
@@ -427,18 +428,11 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
     if (k < wave) upto += wave_units[k];
     units += wave_units[k];
   }
-  if (blockIdx.x == 0 && a.split) {           // for the launch that joins
-    int32_t* prefix = a.prefix + (size_t)blockIdx.y * (a.R + 1);
-    int at = upto - mine;
-    for (int r = r0; r < r1; r++) {
-      prefix[r] = at;
-      at += shared_units(r);
-    }
-    if (tid == 0) prefix[a.R] = units;
-  }
   const AttendShares shares(__builtin_amdgcn_readfirstlane(units) * H, a.workgroups);
-  if ((int)blockIdx.x >= shares.n) return;
-  const int begin = shares.begin(blockIdx.x);
+  const int w = blockIdx.x;
+  if (a.split && tid == 0) a.joins[w] = int4{0, 0, 0, 0};
+  if (w >= shares.n) return;
+  const int begin = shares.begin(w);
   if ((upto - mine) * H <= begin && begin < upto * H) {
     int at = upto - mine;
     for (int r = r0; r < r1; r++) {
@@ -454,20 +448,22 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
   __syncthreads();
   AttendCursor cursor;
   cursor.r = __builtin_amdgcn_readfirstlane(found[0]);
-  cursor.look(a, cursor.r, row0, ROWS);
+  cursor.look(a, cursor.r);
   {
     const int rel = __builtin_amdgcn_readfirstlane(found[1]), u = a.split ? __builtin_amdgcn_readlane(cursor.units, 0) + kItemCost : 1;
     cursor.head = rel / u;
     cursor.j = attend_cut(rel - cursor.head * u);
     cursor.x = begin - (rel - cursor.head * u);
-    cursor.end = shares.begin(blockIdx.x + 1);
+    cursor.end = shares.begin(w + 1);
   }
   if (!cursor.more(a)) return;
+  if (tid == 0 && cursor.j > 0 && attend_cut(shares.begin(w - 1) - cursor.x) == 0)      // the first border in this item
+    a.joins[w] = int4{shares.owner(cursor.x + __builtin_amdgcn_readlane(cursor.units, 0) + kItemCost - 1) - w + 2, cursor.r, cursor.head, 0};
 
   AttendRows<D, GROUP> rows[NQ];
 #pragma unroll
-  for (int q = 0; q < NQ; q++) rows[q].place(a, row0 + 16 * q);
-  AttendPiece piece = cursor.next(a, row0, ROWS);
+  for (int q = 0; q < NQ; q++) rows[q].place(a, 16 * q);
+  AttendPiece piece = cursor.next(a);
   int first, count;           // the wave's tiles: `count`, every 128 tokens from `first`
   int pages;                  // a lane has the page of one of the wave's next 64 tiles: a tile's address then waits for no load
   unsigned exists;            // of the tiles in the ring
@@ -498,7 +494,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
   start();
 
   for (;;) {
-    const int all_see = a.causal ? piece.first_sees + row0 / a.G : piece.len;       // keys that every row of the tile sees
+    const int all_see = a.causal ? piece.first_sees : piece.len;       // keys that every row sees
 #pragma unroll
     for (int q = 0; q < NQ; q++) rows[q].begin();
     int slot = 0;
@@ -523,11 +519,11 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
     const AttendPiece done = piece;
     const bool more = cursor.more(a);
     if (more) {
-      piece = cursor.next(a, row0, ROWS);
+      piece = cursor.next(a);
       look();
     }
     const bool whole = done.j0 == 0 && done.j1 == done.u;
-    const size_t part = ((size_t)blockIdx.y * a.workgroups + blockIdx.x) * 2 + (done.j0 == 0 ? 1 : 0);
+    const size_t part = (size_t)w * 2 + (done.j0 == 0 ? 1 : 0);
     barrier_lds_only();           // (the sums of the piece before are read)
 #pragma unroll
     for (int q = 0; q < NQ; q++) {
@@ -559,10 +555,10 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
         v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < 4; w++) o += *(const v4f*)&stage[w][row][c] * f[w];
-        if (row0 + k < done.n_rows) {
+        if (k < done.n_rows) {
           const int channel = 64 * half + c;
           if (whole) {
-            attend_store<4>(a, done.begin, done.head, row0 + k, D, channel, M, l, (const float*)&o);
+            attend_store<4>(a, done.begin, done.head, k, D, channel, M, l, (const float*)&o);
           } else {
             *(v4f*)(a.sums + (part * ROWS + k) * D + channel) = o;
             if (channel == 0) a.stats[part * ROWS + k] = float2{M, l};
@@ -574,35 +570,22 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
   }
 }
 
-// Items that several workgroups had parts of.  Workgroup (w, row) looks at the border in front of workgroup w's share and joins the item
-// that it divides, if it is the first border to do so.  Every lane weighs a part; then the four waves take every fourth part, several
-// loads in flight (one wave a row and one part after the other: 97 us for the 128 parts of a request alone, now JOINUS), and meet in LDS:
-// the order of the sums does not depend on timing.
-template <int D, int NQ>
+// Joins the parts of an item that several workgroups had, in the order of the keys: the workgroup at the first border inside it has left word
+// (AttendArgs::joins).  WAVES waves a row: with four every lane weighs a part, then each wave takes every fourth part, several loads in
+// flight, and they meet in LDS (one wave and one part after the other took 97 us for the 128 parts of a request alone, now 7); of many
+// rows, with few parts each, a wave has its own.
+template <int D, int ROWS, int WAVES>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
-  constexpr int ROWS = 16 * NQ, NC = D / 64, MOST = 256;
-  __shared__ float weight[MOST], meet[4][D + 2];
-  const int32_t* prefix = a.prefix + (size_t)blockIdx.z * (a.R + 1);
-  const int H = a.g.H;
-  const AttendShares shares(prefix[a.R] * H, a.workgroups);
+  constexpr int NC = D / 64, MOST = 256;
   const int w = blockIdx.x + 1;
-  if (w >= shares.n) return;
-  const int border = shares.begin(w);
-  int r = 0;
-  for (int hi = a.R; hi - r > 1;) {
-    const int mid = (r + hi) >> 1;
-    if (prefix[mid] * H <= border) r = mid;
-    else hi = mid;
-  }
-  const int u = prefix[r + 1] - prefix[r], rel = border - prefix[r] * H, head = rel / u;
-  const int first = border - (rel - head * u), last = first + u;
-  if (attend_cut(border - first) == 0 || attend_cut(shares.begin(w - 1) - first) > 0) return;
-  const AttendRequest rq = attend_request(a, r);
-  const int k = blockIdx.y, row = blockIdx.z * ROWS + k;
-  if (row >= rq.rows) return;
+  const int4 join = a.joins[w];
+  const int parts = join.x;
+  if (parts == 0) return;
+  const AttendRequest rq = attend_request(a, join.y);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const size_t slot0 = ((size_t)blockIdx.z * a.workgroups + w) * 2;
-  const int parts = shares.owner(last - 1) - w + 2;        // of workgroups w - 1 .. the one that has the last unit
+  const int k = WAVES == 4 ? blockIdx.y : blockIdx.y * 4 + wave, row = join.w + k;
+  if (row >= rq.rows) return;
+  const size_t slot0 = (size_t)w * 2;
   const auto at = [&](int p) { return (p == 0 ? slot0 - 1 : slot0 + 2 * (p - 1)) * ROWS + k; };
   float M = -INFINITY;
   for (int p = lane; p < parts; p += 64) M = fmaxf(M, a.stats[at(p)].x);
@@ -610,34 +593,47 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
   float o[NC], l = 0.f;
 #pragma unroll
   for (int i = 0; i < NC; i++) o[i] = 0.f;
-  for (int p0 = 0; p0 < parts; p0 += MOST) {
-    const int here = min(parts - p0, MOST);
-    __syncthreads();
-    if (tid < here) {
-      const float2 s = a.stats[at(p0 + tid)];
+  if constexpr (WAVES == 1) {
+#pragma unroll 2
+    for (int p = 0; p < parts; p++) {
+      const float2 s = a.stats[at(p)];
       const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - M);
-      weight[tid] = f;
       l += s.y * f;
-    }
-    __syncthreads();
-#pragma unroll 4
-    for (int p = wave; p < here; p += 4) {
-      const float f = weight[p];
-      const float* x = a.sums + at(p0 + p) * D + NC * lane;
+      const float* x = a.sums + at(p) * D + NC * lane;
 #pragma unroll
       for (int i = 0; i < NC; i++) o[i] += x[i] * f;
     }
+  } else {
+    __shared__ float weight[MOST], meet[4][D + 2];
+    for (int p0 = 0; p0 < parts; p0 += MOST) {
+      const int here = min(parts - p0, MOST);
+      __syncthreads();
+      if (tid < here) {
+        const float2 s = a.stats[at(p0 + tid)];
+        const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - M);
+        weight[tid] = f;
+        l += s.y * f;
+      }
+      __syncthreads();
+#pragma unroll 4
+      for (int p = wave; p < here; p += 4) {
+        const float f = weight[p];
+        const float* x = a.sums + at(p0 + p) * D + NC * lane;
+#pragma unroll
+        for (int i = 0; i < NC; i++) o[i] += x[i] * f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NC; i++) meet[wave][NC * lane + i] = o[i];
+    for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
+    if (lane == 0) meet[wave][D] = l;
+    __syncthreads();
+    if (wave != 0) return;
+    l = (meet[0][D] + meet[1][D]) + (meet[2][D] + meet[3][D]);
+#pragma unroll
+    for (int i = 0; i < NC; i++) o[i] = (meet[0][NC * lane + i] + meet[1][NC * lane + i]) + (meet[2][NC * lane + i] + meet[3][NC * lane + i]);
   }
-#pragma unroll
-  for (int i = 0; i < NC; i++) meet[wave][NC * lane + i] = o[i];
-  for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
-  if (lane == 0) meet[wave][D] = l;
-  __syncthreads();
-  if (wave != 0) return;
-  l = (meet[0][D] + meet[1][D]) + (meet[2][D] + meet[3][D]);
-#pragma unroll
-  for (int i = 0; i < NC; i++) o[i] = (meet[0][NC * lane + i] + meet[1][NC * lane + i]) + (meet[2][NC * lane + i] + meet[3][NC * lane + i]);
-  attend_store<NC>(a, rq.begin, head, row, D, NC * lane, M, l, o);
+  attend_store<NC>(a, rq.begin, join.z, row, D, NC * lane, M, l, o);
 }
 
 }  // namespace sage

@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "cache_attend_kernel.h"
+#include "cache_chunk_kernel.h"
 #include "cache_kernels.h"
 #include "rotary_kernel.h"
 
@@ -44,23 +45,32 @@ int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c) {
       !stride_ok(c->q_head_stride))
     return SAGEBWD_INVALID_ARG;
   if (c->Hq % p->H != 0 || c->Hq / p->H > 64 || (int64_t)c->T * c->Hq * p->d >= kMostElements || c->R > 1 << 20 ||
-      (int64_t)c->columns * p->page > INT32_MAX / 2 || (int64_t)c->R * p->H * (c->columns * (int64_t)p->page / kUnit + 1 + kItemCost) > 1 << 30 || (int64_t)c->T * (c->Hq / p->H) > INT32_MAX / 2)
+      (int64_t)c->columns * p->page > INT32_MAX / 2 || (int64_t)c->R * p->H * (c->columns * (int64_t)p->page / kUnit + 1 + kItemCost) > 1 << 30 ||
+      ((int64_t)c->T * (c->Hq / p->H) / kChunkRows + c->R) * p->H > 1 << 30 || (int64_t)c->T * (c->Hq / p->H) > INT32_MAX / 2)
     return SAGEBWD_UNSUPPORTED_SHAPE;
   return SAGEBWD_OK;
 }
 
-constexpr int kSlots = 512;      // workgroups of the attention that the machine takes at a time, at most
-
+constexpr int kCus = 256;
+constexpr int kFewRows = 64;      // query rows of a request and head that cache_attend_kernel takes
 // Keys of a request up to this many units are not divided (four requests of 500 tokens 11.0 -> 9.3 us, 256 of 650 56.4 -> 52.0: the joining
 // launch is 4 to 5 us, a unit 0.6 where the machine is empty).
 constexpr int kWholeUnits = 8;
 
-// How a call is laid out: row tiles, workgroups, workspace.
+// One of the two kernels' part of a call.
+struct AttendLaunch {
+  int rows_from, rows_to;      // of the requests that it has
+  int nq;                      // cache_attend_kernel: tiles of 16 rows
+  int workgroups, join_rows;
+  bool split;
+  size_t joins, sums, stats;
+};
+// How a call is laid out.
 struct AttendPlan {
-  int nq, row_tiles, workgroups, max_length;
-  bool split;         // keys of a request over several workgroups
-  int join_rows;      // of a tile, that any request has
-  size_t prefix, sums, stats, total;
+  int max_length;
+  bool few, many;              // there may be requests for either kernel
+  AttendLaunch f, m;
+  size_t total;
 };
 inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 
@@ -71,41 +81,86 @@ AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& 
   w.max_length = (int)(c.max_length > 0 && c.max_length < all ? c.max_length : all);
   const int64_t most = (int64_t)(c.max_new < c.T ? c.max_new : c.T) * G;      // query rows of a request and head
   const int64_t rows = most > 0 ? most : 1;
-  w.nq = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  w.row_tiles = (int)((rows + 16 * w.nq - 1) / (16 * w.nq));
-  w.join_rows = (int)(rows < 16 * w.nq ? rows : 16 * w.nq);
-  const int most_units = (w.max_length + kUnit - 1) / kUnit;
-  w.split = most_units > kWholeUnits;
-  const int64_t units = (int64_t)c.R * p.H * (w.split ? most_units + kItemCost : 1);
-  const int64_t slots = kSlots / w.row_tiles > 8 ? kSlots / w.row_tiles : 8;
-  w.workgroups = (int)(units < slots ? (units > 0 ? units : 1) : slots);
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
-  w.prefix = take((size_t)w.row_tiles * (c.R + 1) * 4);
-  const size_t parts = !w.split ? 0 : (size_t)w.row_tiles * w.workgroups * 2 * 16 * w.nq;
-  w.sums = take(parts * p.d * 4);
-  w.stats = take(parts * 8);
+  const auto lay_out = [&](AttendLaunch& l, int tile) {
+    const size_t parts = l.split ? (size_t)l.workgroups * 2 * tile : 0;
+    l.joins = take((size_t)l.workgroups * 16);
+    l.sums = take(parts * p.d * 4);
+    l.stats = take(parts * 8);
+  };
+  // Few rows a request: all of them to the one kernel.  Else the requests of one new token (and what fits the same tiles) go to it, the others to
+  // the kernel for many rows; where every request brings the same number there are none of the former.
+  w.many = rows > kFewRows;
+  w.few = !w.many || (int64_t)c.T < (int64_t)c.R * c.max_new;
+  if (w.few) {
+    AttendLaunch& l = w.f;
+    const int64_t here = w.many ? (G > 16 ? G : 16) : rows;
+    l.nq = here <= 16 ? 1 : here <= 32 ? 2 : 4;
+    l.rows_from = 0;
+    l.rows_to = 16 * l.nq;
+    l.join_rows = (int)(here < l.rows_to ? here : l.rows_to);
+    const int most_units = (w.max_length + kUnit - 1) / kUnit;
+    l.split = most_units > kWholeUnits;
+    const int64_t units = (int64_t)c.R * p.H * (l.split ? most_units + kItemCost : 1);
+    l.workgroups = (int)(units < 2 * kCus ? (units > 0 ? units : 1) : 2 * kCus);
+    lay_out(l, 16 * l.nq);
+  }
+  if (w.many) {
+    AttendLaunch& l = w.m;
+    l.rows_from = w.few ? w.f.rows_to : 0;
+    l.rows_to = INT32_MAX;
+    const int64_t total = (int64_t)c.T * G;
+    const int64_t with = w.few ? (total / (l.rows_from + 1) < c.R ? total / (l.rows_from + 1) : c.R) : c.R;      // requests that it may have
+    const int64_t tiles = total / kChunkRows + with, units = tiles * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit + kChunkCost);
+    l.split = total * p.H / kChunkRows < 4 * kCus && units < 1 << 30;
+    l.workgroups = (int)(l.split ? (units < kCus ? (units > 0 ? units : 1) : kCus) : tiles * p.H);
+    l.join_rows = kChunkRows;
+    lay_out(l, kChunkRows);
+  }
   w.total = off;
   return w;
 }
 
 template <int D, int GROUP, int NQ>
-int launch_attend(const AttendArgs& a, const AttendPlan& w, hipStream_t st) {
-  cache_attend_kernel<D, GROUP, NQ><<<dim3(w.workgroups, w.row_tiles), 256, 0, st>>>(a);
+int launch_few(const AttendArgs& a, const AttendLaunch& l, hipStream_t st) {
+  cache_attend_kernel<D, GROUP, NQ><<<l.workgroups, 256, 0, st>>>(a);
   SERVE_LAUNCH_CHECK();
-  if (w.split && w.workgroups > 1) {
-    cache_join_kernel<D, NQ><<<dim3(w.workgroups - 1, w.join_rows, w.row_tiles), 256, 0, st>>>(a);
+  if (l.split && l.workgroups > 1) {
+    cache_join_kernel<D, 16 * NQ, 4><<<dim3(l.workgroups - 1, l.join_rows), 256, 0, st>>>(a);
     SERVE_LAUNCH_CHECK();
   }
   return SAGEBWD_OK;
 }
 template <int D, int GROUP>
-int launch_attend(const AttendArgs& a, const AttendPlan& w, hipStream_t st) {
-  switch (w.nq) {
-    case 1: return launch_attend<D, GROUP, 1>(a, w, st);
-    case 2: return launch_attend<D, GROUP, 2>(a, w, st);
-    default: return launch_attend<D, GROUP, 4>(a, w, st);
+int launch_attend(AttendArgs a, const AttendPlan& w, char* ws, hipStream_t st) {
+  const auto with = [&](const AttendLaunch& l) {
+    a.joins = (int4*)(ws + l.joins);
+    a.sums = (float*)(ws + l.sums);
+    a.stats = (float2*)(ws + l.stats);
+    a.workgroups = l.workgroups;
+    a.split = l.split;
+    a.rows_from = l.rows_from;
+    a.rows_to = l.rows_to;
+  };
+  if (w.many) {
+    with(w.m);
+    cache_chunk_kernel<D, GROUP><<<w.m.workgroups, 512, 0, st>>>(a);
+    SERVE_LAUNCH_CHECK();
+    if (w.m.split && w.m.workgroups > 1) {
+      cache_join_kernel<D, kChunkRows, 1><<<dim3(w.m.workgroups - 1, kChunkRows / 4), 256, 0, st>>>(a);
+      SERVE_LAUNCH_CHECK();
+    }
   }
+  if (w.few) {
+    with(w.f);
+    switch (w.f.nq) {
+      case 1: return launch_few<D, GROUP, 1>(a, w.f, st);
+      case 2: return launch_few<D, GROUP, 2>(a, w.f, st);
+      default: return launch_few<D, GROUP, 4>(a, w.f, st);
+    }
+  }
+  return SAGEBWD_OK;
 }
 
 template <typename F>
@@ -232,9 +287,6 @@ int sagebwd_cache_attention(const void* Q, const void* pool, const int32_t* bloc
   a.v_mean = v_mean;
   a.O = (__bf16*)O;
   a.LSE = LSE;
-  a.prefix = (int32_t*)(ws + w.prefix);
-  a.sums = (float*)(ws + w.sums);
-  a.stats = (float2*)(ws + w.stats);
   a.g = geometry(*params);
   a.R = call->R;
   a.T = call->T;
@@ -247,9 +299,7 @@ int sagebwd_cache_attention(const void* Q, const void* pool, const int32_t* bloc
   a.scale_log2 = (call->sm_scale > 0.f ? call->sm_scale : 1.f / sqrtf((float)params->d)) * 1.4426950408889634f;
   a.q_token = call->q_token_stride;
   a.q_head = call->q_head_stride;
-  a.workgroups = w.workgroups;
-  a.split = w.split;
-  return with_format(*params, [&](auto d, auto group) { return launch_attend<decltype(d)::value, decltype(group)::value>(a, w, (hipStream_t)stream); });
+  return with_format(*params, [&](auto d, auto group) { return launch_attend<decltype(d)::value, decltype(group)::value>(a, w, ws, (hipStream_t)stream); });
 }
 
 int sagebwd_rotary(const void* Q, const void* K, void* Qo, void* Ko, const void* positions, const float* inv_freq,
