@@ -17,6 +17,7 @@
 
 namespace sage {
 
+struct WideTile;
 struct AttendArgs {
   const __bf16* Q;
   const unsigned char* pool;
@@ -27,6 +28,10 @@ struct AttendArgs {
   int4* joins;          // of every workgroup: parts (or 0), request, head, first row of the item that its first unit divides
   float* sums;          // [2 slots of every workgroup, rows, D]: parts of items that workgroups share
   float2* stats;        // their maximum (log2) and sum
+  char* unpacked;       // where keys and values are unpacked beforehand: fragments of 64 tokens of a head,
+  WideTile* tiles;   // what is to be known of each,
+  unsigned char* poison;    // and tokens that are not numbers
+  int most_tiles;           // that there is room for
   CacheGeometry g;
   int R, T, Hq, G, columns, max_new, max_length, causal;
   float scale_log2;     // sm_scale * log2(e)
@@ -73,6 +78,7 @@ __device__ __forceinline__ int attend_units(const AttendArgs& a, int r) {
 __device__ __forceinline__ int attend_cut(int offset) { return max(0, offset - kItemCost); }
 struct AttendShares {
   int each, more, n;
+  __device__ __forceinline__ AttendShares() {}
   __device__ __forceinline__ AttendShares(int total, int workgroups) {
     n = min(workgroups, total);
     each = n > 0 ? total / n : 0;

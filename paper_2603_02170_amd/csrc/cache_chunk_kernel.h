@@ -124,237 +124,449 @@ __device__ __forceinline__ int chunk_weight(const AttendArgs& a, const AttendReq
   for (int t = 0; t < tiles; t++) w += chunk_units(a, q, t) + kChunkCost;
   return w;
 }
+// Tiles of 64 tokens that a head of the request has for the rows to see.
+__device__ __forceinline__ int chunk_key_tiles(const AttendRequest& q) { return q.rows == 0 ? 0 : max(1, (q.len + kChunkUnit - 1) / kChunkUnit); }
 __device__ __forceinline__ int chunk_cut(int offset) { return max(0, offset - kChunkCost); }
+
+// A workgroup's way along the line: (request, head, row tile) from unit j0 on.
+struct ChunkWalk {
+  int w, x, end, j0;       // its number; where its item begins in the line; where its share ends
+  int r, head, tile;
+  int before;              // tiles of 64 tokens of the requests in front (of one head)
+  AttendRequest rq;
+  AttendShares shares;
+  struct Scratch {
+    int sums[8], tiles[8], found[4];
+  };
+
+  // All 512 threads; false: the workgroup has nothing.  Leaves no word for the joining launch.
+  __device__ __forceinline__ bool start(const AttendArgs& a, Scratch& s) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, H = a.g.H;
+    const int per = (a.R + 511) / 512, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
+    int mine = 0, tiles = 0;
+    for (int i = r0; i < r1; i++) {
+      const AttendRequest q = attend_request(a, i);
+      mine += chunk_weight(a, q);
+      tiles += chunk_key_tiles(q);
+    }
+    int upto = mine, tiles_to = tiles;
+    for (int k = 1; k < 64; k <<= 1) {
+      const int u = __shfl_up(upto, k), v = __shfl_up(tiles_to, k);
+      if (lane >= k) {
+        upto += u;
+        tiles_to += v;
+      }
+    }
+    if (lane == 63) {
+      s.sums[wave] = upto;
+      s.tiles[wave] = tiles_to;
+    }
+    __syncthreads();
+    int units = 0;
+#pragma unroll
+    for (int k = 0; k < 8; k++) {
+      if (k < wave) {
+        upto += s.sums[k];
+        tiles_to += s.tiles[k];
+      }
+      units += s.sums[k];
+    }
+    shares = AttendShares(__builtin_amdgcn_readfirstlane(units) * H, a.workgroups);
+    // (neighbours in the line to one XCD, whose L2 then holds a head's keys for all its row tiles)
+    w = a.split && shares.n == a.workgroups && shares.n % 8 == 0 ? (blockIdx.x & 7) * (shares.n / 8) + (blockIdx.x >> 3) : blockIdx.x;
+    if (tid == 0) a.joins[w] = int4{0, 0, 0, 0};
+    if (w >= shares.n) return false;
+    const int begin = shares.begin(w);
+    end = shares.begin(w + 1);
+    if ((upto - mine) * H <= begin && begin < upto * H) {
+      int at = upto - mine, t = tiles_to - tiles;
+      for (int i = r0; i < r1; i++) {
+        const AttendRequest q = attend_request(a, i);
+        const int u = chunk_weight(a, q);
+        if (begin < (at + u) * H) {
+          s.found[0] = i;
+          s.found[1] = at * H;
+          s.found[2] = u;
+          s.found[3] = t;
+          break;
+        }
+        at += u;
+        t += chunk_key_tiles(q);
+      }
+    }
+    __syncthreads();
+    r = __builtin_amdgcn_readfirstlane(s.found[0]);
+    x = __builtin_amdgcn_readfirstlane(s.found[1]);
+    before = __builtin_amdgcn_readfirstlane(s.found[3]);
+    const int weight = __builtin_amdgcn_readfirstlane(s.found[2]);
+    rq = attend_request(a, r);
+    j0 = 0;
+    if (a.split) {
+      head = (begin - x) / weight;
+      x += head * weight;
+      tile = 0;
+      for (int u; x + (u = chunk_units(a, rq, tile) + kChunkCost) <= begin; tile++) x += u;
+      j0 = chunk_cut(begin - x);
+    } else {
+      const int i = begin - x;
+      tile = weight - 1 - i / H;
+      head = i - i / H * H;
+      x = begin;
+    }
+    head = __builtin_amdgcn_readfirstlane(head);
+    tile = __builtin_amdgcn_readfirstlane(tile);
+    x = __builtin_amdgcn_readfirstlane(x);
+    j0 = __builtin_amdgcn_readfirstlane(j0);
+    return a.split ? chunk_cut(end - x) > j0 : true;
+  }
+  // Units j0 .. of the item that are this workgroup's; leaves word for the joining launch at the first border inside it.
+  __device__ __forceinline__ int last_unit(const AttendArgs& a, int units) const {
+    if (j0 > 0 && chunk_cut(shares.begin(w - 1) - x) == 0 && threadIdx.x == 0)
+      a.joins[w] = int4{shares.owner(x + units + kChunkCost - 1) - w + 2, r, head, tile * kChunkRows};
+    return a.split ? min(units, chunk_cut(end - x)) : units;
+  }
+  // Behind an item of so many units of which all up to j1 are done: false at the share's end.
+  __device__ __forceinline__ bool next(const AttendArgs& a, int units, int j1) {
+    if (j1 < units || !a.split) return false;        // (not split, a workgroup has one)
+    x += units + kChunkCost;
+    if (chunk_cut(end - x) <= 0) return false;
+    j0 = 0;
+    if (++tile == chunk_tiles(rq.rows)) {
+      tile = 0;
+      if (++head == a.g.H) {
+        head = 0;
+        before += chunk_key_tiles(rq);
+        do rq = attend_request(a, ++r); while (rq.rows == 0);     // (there is one: the share goes on)
+      }
+    }
+    return true;
+  }
+};
+
+// The rows of a wave: 32 queries, a lane (n, h) has half of the channels of one.
+template <int D>
+struct ChunkRows {
+  static constexpr int NK = D / 16, NC = D / 32;
+  v4i q[NK];
+  v16f o[NC];
+  float m, l;
+  int token, head_of, sees, all_see, wave_sees;
+  bool real;
+
+  __device__ __forceinline__ void begin(const AttendArgs& a, const AttendRequest& rq, int head, int wave_row0) {
+    const int n = threadIdx.x & 31, h = threadIdx.x >> 5 & 1, row = wave_row0 + n;
+    token = row / a.G;
+    head_of = row - token * a.G;
+    real = row < rq.rows;
+    const __bf16* p = a.Q + (int64_t)(rq.begin + (real ? token : 0)) * a.q_token + (int64_t)(head * a.G + (real ? head_of : 0)) * a.q_head + 8 * h;
+#pragma unroll
+    for (int s = 0; s < NK; s++) q[s] = real ? *(const v4i*)(p + 16 * s) : v4i{0, 0, 0, 0};
+    sees = real && a.causal ? min(rq.len, rq.first_sees + token) : rq.len;
+    all_see = __builtin_amdgcn_readfirstlane(a.causal ? rq.first_sees + wave_row0 / a.G : rq.len);
+    wave_sees = __builtin_amdgcn_readfirstlane(wave_row0 < rq.rows ? attend_visible(a, rq, wave_row0, 32) : 0);
+#pragma unroll
+    for (int c = 0; c < NC; c++) o[c] = v16f{};
+    m = -INFINITY;
+    l = 0.f;
+  }
+  // N products whose operand comes from LDS, kAhead reads ahead of each, in this order.  (The compiler by itself reads, waits and multiplies,
+  // one after the other, and looks past groups of instructions that it is asked for.)
+  static constexpr int kAhead = 4;
+  template <int N, typename Read, typename Product>
+  static __device__ __forceinline__ void products(Read read, Product product) {
+    v4i f[kAhead];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < kAhead; i++) f[i] = read(i);
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      __builtin_amdgcn_sched_barrier(0);
+      product(i, as_bf16(f[i % kAhead]));
+      if (i + kAhead < N) f[i % kAhead] = read(i + kAhead);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __device__ __forceinline__ void logits(const char* K, v16f (&s)[2]) const {
+    K += (threadIdx.x & 63) * 16;
+    s[0] = v16f{};
+    s[1] = v16f{};
+    products<2 * NK>([&](int i) { return *(const v4i*)(K + ((i & 1) * NK + (i >> 1)) * 1024); },
+                     [&](int i, const v8bf& f) { s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, as_bf16(q[i >> 1]), s[i & 1], 0, 0, 0); });
+  }
+  // Logits of the tokens t0 .. t0 + 63 to probabilities; e0, e1: whether its halves' pages exist.
+  __device__ __forceinline__ void softmax(v16f (&s)[2], v8bf (&p)[4], int t0, int e0, int e1, float scale_log2) {
+    if (t0 + kChunkUnit > all_see || e0 + e1 != 2) {
+      const int h = threadIdx.x >> 5 & 1;
+#pragma unroll
+      for (int b = 0; b < 2; b++) {
+        const int behind = (b ? e1 : e0) ? sees - t0 - 32 * b - 8 * h : 0;
+#pragma unroll
+        for (int i = 0; i < 16; i++) s[b][i] = 16 * (i / 8) + i % 8 < behind ? s[b][i] : -INFINITY;
+      }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < 2; b++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) top = fmaxf(top, s[b][i]);
+    if (__any(top * scale_log2 > m + 8.f)) {
+      const float to = fmaxf(m, half_swap_max_f32(top) * scale_log2);
+      const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+#pragma unroll
+      for (int c = 0; c < NC; c++) o[c] *= f;
+      l *= f;
+      m = to;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int b = 0; b < 2; b++) {
+#pragma unroll
+      for (int i = 0; i < 16; i++) {
+        s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale_log2, -ref));
+        l += s[b][i];
+      }
+#pragma unroll
+      for (int k = 0; k < 2; k++)
+        p[2 * b + k] = as_bf16(v4i{pack_bf16(s[b][8 * k], s[b][8 * k + 1]), pack_bf16(s[b][8 * k + 2], s[b][8 * k + 3]),
+                                   pack_bf16(s[b][8 * k + 4], s[b][8 * k + 5]), pack_bf16(s[b][8 * k + 6], s[b][8 * k + 7])});
+    }
+  }
+  __device__ __forceinline__ void values(const char* V, const v8bf (&p)[4]) {
+    V += (threadIdx.x & 63) * 16;
+    products<4 * NC>([&](int i) { return *(const v4i*)(V + (i % NC * 4 + i / NC) * 1024); },
+                     [&](int i, const v8bf& f) { o[i % NC] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p[i / NC], o[i % NC], 0, 0, 0); });
+  }
+  // Tokens whose values are not numbers, to the rows that see them.
+  __device__ __forceinline__ void poison(const unsigned char* bad, int group, int t0, int e0, int e1) {
+    for (int t = 0; t < kChunkUnit; t++)
+#pragma unroll
+      for (int c = 0; c < NC; c++)
+        if (bad[32 * c / group * 64 + t] && (t < 32 ? e0 : e1) && t < sees - t0) o[c] += __builtin_nanf("");
+  }
+  // A finished row, or (part) what a workgroup has of it.
+  __device__ __forceinline__ void end(const AttendArgs& a, const AttendRequest& rq, int head, bool whole, size_t part) {
+    const int h = threadIdx.x >> 5 & 1;
+    l = half_swap_sum_f32(l);
+    if (!real) return;
+    if (whole) {
+      const bool any = !(l == 0.f);
+      const float f = any ? 1.f / l : 0.f;
+      const int hq = head * a.G + head_of;
+      __bf16* p = a.O + ((int64_t)(rq.begin + token) * a.Hq + hq) * D;
+#pragma unroll
+      for (int c = 0; c < NC; c++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          float y[4];
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const float mean = a.v_mean != nullptr ? a.v_mean[head * D + 32 * c + 8 * i + 4 * h + e] : 0.f;
+            y[e] = any ? o[c][4 * i + e] * f + mean : 0.f;
+          }
+          *(v2i*)(p + 32 * c + 8 * i + 4 * h) = v2i{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+        }
+      if (h == 0 && a.LSE != nullptr) a.LSE[(int64_t)hq * a.T + rq.begin + token] = any ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+    } else {
+#pragma unroll
+      for (int c = 0; c < NC; c++)
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+          *(v4f*)(a.sums + part * D + 32 * c + 8 * i + 4 * h) = v4f{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
+      if (h == 0) a.stats[part] = float2{m, l};
+    }
+  }
+};
 
 template <int D, int GROUP>
 __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
   typedef ChunkTile<D, GROUP> Tile;
-  constexpr int NK = D / 16, NC = D / 32, HALF = 2 * Tile::FRAG;
+  constexpr int HALF = 2 * Tile::FRAG;
   __shared__ __attribute__((aligned(16))) char Ks[2][HALF], Vs[2][HALF];
   __shared__ unsigned char poison[2][Tile::NG * 64];
   __shared__ int exists[2][2], poisoned[2];
-  __shared__ int wave_units[8], found[3];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
-  const int H = a.g.H;
+  __shared__ ChunkWalk::Scratch scratch;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (tid < 2) poisoned[tid] = -1;
+  ChunkWalk walk;
+  if (!walk.start(a, scratch)) return;
+  int tag = 0;      // of a tile, over all items
+  for (bool more = true; more;) {
+    const AttendRequest& rq = walk.rq;
+    const int visible = __builtin_amdgcn_readfirstlane(attend_visible(a, rq, walk.tile * kChunkRows, kChunkRows));
+    const int u = max(1, (visible + kChunkUnit - 1) / kChunkUnit), j0 = walk.j0, j1 = walk.last_unit(a, u);
+    ChunkRows<D> rows;
+    rows.begin(a, rq, walk.head, walk.tile * kChunkRows + 32 * wave);
+    // a lane has the page of one of the next 64 blocks of 32 tokens
+    const int32_t* table = a.table + (size_t)walk.r * a.columns;
+    const auto pages_from = [&](int j) { return table[min(j * kChunkUnit + 32 * lane, max(visible - 1, 0)) >> a.g.page_shift]; };
+    int pages = pages_from(j0);
+    const auto load = [&](Tile& t, int j) {
+      const int k = 2 * (j - j0) & 63;
+      if (k == 0 && j != j0) pages = pages_from(j);
+      t.load(a, walk.head, j * kChunkUnit, __builtin_amdgcn_readlane(pages, k), __builtin_amdgcn_readlane(pages, k + 1), visible);
+    };
+    Tile next;
+    const int count = visible > 0 ? j1 - j0 : 0;
+    const auto store = [&](int k) { next.store(Ks[k & 1], Vs[k & 1], exists[k & 1], poison[k & 1], &poisoned[k & 1], tag + k); };
+    if (count > 0) {
+      load(next, j0);
+      store(0);
+      if (count > 1) load(next, j0 + 1);
+    }
+    __syncthreads();
+    for (int k = 0; k < count; k++) {
+      const int t0 = (j0 + k) * kChunkUnit, at = k & 1;
+      const bool busy = t0 < rows.wave_sees;
+      v16f s[2];
+      if (busy) rows.logits(Ks[at], s);
+      if (k + 1 < count) {
+        store(k + 1);
+        if (k + 2 < count) load(next, j0 + k + 2);
+      }
+      if (busy) {
+        v8bf p[4];
+        rows.softmax(s, p, t0, exists[at][0], exists[at][1], a.scale_log2);
+        rows.values(Vs[at], p);
+        if (poisoned[at] == tag + k) rows.poison(poison[at], GROUP, t0, exists[at][0], exists[at][1]);
+      }
+      __syncthreads();
+    }
+    tag += count;
+    rows.end(a, rq, walk.head, j0 == 0 && j1 == u, ((size_t)walk.w * 2 + (j0 == 0 ? 1 : 0)) * kChunkRows + 32 * wave + (lane & 31));
+    more = walk.next(a, u, j1);
+  }
+}
 
+// ---- the same with the keys and values unpacked beforehand ------------------------------------------------------------
+// Where a request's keys meet several row tiles, unpacking them in each costs more vector instructions than the softmax: a launch writes the
+// fragments to the workspace once (as they lie in LDS, 256 d bytes for 64 tokens of a head, request after request, head, tile), and the
+// attention copies them into a ring past the registers.
+struct WideTile {
+  int flags;        // bit 0, 1: the pages of its halves exist; bit 2: some value is not a number
+};
+
+template <int D, int GROUP>
+__global__ __launch_bounds__(512) void cache_unpack_kernel(AttendArgs a) {
+  typedef ChunkTile<D, GROUP> Tile;
+  __shared__ ChunkWalk::Scratch s;
+  __shared__ int exists[2], poisoned;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, H = a.g.H;
   const int per = (a.R + 511) / 512, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
-  int mine = 0;
-  for (int r = r0; r < r1; r++) mine += chunk_weight(a, attend_request(a, r));
-  int upto = mine;
+  int tiles = 0;
+  for (int i = r0; i < r1; i++) tiles += chunk_key_tiles(attend_request(a, i));
+  int upto = tiles;
   for (int k = 1; k < 64; k <<= 1) {
     const int u = __shfl_up(upto, k);
     if (lane >= k) upto += u;
   }
-  if (lane == 63) wave_units[wave] = upto;
-  if (tid < 2) poisoned[tid] = -1;
+  if (lane == 63) s.tiles[wave] = upto;
+  if (tid == 0) poisoned = -1;
   __syncthreads();
-  int units = 0;
+  int all = 0;
 #pragma unroll
   for (int k = 0; k < 8; k++) {
-    if (k < wave) upto += wave_units[k];
-    units += wave_units[k];
+    if (k < wave) upto += s.tiles[k];
+    all += s.tiles[k];
   }
-  const AttendShares shares(__builtin_amdgcn_readfirstlane(units) * H, a.workgroups);
-  // (neighbours in the line to one XCD, whose L2 then holds a head's keys for all its row tiles)
-  const int w = a.split && shares.n == a.workgroups && shares.n % 8 == 0 ? (blockIdx.x & 7) * (shares.n / 8) + (blockIdx.x >> 3) : blockIdx.x;
-  if (tid == 0) a.joins[w] = int4{0, 0, 0, 0};
-  if (w >= shares.n) return;
-  const int begin = shares.begin(w), end = shares.begin(w + 1);
-  if ((upto - mine) * H <= begin && begin < upto * H) {
-    int at = upto - mine;
-    for (int r = r0; r < r1; r++) {
-      const int u = chunk_weight(a, attend_request(a, r));
+  const AttendShares shares(__builtin_amdgcn_readfirstlane(all) * H, gridDim.x);
+  if ((int)blockIdx.x >= shares.n) return;
+  // (the workspace has room for every request that `cu` can hold, if it rises: what does not fit is left)
+  const int begin = shares.begin(blockIdx.x), end = min(shares.begin(blockIdx.x + 1), a.most_tiles);
+  if ((upto - tiles) * H <= begin && begin < upto * H) {
+    int at = upto - tiles;
+    for (int i = r0; i < r1; i++) {
+      const int u = chunk_key_tiles(attend_request(a, i));
       if (begin < (at + u) * H) {
-        found[0] = r;
-        found[1] = at * H;
-        found[2] = u;
+        s.found[0] = i;
+        s.found[1] = at * H;
         break;
       }
       at += u;
     }
   }
   __syncthreads();
-  int r = __builtin_amdgcn_readfirstlane(found[0]), weight = __builtin_amdgcn_readfirstlane(found[2]);
-  int x = __builtin_amdgcn_readfirstlane(found[1]);      // where (r, head, tile) begins in the line
-  int head, tile;
+  int r = __builtin_amdgcn_readfirstlane(s.found[0]), x = __builtin_amdgcn_readfirstlane(s.found[1]);
   AttendRequest rq = attend_request(a, r);
-  if (a.split) {
-    head = (begin - x) / weight;
-    x += head * weight;
-    tile = 0;
-    for (int u; x + (u = chunk_units(a, rq, tile) + kChunkCost) <= begin; tile++) x += u;
-  } else {
-    const int i = begin - x;
-    tile = weight - 1 - i / H;
-    head = i - i / H * H;
-    x = begin;
-  }
-  head = __builtin_amdgcn_readfirstlane(head);
-  tile = __builtin_amdgcn_readfirstlane(tile);
-  x = __builtin_amdgcn_readfirstlane(x);
-  int j0 = a.split ? chunk_cut(begin - x) : 0;
-
-  int tag = 0;      // of a tile, over all items
-  while (a.split ? chunk_cut(end - x) > j0 : x < end) {
-    const int row0 = tile * kChunkRows;
-    const int visible = __builtin_amdgcn_readfirstlane(attend_visible(a, rq, row0, kChunkRows));
-    const int u = max(1, (visible + kChunkUnit - 1) / kChunkUnit), j1 = a.split ? min(u, chunk_cut(end - x)) : u;
-    if (j0 > 0 && chunk_cut(shares.begin(w - 1) - x) == 0 && tid == 0)      // the first border in this item
-      a.joins[w] = int4{shares.owner(x + u + kChunkCost - 1) - w + 2, r, head, row0};
-    // the wave's queries
-    const int row = row0 + 32 * wave + n, token = row / a.G;
-    const bool real = row < rq.rows;
-    v4i q[NK];
-    {
-      const __bf16* p = a.Q + (int64_t)(rq.begin + (real ? token : 0)) * a.q_token + (int64_t)(head * a.G + (real ? row - token * a.G : 0)) * a.q_head + 8 * h;
-#pragma unroll
-      for (int s = 0; s < NK; s++) q[s] = real ? *(const v4i*)(p + 16 * s) : v4i{0, 0, 0, 0};
+  for (int y = begin; y < end; y++) {
+    while (y >= x + chunk_key_tiles(rq) * H) {
+      x += chunk_key_tiles(rq) * H;
+      rq = attend_request(a, ++r);
     }
-    const int sees = real && a.causal ? min(rq.len, rq.first_sees + token) : rq.len;
-    const int wave_row0 = row0 + 32 * wave;
-    const int all_see = __builtin_amdgcn_readfirstlane(a.causal ? rq.first_sees + wave_row0 / a.G : rq.len);
-    const int wave_sees = __builtin_amdgcn_readfirstlane(wave_row0 < rq.rows ? attend_visible(a, rq, wave_row0, 32) : 0);
-    v16f o[NC];
-#pragma unroll
-    for (int c = 0; c < NC; c++) o[c] = v16f{};
-    float m = -INFINITY, l = 0.f;
-
-    // a lane has the page of one of the next 64 blocks of 32 tokens
+    const int n = chunk_key_tiles(rq), head = (y - x) / n, j = y - x - head * n;
     const int32_t* table = a.table + (size_t)r * a.columns;
-    const auto pages_from = [&](int j) { return table[min(j * kChunkUnit + 32 * lane, max(visible - 1, 0)) >> a.g.page_shift]; };
-    int pages = pages_from(j0);
-    const auto load = [&](Tile& t, int j) {
-      const int k = 2 * (j - j0) & 63;
-      if (k == 0 && j != j0) pages = pages_from(j);
-      t.load(a, head, j * kChunkUnit, __builtin_amdgcn_readlane(pages, k), __builtin_amdgcn_readlane(pages, k + 1), visible);
-    };
-    Tile next;
-    const int count = visible > 0 ? j1 - j0 : 0;
-    if (count > 0) {
-      load(next, j0);
-      next.store(Ks[0], Vs[0], exists[0], poison[0], &poisoned[0], tag);
-      if (count > 1) load(next, j0 + 1);
-    }
+    const int last = max(rq.len - 1, 0), t0 = j * kChunkUnit;
+    Tile t;
+    t.load(a, head, t0, table[min(t0, last) >> a.g.page_shift], table[min(t0 + 32, last) >> a.g.page_shift], rq.len);
+    char* to = a.unpacked + (size_t)y * (256 * D);
+    t.store(to, to + 128 * D, exists, a.poison + (size_t)y * (Tile::NG * 64), &poisoned, y);
     __syncthreads();
+    if (tid == 0) a.tiles[y].flags = (exists[0] != 0) | (exists[1] != 0) << 1 | (poisoned == y) << 2;
+    __syncthreads();
+  }
+}
+
+constexpr int kWideStages = 4;
+
+template <int D, int GROUP>
+__global__ __launch_bounds__(512, 2) void cache_wide_kernel(AttendArgs a) {
+  constexpr int TILE = 256 * D, COPIES = TILE / 8 / 1024;
+  __shared__ __attribute__((aligned(16))) char ring[kWideStages][TILE];
+  __shared__ ChunkWalk::Scratch scratch;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  ChunkWalk walk;
+  if (!walk.start(a, scratch)) return;
+  const bool late = wave >= 4;
+  for (bool more = true; more;) {
+    const AttendRequest& rq = walk.rq;
+    const int visible = __builtin_amdgcn_readfirstlane(attend_visible(a, rq, walk.tile * kChunkRows, kChunkRows));
+    const int u = max(1, (visible + kChunkUnit - 1) / kChunkUnit), j0 = walk.j0, j1 = walk.last_unit(a, u);
+    int count = visible > 0 ? j1 - j0 : 0;
+    size_t tile0 = (size_t)walk.before * a.g.H + (size_t)walk.head * chunk_key_tiles(rq) + j0;      // of the unpacked ones
+    if (tile0 + max(count, 1) > (size_t)a.most_tiles) tile0 = count = 0;
+    ChunkRows<D> rows;
+    rows.begin(a, rq, walk.head, walk.tile * kChunkRows + 32 * wave);
+    int flags = a.tiles[tile0 + min(lane, max(count - 1, 0))].flags;        // of the next 64 tiles, one a lane
+    const auto fetch = [&](int k) {
+      const gbytes_t from = uniform(a.unpacked + (tile0 + k) * TILE + wave * (COPIES * 1024));
+#pragma unroll
+      for (int c = 0; c < COPIES; c++) copy_16(from + c * 1024 + lane * 16, ring[k % kWideStages] + wave * (COPIES * 1024) + c * 1024);
+    };
+    // Half of the waves take a tile's values an interval later than the others: of the two of a SIMD one is in its softmax while the other
+    // has the matrix pipe.
+    v8bf p[4];
+    bool due = false;
+    const auto values = [&](int k, int flag) {
+      rows.values(ring[k % kWideStages] + TILE / 2, p);
+      if (flag & 4) rows.poison(a.poison + (tile0 + k) * (D / GROUP * 64), GROUP, (j0 + k) * kChunkUnit, flag & 1, flag >> 1 & 1);
+    };
+    compiler_fence();
+    fetch(0);
+    if (count > 1) fetch(1);
+    int flag_before = 0;
     for (int k = 0; k < count; k++) {
-      const int t0 = (j0 + k) * kChunkUnit, at = k & 1;
-      const bool busy = t0 < wave_sees;
-      v16f s[2];
-      if (busy) {
-#pragma unroll
-        for (int b = 0; b < 2; b++) {
-          s[b] = v16f{};
-#pragma unroll
-          for (int c = 0; c < NK; c++) {
-            const v4i f = *(const v4i*)(Ks[at] + b * Tile::FRAG + c * 1024 + lane * 16);
-            s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(f), as_bf16(q[c]), s[b], 0, 0, 0);
-          }
-        }
-      }
-      if (k + 1 < count) {
-        next.store(Ks[at ^ 1], Vs[at ^ 1], exists[at ^ 1], poison[at ^ 1], &poisoned[at ^ 1], tag + 1);
-        if (k + 2 < count) load(next, j0 + k + 2);
-      }
-      if (busy) {
-        if (t0 + kChunkUnit > all_see || exists[at][0] + exists[at][1] != 2) {
-#pragma unroll
-          for (int b = 0; b < 2; b++) {
-            const int behind = exists[at][b] ? sees - t0 - 32 * b - 8 * h : 0;
-#pragma unroll
-            for (int i = 0; i < 16; i++) s[b][i] = 16 * (i / 8) + i % 8 < behind ? s[b][i] : -INFINITY;
-          }
-        }
-        float top = -INFINITY;
-#pragma unroll
-        for (int b = 0; b < 2; b++)
-#pragma unroll
-          for (int i = 0; i < 16; i++) top = fmaxf(top, s[b][i]);
-        if (__any(top * a.scale_log2 > m + 8.f)) {
-          const float to = fmaxf(m, half_swap_max_f32(top) * a.scale_log2);
-          const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
-#pragma unroll
-          for (int c = 0; c < NC; c++) o[c] *= f;
-          l *= f;
-          m = to;
-        }
-        const float ref = m == -INFINITY ? 0.f : m;
-        v8bf p[4];
-#pragma unroll
-        for (int b = 0; b < 2; b++) {
-#pragma unroll
-          for (int i = 0; i < 16; i++) {
-            s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], a.scale_log2, -ref));
-            l += s[b][i];
-          }
-#pragma unroll
-          for (int kk = 0; kk < 2; kk++)
-            p[2 * b + kk] = as_bf16(v4i{pack_bf16(s[b][8 * kk], s[b][8 * kk + 1]), pack_bf16(s[b][8 * kk + 2], s[b][8 * kk + 3]),
-                                        pack_bf16(s[b][8 * kk + 4], s[b][8 * kk + 5]), pack_bf16(s[b][8 * kk + 6], s[b][8 * kk + 7])});
-        }
-#pragma unroll
-        for (int c = 0; c < NC; c++)
-#pragma unroll
-          for (int kk = 0; kk < 4; kk++) {
-            const v4i f = *(const v4i*)(Vs[at] + (c * 4 + kk) * 1024 + lane * 16);
-            o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(f), p[kk], o[c], 0, 0, 0);
-          }
-        if (poisoned[at] == tag) {
-          for (int t = 0; t < kChunkUnit; t++)
-#pragma unroll
-            for (int c = 0; c < NC; c++)
-              if (poison[at][32 * c / GROUP * 64 + t] && exists[at][t / 32] && t < sees - t0) o[c] += __builtin_nanf("");
-        }
-      }
-      tag++;
-      __syncthreads();
-    }
-    l = half_swap_sum_f32(l);
-    if (real) {
-      if (j0 == 0 && j1 == u) {
-        const bool any = !(l == 0.f);
-        const float f = any ? 1.f / l : 0.f;
-        const int hq = head * a.G + row - token * a.G;
-        __bf16* p = a.O + ((int64_t)(rq.begin + token) * a.Hq + hq) * D;
-#pragma unroll
-        for (int c = 0; c < NC; c++) {
-          int d[4][2];
-#pragma unroll
-          for (int i = 0; i < 4; i++) {
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-              const float mean = a.v_mean != nullptr ? a.v_mean[head * D + 32 * c + 8 * i + 4 * h + e] : 0.f;
-              y[e] = any ? o[c][4 * i + e] * f + mean : 0.f;
-            }
-            d[i][0] = pack_bf16(y[0], y[1]);
-            d[i][1] = pack_bf16(y[2], y[3]);
-            *(v2i*)(p + 32 * c + 8 * i + 4 * h) = v2i{d[i][0], d[i][1]};
-          }
-        }
-        if (h == 0 && a.LSE != nullptr) a.LSE[(int64_t)hq * a.T + rq.begin + token] = any ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
-      } else {
-        const size_t at = ((size_t)w * 2 + (j0 == 0 ? 1 : 0)) * kChunkRows + 32 * wave + n;
-#pragma unroll
-        for (int c = 0; c < NC; c++)
-#pragma unroll
-          for (int i = 0; i < 4; i++)
-            *(v4f*)(a.sums + at * D + 32 * c + 8 * i + 4 * h) = v4f{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
-        if (h == 0) a.stats[at] = float2{m, l};
+      compiler_fence();
+      if (k + 1 < count) __builtin_amdgcn_s_waitcnt(vmcnt_only(COPIES));
+      else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+      barrier_lds_only();                  // the tile has landed, and every wave is through with the one two before it
+      compiler_fence();
+      if (k + 2 < count) fetch(k + 2);
+      compiler_fence();
+      if (k % 64 == 0 && k != 0) flags = a.tiles[tile0 + min(k + lane, count - 1)].flags;
+      const int flag = __builtin_amdgcn_readlane(flags, k % 64), t0 = (j0 + k) * kChunkUnit;
+      if (late && due) values(k - 1, flag_before);
+      due = t0 < rows.wave_sees;
+      flag_before = flag;
+      if (due) {
+        v16f s[2];
+        rows.logits(ring[k % kWideStages], s);
+        rows.softmax(s, p, t0, flag & 1, flag >> 1 & 1, a.scale_log2);
+        if (!late) values(k, flag);
       }
     }
-    // the next item
-    if (j1 < u || !a.split) break;        // (not split, a workgroup has one)
-    x += u + kChunkCost;
-    j0 = 0;
-    if (++tile == chunk_tiles(rq.rows)) {
-      tile = 0;
-      if (++head == H) {
-        head = 0;
-        do r++; while (r < a.R && (rq = attend_request(a, r)).rows == 0);
-        if (r == a.R) break;
-        r = __builtin_amdgcn_readfirstlane(r);
-      }
-    }
+    if (late && due) values(count - 1, flag_before);
+    rows.end(a, rq, walk.head, j0 == 0 && j1 == u, ((size_t)walk.w * 2 + (j0 == 0 ? 1 : 0)) * kChunkRows + 32 * wave + (lane & 31));
+    more = walk.next(a, u, j1);
+    barrier_all_memory();                  // (the ring is the next item's)
   }
 }
 

@@ -52,10 +52,17 @@ int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c) {
 }
 
 constexpr int kCus = 256;
-constexpr int kFewRows = 64;      // query rows of a request and head that cache_attend_kernel takes
+constexpr int kFewRows = 32;      // query rows of a request and head that cache_attend_kernel takes
 // Keys of a request up to this many units are not divided (four requests of 500 tokens 11.0 -> 9.3 us, 256 of 650 56.4 -> 52.0: the joining
 // launch is 4 to 5 us, a unit 0.6 where the machine is empty).
 constexpr int kWholeUnits = 8;
+constexpr int64_t kMostUnpacked = (int64_t)4 << 30;      // bytes of workspace for unpacked keys and values
+#ifndef KWD
+#define KWD 1
+#endif
+#ifndef KWR
+#define KWR 4
+#endif
 
 // One of the two kernels' part of a call.
 struct AttendLaunch {
@@ -64,6 +71,9 @@ struct AttendLaunch {
   int workgroups, join_rows;
   bool split;
   size_t joins, sums, stats;
+  bool wide;                   // the keys and values are unpacked beforehand
+  int unpack_workgroups, most_tiles;
+  size_t unpacked, tiles, poison;
 };
 // How a call is laid out.
 struct AttendPlan {
@@ -117,6 +127,15 @@ AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& 
     l.workgroups = (int)(l.split ? (units < kCus ? (units > 0 ? units : 1) : kCus) : tiles * p.H);
     l.join_rows = kChunkRows;
     lay_out(l, kChunkRows);
+    const int64_t key_tiles = with * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit);
+    l.wide = KWD && total >= KWR * kChunkRows * with && key_tiles * p.d * 256 <= kMostUnpacked;
+    if (l.wide) {
+      l.unpack_workgroups = (int)(key_tiles < 4 * kCus ? key_tiles : 4 * kCus);
+      l.most_tiles = (int)key_tiles;
+      l.unpacked = take((size_t)key_tiles * p.d * 256);
+      l.tiles = take((size_t)key_tiles * sizeof(WideTile));
+      l.poison = take((size_t)key_tiles * (p.d / p.group) * 64);
+    }
   }
   w.total = off;
   return w;
@@ -145,7 +164,17 @@ int launch_attend(AttendArgs a, const AttendPlan& w, char* ws, hipStream_t st) {
   };
   if (w.many) {
     with(w.m);
-    cache_chunk_kernel<D, GROUP><<<w.m.workgroups, 512, 0, st>>>(a);
+    if (w.m.wide) {
+      a.most_tiles = w.m.most_tiles;
+      a.unpacked = ws + w.m.unpacked;
+      a.tiles = (WideTile*)(ws + w.m.tiles);
+      a.poison = (unsigned char*)(ws + w.m.poison);
+      cache_unpack_kernel<D, GROUP><<<w.m.unpack_workgroups, 512, 0, st>>>(a);
+      SERVE_LAUNCH_CHECK();
+      cache_wide_kernel<D, GROUP><<<w.m.workgroups, 512, 0, st>>>(a);
+    } else {
+      cache_chunk_kernel<D, GROUP><<<w.m.workgroups, 512, 0, st>>>(a);
+    }
     SERVE_LAUNCH_CHECK();
     if (w.m.split && w.m.workgroups > 1) {
       cache_join_kernel<D, kChunkRows, 1><<<dim3(w.m.workgroups - 1, kChunkRows / 4), 256, 0, st>>>(a);
@@ -278,7 +307,7 @@ int sagebwd_cache_attention(const void* Q, const void* pool, const int32_t* bloc
   if (workspace_bytes < w.total) return SAGEBWD_WORKSPACE_TOO_SMALL;
   if (workspace == nullptr || !aligned(workspace, 256)) return SAGEBWD_INVALID_ARG;
   char* ws = (char*)workspace;
-  AttendArgs a;
+  AttendArgs a = {};
   a.Q = (const __bf16*)Q;
   a.pool = (const unsigned char*)pool;
   a.table = block_table;
