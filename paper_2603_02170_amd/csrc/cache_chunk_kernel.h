@@ -116,6 +116,9 @@ __device__ __forceinline__ int chunk_tiles(int rows) { return (rows + kChunkRows
 __device__ __forceinline__ int chunk_units(const AttendArgs& a, const AttendRequest& q, int tile) {
   return max(1, (attend_visible(a, q, tile * kChunkRows, kChunkRows) + kChunkUnit - 1) / kChunkUnit);
 }
+// The row tile at a place of a head's line: the last ones see most, so light and heavy take turns and a share of average length cuts every
+// second item instead of each.
+__device__ __forceinline__ int chunk_tile_at(int place, int tiles) { return place & 1 ? tiles - 1 - (place >> 1) : place >> 1; }
 // of a request and head
 __device__ __forceinline__ int chunk_weight(const AttendArgs& a, const AttendRequest& q) {
   const int tiles = chunk_tiles(q.rows);
@@ -131,7 +134,7 @@ __device__ __forceinline__ int chunk_cut(int offset) { return max(0, offset - kC
 // A workgroup's way along the line: (request, head, row tile) from unit j0 on.
 struct ChunkWalk {
   int w, x, end, j0;       // its number; where its item begins in the line; where its share ends
-  int r, head, tile;
+  int r, head, place, tile;
   int before;              // tiles of 64 tokens of the requests in front (of one head)
   AttendRequest rq;
   AttendShares shares;
@@ -204,8 +207,10 @@ struct ChunkWalk {
     if (a.split) {
       head = (begin - x) / weight;
       x += head * weight;
-      tile = 0;
-      for (int u; x + (u = chunk_units(a, rq, tile) + kChunkCost) <= begin; tile++) x += u;
+      place = 0;
+      for (int u; x + (u = chunk_units(a, rq, chunk_tile_at(place, chunk_tiles(rq.rows))) + kChunkCost) <= begin; place++) x += u;
+      place = __builtin_amdgcn_readfirstlane(place);
+      tile = chunk_tile_at(place, chunk_tiles(rq.rows));
       j0 = chunk_cut(begin - x);
     } else {
       const int i = begin - x;
@@ -231,14 +236,15 @@ struct ChunkWalk {
     x += units + kChunkCost;
     if (chunk_cut(end - x) <= 0) return false;
     j0 = 0;
-    if (++tile == chunk_tiles(rq.rows)) {
-      tile = 0;
+    if (++place == chunk_tiles(rq.rows)) {
+      place = 0;
       if (++head == a.g.H) {
         head = 0;
         before += chunk_key_tiles(rq);
         do rq = attend_request(a, ++r); while (rq.rows == 0);     // (there is one: the share goes on)
       }
     }
+    tile = chunk_tile_at(place, chunk_tiles(rq.rows));
     return true;
   }
 };
@@ -381,12 +387,13 @@ template <int D, int GROUP>
 __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
   typedef ChunkTile<D, GROUP> Tile;
   constexpr int HALF = 2 * Tile::FRAG;
-  __shared__ __attribute__((aligned(16))) char Ks[2][HALF], Vs[2][HALF];
-  __shared__ unsigned char poison[2][Tile::NG * 64];
-  __shared__ int exists[2][2], poisoned[2];
+  __shared__ __attribute__((aligned(16))) char Ks[2][HALF], Vs[3][HALF];
+  __shared__ unsigned char poison[4][Tile::NG * 64];
+  __shared__ int exists[4][2], poisoned[4];
   __shared__ ChunkWalk::Scratch scratch;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (tid < 2) poisoned[tid] = -1;
+  if (tid < 4) poisoned[tid] = -1;
+  const bool late = wave >= 4;
   ChunkWalk walk;
   if (!walk.start(a, scratch)) return;
   int tag = 0;      // of a tile, over all items
@@ -407,27 +414,38 @@ __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
     };
     Tile next;
     const int count = visible > 0 ? j1 - j0 : 0;
-    const auto store = [&](int k) { next.store(Ks[k & 1], Vs[k & 1], exists[k & 1], poison[k & 1], &poisoned[k & 1], tag + k); };
+    int v_at = 0;      // (k + 1) % 3 of the tile that is stored next
+    const auto store = [&](int k) {
+      next.store(Ks[k & 1], Vs[v_at], exists[k & 3], poison[k & 3], &poisoned[k & 3], tag + k);
+      v_at = v_at == 2 ? 0 : v_at + 1;
+    };
     if (count > 0) {
       load(next, j0);
       store(0);
       if (count > 1) load(next, j0 + 1);
     }
     __syncthreads();
-    for (int k = 0; k < count; k++) {
-      const int t0 = (j0 + k) * kChunkUnit, at = k & 1;
-      const bool busy = t0 < rows.wave_sees;
-      v16f s[2];
-      if (busy) rows.logits(Ks[at], s);
+    // In interval k every wave has the values of tile k - 1 and the logits of tile k on the matrix pipe; half of the waves form tile k's
+    // probabilities after that, the other half tile k - 1's before it, so that of the two waves of a SIMD one multiplies under the
+    // softmax and the unpacking of the other.
+    v16f s[2];
+    v8bf p[4];
+    const auto probabilities = [&](int k) {
+      const int t0 = (j0 + k) * kChunkUnit;
+      if (t0 < rows.wave_sees) rows.softmax(s, p, t0, exists[k & 3][0], exists[k & 3][1], a.scale_log2);
+    };
+    for (int k = 0, v = 2; k <= count; k++, v = v == 2 ? 0 : v + 1) {      // v = (k + 2) % 3
+      if (late && k > 0) probabilities(k - 1);
+      if (k > 0 && (j0 + k - 1) * kChunkUnit < rows.wave_sees) {
+        rows.values(Vs[v], p);
+        if (poisoned[k - 1 & 3] == tag + k - 1)
+          rows.poison(poison[k - 1 & 3], GROUP, (j0 + k - 1) * kChunkUnit, exists[k - 1 & 3][0], exists[k - 1 & 3][1]);
+      }
+      if (k < count && (j0 + k) * kChunkUnit < rows.wave_sees) rows.logits(Ks[k & 1], s);
+      if (!late && k < count) probabilities(k);
       if (k + 1 < count) {
         store(k + 1);
         if (k + 2 < count) load(next, j0 + k + 2);
-      }
-      if (busy) {
-        v8bf p[4];
-        rows.softmax(s, p, t0, exists[at][0], exists[at][1], a.scale_log2);
-        rows.values(Vs[at], p);
-        if (poisoned[at] == tag + k) rows.poison(poison[at], GROUP, t0, exists[at][0], exists[at][1]);
       }
       __syncthreads();
     }
@@ -508,7 +526,7 @@ __global__ __launch_bounds__(512) void cache_unpack_kernel(AttendArgs a) {
 constexpr int kWideStages = 4;
 
 template <int D, int GROUP>
-__global__ __launch_bounds__(512, 2) void cache_wide_kernel(AttendArgs a) {
+__global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache_wide_kernel(AttendArgs a) {
   constexpr int TILE = 256 * D, COPIES = TILE / 8 / 1024;
   __shared__ __attribute__((aligned(16))) char ring[kWideStages][TILE];
   __shared__ ChunkWalk::Scratch scratch;
@@ -531,19 +549,18 @@ __global__ __launch_bounds__(512, 2) void cache_wide_kernel(AttendArgs a) {
 #pragma unroll
       for (int c = 0; c < COPIES; c++) copy_16(from + c * 1024 + lane * 16, ring[k % kWideStages] + wave * (COPIES * 1024) + c * 1024);
     };
-    // Half of the waves take a tile's values an interval later than the others: of the two of a SIMD one is in its softmax while the other
-    // has the matrix pipe.
+    // (intervals as in cache_chunk_kernel)
+    v16f s[2];
     v8bf p[4];
-    bool due = false;
-    const auto values = [&](int k, int flag) {
-      rows.values(ring[k % kWideStages] + TILE / 2, p);
-      if (flag & 4) rows.poison(a.poison + (tile0 + k) * (D / GROUP * 64), GROUP, (j0 + k) * kChunkUnit, flag & 1, flag >> 1 & 1);
+    int flag = 0, flag_before = 0;
+    const auto probabilities = [&](int k, int flag) {
+      const int t0 = (j0 + k) * kChunkUnit;
+      if (t0 < rows.wave_sees) rows.softmax(s, p, t0, flag & 1, flag >> 1 & 1, a.scale_log2);
     };
     compiler_fence();
     fetch(0);
     if (count > 1) fetch(1);
-    int flag_before = 0;
-    for (int k = 0; k < count; k++) {
+    for (int k = 0; k <= count; k++) {
       compiler_fence();
       if (k + 1 < count) __builtin_amdgcn_s_waitcnt(vmcnt_only(COPIES));
       else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
@@ -552,18 +569,19 @@ __global__ __launch_bounds__(512, 2) void cache_wide_kernel(AttendArgs a) {
       if (k + 2 < count) fetch(k + 2);
       compiler_fence();
       if (k % 64 == 0 && k != 0) flags = a.tiles[tile0 + min(k + lane, count - 1)].flags;
-      const int flag = __builtin_amdgcn_readlane(flags, k % 64), t0 = (j0 + k) * kChunkUnit;
-      if (late && due) values(k - 1, flag_before);
-      due = t0 < rows.wave_sees;
       flag_before = flag;
-      if (due) {
-        v16f s[2];
-        rows.logits(ring[k % kWideStages], s);
-        rows.softmax(s, p, t0, flag & 1, flag >> 1 & 1, a.scale_log2);
-        if (!late) values(k, flag);
+      flag = __builtin_amdgcn_readlane(flags, k % 64);
+      if (late && k > 0) probabilities(k - 1, flag_before);
+      if (k > 0 && (j0 + k - 1) * kChunkUnit < rows.wave_sees) {
+        rows.values(ring[(k - 1) % kWideStages] + TILE / 2, p);
+        if (flag_before & 4)
+          rows.poison(a.poison + (tile0 + k - 1) * (D / GROUP * 64), GROUP, (j0 + k - 1) * kChunkUnit, flag_before & 1, flag_before >> 1 & 1);
+      }
+      if (k < count) {
+        if ((j0 + k) * kChunkUnit < rows.wave_sees) rows.logits(ring[k % kWideStages], s);
+        if (!late) probabilities(k, flag);
       }
     }
-    if (late && due) values(count - 1, flag_before);
     rows.end(a, rq, walk.head, j0 == 0 && j1 == u, ((size_t)walk.w * 2 + (j0 == 0 ? 1 : 0)) * kChunkRows + 32 * wave + (lane & 31));
     more = walk.next(a, u, j1);
     barrier_all_memory();                  // (the ring is the next item's)

@@ -61,7 +61,7 @@ constexpr int64_t kMostUnpacked = (int64_t)4 << 30;      // bytes of workspace f
 #define KWD 1
 #endif
 #ifndef KWR
-#define KWR 4
+#define KWR 8
 #endif
 
 // One of the two kernels' part of a call.
@@ -123,12 +123,13 @@ AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& 
     const int64_t total = (int64_t)c.T * G;
     const int64_t with = w.few ? (total / (l.rows_from + 1) < c.R ? total / (l.rows_from + 1) : c.R) : c.R;      // requests that it may have
     const int64_t tiles = total / kChunkRows + with, units = tiles * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit + kChunkCost);
+    const int64_t key_tiles = with * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit);
+    l.wide = most >= KWR * kChunkRows && (w.few || total >= KWR * kChunkRows * with) && key_tiles * p.d * 256 <= kMostUnpacked;
     l.split = total * p.H / kChunkRows < 4 * kCus && units < 1 << 30;
-    l.workgroups = (int)(l.split ? (units < kCus ? (units > 0 ? units : 1) : kCus) : tiles * p.H);
+    const int64_t slots = l.wide && p.d == 64 ? 2 * kCus : kCus;      // (workgroups that the machine takes at a time)
+    l.workgroups = (int)(l.split ? (units < slots ? (units > 0 ? units : 1) : slots) : tiles * p.H);
     l.join_rows = kChunkRows;
     lay_out(l, kChunkRows);
-    const int64_t key_tiles = with * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit);
-    l.wide = KWD && total >= KWR * kChunkRows * with && key_tiles * p.d * 256 <= kMostUnpacked;
     if (l.wide) {
       l.unpack_workgroups = (int)(key_tiles < 4 * kCus ? key_tiles : 4 * kCus);
       l.most_tiles = (int)key_tiles;
