@@ -350,23 +350,37 @@ struct AttendPiece {
   int begin, n_rows, len, first_sees, visible;
 };
 
+constexpr int kKnown = 256;
 // 64 requests at a time, one a lane: where one ends the next one's sizes are at hand.
 struct AttendCursor {
   int base;                                                // request of lane 0
   int begin, n_rows, len, first_sees, visible, units;      // of request base + lane
   int r, head, j;                                          // the next piece begins here: request, head, unit
+  int (*known)[kKnown];                                    // the same of all requests in LDS, if they are few
   int x, end;                                              // where its item begins in what is dealt out, and where the share ends
   __device__ __forceinline__ bool more(const AttendArgs& a) const { return a.split ? attend_cut(end - x) > j : x < end; }
 
-  __device__ __forceinline__ void look(const AttendArgs& a, int from) {
-    base = from;
-    const AttendRequest q = attend_request(a, min(from + (int)(threadIdx.x & 63), a.R - 1));
+  __device__ __forceinline__ void take(const AttendArgs& a, const AttendRequest& q) {
     begin = q.begin;
     n_rows = q.rows;
     len = q.len;
     first_sees = q.first_sees;
     visible = q.rows > 0 ? attend_visible(a, q, 0, q.rows) : 0;
     units = q.rows > 0 ? max(1, (visible + kUnit - 1) / kUnit) : 0;
+  }
+  __device__ __forceinline__ void look(const AttendArgs& a, int from) {
+    base = from;
+    const int i = min(from + (int)(threadIdx.x & 63), a.R - 1);
+    if (a.R <= kKnown) {
+      begin = known[0][i];
+      n_rows = known[1][i];
+      len = known[2][i];
+      first_sees = known[3][i];
+      visible = known[4][i];
+      units = known[5][i];
+    } else {
+      take(a, attend_request(a, i));
+    }
   }
   // (more)
   __device__ __forceinline__ AttendPiece next(const AttendArgs& a) {
@@ -401,26 +415,35 @@ struct AttendCursor {
 };
 
 template <int D, int GROUP, int NQ>
-__global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
   typedef CacheTile<D, GROUP> Tile;
   constexpr int ROWS = 16 * NQ, PITCH = 64 + 4, RING = kStages * Tile::SLOT;
   __shared__ __attribute__((aligned(16))) char lds[4 * RING];          // the ring of every wave
   __shared__ __attribute__((aligned(16))) float stage[4][16][PITCH];   // their sums for 16 rows and 64 channels
   __shared__ float wave_m[4][ROWS], wave_l[4][ROWS];
-  __shared__ int wave_units[4], found[2];
+  __shared__ int wave_units[4], found[2], known[6][kKnown];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int H = a.g.H;
   char* ring = lds + wave * RING;
   const Unpack un;
-  const auto shared_units = [&](int r) {           // what is dealt out of a request and head: its units, or all of it
-    const int u = attend_units(a, r);
-    return u == 0 ? 0 : a.split ? u + kItemCost : 1;
-  };
+  const auto shared_units = [&](int u) { return u == 0 ? 0 : a.split ? u + kItemCost : 1; };      // what is dealt out of an item
 
-  // units up to every thread's requests (R / 256 each)
+  // units up to every thread's requests (R / 256 each; where that is one it is kept)
   const int per = (a.R + 255) / 256, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
+  AttendCursor cursor;
+  cursor.known = known;
   int mine = 0;
-  for (int r = r0; r < r1; r++) mine += shared_units(r);
+  if (a.R <= kKnown) {
+    if (tid < a.R) {
+      cursor.take(a, attend_request(a, tid));
+      const int x[6] = {cursor.begin, cursor.n_rows, cursor.len, cursor.first_sees, cursor.visible, cursor.units};
+#pragma unroll
+      for (int i = 0; i < 6; i++) known[i][tid] = x[i];
+      mine = shared_units(cursor.units);
+    }
+  } else {
+    for (int r = r0; r < r1; r++) mine += shared_units(attend_units(a, r));
+  }
   int upto = mine;
   for (int k = 1; k < 64; k <<= 1) {
     const int u = __shfl_up(upto, k);
@@ -442,7 +465,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
   if ((upto - mine) * H <= begin && begin < upto * H) {
     int at = upto - mine;
     for (int r = r0; r < r1; r++) {
-      const int u = shared_units(r);
+      const int u = shared_units(a.R <= kKnown ? known[5][r] : attend_units(a, r));
       if (begin < (at + u) * H) {
         found[0] = r;
         found[1] = begin - at * H;
@@ -452,7 +475,6 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void cache_attend_kernel(Atte
     }
   }
   __syncthreads();
-  AttendCursor cursor;
   cursor.r = __builtin_amdgcn_readfirstlane(found[0]);
   cursor.look(a, cursor.r);
   {

@@ -95,25 +95,26 @@ AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& 
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
   const auto lay_out = [&](AttendLaunch& l, int tile) {
     const size_t parts = l.split ? (size_t)l.workgroups * 2 * tile : 0;
-    l.joins = take((size_t)l.workgroups * 16);
+    l.joins = take((size_t)l.workgroups * sizeof(int4));
     l.sums = take(parts * p.d * 4);
     l.stats = take(parts * 8);
   };
   // Few rows a request: all of them to the one kernel.  Else the requests of one new token (and what fits the same tiles) go to it, the others to
   // the kernel for many rows; where every request brings the same number there are none of the former.
   w.many = rows > kFewRows;
-  w.few = !w.many || (int64_t)c.T < (int64_t)c.R * c.max_new;
+  w.few = !w.many || (G <= kFewRows && (int64_t)c.T < (int64_t)c.R * c.max_new);
   if (w.few) {
     AttendLaunch& l = w.f;
     const int64_t here = w.many ? (G > 16 ? G : 16) : rows;
-    l.nq = here <= 16 ? 1 : here <= 32 ? 2 : 4;
+    l.nq = here <= 16 ? 1 : 2;
     l.rows_from = 0;
     l.rows_to = 16 * l.nq;
     l.join_rows = (int)(here < l.rows_to ? here : l.rows_to);
     const int most_units = (w.max_length + kUnit - 1) / kUnit;
     l.split = most_units > kWholeUnits;
     const int64_t units = (int64_t)c.R * p.H * (l.split ? most_units + kItemCost : 1);
-    l.workgroups = (int)(units < 2 * kCus ? (units > 0 ? units : 1) : 2 * kCus);
+    const int64_t slots = 2 * kCus;
+    l.workgroups = (int)(units < slots ? (units > 0 ? units : 1) : slots);
     lay_out(l, 16 * l.nq);
   }
   if (w.many) {
@@ -184,11 +185,7 @@ int launch_attend(AttendArgs a, const AttendPlan& w, char* ws, hipStream_t st) {
   }
   if (w.few) {
     with(w.f);
-    switch (w.f.nq) {
-      case 1: return launch_few<D, GROUP, 1>(a, w.f, st);
-      case 2: return launch_few<D, GROUP, 2>(a, w.f, st);
-      default: return launch_few<D, GROUP, 4>(a, w.f, st);
-    }
+    return w.f.nq == 1 ? launch_few<D, GROUP, 1>(a, w.f, st) : launch_few<D, GROUP, 2>(a, w.f, st);
   }
   return SAGEBWD_OK;
 }
