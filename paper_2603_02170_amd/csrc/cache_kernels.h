@@ -19,20 +19,31 @@ struct CacheGeometry {
 };
 
 // ---- bookkeeping -----------------------------------------------------------------------------------------------
-// Inclusive sum over the 1024 threads of a workgroup.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* wave_sums) {
+// Inclusive sums over the threads of a workgroup of WAVES waves, N of them at once, that stop at kFull (sizes that are not valid are taken out
+// before, but many valid ones may sum to more than 32 bits hold; what they are compared with is less).
+constexpr unsigned kFull = 0x7FFFFFFFu;
+template <int WAVES, int N>
+__device__ __forceinline__ void block_scan(unsigned (&v)[N], unsigned (*wave_sums)[N]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
   for (int k = 1; k < 64; k <<= 1) {
-    const int64_t u = __shfl_up(v, k);
-    if (lane >= k) v += u;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const unsigned u = __shfl_up(v[i], k);
+      if (lane >= k) v[i] = min(v[i] + u, kFull);
+    }
+  }
+  if (WAVES == 1) return;
+  __syncthreads();
+  if (lane == 63) {
+#pragma unroll
+    for (int i = 0; i < N; i++) wave_sums[wave][i] = v[i];
   }
   __syncthreads();
-  if (lane == 63) wave_sums[wave] = v;
-  __syncthreads();
-  int64_t before = 0;
-  for (int k = 0; k < 16; k++)
-    if (k < wave) before += wave_sums[k];
-  return v + before;
+  for (int k = 0; k < wave; k++) {
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = min(v[i] + wave_sums[k][i], kFull);
+  }
 }
 
 struct PlanArgs {
@@ -43,20 +54,20 @@ struct PlanArgs {
   int R, columns, page_shift, capacity, rows;
 };
 
-// Slot and position of row `row`; `cu`, `lengths`, `granted` and the table are complete.
-__device__ __forceinline__ void plan_row(const PlanArgs& a, int row) {
+// Slot and position of row `row`; `cu` (the array or a copy of it), `lengths`, `granted` and the table are complete.
+__device__ __forceinline__ void plan_row(const PlanArgs& a, const int32_t* cu, int row) {
   int64_t slot = -1;
   int position = 0;
-  if (row < a.cu[a.R]) {
+  if (row < cu[a.R]) {
     int lo = 0, hi = a.R;            // the last request that begins at or before the row and has tokens
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (a.cu[mid] <= row) lo = mid;
+      if (cu[mid] <= row) lo = mid;
       else hi = mid;
     }
     if (a.granted[lo]) {
-      const int n = a.cu[lo + 1] - a.cu[lo];
-      position = a.lengths[lo] - n + row - a.cu[lo];
+      const int n = cu[lo + 1] - cu[lo];
+      position = a.lengths[lo] - n + row - cu[lo];
       const int entry = a.table[(size_t)lo * a.columns + (position >> a.page_shift)];
       if (entry >= 0) slot = ((int64_t)entry << a.page_shift) + (position & ((1 << a.page_shift) - 1));
     }
@@ -65,40 +76,46 @@ __device__ __forceinline__ void plan_row(const PlanArgs& a, int row) {
   a.positions[row] = position;
 }
 
-// Everything but the rows (and those too where ROWS: few of them).  One workgroup: the sums over the requests are what everything waits
-// for, and a thousand requests are one step of them.
-template <bool ROWS>
-__global__ __launch_bounds__(1024) void cache_plan_kernel(PlanArgs a) {
-  __shared__ int64_t wave_sums[16];
-  __shared__ int64_t taken_to[1024];      // pages granted up to and with a request of this step
-  __shared__ int first_page[1024];        // column of a request's first new page
-  __shared__ int64_t total[3];
+// Everything but the rows (and those too where `with_rows`: few of them).  One workgroup: the sums over the requests are what everything
+// waits for, and as many requests as it has threads are one step of them.  (32 requests take 1 wave 4.0 us, 4 waves 4.4, 16 waves 5.9.)
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void cache_plan_kernel(PlanArgs a, int with_rows) {
+  constexpr int THREADS = 64 * WAVES;
+  __shared__ unsigned sums2[WAVES][2], sums1[WAVES][1];
+  __shared__ unsigned taken_to[THREADS];      // pages granted up to and with a request of this step
+  __shared__ int first_page[THREADS];         // column of a request's first new page
+  __shared__ unsigned total[3];
   const int tid = threadIdx.x;
   const int64_t page = 1 << a.page_shift;
-  const int count = max(0, min(a.free_count[0], a.capacity));
-  int64_t tokens0 = 0, need0 = 0, taken0 = 0;      // sums of the steps before
-  for (int base = 0; base < a.R; base += 1024) {
+  const unsigned count = (unsigned)max(0, min(a.free_count[0], a.capacity));
+  unsigned tokens0 = 0, need0 = 0, taken0 = 0;      // sums of the steps before
+  for (int base = 0; base < a.R; base += THREADS) {
     const int r = base + tid;
-    int64_t held = 0, n = 0, need = 0;
+    int64_t held = 0, n = 0;
+    unsigned need = 0;
     bool valid = false;
     if (r < a.R) {
       held = a.held[r];
       n = a.added[r];
       valid = held >= 0 && n >= 0 && held + n <= (int64_t)a.columns * page;
       if (!valid) n = 0;
-      need = valid ? ((held + n + page - 1) >> a.page_shift) - ((held + page - 1) >> a.page_shift) : 0;
+      need = valid ? (unsigned)(((held + n + page - 1) >> a.page_shift) - ((held + page - 1) >> a.page_shift)) : 0;
     }
-    const int64_t tokens = tokens0 + block_scan(n, wave_sums), needs = need0 + block_scan(need, wave_sums);
-    const bool granted = valid && tokens <= a.rows && (need == 0 || needs <= count);
-    const int64_t taken = taken0 + block_scan(granted ? need : 0, wave_sums);
+    unsigned both[2] = {(unsigned)n, need};
+    block_scan<WAVES>(both, sums2);
+    const unsigned tokens = min(tokens0 + both[0], kFull), needs = min(need0 + both[1], kFull);
+    const bool granted = valid && tokens <= (unsigned)a.rows && (need == 0 || needs <= count);
+    unsigned one[1] = {granted ? need : 0};
+    block_scan<WAVES>(one, sums1);
+    const unsigned taken = taken0 + one[0];           // (at most count)
     taken_to[tid] = taken;
     first_page[tid] = (int)((held + page - 1) >> a.page_shift);
     if (r < a.R) {
-      a.cu[r + 1] = (int)min(tokens, (int64_t)a.rows);
+      a.cu[r + 1] = (int)min(tokens, (unsigned)a.rows);
       a.granted[r] = granted;
       a.lengths[r] = (int)(granted ? held + n : held);
     }
-    if (tid == 1023) {
+    if (tid == THREADS - 1) {
       total[0] = tokens;
       total[1] = needs;
       total[2] = taken;
@@ -106,15 +123,15 @@ __global__ __launch_bounds__(1024) void cache_plan_kernel(PlanArgs a) {
     __syncthreads();
     tokens0 = total[0];
     need0 = total[1];
-    const int64_t end = total[2];
-    for (int64_t k = taken0 + tid; k < end; k += 1024) {       // (k < end <= count <= capacity)
-      int lo = 0, hi = 1023;         // the first request of this step with taken_to > k
+    const unsigned end = total[2];
+    for (unsigned k = taken0 + tid; k < end; k += THREADS) {       // (k < end <= count <= capacity)
+      int lo = 0, hi = THREADS - 1;         // the first request of this step with taken_to > k
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (taken_to[mid] > k) hi = mid;
         else lo = mid + 1;
       }
-      const int64_t before = lo > 0 ? taken_to[lo - 1] : taken0;
+      const unsigned before = lo > 0 ? taken_to[lo - 1] : taken0;
       a.table[(size_t)(base + lo) * a.columns + first_page[lo] + (k - before)] = a.free_pages[count - 1 - k];
     }
     taken0 = end;
@@ -122,17 +139,27 @@ __global__ __launch_bounds__(1024) void cache_plan_kernel(PlanArgs a) {
   }
   if (tid == 0) {
     a.cu[0] = 0;
-    a.free_left[0] = count - (int)taken0;
+    a.free_left[0] = (int)(count - taken0);
   }
-  if (ROWS) {
+  if (with_rows) {
     __threadfence_block();
     __syncthreads();
-    for (int row = tid; row < a.rows; row += 1024) plan_row(a, row);
+    for (int row = tid; row < a.rows; row += THREADS) plan_row(a, a.cu, row);
   }
 }
+// (the search of a row's request runs in LDS where cu fits: 300 requests, 4739 rows 4.6 -> ROWUS us)
 __global__ __launch_bounds__(256) void cache_plan_rows_kernel(PlanArgs a) {
+  constexpr int MOST = 4096;
+  __shared__ int32_t cu[MOST];
   const int row = blockIdx.x * 256 + threadIdx.x;
-  if (row < a.rows) plan_row(a, row);
+  const bool fits = a.R < MOST;
+  if (fits) {
+    for (int i = threadIdx.x; i <= a.R; i += 256) cu[i] = a.cu[i];
+    __syncthreads();
+  }
+  if (row >= a.rows) return;
+  if (fits) plan_row(a, cu, row);
+  else plan_row(a, a.cu, row);
 }
 
 struct TrimArgs {
@@ -141,56 +168,57 @@ struct TrimArgs {
   int R, columns, page_shift, capacity;
 };
 __global__ __launch_bounds__(1024) void cache_trim_kernel(TrimArgs a) {
-  __shared__ int64_t wave_sums[16];
-  __shared__ int64_t freed_to[1024];
+  __shared__ unsigned sums[16][1];
+  __shared__ unsigned freed_to[1024];
   __shared__ int first_page[1024];
-  __shared__ int64_t total;
+  __shared__ unsigned total;
   const int tid = threadIdx.x;
   const int64_t page = 1 << a.page_shift;
-  const int count = max(0, min(a.free_count[0], a.capacity));
+  const unsigned count = (unsigned)max(0, min(a.free_count[0], a.capacity));
   // pages of a request from the first it loses to its last
-  auto freed_of = [&](int r, int& first) -> int {
+  auto freed_of = [&](int r, int& first) -> unsigned {
     const int len = a.lengths[r], keep = a.keep[r];
     first = 0;
     if (keep < 0 || keep > len) return 0;
     first = (int)((keep + page - 1) >> a.page_shift);
     const int end = (int)min((len + page - 1) >> a.page_shift, (int64_t)a.columns);
-    return max(0, end - first);
+    return (unsigned)max(0, end - first);
   };
-  int64_t all = 0;
+  unsigned all = 0;
   {
-    int64_t mine = 0;
+    unsigned mine[1] = {0};
     for (int r = tid; r < a.R; r += 1024) {
       int first;
-      mine += freed_of(r, first);
+      mine[0] = min(mine[0] + freed_of(r, first), kFull);
     }
-    const int64_t s = block_scan(mine, wave_sums);
-    if (tid == 1023) total = s;
+    block_scan<16>(mine, sums);
+    if (tid == 1023) total = mine[0];
     __syncthreads();
     all = total;
     __syncthreads();
   }
-  int64_t before_step = 0;
+  unsigned before_step = 0;
   for (int base = 0; base < a.R; base += 1024) {
     const int r = base + tid;
     int first = 0;
-    const int n = r < a.R ? freed_of(r, first) : 0;
-    const int64_t to = before_step + block_scan(n, wave_sums);
+    unsigned n[1] = {r < a.R ? freed_of(r, first) : 0};
+    block_scan<16>(n, sums);
+    const unsigned to = min(before_step + n[0], kFull);
     freed_to[tid] = to;
     first_page[tid] = first;
     if (tid == 1023) total = to;
     __syncthreads();
-    const int64_t end = total;
-    for (int64_t k = before_step + tid; k < end; k += 1024) {
+    const unsigned end = total;
+    for (unsigned k = before_step + tid; k < end; k += 1024) {
       int lo = 0, hi = 1023;
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (freed_to[mid] > k) hi = mid;
         else lo = mid + 1;
       }
-      const int64_t before = lo > 0 ? freed_to[lo - 1] : before_step;
+      const unsigned before = lo > 0 ? freed_to[lo - 1] : before_step;
       int32_t* entry = a.table + (size_t)(base + lo) * a.columns + first_page[lo] + (k - before);
-      const int64_t at = count + (all - 1 - k);      // the first page freed ends on top
+      const int64_t at = (int64_t)count + (all - 1 - k);      // the first page freed ends on top
       if (at < a.capacity) a.free_pages[at] = *entry;
       *entry = -1;
     }
@@ -201,7 +229,7 @@ __global__ __launch_bounds__(1024) void cache_trim_kernel(TrimArgs a) {
     before_step = end;
     __syncthreads();
   }
-  if (tid == 0) a.free_count[0] = (int)min(count + all, (int64_t)a.capacity);
+  if (tid == 0) a.free_count[0] = (int)min((int64_t)count + all, (int64_t)a.capacity);
 }
 
 // ---- storing and reading ---------------------------------------------------------------------------------------
@@ -247,6 +275,14 @@ struct StoreArgs {
   CacheGeometry g;
 };
 
+__device__ __forceinline__ void subtract_mean(float* x, const float* mean, int at) {
+  typedef v4f v4f_dword __attribute__((aligned(4)));
+  if (mean == nullptr) return;
+  const v4f a = *(const v4f_dword*)(mean + at), b = *(const v4f_dword*)(mean + at + 4);
+#pragma unroll
+  for (int i = 0; i < 8; i++) x[i] -= i < 4 ? a[i & 3] : b[i & 3];
+}
+
 // d / 8 lanes have a token of a head, 8 channels each.  A lane's channels of K are one word; of V they lie in eight half-words, whose
 // other nibbles three lanes of the same half have (2, 4 and 6 away): those are joined and each lane stores two.
 template <int D, int GROUP>
@@ -264,9 +300,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(StoreArgs a) {
     const v8bf x = *(const v8bf*)(a.K + t * a.ks[0] + h * a.ks[1] + c), y = *(const v8bf*)(a.V + t * a.vs[0] + h * a.vs[1] + c);
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      k[i] = (float)x[i] - (a.k_mean != nullptr ? a.k_mean[h * D + c + i] : 0.f);
-      v[i] = (float)y[i] - (a.v_mean != nullptr ? a.v_mean[h * D + c + i] : 0.f);
+      k[i] = (float)x[i];
+      v[i] = (float)y[i];
     }
+    subtract_mean(k, a.k_mean, h * D + c);
+    subtract_mean(v, a.v_mean, h * D + c);
   }
   int kq[8], vq[8];
   const unsigned short ksc = quantise4<GROUP>(k, kq), vsc = quantise4<GROUP>(v, vq);

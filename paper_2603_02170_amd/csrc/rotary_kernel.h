@@ -14,7 +14,7 @@ struct RotaryArgs {
   int N, tokens, d, half;   // half = rotary_dim / 2 frequencies
   int heads[2];
   int axes, end[4];         // end[a]: first frequency behind axis a
-  int pieces;               // threads a token and group of heads takes: ceil(d / 16)
+  int pieces;               // threads a token and group of heads takes: d / (2 F)
   int heads_per_thread, head_groups[2];
   float sign;
 };
@@ -31,14 +31,15 @@ __device__ __forceinline__ void turn_of(double turns, float sign, float& c, floa
   s = sign * sv;
 }
 
-// A thread has 16 channels of a token (8 frequencies, or 16 channels that are copied) and up to heads_per_thread heads, for which it
-// forms sine and cosine once: y1 = x1 cos - x2 sin, y2 = x2 cos + x1 sin.  The bytes of x and y are what bounds it; the angles cost
-// about 50 instructions a frequency, which several heads share.
-template <bool ADJACENT, typename POS>
+// A thread has F frequencies of a token (2 F channels; or 2 F channels that are copied) and up to heads_per_thread heads, for which it forms sine
+// and cosine once: y1 = x1 cos - x2 sin, y2 = x2 cos + x1 sin.  The bytes of x and y are what bounds it; the angles cost about 50
+// instructions a frequency, which eight heads share (16381 tokens of 32 heads of 64: 56 us, 4.8 TB/s).  A few tokens are bound by a thread's own
+// chain: they take two frequencies a thread (32 tokens of 40 heads of 128: ROTUS).
+template <int F, bool ADJACENT, typename POS>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
-  const unsigned per_token = a.pieces;
+  typedef __bf16 vec __attribute__((ext_vector_type(F)));
   const unsigned id = blockIdx.x * 256u + threadIdx.x;
-  const unsigned token = id / per_token, piece = id % per_token;
+  const unsigned token = id / (unsigned)a.pieces, piece = id % (unsigned)a.pieces;
   if (token >= (unsigned)a.tokens) return;
   int group = blockIdx.y;
   const int which = group >= a.head_groups[0];
@@ -50,52 +51,52 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   __bf16* y = a.y[which] + b * a.ys[which][0] + n * a.ys[which][1];
   const int64_t xh = a.xs[which][2], yh = a.ys[which][2];
 
-  const int f0 = piece * 8;          // first frequency, or (f0 >= half) channels 2 f0 ..  that pass through
-  if (f0 >= a.half) {
-    const int c = 2 * f0;
-    for (int h = h0; h < h1; h++) {
-      const v4i u = *(const v4i*)(x + h * xh + c), w = *(const v4i*)(x + h * xh + c + 8);
-      *(v4i*)(y + h * yh + c) = u;
-      *(v4i*)(y + h * yh + c + 8) = w;
-    }
-    return;
-  }
-  float cs[8], sn[8];
-  {
+  // halves: F channels from f0 and F from half + f0; adjacent, or channels that pass through: 2 F channels from 2 f0
+  const int f0 = piece * F;
+  const bool passes = f0 >= a.half, split = !ADJACENT && !passes;
+  const int c0 = split ? f0 : 2 * f0, c1 = split ? a.half + f0 : 2 * f0 + F;
+  vec u = *(const vec*)(x + h0 * xh + c0), w = *(const vec*)(x + h0 * xh + c1);      // (the angles are formed under the loads)
+  float cs[F], sn[F];
+  if (!passes) {
     const POS* pos = (const POS*)a.positions + token;
     double p[4];
 #pragma unroll
     for (int k = 0; k < 4; k++) p[k] = k < a.axes ? (double)pos[(size_t)k * a.tokens] : 0.0;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
+    for (int i = 0; i < F; i++) {
       const int f = f0 + i;
       const double at = f < a.end[0] ? p[0] : f < a.end[1] ? p[1] : f < a.end[2] ? p[2] : p[3];
       turn_of(at * (double)a.inv_freq[f] * 0.15915494309189533577, a.sign, cs[i], sn[i]);
     }
   }
-  // halves: 8 channels from f0 and 8 from half + f0; adjacent: 16 channels from 2 f0
-  const int c0 = ADJACENT ? 2 * f0 : f0, c1 = ADJACENT ? 2 * f0 + 8 : a.half + f0;
   for (int h = h0; h < h1; h++) {
-    const v8bf u = *(const v8bf*)(x + h * xh + c0), w = *(const v8bf*)(x + h * xh + c1);
-    v8bf r, t;
+    if (h > h0) {
+      u = *(const vec*)(x + h * xh + c0);
+      w = *(const vec*)(x + h * xh + c1);
+    }
+    vec r = u, t = w;
+    if (!passes) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const float x1 = ADJACENT ? (float)(i < 4 ? u[2 * (i & 3)] : w[2 * (i & 3)]) : (float)u[i];
-      const float x2 = ADJACENT ? (float)(i < 4 ? u[2 * (i & 3) + 1] : w[2 * (i & 3) + 1]) : (float)w[i];
-      const __bf16 y1 = (__bf16)(x1 * cs[i] - x2 * sn[i]), y2 = (__bf16)(x2 * cs[i] + x1 * sn[i]);
-      if (!ADJACENT) {
-        r[i] = y1;
-        t[i] = y2;
-      } else if (i < 4) {
-        r[2 * i] = y1;
-        r[2 * i + 1] = y2;
-      } else {
-        t[2 * (i - 4)] = y1;
-        t[2 * (i - 4) + 1] = y2;
+      for (int i = 0; i < F; i++) {
+        // pair i: (u[i], w[i]), or channels 2 i, 2 i + 1 of the two pieces
+        const int j = 2 * i % F;
+        const float x1 = ADJACENT ? (float)(2 * i < F ? u[j] : w[j]) : (float)u[i];
+        const float x2 = ADJACENT ? (float)(2 * i < F ? u[j + 1] : w[j + 1]) : (float)w[i];
+        const __bf16 y1 = (__bf16)(x1 * cs[i] - x2 * sn[i]), y2 = (__bf16)(x2 * cs[i] + x1 * sn[i]);
+        if (!ADJACENT) {
+          r[i] = y1;
+          t[i] = y2;
+        } else if (2 * i < F) {
+          r[j] = y1;
+          r[j + 1] = y2;
+        } else {
+          t[j] = y1;
+          t[j + 1] = y2;
+        }
       }
     }
-    *(v8bf*)(y + h * yh + c0) = r;
-    *(v8bf*)(y + h * yh + c1) = t;
+    *(vec*)(y + h * yh + c0) = r;
+    *(vec*)(y + h * yh + c1) = t;
   }
 }
 

@@ -222,13 +222,15 @@ int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block
   const PlanArgs a{held, added, free_pages, free_count, block_table, slots, positions, cu_new, lengths, granted, free_left,
                    R, columns, page_shift_of(page), capacity, rows};
   hipStream_t st = (hipStream_t)stream;
-  if (rows <= 2048) {
-    cache_plan_kernel<true><<<1, 1024, 0, st>>>(a);
-    SERVE_LAUNCH_CHECK();
-    return SAGEBWD_OK;
-  }
-  cache_plan_kernel<false><<<1, 1024, 0, st>>>(a);
+  const int with_rows = rows <= 2048;        // (else a launch of their own, over the machine)
+#ifndef PW1
+#define PW1 64
+#endif
+  if (R <= PW1 && rows <= 4 * PW1) cache_plan_kernel<1><<<1, 64, 0, st>>>(a, with_rows);
+  else if (R <= 256 && rows <= 1024) cache_plan_kernel<4><<<1, 256, 0, st>>>(a, with_rows);
+  else cache_plan_kernel<16><<<1, 1024, 0, st>>>(a, with_rows);
   SERVE_LAUNCH_CHECK();
+  if (with_rows) return SAGEBWD_OK;
   cache_plan_rows_kernel<<<(rows + 255) / 256, 256, 0, st>>>(a);
   SERVE_LAUNCH_CHECK();
   return SAGEBWD_OK;
@@ -375,20 +377,22 @@ int sagebwd_rotary(const void* Q, const void* K, void* Qo, void* Ko, const void*
     if (k < p->axes) at += p->sections[k];
     a.end[k] = at;
   }
-  a.pieces = p->d / 16;
   a.sign = p->inverse ? -1.f : 1.f;
-  const int64_t threads = (int64_t)a.tokens * a.pieces;
-  a.heads_per_thread = threads >= 65536 ? 8 : 1;
+  // Many tokens: eight frequencies a thread, for eight heads; few: two, for one head.
+  const int64_t many = (int64_t)a.tokens * (p->d / 16);
+  const bool wide = many >= 4096;
+  a.pieces = p->d / (wide ? 16 : 4);
+  a.heads_per_thread = many >= 65536 ? 8 : 1;
   for (int k = 0; k < 2; k++) a.head_groups[k] = (a.heads[k] + a.heads_per_thread - 1) / a.heads_per_thread;
-  const dim3 grid((unsigned)((threads + 255) / 256), a.head_groups[0] + a.head_groups[1]);
+  const dim3 grid((unsigned)(((int64_t)a.tokens * a.pieces + 255) / 256), a.head_groups[0] + a.head_groups[1]);
   hipStream_t st = (hipStream_t)stream;
-  if (p->adjacent) {
-    if (p->positions64) rotary_kernel<true, int64_t><<<grid, 256, 0, st>>>(a);
-    else rotary_kernel<true, int32_t><<<grid, 256, 0, st>>>(a);
-  } else {
-    if (p->positions64) rotary_kernel<false, int64_t><<<grid, 256, 0, st>>>(a);
-    else rotary_kernel<false, int32_t><<<grid, 256, 0, st>>>(a);
-  }
+  const auto launch = [&](auto adjacent, auto pos) {
+    typedef decltype(pos) P;
+    if (wide) rotary_kernel<8, decltype(adjacent)::value, P><<<grid, 256, 0, st>>>(a);
+    else rotary_kernel<2, decltype(adjacent)::value, P><<<grid, 256, 0, st>>>(a);
+  };
+  if (p->adjacent) p->positions64 ? launch(std::true_type(), int64_t()) : launch(std::true_type(), int32_t());
+  else p->positions64 ? launch(std::false_type(), int64_t()) : launch(std::false_type(), int32_t());
   SERVE_LAUNCH_CHECK();
   return SAGEBWD_OK;
 }
