@@ -136,7 +136,7 @@ __device__ __forceinline__ float column_sum(float v) {
 
 // 32 tokens of a head.  They come past the registers into a ring of the wave's own in LDS (K's codes, V's, the scales, as they lie in
 // the page), two tiles ahead; a lane (column m, g) then takes its operands.  (In registers one tile ahead was all that fitted, and
-// the 16 lanes of a group each fetched the same scales: 61 us for 64 requests that now take RINGUS.)
+// the 16 lanes of a group each fetched the same scales: the launch of 64 requests took 61 us, then 53.)
 template <int D, int GROUP>
 struct CacheTile {
   static constexpr int NG = D / GROUP, CODES = 16 * D, SCALES = 64 * NG, SLOT = 2 * CODES + (2 * SCALES > 256 ? 2 * SCALES : 256);
@@ -264,18 +264,20 @@ __device__ __forceinline__ void attend_tile(AttendRows<D, GROUP> (&rows)[NQ], Ca
     }
   }
   __builtin_amdgcn_sched_barrier(0);           // (left to itself the compiler unpacks everything first, which the registers do not hold)
-  v8bf pt[NQ][NG];
+  int seen[NQ][4];
 #pragma unroll
   for (int q = 0; q < NQ; q++) {
     AttendRows<D, GROUP>& R = rows[q];
-    int seen[4] = {-1, -1, -1, -1};              // of the octet's scales of V: one that is not seen may be anything
+    // of the octet's scales of V: one that is not seen may be anything
+#pragma unroll
+    for (int i = 0; i < 4; i++) seen[q][i] = -1;
     if (masked) {
       asm volatile("");                          // (stays a branch: as selects it is a tenth of the tile's instructions)
       const int behind = R.sees - t0 - 8 * g;    // tokens of the octet that the query sees
 #pragma unroll
       for (int i = 0; i < 8; i++) s[q][i] = i < behind ? s[q][i] : -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 4; i++) seen[i] = (2 * i < behind ? 0xFFFF : 0) | (2 * i + 1 < behind ? (int)0xFFFF0000 : 0);
+      for (int i = 0; i < 4; i++) seen[q][i] = (2 * i < behind ? 0xFFFF : 0) | (2 * i + 1 < behind ? (int)0xFFFF0000 : 0);
     }
     float top = -INFINITY;
 #pragma unroll
@@ -290,40 +292,43 @@ __device__ __forceinline__ void attend_tile(AttendRows<D, GROUP> (&rows)[NQ], Ca
       R.m = to;
     }
     const float ref = R.m == -INFINITY ? 0.f : R.m;
-    float p[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][i], scale_log2, -ref));
-      R.l += p[i];
-    }
-#pragma unroll
-    for (int gr = 0; gr < NG; gr++) {
-      v4i pb;
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const int w = t.vs[gr][i] & seen[i];
-        pb[i] = pack_bf16(p[2 * i] * low_bf16(w), p[2 * i + 1] * high_bf16(w));
-      }
-      pt[q][gr] = as_bf16(pb);
+      s[q][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][i], scale_log2, -ref));
+      R.l += s[q][i];
     }
   }
-  __builtin_amdgcn_sched_barrier(0);
   const int minus24 = (int)0xC1C0C1C0;
   const v8bf less = as_bf16(v4i{minus24, minus24, minus24, minus24});
 #pragma unroll
-  for (int v = 0; v < D / 16; v++) {
-    const v4i& w = t.v[v / 4];
-    v4i x;
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-      x[i] = v % 4 == 0 ? un.pair<0>(w[i]) : v % 4 == 1 ? un.pair<1>(w[i]) : v % 4 == 2 ? un.pair<2>(w[i]) : un.pair<3>(w[i]);
+  for (int gr = 0; gr < NG; gr++) {
+    __builtin_amdgcn_sched_barrier(0);
+    v8bf pt[NQ];
 #pragma unroll
     for (int q = 0; q < NQ; q++) {
-      rows[q].o[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(less, pt[q][16 * v / GROUP], rows[q].o[v], 0, 0, 0);
-      rows[q].o[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(x), pt[q][16 * v / GROUP], rows[q].o[v], 0, 0, 0);
+      v4i pb;
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const int w = t.vs[gr][i] & seen[q][i];
+        pb[i] = pack_bf16(s[q][2 * i] * low_bf16(w), s[q][2 * i + 1] * high_bf16(w));
+      }
+      pt[q] = as_bf16(pb);
     }
-    if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int v = gr * GROUP / 16; v < (gr + 1) * GROUP / 16; v++) {
+      const v4i& w = t.v[v / 4];
+      v4i x;
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+        x[i] = v % 4 == 0 ? un.pair<0>(w[i]) : v % 4 == 1 ? un.pair<1>(w[i]) : v % 4 == 2 ? un.pair<2>(w[i]) : un.pair<3>(w[i]);
+#pragma unroll
+      for (int q = 0; q < NQ; q++) {
+        rows[q].o[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(less, pt[q], rows[q].o[v], 0, 0, 0);
+        rows[q].o[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(x), pt[q], rows[q].o[v], 0, 0, 0);
+      }
+    }
   }
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // Writes channels c .. c + N - 1 of a finished row.
@@ -601,7 +606,8 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
 // Joins the parts of an item that several workgroups had, in the order of the keys: the workgroup at the first border inside it has left word
 // (AttendArgs::joins).  WAVES waves a row: with four every lane weighs a part, then each wave takes every fourth part, several loads in
 // flight, and they meet in LDS (one wave and one part after the other took 97 us for the 128 parts of a request alone, now 7); of many
-// rows, with few parts each, a wave has its own.
+// rows, with few parts each, a wave has its own, and several of them (workgroups that find nothing to join cost: 511 borders of 64 workgroups
+// each 13.7 us, of 16 18.1; 255 that nearly all join 22 and 21).
 template <int D, int ROWS, int WAVES>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
   constexpr int NC = D / 64, MOST = 256;
@@ -611,57 +617,57 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
   if (parts == 0) return;
   const AttendRequest rq = attend_request(a, join.y);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int k = WAVES == 4 ? blockIdx.y : blockIdx.y * 4 + wave, row = join.w + k;
-  if (row >= rq.rows) return;
   const size_t slot0 = (size_t)w * 2;
-  const auto at = [&](int p) { return (p == 0 ? slot0 - 1 : slot0 + 2 * (p - 1)) * ROWS + k; };
-  float M = -INFINITY;
-  for (int p = lane; p < parts; p += 64) M = fmaxf(M, a.stats[at(p)].x);
-  M = wave_max_f32(M);
-  float o[NC], l = 0.f;
+  for (int k = WAVES == 4 ? blockIdx.y : blockIdx.y * 4 + wave; k < ROWS && join.w + k < rq.rows; k += WAVES == 4 ? ROWS : gridDim.y * 4) {
+    const auto at = [&](int p) { return (p == 0 ? slot0 - 1 : slot0 + 2 * (p - 1)) * ROWS + k; };
+    float M = -INFINITY;
+    for (int p = lane; p < parts; p += 64) M = fmaxf(M, a.stats[at(p)].x);
+    M = wave_max_f32(M);
+    float o[NC], l = 0.f;
 #pragma unroll
-  for (int i = 0; i < NC; i++) o[i] = 0.f;
-  if constexpr (WAVES == 1) {
+    for (int i = 0; i < NC; i++) o[i] = 0.f;
+    if constexpr (WAVES == 1) {
 #pragma unroll 2
-    for (int p = 0; p < parts; p++) {
-      const float2 s = a.stats[at(p)];
-      const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - M);
-      l += s.y * f;
-      const float* x = a.sums + at(p) * D + NC * lane;
-#pragma unroll
-      for (int i = 0; i < NC; i++) o[i] += x[i] * f;
-    }
-  } else {
-    __shared__ float weight[MOST], meet[4][D + 2];
-    for (int p0 = 0; p0 < parts; p0 += MOST) {
-      const int here = min(parts - p0, MOST);
-      __syncthreads();
-      if (tid < here) {
-        const float2 s = a.stats[at(p0 + tid)];
+      for (int p = 0; p < parts; p++) {
+        const float2 s = a.stats[at(p)];
         const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - M);
-        weight[tid] = f;
         l += s.y * f;
-      }
-      __syncthreads();
-#pragma unroll 4
-      for (int p = wave; p < here; p += 4) {
-        const float f = weight[p];
-        const float* x = a.sums + at(p0 + p) * D + NC * lane;
+        const float* x = a.sums + at(p) * D + NC * lane;
 #pragma unroll
         for (int i = 0; i < NC; i++) o[i] += x[i] * f;
       }
+    } else {
+      __shared__ float weight[MOST], meet[4][D + 2];
+      for (int p0 = 0; p0 < parts; p0 += MOST) {
+        const int here = min(parts - p0, MOST);
+        __syncthreads();
+        if (tid < here) {
+          const float2 s = a.stats[at(p0 + tid)];
+          const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - M);
+          weight[tid] = f;
+          l += s.y * f;
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int p = wave; p < here; p += 4) {
+          const float f = weight[p];
+          const float* x = a.sums + at(p0 + p) * D + NC * lane;
+#pragma unroll
+          for (int i = 0; i < NC; i++) o[i] += x[i] * f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NC; i++) meet[wave][NC * lane + i] = o[i];
+      for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
+      if (lane == 0) meet[wave][D] = l;
+      __syncthreads();
+      if (wave != 0) return;
+      l = (meet[0][D] + meet[1][D]) + (meet[2][D] + meet[3][D]);
+#pragma unroll
+      for (int i = 0; i < NC; i++) o[i] = (meet[0][NC * lane + i] + meet[1][NC * lane + i]) + (meet[2][NC * lane + i] + meet[3][NC * lane + i]);
     }
-#pragma unroll
-    for (int i = 0; i < NC; i++) meet[wave][NC * lane + i] = o[i];
-    for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
-    if (lane == 0) meet[wave][D] = l;
-    __syncthreads();
-    if (wave != 0) return;
-    l = (meet[0][D] + meet[1][D]) + (meet[2][D] + meet[3][D]);
-#pragma unroll
-    for (int i = 0; i < NC; i++) o[i] = (meet[0][NC * lane + i] + meet[1][NC * lane + i]) + (meet[2][NC * lane + i] + meet[3][NC * lane + i]);
+    attend_store<NC>(a, rq.begin, join.z, join.w + k, D, NC * lane, M, l, o);
   }
-  attend_store<NC>(a, rq.begin, join.z, row, D, NC * lane, M, l, o);
 }
 
 }  // namespace sage

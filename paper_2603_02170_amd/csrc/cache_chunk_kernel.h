@@ -139,41 +139,31 @@ struct ChunkWalk {
   AttendRequest rq;
   AttendShares shares;
   struct Scratch {
-    int sums[8], tiles[8], found[4];
+    unsigned sums[8][2];
+    int total, found[4];
   };
 
   // All 512 threads; false: the workgroup has nothing.  Leaves no word for the joining launch.
   __device__ __forceinline__ bool start(const AttendArgs& a, Scratch& s) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, H = a.g.H;
+    const int tid = threadIdx.x, H = a.g.H;
     const int per = (a.R + 511) / 512, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
-    int mine = 0, tiles = 0;
+    unsigned mine = 0, tiles = 0;
     for (int i = r0; i < r1; i++) {
       const AttendRequest q = attend_request(a, i);
-      mine += chunk_weight(a, q);
+      mine = min(mine + (unsigned)chunk_weight(a, q), kFull);
       tiles += chunk_key_tiles(q);
     }
-    int upto = mine, tiles_to = tiles;
-    for (int k = 1; k < 64; k <<= 1) {
-      const int u = __shfl_up(upto, k), v = __shfl_up(tiles_to, k);
-      if (lane >= k) {
-        upto += u;
-        tiles_to += v;
-      }
-    }
-    if (lane == 63) {
-      s.sums[wave] = upto;
-      s.tiles[wave] = tiles_to;
-    }
+    unsigned to[2] = {mine, tiles};
+    block_scan<8>(to, s.sums);
+    if (tid == 511) s.total = (int)to[0];
     __syncthreads();
-    int units = 0;
-#pragma unroll
-    for (int k = 0; k < 8; k++) {
-      if (k < wave) {
-        upto += s.sums[k];
-        tiles_to += s.tiles[k];
-      }
-      units += s.sums[k];
+    const int units = s.total;
+    // (the host has bounded this for a `cu` that rises; another one gets nothing)
+    if ((int64_t)units * H > 1 << 30) {
+      if (tid == 0) a.joins[blockIdx.x] = int4{0, 0, 0, 0};
+      return false;
     }
+    const int upto = (int)to[0], tiles_to = (int)to[1];
     shares = AttendShares(__builtin_amdgcn_readfirstlane(units) * H, a.workgroups);
     // (neighbours in the line to one XCD, whose L2 then holds a head's keys for all its row tiles)
     w = a.split && shares.n == a.workgroups && shares.n % 8 == 0 ? (blockIdx.x & 7) * (shares.n / 8) + (blockIdx.x >> 3) : blockIdx.x;
@@ -181,8 +171,8 @@ struct ChunkWalk {
     if (w >= shares.n) return false;
     const int begin = shares.begin(w);
     end = shares.begin(w + 1);
-    if ((upto - mine) * H <= begin && begin < upto * H) {
-      int at = upto - mine, t = tiles_to - tiles;
+    if ((upto - (int)mine) * H <= begin && begin < upto * H) {
+      int at = upto - (int)mine, t = tiles_to - (int)tiles;
       for (int i = r0; i < r1; i++) {
         const AttendRequest q = attend_request(a, i);
         const int u = chunk_weight(a, q);
@@ -468,30 +458,22 @@ __global__ __launch_bounds__(512) void cache_unpack_kernel(AttendArgs a) {
   typedef ChunkTile<D, GROUP> Tile;
   __shared__ ChunkWalk::Scratch s;
   __shared__ int exists[2], poisoned;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, H = a.g.H;
+  const int tid = threadIdx.x, H = a.g.H;
   const int per = (a.R + 511) / 512, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
-  int tiles = 0;
+  unsigned tiles = 0;
   for (int i = r0; i < r1; i++) tiles += chunk_key_tiles(attend_request(a, i));
-  int upto = tiles;
-  for (int k = 1; k < 64; k <<= 1) {
-    const int u = __shfl_up(upto, k);
-    if (lane >= k) upto += u;
-  }
-  if (lane == 63) s.tiles[wave] = upto;
+  unsigned to[2] = {tiles, 0};
+  block_scan<8>(to, s.sums);
   if (tid == 0) poisoned = -1;
+  if (tid == 511) s.total = (int)to[0];
   __syncthreads();
-  int all = 0;
-#pragma unroll
-  for (int k = 0; k < 8; k++) {
-    if (k < wave) upto += s.tiles[k];
-    all += s.tiles[k];
-  }
-  const AttendShares shares(__builtin_amdgcn_readfirstlane(all) * H, gridDim.x);
+  const int upto = (int)to[0];
+  const AttendShares shares(__builtin_amdgcn_readfirstlane(s.total) * H, gridDim.x);
   if ((int)blockIdx.x >= shares.n) return;
   // (the workspace has room for every request that `cu` can hold, if it rises: what does not fit is left)
   const int begin = shares.begin(blockIdx.x), end = min(shares.begin(blockIdx.x + 1), a.most_tiles);
-  if ((upto - tiles) * H <= begin && begin < upto * H) {
-    int at = upto - tiles;
+  if ((upto - (int)tiles) * H <= begin && begin < upto * H) {
+    int at = upto - (int)tiles;
     for (int i = r0; i < r1; i++) {
       const int u = chunk_key_tiles(attend_request(a, i));
       if (begin < (at + u) * H) {

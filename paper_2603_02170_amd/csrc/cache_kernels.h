@@ -77,7 +77,8 @@ __device__ __forceinline__ void plan_row(const PlanArgs& a, const int32_t* cu, i
 }
 
 // Everything but the rows (and those too where `with_rows`: few of them).  One workgroup: the sums over the requests are what everything
-// waits for, and as many requests as it has threads are one step of them.  (32 requests take 1 wave 4.0 us, 4 waves 4.4, 16 waves 5.9.)
+// waits for, and as many requests as it has threads are one step of them.  (32 requests take 1 wave 2.9 us, 4 waves 3.4; 16
+// waves, of which each knew its 64-bit sums only, 5.9.)
 template <int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void cache_plan_kernel(PlanArgs a, int with_rows) {
   constexpr int THREADS = 64 * WAVES;
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(64 * WAVES) void cache_plan_kernel(PlanArgs a, int 
     for (int row = tid; row < a.rows; row += THREADS) plan_row(a, a.cu, row);
   }
 }
-// (the search of a row's request runs in LDS where cu fits: 300 requests, 4739 rows 4.6 -> ROWUS us)
+// (the search of a row's request runs in LDS where cu fits: 300 requests, 4739 rows 5.0 -> 3.5 us)
 __global__ __launch_bounds__(256) void cache_plan_rows_kernel(PlanArgs a) {
   constexpr int MOST = 4096;
   __shared__ int32_t cu[MOST];
@@ -284,14 +285,16 @@ __device__ __forceinline__ void subtract_mean(float* x, const float* mean, int a
 }
 
 // d / 8 lanes have a token of a head, 8 channels each.  A lane's channels of K are one word; of V they lie in eight half-words, whose
-// other nibbles three lanes of the same half have (2, 4 and 6 away): those are joined and each lane stores two.
+// other nibbles three lanes of the same half have (2, 4 and 6 away): those are joined and each lane stores two.  Neighbouring rows are
+// neighbouring tokens, whose bytes of V are neighbours: in the L2 they meet (8191 tokens of 8 heads of 128: 12.5 us, 3.4 TB/s; with the heads of
+// a token as neighbours 15.6).
 template <int D, int GROUP>
 __global__ __launch_bounds__(256) void cache_append_kernel(StoreArgs a) {
   constexpr int LANES = D / 8, ROWS = 256 / LANES;
   const int l = threadIdx.x % LANES;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
   const bool exists = row < (int64_t)a.T * a.g.H;
-  const int t = exists ? (int)(row / a.g.H) : 0, h = exists ? (int)(row % a.g.H) : 0;
+    const int h = exists ? (int)(row / a.T) : 0, t = exists ? (int)(row % a.T) : 0;
   const int64_t slot = a.slots[t];
   const bool stored = exists && slot >= 0 && slot < ((int64_t)a.g.pages << a.g.page_shift);
   const int c = 8 * l;
@@ -341,7 +344,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(StoreArgs a) {
   const int l = threadIdx.x % LANES;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
   const bool exists = row < (int64_t)a.T * a.g.H;
-  const int t = exists ? (int)(row / a.g.H) : 0, h = exists ? (int)(row % a.g.H) : 0;
+    const int h = exists ? (int)(row / a.T) : 0, t = exists ? (int)(row % a.T) : 0;
   const int64_t slot = a.slots[t];
   const bool stored = slot >= 0 && slot < ((int64_t)a.g.pages << a.g.page_shift);
   const int c = 8 * l, j = l / 2 % 4;
@@ -368,8 +371,9 @@ __global__ __launch_bounds__(256) void cache_read_kernel(StoreArgs a) {
     k[e] = (__bf16)(stored ? x : 0.f);
     v[e] = (__bf16)(stored ? y : 0.f);
   }
-  *(v8bf*)(a.Ko + row * D + c) = k;
-  *(v8bf*)(a.Vo + row * D + c) = v;
+  const size_t to = ((size_t)t * a.g.H + h) * D + c;
+  *(v8bf*)(a.Ko + to) = k;
+  *(v8bf*)(a.Vo + to) = v;
 }
 
 }  // namespace sage

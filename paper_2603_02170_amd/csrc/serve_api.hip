@@ -45,24 +45,25 @@ int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c) {
       !stride_ok(c->q_head_stride))
     return SAGEBWD_INVALID_ARG;
   if (c->Hq % p->H != 0 || c->Hq / p->H > 64 || (int64_t)c->T * c->Hq * p->d >= kMostElements || c->R > 1 << 20 ||
-      (int64_t)c->columns * p->page > INT32_MAX / 2 || (int64_t)c->R * p->H * (c->columns * (int64_t)p->page / kUnit + 1 + kItemCost) > 1 << 30 ||
+      (int64_t)c->columns * p->page > INT32_MAX / 2 || (int64_t)c->R * p->H * (c->columns * (int64_t)p->page / kUnit + 1 + kItemCost) > 1 << 29 ||
       ((int64_t)c->T * (c->Hq / p->H) / kChunkRows + c->R) * p->H > 1 << 30 || (int64_t)c->T * (c->Hq / p->H) > INT32_MAX / 2)
     return SAGEBWD_UNSUPPORTED_SHAPE;
   return SAGEBWD_OK;
 }
 
 constexpr int kCus = 256;
-constexpr int kFewRows = 32;      // query rows of a request and head that cache_attend_kernel takes
+// Query rows of a request and head that cache_attend_kernel takes (32 requests of 4096 tokens, 32 rows: 59 us, the kernel for many rows 135; 64 rows in
+// four tiles a wave, which its registers do not hold at d = 128, 206).
+constexpr int kFewRows = 32;
 // Keys of a request up to this many units are not divided (four requests of 500 tokens 11.0 -> 9.3 us, 256 of 650 56.4 -> 52.0: the joining
 // launch is 4 to 5 us, a unit 0.6 where the machine is empty).
 constexpr int kWholeUnits = 8;
-constexpr int64_t kMostUnpacked = (int64_t)4 << 30;      // bytes of workspace for unpacked keys and values
-#ifndef KWD
-#define KWD 1
-#endif
-#ifndef KWR
-#define KWR 8
-#endif
+// Keys and values are unpacked beforehand where a request's meet so many row tiles (us, unpacked by every tile -> beforehand: 8 requests of 128
+// new tokens x 4 heads of the group against 16384, 2 tiles, 349 -> 485; 4 of 256, 4 tiles, 324 -> 380; one of 512 against 32768, 8 tiles, 315 ->
+// 304; one of 2048 against 10000, 32 tiles, 365 -> 326, at d = 64 501 -> 331), and the workspace for them is at most this.
+constexpr int kWideTiles = 8;
+constexpr int64_t kMostUnpacked = (int64_t)4 << 30;
+constexpr int kJoinGroups = 32;     // workgroups that look at a border between row tiles of 256: 8 rows each
 
 // One of the two kernels' part of a call.
 struct AttendLaunch {
@@ -125,7 +126,7 @@ AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& 
     const int64_t with = w.few ? (total / (l.rows_from + 1) < c.R ? total / (l.rows_from + 1) : c.R) : c.R;      // requests that it may have
     const int64_t tiles = total / kChunkRows + with, units = tiles * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit + kChunkCost);
     const int64_t key_tiles = with * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit);
-    l.wide = most >= KWR * kChunkRows && (w.few || total >= KWR * kChunkRows * with) && key_tiles * p.d * 256 <= kMostUnpacked;
+    l.wide = most >= kWideTiles * kChunkRows && (w.few || total >= kWideTiles * kChunkRows * with) && key_tiles * p.d * 256 <= kMostUnpacked;
     l.split = total * p.H / kChunkRows < 4 * kCus && units < 1 << 30;
     const int64_t slots = l.wide && p.d == 64 ? 2 * kCus : kCus;      // (workgroups that the machine takes at a time)
     l.workgroups = (int)(l.split ? (units < slots ? (units > 0 ? units : 1) : slots) : tiles * p.H);
@@ -179,7 +180,7 @@ int launch_attend(AttendArgs a, const AttendPlan& w, char* ws, hipStream_t st) {
     }
     SERVE_LAUNCH_CHECK();
     if (w.m.split && w.m.workgroups > 1) {
-      cache_join_kernel<D, kChunkRows, 1><<<dim3(w.m.workgroups - 1, kChunkRows / 4), 256, 0, st>>>(a);
+      cache_join_kernel<D, kChunkRows, 1><<<dim3(w.m.workgroups - 1, kJoinGroups), 256, 0, st>>>(a);
       SERVE_LAUNCH_CHECK();
     }
   }
@@ -223,10 +224,7 @@ int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block
                    R, columns, page_shift_of(page), capacity, rows};
   hipStream_t st = (hipStream_t)stream;
   const int with_rows = rows <= 2048;        // (else a launch of their own, over the machine)
-#ifndef PW1
-#define PW1 64
-#endif
-  if (R <= PW1 && rows <= 4 * PW1) cache_plan_kernel<1><<<1, 64, 0, st>>>(a, with_rows);
+  if (R <= 64 && rows <= 256) cache_plan_kernel<1><<<1, 64, 0, st>>>(a, with_rows);
   else if (R <= 256 && rows <= 1024) cache_plan_kernel<4><<<1, 256, 0, st>>>(a, with_rows);
   else cache_plan_kernel<16><<<1, 1024, 0, st>>>(a, with_rows);
   SERVE_LAUNCH_CHECK();
