@@ -19,6 +19,9 @@ using namespace sage;
 #define SERVE_LAUNCH_CHECK() do { if (hipGetLastError() != hipSuccess) return SAGEBWD_HIP_ERROR; } while (0)
 
 constexpr int64_t kMostElements = (int64_t)1 << 40;
+// A launch's threads are counted in 32 bits, its workgroups along y in 16.
+constexpr int64_t kMostThreads = (int64_t)1 << 31;
+constexpr int kMostInY = 65535;
 
 inline bool aligned(const void* p, size_t to = 16) { return ((uintptr_t)p & (to - 1)) == 0; }
 inline bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s <= kMostElements; }
@@ -37,6 +40,17 @@ int check_cache(const sagebwd_cache_params* p, bool pool) {
 }
 CacheGeometry geometry(const sagebwd_cache_params& p) { return CacheGeometry{p.H, p.d, page_shift_of(p.page), p.group, p.pages}; }
 
+constexpr int kCus = 256;
+// Query rows of a request and head that cache_attend_kernel takes (32 requests of 4096 tokens, 32 rows: 59 us, the kernel for many rows 135; 64 rows in
+// four tiles a wave, which its registers do not hold at d = 128, 206).
+constexpr int kFewRows = 32;
+// Row tiles of the kernel for many rows, over all heads, at most; 0 where no request goes to it.
+int64_t chunk_tiles_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
+  const int64_t G = c.Hq / p.H;
+  if ((c.max_new < c.T ? c.max_new : c.T) * G <= kFewRows) return 0;
+  return (c.T * G / kChunkRows + c.R) * p.H;
+}
+
 int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c) {
   const int rc = check_cache(p, true);
   if (rc != SAGEBWD_OK) return rc;
@@ -46,15 +60,11 @@ int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c) {
     return SAGEBWD_INVALID_ARG;
   if (c->Hq % p->H != 0 || c->Hq / p->H > 64 || (int64_t)c->T * c->Hq * p->d >= kMostElements || c->R > 1 << 20 ||
       (int64_t)c->columns * p->page > INT32_MAX / 2 || (int64_t)c->R * p->H * (c->columns * (int64_t)p->page / kUnit + 1 + kItemCost) > 1 << 29 ||
-      ((int64_t)c->T * (c->Hq / p->H) / kChunkRows + c->R) * p->H > 1 << 30 || (int64_t)c->T * (c->Hq / p->H) > INT32_MAX / 2)
+      chunk_tiles_of(*p, *c) > kMostThreads / 512 || (int64_t)c->T * (c->Hq / p->H) > INT32_MAX / 2)
     return SAGEBWD_UNSUPPORTED_SHAPE;
   return SAGEBWD_OK;
 }
 
-constexpr int kCus = 256;
-// Query rows of a request and head that cache_attend_kernel takes (32 requests of 4096 tokens, 32 rows: 59 us, the kernel for many rows 135; 64 rows in
-// four tiles a wave, which its registers do not hold at d = 128, 206).
-constexpr int kFewRows = 32;
 // Keys of a request up to this many units are not divided (four requests of 500 tokens 11.0 -> 9.3 us, 256 of 650 56.4 -> 52.0: the joining
 // launch is 4 to 5 us, a unit 0.6 where the machine is empty).
 constexpr int kWholeUnits = 8;
@@ -257,7 +267,7 @@ int sagebwd_cache_append(const void* K, const void* V, int64_t k_token_stride, i
   if (T == 0) return SAGEBWD_OK;
   if (K == nullptr || V == nullptr || slots == nullptr || pool == nullptr || !aligned(K) || !aligned(V) || !aligned(pool)) return SAGEBWD_INVALID_ARG;
   const int64_t rows = (int64_t)T * params->H, per = 256 / (params->d / 8);
-  if ((rows + per - 1) / per > INT32_MAX) return SAGEBWD_UNSUPPORTED_SHAPE;
+  if ((rows + per - 1) / per * 256 > kMostThreads) return SAGEBWD_UNSUPPORTED_SHAPE;
   const StoreArgs a{(const __bf16*)K, (const __bf16*)V, {k_token_stride, k_head_stride}, {v_token_stride, v_head_stride}, slots, k_mean, v_mean,
                     (unsigned char*)pool, nullptr, nullptr, T, geometry(*params)};
   return with_format(*params, [&](auto d, auto group) -> int {
@@ -275,7 +285,7 @@ int sagebwd_cache_read(const int64_t* slots, int32_t T, const float* k_mean, con
   if (T == 0) return SAGEBWD_OK;
   if (K == nullptr || V == nullptr || slots == nullptr || pool == nullptr || !aligned(K) || !aligned(V) || !aligned(pool)) return SAGEBWD_INVALID_ARG;
   const int64_t rows = (int64_t)T * params->H, per = 256 / (params->d / 8);
-  if ((rows + per - 1) / per > INT32_MAX) return SAGEBWD_UNSUPPORTED_SHAPE;
+  if ((rows + per - 1) / per * 256 > kMostThreads) return SAGEBWD_UNSUPPORTED_SHAPE;
   const StoreArgs a{nullptr, nullptr, {0, 0}, {0, 0}, slots, k_mean, v_mean, (unsigned char*)pool, (__bf16*)K, (__bf16*)V, T, geometry(*params)};
   return with_format(*params, [&](auto d, auto group) -> int {
     cache_read_kernel<decltype(d)::value, decltype(group)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, (hipStream_t)stream>>>(a);
@@ -335,7 +345,7 @@ int sagebwd_rotary(const void* Q, const void* K, void* Qo, void* Ko, const void*
       (p->inverse != 0 && p->inverse != 1) || (p->positions64 != 0 && p->positions64 != 1))
     return SAGEBWD_INVALID_ARG;
   if (p->d < 16 || p->d > 512 || p->d % 16 != 0 || p->rotary_dim < 16 || p->rotary_dim > p->d || p->rotary_dim % 16 != 0 ||
-      (int64_t)p->B * p->N > INT32_MAX / 64 || p->Hq > 65535 || p->Hk > 65535)
+      (int64_t)p->B * p->N > INT32_MAX / 64 || (int64_t)p->Hq + p->Hk > kMostInY)
     return SAGEBWD_UNSUPPORTED_SHAPE;
   int64_t sum = 0;
   for (int k = 0; k < p->axes; k++) {

@@ -163,3 +163,24 @@ def test_device_tensors_that_do_not_fit(lib):
             sage_rotary(*args, **kw)
     with pytest.raises(binding.SageError):
         sage_rotary(Q, None, torch.zeros(3, **i32), torch.ones(40, **cu))        # more frequencies than the channels have pairs
+
+
+def test_calls_larger_than_a_launch_are_refused(lib):
+    """A launch has at most 2^31 threads, and 65535 workgroups along y: more is an unsupported shape, not an error of the runtime."""
+    i64, one, null = ctypes.c_int64, _vp(256), _vp(None)
+    p = cache._CCacheParams(1024, 128, 64, 64, 4, 0)
+    T = 1 << 17        # 2^17 tokens x 1024 heads x 16 threads
+    assert lib.sagebwd_cache_append(one, one, i64(0), i64(128), i64(0), i64(128), one, T + 1, null, null, ctypes.byref(p), one, null) == -2
+    assert lib.sagebwd_cache_read(one, T + 1, null, null, ctypes.byref(p), one, one, one, null) == -2
+    # 2^22 row tiles of 512 threads each: 2^20 requests of 2 tokens x 64 heads of the group, 4 key/value heads, and one tile more
+    p = cache._CCacheParams(4, 64, 32, 64, 4, 0)
+    need = lambda R, T, G, new: lib.sagebwd_cache_workspace_bytes(  # noqa: E731
+        ctypes.byref(p), ctypes.byref(Call(R, T, 4 * G, 1, new, 0, 1, 0.0, 256, 64)), ctypes.byref(ctypes.c_size_t()))
+    assert need((1 << 20) - 512, 2048, 64, 2) == 0 and need(1 << 20, 2048, 64, 2) == -2
+    assert need(1 << 20, 2048, 8, 4) == 0         # (32 rows: no request has the kernel with those tiles)
+    x = Rotary(1, 1, 40000, 30000, 16, 16, 1)
+    x.sections[0] = 8
+    for s in (x.q, x.k, x.qo, x.ko):
+        s[0] = s[1] = 0
+        s[2] = 16
+    assert lib.sagebwd_rotary(one, one, one, one, one, one, ctypes.byref(x), null) == -2
