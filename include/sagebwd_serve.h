@@ -85,7 +85,9 @@ int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block
  * The other way: request r keeps its first keep[r] tokens (0: it is done), and the pages that this frees go back on the
  * stack; the first request's first page is on top, so that trim after plan leaves the stack as it was.  lengths,
  * block_table (freed entries become -1), free_pages and free_count are changed in place.  A keep[r] outside 0 ..
- * lengths[r] leaves the request alone.  (Pages beyond `capacity` are lost: the stack has to hold every page.)
+ * lengths[r] leaves the request alone.  Entries that are not pages (negative) give none back.  (Pages beyond `capacity` are lost: the
+ * stack has to hold every page.  A page that stands in two requests' rows comes back from each: who shares pages counts them and trims
+ * the last one alone.)
  */
 int sagebwd_cache_trim(const int32_t* keep, int32_t* lengths, int32_t* block_table, int32_t* free_pages, int32_t* free_count,
                        int32_t R, int32_t columns, int32_t page, int32_t capacity, void* stream);

@@ -172,7 +172,7 @@ __global__ __launch_bounds__(1024) void cache_trim_kernel(TrimArgs a) {
   __shared__ unsigned sums[16][1];
   __shared__ unsigned freed_to[1024];
   __shared__ int first_page[1024];
-  __shared__ unsigned total;
+  __shared__ unsigned total, in_step;
   const int tid = threadIdx.x;
   const int64_t page = 1 << a.page_shift;
   const unsigned count = (unsigned)max(0, min(a.free_count[0], a.capacity));
@@ -185,50 +185,55 @@ __global__ __launch_bounds__(1024) void cache_trim_kernel(TrimArgs a) {
     const int end = (int)min((len + page - 1) >> a.page_shift, (int64_t)a.columns);
     return (unsigned)max(0, end - first);
   };
+  // Twice over what is freed, 1024 entries of the table at a time: how many of them are pages (entries that are not have none to give back),
+  // then each to its place, the first page freed on top.
   unsigned all = 0;
-  {
-    unsigned mine[1] = {0};
-    for (int r = tid; r < a.R; r += 1024) {
-      int first;
-      mine[0] = min(mine[0] + freed_of(r, first), kFull);
-    }
-    block_scan<16>(mine, sums);
-    if (tid == 1023) total = mine[0];
-    __syncthreads();
-    all = total;
-    __syncthreads();
-  }
-  unsigned before_step = 0;
-  for (int base = 0; base < a.R; base += 1024) {
-    const int r = base + tid;
-    int first = 0;
-    unsigned n[1] = {r < a.R ? freed_of(r, first) : 0};
-    block_scan<16>(n, sums);
-    const unsigned to = min(before_step + n[0], kFull);
-    freed_to[tid] = to;
-    first_page[tid] = first;
-    if (tid == 1023) total = to;
-    __syncthreads();
-    const unsigned end = total;
-    for (unsigned k = before_step + tid; k < end; k += 1024) {
-      int lo = 0, hi = 1023;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (freed_to[mid] > k) hi = mid;
-        else lo = mid + 1;
+  for (int pass = 0; pass < 2; pass++) {
+    unsigned before_step = 0, freed = 0;       // entries, and pages among them, of the steps before
+    for (int base = 0; base < a.R; base += 1024) {
+      const int r = base + tid;
+      int first = 0;
+      unsigned n[1] = {r < a.R ? freed_of(r, first) : 0};
+      block_scan<16>(n, sums);
+      const unsigned to = min(before_step + n[0], kFull);
+      freed_to[tid] = to;
+      first_page[tid] = first;
+      if (tid == 1023) total = to;
+      __syncthreads();
+      const unsigned end = total;
+      for (unsigned k0 = before_step; k0 < end; k0 += 1024) {
+        const unsigned k = k0 + tid;
+        int32_t* entry = nullptr;
+        if (k < end) {
+          int lo = 0, hi = 1023;
+          while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (freed_to[mid] > k) hi = mid;
+            else lo = mid + 1;
+          }
+          const unsigned before = lo > 0 ? freed_to[lo - 1] : before_step;
+          entry = a.table + (size_t)(base + lo) * a.columns + first_page[lo] + (k - before);
+        }
+        const bool has = entry != nullptr && *entry >= 0;
+        unsigned rank[1] = {has ? 1u : 0u};
+        block_scan<16>(rank, sums);
+        if (pass == 1 && entry != nullptr) {
+          const int64_t at = (int64_t)count + ((int64_t)all - freed - rank[0]);
+          if (has && at < a.capacity) a.free_pages[at] = *entry;
+          *entry = -1;
+        }
+        if (tid == 1023) in_step = rank[0];
+        __syncthreads();
+        freed += in_step;
       }
-      const unsigned before = lo > 0 ? freed_to[lo - 1] : before_step;
-      int32_t* entry = a.table + (size_t)(base + lo) * a.columns + first_page[lo] + (k - before);
-      const int64_t at = (int64_t)count + (all - 1 - k);      // the first page freed ends on top
-      if (at < a.capacity) a.free_pages[at] = *entry;
-      *entry = -1;
+      if (pass == 1 && r < a.R) {
+        const int len = a.lengths[r], keep = a.keep[r];
+        if (keep >= 0 && keep <= len) a.lengths[r] = keep;
+      }
+      before_step = end;
+      __syncthreads();
     }
-    if (r < a.R) {
-      const int len = a.lengths[r], keep = a.keep[r];
-      if (keep >= 0 && keep <= len) a.lengths[r] = keep;
-    }
-    before_step = end;
-    __syncthreads();
+    all = freed;
   }
   if (tid == 0) a.free_count[0] = (int)min((int64_t)count + all, (int64_t)a.capacity);
 }
@@ -294,7 +299,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(StoreArgs a) {
   const int l = threadIdx.x % LANES;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
   const bool exists = row < (int64_t)a.T * a.g.H;
-    const int h = exists ? (int)(row / a.T) : 0, t = exists ? (int)(row % a.T) : 0;
+  const int h = exists ? (int)(row / a.T) : 0, t = exists ? (int)(row % a.T) : 0;
   const int64_t slot = a.slots[t];
   const bool stored = exists && slot >= 0 && slot < ((int64_t)a.g.pages << a.g.page_shift);
   const int c = 8 * l;
@@ -344,7 +349,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(StoreArgs a) {
   const int l = threadIdx.x % LANES;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
   const bool exists = row < (int64_t)a.T * a.g.H;
-    const int h = exists ? (int)(row / a.T) : 0, t = exists ? (int)(row % a.T) : 0;
+  const int h = exists ? (int)(row / a.T) : 0, t = exists ? (int)(row % a.T) : 0;
   const int64_t slot = a.slots[t];
   const bool stored = slot >= 0 && slot < ((int64_t)a.g.pages << a.g.page_shift);
   const int c = 8 * l, j = l / 2 % 4;

@@ -457,3 +457,31 @@ def test_streams_repeats_and_two_calls_at_once():
             b = cache.sagebwd_cache_attention(d2, f2.pool, f2.table, f2.lengths, c2, p, 70)
         torch.cuda.synchronize()
         assert torch.equal(a[0], O1) and torch.equal(a[1], l1) and torch.equal(b[0], O2) and torch.equal(b[1], l2)
+
+
+def test_trim_gives_back_pages_only():
+    """Entries that are not pages (a request that has let go of its oldest ones) do not come onto the stack; the others keep their order."""
+    page, R, columns = 32, 1500, 7
+    p = CacheParams(1, 64, page=page)
+    g = torch.Generator().manual_seed(5)
+    lens = torch.randint(0, columns * page + 1, (R,), generator=g).tolist()
+    keep = [min(n, int(k)) if k >= 0 else 0 for n, k in zip(lens, torch.randint(-100, columns * page, (R,), generator=g).tolist())]
+    table = torch.full((R, columns), -1, dtype=torch.int32)
+    stack, gone, after = [3, 1], [], table.clone()
+    number = 10
+    for r in range(R):
+        for c in range((lens[r] + page - 1) // page):
+            hole = int(torch.randint(0, 3, (1,), generator=g)) == 0
+            table[r, c] = -1 if hole else number
+            number += not hole
+            if c >= (keep[r] + page - 1) // page:
+                gone += [] if hole else [int(table[r, c])]
+            else:
+                after[r, c] = table[r, c]
+    want = stack + gone[::-1]
+    free_pages = torch.full((number,), -7, dtype=torch.int32)
+    free_pages[:2] = torch.tensor(stack)
+    t, f, c, h = table.cuda(), free_pages.cuda(), _i32([2]), _i32(lens)
+    cache.sagebwd_cache_trim(_i32(keep), h, t, f, c, p)
+    assert h.tolist() == keep and torch.equal(t.cpu(), after) and c.item() == len(want)
+    assert f[: len(want)].tolist() == want and (f[len(want):] == -7).all()
