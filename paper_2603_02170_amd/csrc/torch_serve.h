@@ -485,6 +485,10 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const Tensor* freq = dense(a[3], at::kFloat, {-1}, "inv_freq", dev);
   if (freq == nullptr) return nullptr;
   c.inv_freq = *freq;
+  if (at::GradMode::is_enabled() && freq->requires_grad()) {
+    PyErr_SetString(PyExc_NotImplementedError, "sage_rotary: inv_freq gets no gradient (detach it)");
+    return nullptr;
+  }
   c.sections = {0, 0, 0, 0};
   if (a[4] == Py_None) {
     c.axes = 1;

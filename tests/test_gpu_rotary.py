@@ -188,3 +188,13 @@ def test_outputs_in_the_place_of_the_inputs():
     rc = lib.sagebwd_rotary(vp(Q.data_ptr()), vp(K.data_ptr()), vp(Q.data_ptr()), vp(K.data_ptr()), vp(pos.data_ptr()), vp(f.data_ptr()),
                             ctypes.byref(p), vp(torch.cuda.current_stream().cuda_stream))
     assert rc == 0 and torch.equal(Q, want[0]) and torch.equal(K, want[1])
+
+
+def test_frequencies_that_want_a_gradient_are_refused():
+    Q = torch.randn(3, 2, 64, device="cuda").to(torch.bfloat16)
+    pos, freq = torch.arange(3, device="cuda", dtype=torch.int32), torch.rand(32, device="cuda", requires_grad=True)
+    with pytest.raises(NotImplementedError):
+        sage_rotary(Q, None, pos, freq)
+    with torch.no_grad():
+        a = sage_rotary(Q, None, pos, freq)[0]
+    assert torch.equal(a, sage_rotary(Q, None, pos, freq.detach())[0])
