@@ -25,7 +25,7 @@ struct AttendArgs {
   const float* v_mean;
   __bf16* O;
   float* LSE;
-  int4* joins;          // of every workgroup: parts (or 0), request, head, first row of the item that its first unit divides
+  int4* joins;          // of every workgroup, of the item that its first unit divides: parts (or 0) and 2^16 rows, first row of Q, head, first query row
   float* sums;          // [2 slots of every workgroup, rows, D]: parts of items that workgroups share
   float2* stats;        // their maximum (log2) and sum
   char* unpacked;       // where keys and values are unpacked beforehand: fragments of 64 tokens of a head,
@@ -91,6 +91,8 @@ struct AttendShares {
     return unit < big ? unit / (each + 1) : more + (unit - big) / each;
   }
 };
+// (at most 512 parts, and 256 rows)
+__device__ __forceinline__ int4 join_word(int parts, int rows, int begin, int head, int row0) { return int4{parts | rows << 16, begin, head, row0}; }
 __device__ __forceinline__ float wave_max_f32(float v) {
   for (int k = 1; k < 64; k <<= 1) v = fmaxf(v, __shfl_xor(v, k));
   return v;
@@ -491,7 +493,8 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
   }
   if (!cursor.more(a)) return;
   if (tid == 0 && cursor.j > 0 && attend_cut(shares.begin(w - 1) - cursor.x) == 0)      // the first border in this item
-    a.joins[w] = int4{shares.owner(cursor.x + __builtin_amdgcn_readlane(cursor.units, 0) + kItemCost - 1) - w + 2, cursor.r, cursor.head, 0};
+    a.joins[w] = join_word(shares.owner(cursor.x + __builtin_amdgcn_readlane(cursor.units, 0) + kItemCost - 1) - w + 2,
+                           __builtin_amdgcn_readlane(cursor.n_rows, 0), __builtin_amdgcn_readlane(cursor.begin, 0), cursor.head, 0);
 
   AttendRows<D, GROUP> rows[NQ];
 #pragma unroll
@@ -604,70 +607,94 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
 }
 
 // Joins the parts of an item that several workgroups had, in the order of the keys: the workgroup at the first border inside it has left word
-// (AttendArgs::joins).  WAVES waves a row: with four every lane weighs a part, then each wave takes every fourth part, several loads in
-// flight, and they meet in LDS (one wave and one part after the other took 97 us for the 128 parts of a request alone, now 7); of many
-// rows, with few parts each, a wave has its own, and several of them (workgroups that find nothing to join cost: 511 borders of 64 workgroups
-// each 13.7 us, of 16 18.1; 255 that nearly all join 22 and 21).
-template <int D, int ROWS, int WAVES>
+// (AttendArgs::joins).  Of few rows, with many parts: a workgroup has a row, every lane weighs a part, then each wave takes every fourth part,
+// several loads in flight, and they meet in LDS (one wave and one part after the other took 97 us for the 128 parts of a request alone, now 7).
+template <int D, int ROWS>
 __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
   constexpr int NC = D / 64, MOST = 256;
-  const int w = blockIdx.x + 1;
+  const int w = blockIdx.x + 1, k = blockIdx.y;
   const int4 join = a.joins[w];
-  const int parts = join.x;
-  if (parts == 0) return;
-  const AttendRequest rq = attend_request(a, join.y);
+  const int parts = join.x & 0xFFFF;
+  if (k >= join.x >> 16) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const size_t slot0 = (size_t)w * 2;
-  for (int k = WAVES == 4 ? blockIdx.y : blockIdx.y * 4 + wave; k < ROWS && join.w + k < rq.rows; k += WAVES == 4 ? ROWS : gridDim.y * 4) {
-    const auto at = [&](int p) { return (p == 0 ? slot0 - 1 : slot0 + 2 * (p - 1)) * ROWS + k; };
-    float M = -INFINITY;
-    for (int p = lane; p < parts; p += 64) M = fmaxf(M, a.stats[at(p)].x);
-    M = wave_max_f32(M);
-    float o[NC], l = 0.f;
+  const auto at = [&](int p) { return (p == 0 ? slot0 - 1 : slot0 + 2 * (p - 1)) * ROWS + k; };
+  float M = -INFINITY;
+  for (int p = lane; p < parts; p += 64) M = fmaxf(M, a.stats[at(p)].x);
+  M = wave_max_f32(M);
+  float o[NC], l = 0.f;
 #pragma unroll
-    for (int i = 0; i < NC; i++) o[i] = 0.f;
-    if constexpr (WAVES == 1) {
-#pragma unroll 2
-      for (int p = 0; p < parts; p++) {
-        const float2 s = a.stats[at(p)];
-        const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - M);
-        l += s.y * f;
-        const float* x = a.sums + at(p) * D + NC * lane;
-#pragma unroll
-        for (int i = 0; i < NC; i++) o[i] += x[i] * f;
-      }
-    } else {
-      __shared__ float weight[MOST], meet[4][D + 2];
-      for (int p0 = 0; p0 < parts; p0 += MOST) {
-        const int here = min(parts - p0, MOST);
-        __syncthreads();
-        if (tid < here) {
-          const float2 s = a.stats[at(p0 + tid)];
-          const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - M);
-          weight[tid] = f;
-          l += s.y * f;
-        }
-        __syncthreads();
-#pragma unroll 4
-        for (int p = wave; p < here; p += 4) {
-          const float f = weight[p];
-          const float* x = a.sums + at(p0 + p) * D + NC * lane;
-#pragma unroll
-          for (int i = 0; i < NC; i++) o[i] += x[i] * f;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < NC; i++) meet[wave][NC * lane + i] = o[i];
-      for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
-      if (lane == 0) meet[wave][D] = l;
-      __syncthreads();
-      if (wave != 0) return;
-      l = (meet[0][D] + meet[1][D]) + (meet[2][D] + meet[3][D]);
-#pragma unroll
-      for (int i = 0; i < NC; i++) o[i] = (meet[0][NC * lane + i] + meet[1][NC * lane + i]) + (meet[2][NC * lane + i] + meet[3][NC * lane + i]);
+  for (int i = 0; i < NC; i++) o[i] = 0.f;
+  __shared__ float weight[MOST], meet[4][D + 2];
+  for (int p0 = 0; p0 < parts; p0 += MOST) {
+    const int here = min(parts - p0, MOST);
+    __syncthreads();
+    if (tid < here) {
+      const float2 s = a.stats[at(p0 + tid)];
+      const float f = s.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.x - M);
+      weight[tid] = f;
+      l += s.y * f;
     }
-    attend_store<NC>(a, rq.begin, join.z, join.w + k, D, NC * lane, M, l, o);
+    __syncthreads();
+#pragma unroll 4
+    for (int p = wave; p < here; p += 4) {
+      const float f = weight[p];
+      const float* x = a.sums + at(p0 + p) * D + NC * lane;
+#pragma unroll
+      for (int i = 0; i < NC; i++) o[i] += x[i] * f;
+    }
   }
+#pragma unroll
+  for (int i = 0; i < NC; i++) meet[wave][NC * lane + i] = o[i];
+  for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
+  if (lane == 0) meet[wave][D] = l;
+  __syncthreads();
+  if (wave != 0) return;
+  l = (meet[0][D] + meet[1][D]) + (meet[2][D] + meet[3][D]);
+#pragma unroll
+  for (int i = 0; i < NC; i++) o[i] = (meet[0][NC * lane + i] + meet[1][NC * lane + i]) + (meet[2][NC * lane + i] + meet[3][NC * lane + i]);
+  attend_store<NC>(a, join.y, join.z, join.w + k, D, NC * lane, M, l, o);
+}
+
+// The same of many rows, with few parts each: D / 4 lanes have a row and take four parts at a time, one trip to memory for up to four.  (A wave a row,
+// two channels a lane, the maxima asked for first: vector instructions were 83 % of its cycles; 255 divided tiles of 256 rows of 128
+// channels 20 us, the call 327 -> 319; 511 borders of a mixed batch, 64 channels, 72.5 -> 67.5.)
+template <int D, int ROWS>
+__global__ __launch_bounds__(256) void cache_join_rows_kernel(AttendArgs a) {
+  constexpr int LANES = D / 4, HERE = 256 / LANES, BATCH = 4;
+  const int w = blockIdx.x + 1, k = blockIdx.y * HERE + threadIdx.x / LANES;
+  const int4 join = a.joins[w];
+  const int parts = join.x & 0xFFFF;
+  if (k >= join.x >> 16) return;
+  const int c = threadIdx.x % LANES * 4;
+  const size_t slot0 = (size_t)w * 2;
+  float m = -INFINITY, l = 0.f;
+  v4f o = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < parts; p0 += BATCH) {
+    float2 s[BATCH];
+    v4f x[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; i++) {
+      const int p = min(p0 + i, parts - 1);
+      const size_t at = (p == 0 ? slot0 - 1 : slot0 + 2 * (p - 1)) * ROWS + k;
+      s[i] = a.stats[at];
+      x[i] = *(const v4f*)(a.sums + at * D + c);
+    }
+    float to = m;
+#pragma unroll
+    for (int i = 0; i < BATCH; i++) to = fmaxf(to, s[i].x);
+    const float ref = to == -INFINITY ? 0.f : to, f = __builtin_amdgcn_exp2f(m - ref);
+    l *= f;
+    o *= f;
+#pragma unroll
+    for (int i = 0; i < BATCH; i++) {
+      const float g = p0 + i < parts ? __builtin_amdgcn_exp2f(s[i].x - ref) : 0.f;
+      l = p0 + i < parts ? l + s[i].y * g : l;
+      o = p0 + i < parts ? o + x[i] * g : o;
+    }
+    m = to;
+  }
+  attend_store<4>(a, join.y, join.z, join.w + k, D, c, m, l, (const float*)&o);
 }
 
 }  // namespace sage

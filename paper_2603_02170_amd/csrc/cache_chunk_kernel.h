@@ -217,7 +217,8 @@ struct ChunkWalk {
   // Units j0 .. of the item that are this workgroup's; leaves word for the joining launch at the first border inside it.
   __device__ __forceinline__ int last_unit(const AttendArgs& a, int units) const {
     if (j0 > 0 && chunk_cut(shares.begin(w - 1) - x) == 0 && threadIdx.x == 0)
-      a.joins[w] = int4{shares.owner(x + units + kChunkCost - 1) - w + 2, r, head, tile * kChunkRows};
+      a.joins[w] = join_word(shares.owner(x + units + kChunkCost - 1) - w + 2, min(rq.rows - tile * kChunkRows, kChunkRows), rq.begin, head,
+                             tile * kChunkRows);
     return a.split ? min(units, chunk_cut(end - x)) : units;
   }
   // Behind an item of so many units of which all up to j1 are done: false at the share's end.

@@ -73,7 +73,6 @@ constexpr int kWholeUnits = 8;
 // 304; one of 2048 against 10000, 32 tiles, 365 -> 326, at d = 64 501 -> 331), and the workspace for them is at most this.
 constexpr int kWideTiles = 8;
 constexpr int64_t kMostUnpacked = (int64_t)4 << 30;
-constexpr int kJoinGroups = 32;     // workgroups that look at a border between row tiles of 256: 8 rows each
 
 // One of the two kernels' part of a call.
 struct AttendLaunch {
@@ -159,7 +158,7 @@ int launch_few(const AttendArgs& a, const AttendLaunch& l, hipStream_t st) {
   cache_attend_kernel<D, GROUP, NQ><<<l.workgroups, 256, 0, st>>>(a);
   SERVE_LAUNCH_CHECK();
   if (l.split && l.workgroups > 1) {
-    cache_join_kernel<D, 16 * NQ, 4><<<dim3(l.workgroups - 1, l.join_rows), 256, 0, st>>>(a);
+    cache_join_kernel<D, 16 * NQ><<<dim3(l.workgroups - 1, l.join_rows), 256, 0, st>>>(a);
     SERVE_LAUNCH_CHECK();
   }
   return SAGEBWD_OK;
@@ -190,7 +189,7 @@ int launch_attend(AttendArgs a, const AttendPlan& w, char* ws, hipStream_t st) {
     }
     SERVE_LAUNCH_CHECK();
     if (w.m.split && w.m.workgroups > 1) {
-      cache_join_kernel<D, kChunkRows, 1><<<dim3(w.m.workgroups - 1, kJoinGroups), 256, 0, st>>>(a);
+      cache_join_rows_kernel<D, kChunkRows><<<dim3(w.m.workgroups - 1, kChunkRows / (256 / (D / 4))), 256, 0, st>>>(a);
       SERVE_LAUNCH_CHECK();
     }
   }
