@@ -291,15 +291,15 @@ __device__ __forceinline__ void subtract_mean(float* x, const float* mean, int a
 
 // d / 8 lanes have a token of a head, 8 channels each.  A lane's channels of K are one word; of V they lie in eight half-words, whose
 // other nibbles three lanes of the same half have (2, 4 and 6 away): those are joined and each lane stores two.  Neighbouring rows are
-// neighbouring tokens, whose bytes of V are neighbours: in the L2 they meet (8191 tokens of 8 heads of 128: 12.5 us, 3.4 TB/s; with the heads of
+// neighbouring tokens, whose bytes of V are neighbours: in the L2 they meet (8191 tokens of 8 heads of 128: 10.4 us, 4.1 TB/s, 12.4 where a row was found by a division; with the heads of
 // a token as neighbours 15.6).
 template <int D, int GROUP>
 __global__ __launch_bounds__(256) void cache_append_kernel(StoreArgs a) {
   constexpr int LANES = D / 8, ROWS = 256 / LANES;
   const int l = threadIdx.x % LANES;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
-  const bool exists = row < (int64_t)a.T * a.g.H;
-  const int h = exists ? (int)(row / a.T) : 0, t = exists ? (int)(row % a.T) : 0;
+  const bool exists = row < a.T;
+  const int h = blockIdx.y, t = exists ? (int)row : 0;
   const int64_t slot = a.slots[t];
   const bool stored = exists && slot >= 0 && slot < ((int64_t)a.g.pages << a.g.page_shift);
   const int c = 8 * l;
@@ -348,8 +348,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(StoreArgs a) {
   constexpr int LANES = D / 8, ROWS = 256 / LANES;
   const int l = threadIdx.x % LANES;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
-  const bool exists = row < (int64_t)a.T * a.g.H;
-  const int h = exists ? (int)(row / a.T) : 0, t = exists ? (int)(row % a.T) : 0;
+  const bool exists = row < a.T;
+  const int h = blockIdx.y, t = exists ? (int)row : 0;
   const int64_t slot = a.slots[t];
   const bool stored = slot >= 0 && slot < ((int64_t)a.g.pages << a.g.page_shift);
   const int c = 8 * l, j = l / 2 % 4;

@@ -265,12 +265,12 @@ int sagebwd_cache_append(const void* K, const void* V, int64_t k_token_stride, i
     return SAGEBWD_INVALID_ARG;
   if (T == 0) return SAGEBWD_OK;
   if (K == nullptr || V == nullptr || slots == nullptr || pool == nullptr || !aligned(K) || !aligned(V) || !aligned(pool)) return SAGEBWD_INVALID_ARG;
-  const int64_t rows = (int64_t)T * params->H, per = 256 / (params->d / 8);
-  if ((rows + per - 1) / per * 256 > kMostThreads) return SAGEBWD_UNSUPPORTED_SHAPE;
+  const int64_t per = 256 / (params->d / 8), groups = (T + per - 1) / per;      // tokens of a workgroup, and workgroups of a head
+  if (groups * params->H * 256 > kMostThreads) return SAGEBWD_UNSUPPORTED_SHAPE;
   const StoreArgs a{(const __bf16*)K, (const __bf16*)V, {k_token_stride, k_head_stride}, {v_token_stride, v_head_stride}, slots, k_mean, v_mean,
                     (unsigned char*)pool, nullptr, nullptr, T, geometry(*params)};
   return with_format(*params, [&](auto d, auto group) -> int {
-    cache_append_kernel<decltype(d)::value, decltype(group)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, (hipStream_t)stream>>>(a);
+    cache_append_kernel<decltype(d)::value, decltype(group)::value><<<dim3((unsigned)groups, params->H), 256, 0, (hipStream_t)stream>>>(a);
     SERVE_LAUNCH_CHECK();
     return SAGEBWD_OK;
   });
@@ -283,11 +283,11 @@ int sagebwd_cache_read(const int64_t* slots, int32_t T, const float* k_mean, con
   if (T < 0) return SAGEBWD_INVALID_ARG;
   if (T == 0) return SAGEBWD_OK;
   if (K == nullptr || V == nullptr || slots == nullptr || pool == nullptr || !aligned(K) || !aligned(V) || !aligned(pool)) return SAGEBWD_INVALID_ARG;
-  const int64_t rows = (int64_t)T * params->H, per = 256 / (params->d / 8);
-  if ((rows + per - 1) / per * 256 > kMostThreads) return SAGEBWD_UNSUPPORTED_SHAPE;
+  const int64_t per = 256 / (params->d / 8), groups = (T + per - 1) / per;      // tokens of a workgroup, and workgroups of a head
+  if (groups * params->H * 256 > kMostThreads) return SAGEBWD_UNSUPPORTED_SHAPE;
   const StoreArgs a{nullptr, nullptr, {0, 0}, {0, 0}, slots, k_mean, v_mean, (unsigned char*)pool, (__bf16*)K, (__bf16*)V, T, geometry(*params)};
   return with_format(*params, [&](auto d, auto group) -> int {
-    cache_read_kernel<decltype(d)::value, decltype(group)::value><<<(unsigned)((rows + per - 1) / per), 256, 0, (hipStream_t)stream>>>(a);
+    cache_read_kernel<decltype(d)::value, decltype(group)::value><<<dim3((unsigned)groups, params->H), 256, 0, (hipStream_t)stream>>>(a);
     SERVE_LAUNCH_CHECK();
     return SAGEBWD_OK;
   });
@@ -385,11 +385,15 @@ int sagebwd_rotary(const void* Q, const void* K, void* Qo, void* Ko, const void*
     a.end[k] = at;
   }
   a.sign = p->inverse ? -1.f : 1.f;
-  // Many tokens: eight frequencies a thread, for eight heads; few: two, for one head.
+  // Many tokens: eight frequencies a thread, for as many of up to eight heads as leave the machine 2^16 threads (of a training batch, 4109 tokens of 126
+  // heads of 128, one head 74 us, eight 57; 2048 of 40 14.6 and, with two, 10.2; 8192 of 64 of 64 40 and 30; asked to leave 2^19, 16381
+  // of 32 of 64 go from 122 to 134 forth and back); few: two, for one head.
   const int64_t many = (int64_t)a.tokens * (p->d / 16);
   const bool wide = many >= 4096;
   a.pieces = p->d / (wide ? 16 : 4);
-  a.heads_per_thread = many >= 65536 ? 8 : 1;
+  a.heads_per_thread = 1;
+  for (int n = 8; n > 1 && a.heads_per_thread == 1; n /= 2)
+    if (wide && many * ((p->Hq + n - 1) / n + (p->Hk + n - 1) / n) >= 1 << 16) a.heads_per_thread = n;
   for (int k = 0; k < 2; k++) a.head_groups[k] = (a.heads[k] + a.heads_per_thread - 1) / a.heads_per_thread;
   const dim3 grid((unsigned)(((int64_t)a.tokens * a.pieces + 255) / 256), a.head_groups[0] + a.head_groups[1]);
   hipStream_t st = (hipStream_t)stream;
