@@ -76,17 +76,21 @@ __device__ __forceinline__ void plan_row(const PlanArgs& a, const int32_t* cu, i
   a.positions[row] = position;
 }
 
-// Everything but the rows (and those too where `with_rows`: few of them).  One workgroup: the sums over the requests are what everything
-// waits for, and as many requests as it has threads are one step of them.  (32 requests take 1 wave 2.9 us, 4 waves 3.4; 16
-// waves, of which each knew its 64-bit sums only, 5.9.)
+// Everything but the rows, and those too where `with_rows`.  The sums over the requests are what everything waits for, and as many requests as a
+// workgroup has threads are one step of them.  (32 requests take 1 wave 2.9 us, 4 waves 3.4; 16 waves, of which each knew its 64-bit
+// sums only, 5.9.)  Where one step is all, the rows take what they need from LDS, and of many rows several workgroups each form the
+// sums again, for rows of their own: the first writes the rest.  (300 requests, 4739 rows: with a launch of the rows 8.7 us, so 6.2, of which the host
+// takes 5.5.)
 template <int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void cache_plan_kernel(PlanArgs a, int with_rows) {
   constexpr int THREADS = 64 * WAVES;
   __shared__ unsigned sums2[WAVES][2], sums1[WAVES][1];
   __shared__ unsigned taken_to[THREADS];      // pages granted up to and with a request of this step
   __shared__ int first_page[THREADS];         // column of a request's first new page
+  __shared__ int end_of[THREADS], held_of[THREADS];      // its rows' end, and tokens held (-1: not granted)
   __shared__ unsigned total[3];
   const int tid = threadIdx.x;
+  const bool writes = blockIdx.x == 0;
   const int64_t page = 1 << a.page_shift;
   const unsigned count = (unsigned)max(0, min(a.free_count[0], a.capacity));
   unsigned tokens0 = 0, need0 = 0, taken0 = 0;      // sums of the steps before
@@ -111,8 +115,10 @@ __global__ __launch_bounds__(64 * WAVES) void cache_plan_kernel(PlanArgs a, int 
     const unsigned taken = taken0 + one[0];           // (at most count)
     taken_to[tid] = taken;
     first_page[tid] = (int)((held + page - 1) >> a.page_shift);
-    if (r < a.R) {
-      a.cu[r + 1] = (int)min(tokens, (unsigned)a.rows);
+    end_of[tid] = (int)min(tokens, (unsigned)a.rows);
+    held_of[tid] = granted ? (int)held : -1;
+    if (r < a.R && writes) {
+      a.cu[r + 1] = end_of[tid];
       a.granted[r] = granted;
       a.lengths[r] = (int)(granted ? held + n : held);
     }
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(64 * WAVES) void cache_plan_kernel(PlanArgs a, int 
     tokens0 = total[0];
     need0 = total[1];
     const unsigned end = total[2];
-    for (unsigned k = taken0 + tid; k < end; k += THREADS) {       // (k < end <= count <= capacity)
+    for (unsigned k = taken0 + tid; writes && k < end; k += THREADS) {       // (k < end <= count <= capacity)
       int lo = 0, hi = THREADS - 1;         // the first request of this step with taken_to > k
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
@@ -136,13 +142,36 @@ __global__ __launch_bounds__(64 * WAVES) void cache_plan_kernel(PlanArgs a, int 
       a.table[(size_t)(base + lo) * a.columns + first_page[lo] + (k - before)] = a.free_pages[count - 1 - k];
     }
     taken0 = end;
-    __syncthreads();
+    if (base + THREADS < a.R) __syncthreads();
   }
-  if (tid == 0) {
+  if (tid == 0 && writes) {
     a.cu[0] = 0;
     a.free_left[0] = (int)(count - taken0);
   }
-  if (with_rows) {
+  if (!with_rows) return;
+  if (a.R <= THREADS) {
+    const int end = (int)min(tokens0, (unsigned)a.rows);
+    for (int row = blockIdx.x * THREADS + tid; row < a.rows; row += gridDim.x * THREADS) {
+      int64_t slot = -1;
+      int position = 0;
+      if (row < end) {
+        int lo = 0, hi = a.R - 1;        // the first request that ends behind the row
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (end_of[mid] > row) hi = mid;
+          else lo = mid + 1;
+        }
+        if (held_of[lo] >= 0) {
+          position = held_of[lo] + row - (lo > 0 ? end_of[lo - 1] : 0);
+          const int column = position >> a.page_shift, k = column - first_page[lo];      // (a new page: what goes into the table, from the stack)
+          const int entry = k < 0 ? a.table[(size_t)lo * a.columns + column] : a.free_pages[count - 1 - ((lo > 0 ? taken_to[lo - 1] : 0) + k)];
+          if (entry >= 0) slot = ((int64_t)entry << a.page_shift) + (position & ((1 << a.page_shift) - 1));
+        }
+      }
+      a.slots[row] = slot;
+      a.positions[row] = position;
+    }
+  } else {
     __threadfence_block();
     __syncthreads();
     for (int row = tid; row < a.rows; row += THREADS) plan_row(a, a.cu, row);

@@ -232,10 +232,14 @@ int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block
   const PlanArgs a{held, added, free_pages, free_count, block_table, slots, positions, cu_new, lengths, granted, free_left,
                    R, columns, page_shift_of(page), capacity, rows};
   hipStream_t st = (hipStream_t)stream;
-  const int with_rows = rows <= 2048;        // (else a launch of their own, over the machine)
-  if (R <= 64 && rows <= 256) cache_plan_kernel<1><<<1, 64, 0, st>>>(a, with_rows);
-  else if (R <= 256 && rows <= 1024) cache_plan_kernel<4><<<1, 256, 0, st>>>(a, with_rows);
-  else cache_plan_kernel<16><<<1, 1024, 0, st>>>(a, with_rows);
+  // Several workgroups read what one of them writes where the lengths are updated in place; more requests than a workgroup has threads are summed
+  // in several steps: many rows are then a launch of their own.
+  const bool in_place = lengths == held || free_left == free_count;
+  const bool several = R <= 1024 && !in_place;
+  const int with_rows = several || rows <= 2048;
+  if (R <= 64 && rows <= 256) cache_plan_kernel<1><<<1, 64, 0, st>>>(a, 1);
+  else if (R <= 256 && rows <= 1024) cache_plan_kernel<4><<<1, 256, 0, st>>>(a, 1);
+  else cache_plan_kernel<16><<<several && rows > 0 ? (rows + 1023) / 1024 : 1, 1024, 0, st>>>(a, with_rows);
   SERVE_LAUNCH_CHECK();
   if (with_rows) return SAGEBWD_OK;
   cache_plan_rows_kernel<<<(rows + 255) / 256, 256, 0, st>>>(a);

@@ -485,3 +485,28 @@ def test_trim_gives_back_pages_only():
     cache.sagebwd_cache_trim(_i32(keep), h, t, f, c, p)
     assert h.tolist() == keep and torch.equal(t.cpu(), after) and c.item() == len(want)
     assert f[: len(want)].tolist() == want and (f[len(want):] == -7).all()
+
+
+@pytest.mark.parametrize("R,most,rows_of", [(300, 60, 1), (1024, 9, 0.7), (3, 4000, 1), (1025, 9, 1)])
+def test_plan_of_many_rows_with_lengths_in_place_and_not(R, most, rows_of):
+    """More rows than a workgroup takes, with outputs of their own (several workgroups) and updated in place (a launch for the rows): the same."""
+    g, page = np.random.default_rng(R + most), 32
+    held, added = g.integers(0, 200, R).tolist(), g.integers(0, most + 1, R).tolist()
+    columns, rows = -(-(200 + most) // page), int(sum(added) * rows_of)
+    need = sum(-(-(a + n) // page) - -(-a // page) for a, n in zip(held, added))
+    assert rows > 2048
+    table = g.integers(0, 1000, (R, columns)).tolist()
+    stack = [int(x) for x in g.permutation(need + 3)]
+    for count in (need, need // 3):
+        want_table = [list(r) for r in table]
+        want = ref.plan(held, added, want_table, stack, count, page, rows)
+        for in_place in (False, True):
+            h, c, t = _i32(held), _i32([count]), _i32(table).reshape(R, columns)
+            out = None
+            if in_place:
+                new = lambda n, dtype=torch.int32: torch.empty(n, dtype=dtype, device="cuda")  # noqa: E731
+                out = cache.CachePlan(new(rows, torch.int64), new(rows), new(R + 1), h, new(R), c)
+            got = cache.sagebwd_cache_plan(h, _i32(added), t, _i32(stack), c, CacheParams(1, 64, page=page), rows, out=out)
+            for name, x in got._asdict().items():
+                assert x.tolist() == want[name], (name, count, in_place)
+            assert t.tolist() == want_table
