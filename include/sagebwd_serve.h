@@ -126,9 +126,16 @@ typedef struct sagebwd_cache_call {
  * the matrix instruction.  A row that sees no key (a request of length 0; with the mask the first rows of one shorter
  * than its new tokens; pages that do not exist) gives O = 0, LSE = -infinity.  What stands in the cache behind a
  * request's length reaches nothing.
- * Requests with few query rows (new tokens x Hq / H) have their keys divided over the machine and the parts joined by
- * a second launch; how they are divided depends on all requests of the call, so that O agrees between calls of different
- * batches to its rounding, and bit for bit between equal calls.
+ * Requests of up to 32 query rows (new tokens x Hq / H) go to a kernel for few rows, the others to one for many; a call that may hold both kinds
+ * (max_new tokens are more than 32 rows, T is less than R * max_new, Hq / H at most 32) launches both.  Where a call has few items for
+ * the machine their keys are divided over it and the parts joined by a further launch; from 2048 rows a request on, keys and values are
+ * unpacked to bf16 in the workspace first (256 d bytes for 64 tokens and head; at most 4 GiB, else each tile unpacks its own).  How
+ * work is divided depends on all requests of the call, so that O agrees between calls of different batches to its rounding, and bit
+ * for bit between equal calls.
+ * The workspace depends on the host's sizes alone; its contents before the call do not matter, and calls in flight at a time (on two
+ * streams, in two graphs) need one each.
+ * Bounds: R <= 2^20, columns * page < 2^30, R * H * (columns * page / 128 + 3) <= 2^29, T * Hq / H < 2^30; with more than 32 rows a request
+ * (T * Hq / H / 64 + R) * H <= 2^22.
  */
 int sagebwd_cache_workspace_bytes(const sagebwd_cache_params* params, const sagebwd_cache_call* call, size_t* bytes);
 int sagebwd_cache_attention(const void* Q, const void* pool, const int32_t* block_table, const int32_t* lengths, const int32_t* cu,

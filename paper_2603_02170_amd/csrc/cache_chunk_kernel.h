@@ -13,6 +13,7 @@
 namespace sage {
 
 constexpr int kChunkRows = 256, kChunkUnit = 64;
+constexpr int kChunkCost = 6;        // what an item costs beside its units, in units
 
 // 64 tokens on their way from the pages to bf16 fragments: waves 0 to 3 have K's, the others V's.
 template <int D, int GROUP>
@@ -75,76 +76,89 @@ struct ChunkTile {
     }
     if (D == 64 && u >= 128) return;
     const int o = D == 128 ? u >> 5 : u >> 4, f = D == 128 ? u >> 4 & 1 : 0, m = u & 15;
+    constexpr int NS = GROUP == 32 ? 2 : 1;      // scales of a token over the thread's channels m + 16 j
+    v4i sc[NS];
+    sc[0] = s0;
+    if (NS == 2) sc[NS - 1] = s1;
+    unsigned top = 0;                            // (an exponent of ones carries into the sign's place)
 #pragma unroll
-    for (int pair = 0; pair < 2; pair++) {      // channels m + 16 j, j = 2 pair and 2 pair + 1
-      const v4i& sc = GROUP == 32 && pair == 1 ? s1 : s0;
-      float s[8], s8[8];
-      unsigned bad = 0;
+    for (int k = 0; k < NS; k++)
 #pragma unroll
-      for (int i = 0; i < 8; i++) {
-        const float x = i % 2 == 0 ? low_bf16(sc[i / 2]) : high_bf16(sc[i / 2]);
-        const bool number = fabsf(x) < INFINITY;
-        if (!number && i < valid) bad |= 1u << i;
-        s[i] = i < valid && number ? x : 0.f;
-        s8[i] = -8.f * s[i];
-      }
-      if (__any(bad != 0)) *poisoned = tag;
-      if (m == 0 && (GROUP == 32 || pair == 0)) {
-        const int group = f * (64 / GROUP) + pair;
+      for (int i = 0; i < 4; i++) top |= ((unsigned)sc[k][i] & 0x7F807F80u) + 0x00800080u;
+    unsigned bad[NS] = {};
+    if (__any(valid < 8 || (top & 0x80008000u) != 0)) {
+      asm volatile("");                          // (stays a branch)
 #pragma unroll
-        for (int i = 0; i < 8; i++) poison[group * 64 + 8 * o + i] = bad >> i & 1;
-      }
+      for (int k = 0; k < NS; k++) {
 #pragma unroll
-      for (int k = 0; k < 2; k++) {
-        const int j = 2 * pair + k;
-        v4i x;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const unsigned w = (unsigned)code[i] >> 4 * j;
-          x[i] = pack_bf16(__builtin_fmaf((float)(w & 15), s[2 * i], s8[2 * i]), __builtin_fmaf((float)(w >> 16 & 15), s[2 * i + 1], s8[2 * i + 1]));
+        for (int i = 0; i < 8; i++) {
+          const int half = i % 2 == 0 ? 0xFFFF : (int)0xFFFF0000;
+          const bool number = (sc[k][i / 2] & half & 0x7F807F80) != (half & 0x7F807F80);
+          if (!number && i < valid) bad[k] |= 1u << i;
+          sc[k][i / 2] = number && i < valid ? sc[k][i / 2] : sc[k][i / 2] & ~half;
         }
-        *(v4i*)(V + ((2 * f + pair) * 4 + (o >> 1)) * 1024 + ((o & 1) * 32 + 16 * k + m) * 16) = x;
+        if (__any(bad[k] != 0)) *poisoned = tag;
       }
     }
+    if (m == 0) {
+#pragma unroll
+      for (int k = 0; k < NS; k++)               // a byte a token
+        *(uint2*)(poison + (f * (64 / GROUP) + k) * 64 + 8 * o) = uint2{(bad[k] & 15) * 0x00204081u & 0x01010101u, (bad[k] >> 4) * 0x00204081u & 0x01010101u};
+    }
+    v4i x[4];                                    // channel m + 16 j
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const unsigned lo = (unsigned)code[i] & 0x0F0F0F0Fu, hi = (unsigned)code[i] >> 4 & 0x0F0F0F0Fu;
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const int w = sc[NS == 2 ? j / 2 : 0][i];
+        const float s = low_bf16(w), t = high_bf16(w);
+        const unsigned bytes = (j % 2 ? hi : lo) >> 8 * (j / 2);
+        x[j][i] = pack_bf16(__builtin_fmaf((float)(bytes & 255), s, -8.f * s), __builtin_fmaf((float)(bytes >> 16 & 255), t, -8.f * t));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++) *(v4i*)(V + ((2 * f + j / 2) * 4 + (o >> 1)) * 1024 + ((o & 1) * 32 + 16 * (j % 2) + m) * 16) = x[j];
   }
 };
 
-// Line of what is dealt out: request, then head, then row tile of 256, each attend_units(tile) + kChunkCost; or (not split) one each,
+// Line of what is dealt out: request, then head, then row tile of 256, each its units + a cost of its own; or (not split) one each,
 // request, then row tile from the last, which sees most, then head.
-constexpr int kChunkCost = 6;
-__device__ __forceinline__ int chunk_tiles(int rows) { return (rows + kChunkRows - 1) / kChunkRows; }
-__device__ __forceinline__ int chunk_units(const AttendArgs& a, const AttendRequest& q, int tile) {
-  return max(1, (attend_visible(a, q, tile * kChunkRows, kChunkRows) + kChunkUnit - 1) / kChunkUnit);
-}
 // The row tile at a place of a head's line: the last ones see most, so light and heavy take turns and a share of average length cuts every
 // second item instead of each.
 __device__ __forceinline__ int chunk_tile_at(int place, int tiles) { return place & 1 ? tiles - 1 - (place >> 1) : place >> 1; }
-// of a request and head
-__device__ __forceinline__ int chunk_weight(const AttendArgs& a, const AttendRequest& q) {
-  const int tiles = chunk_tiles(q.rows);
-  if (!a.split) return tiles;
-  int w = 0;
-  for (int t = 0; t < tiles; t++) w += chunk_units(a, q, t) + kChunkCost;
-  return w;
-}
 // Tiles of 64 tokens that a head of the request has for the rows to see.
 __device__ __forceinline__ int chunk_key_tiles(const AttendRequest& q) { return q.rows == 0 ? 0 : max(1, (q.len + kChunkUnit - 1) / kChunkUnit); }
-__device__ __forceinline__ int chunk_cut(int offset) { return max(0, offset - kChunkCost); }
 
-// A workgroup's way along the line: (request, head, row tile) from unit j0 on.
+struct ChunkScratch {
+  unsigned sums[8][2];
+  int total, found[4];
+};
+// A workgroup's way along the line: (request, head, row tile of ROWS) from unit j0 (of UNIT tokens) on.
+template <int ROWS, int UNIT, int COST>
 struct ChunkWalk {
+  static __device__ __forceinline__ int chunk_tiles(int rows) { return (rows + ROWS - 1) / ROWS; }
+  static __device__ __forceinline__ int chunk_units(const AttendArgs& a, const AttendRequest& q, int tile) {
+    return max(1, (attend_visible(a, q, tile * ROWS, ROWS) + UNIT - 1) / UNIT);
+  }
+  static __device__ __forceinline__ int chunk_cut(int offset) { return max(0, offset - COST); }
+  // of a request and head
+  static __device__ __forceinline__ int chunk_weight(const AttendArgs& a, const AttendRequest& q) {
+    const int tiles = chunk_tiles(q.rows);
+    if (!a.split) return tiles;
+    int w = 0;
+    for (int t = 0; t < tiles; t++) w += chunk_units(a, q, t) + COST;
+    return w;
+  }
+
   int w, x, end, j0;       // its number; where its item begins in the line; where its share ends
   int r, head, place, tile;
   int before;              // tiles of 64 tokens of the requests in front (of one head)
   AttendRequest rq;
   AttendShares shares;
-  struct Scratch {
-    unsigned sums[8][2];
-    int total, found[4];
-  };
 
   // All 512 threads; false: the workgroup has nothing.  Leaves no word for the joining launch.
-  __device__ __forceinline__ bool start(const AttendArgs& a, Scratch& s) {
+  __device__ __forceinline__ bool start(const AttendArgs& a, ChunkScratch& s) {
     const int tid = threadIdx.x, H = a.g.H;
     const int per = (a.R + 511) / 512, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
     unsigned mine = 0, tiles = 0;
@@ -198,7 +212,7 @@ struct ChunkWalk {
       head = (begin - x) / weight;
       x += head * weight;
       place = 0;
-      for (int u; x + (u = chunk_units(a, rq, chunk_tile_at(place, chunk_tiles(rq.rows))) + kChunkCost) <= begin; place++) x += u;
+      for (int u; x + (u = chunk_units(a, rq, chunk_tile_at(place, chunk_tiles(rq.rows))) + COST) <= begin; place++) x += u;
       place = __builtin_amdgcn_readfirstlane(place);
       tile = chunk_tile_at(place, chunk_tiles(rq.rows));
       j0 = chunk_cut(begin - x);
@@ -217,14 +231,14 @@ struct ChunkWalk {
   // Units j0 .. of the item that are this workgroup's; leaves word for the joining launch at the first border inside it.
   __device__ __forceinline__ int last_unit(const AttendArgs& a, int units) const {
     if (j0 > 0 && chunk_cut(shares.begin(w - 1) - x) == 0 && threadIdx.x == 0)
-      a.joins[w] = join_word(shares.owner(x + units + kChunkCost - 1) - w + 2, min(rq.rows - tile * kChunkRows, kChunkRows), rq.begin, head,
-                             tile * kChunkRows);
+      a.joins[w] = join_word(shares.owner(x + units + COST - 1) - w + 2, min(rq.rows - tile * ROWS, ROWS), rq.begin, head,
+                             tile * ROWS);
     return a.split ? min(units, chunk_cut(end - x)) : units;
   }
   // Behind an item of so many units of which all up to j1 are done: false at the share's end.
   __device__ __forceinline__ bool next(const AttendArgs& a, int units, int j1) {
     if (j1 < units || !a.split) return false;        // (not split, a workgroup has one)
-    x += units + kChunkCost;
+    x += units + COST;
     if (chunk_cut(end - x) <= 0) return false;
     j0 = 0;
     if (++place == chunk_tiles(rq.rows)) {
@@ -379,13 +393,13 @@ __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
   typedef ChunkTile<D, GROUP> Tile;
   constexpr int HALF = 2 * Tile::FRAG;
   __shared__ __attribute__((aligned(16))) char Ks[2][HALF], Vs[3][HALF];
-  __shared__ unsigned char poison[4][Tile::NG * 64];
+  __shared__ __attribute__((aligned(8))) unsigned char poison[4][Tile::NG * 64];
   __shared__ int exists[4][2], poisoned[4];
-  __shared__ ChunkWalk::Scratch scratch;
+  __shared__ ChunkScratch scratch;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (tid < 4) poisoned[tid] = -1;
   const bool late = wave >= 4;
-  ChunkWalk walk;
+  ChunkWalk<kChunkRows, kChunkUnit, kChunkCost> walk;
   if (!walk.start(a, scratch)) return;
   int tag = 0;      // of a tile, over all items
   for (bool more = true; more;) {
@@ -446,6 +460,127 @@ __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
   }
 }
 
+// ---- up to 128 query rows a request ---------------------------------------------------------------------------------
+// Of the 256 rows of cache_chunk_kernel's tile most do not exist then, and their waves wait.  Here a workgroup's eight waves are RG groups
+// of 32 rows by KG = 8 / RG tiles of 64 tokens: all of them unpack KG tiles, then every wave has its rows by one of the tiles, and at an
+// item's end the KG sums of a row meet in LDS.  The next tiles' codes are on their way to registers meanwhile; where LDS holds two sets they
+// are unpacked while slower waves still multiply.  Unpacking is what bounds it: about 1300 vector instructions for 64 tokens of 128 channels.
+// (32 requests of 4096 tokens, 8 heads, 64 rows: 123 -> 87 us, 128 rows 126 -> 107; at d = 64 102 -> 73, 119 -> 91.  With a branch round each tile
+// behind the last token, which a request's last unit may have, the tiles are unpacked one after the other: 108.)
+template <int RG>
+struct SpanShape {
+  static constexpr int KG = 8 / RG, ROWS = 32 * RG, UNIT = 64 * KG, COST = KG == 4 ? 2 : 3;
+};
+template <int D, int GROUP, int RG>
+__global__ __launch_bounds__(512, 2) void cache_span_kernel(AttendArgs a) {
+  typedef ChunkTile<D, GROUP> Tile;
+  typedef SpanShape<RG> Shape;
+  constexpr int KG = Shape::KG, ROWS = Shape::ROWS, UNIT = Shape::UNIT, HALF = 2 * Tile::FRAG, SETS = KG * 4 * HALF <= 131072 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char lds[SETS][KG][2 * HALF];
+  __shared__ __attribute__((aligned(8))) unsigned char poison[SETS][KG][Tile::NG * 64];
+  __shared__ int exists[SETS][KG][2], poisoned[SETS][KG];
+  __shared__ ChunkScratch scratch;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wave % RG, kg = wave / RG;
+  if (tid < SETS * KG) (&poisoned[0][0])[tid] = -1;
+  ChunkWalk<ROWS, UNIT, Shape::COST> walk;
+  if (!walk.start(a, scratch)) return;
+  int tag = 0;      // of a unit, over all items
+  for (bool more = true; more;) {
+    const AttendRequest& rq = walk.rq;
+    const int visible = __builtin_amdgcn_readfirstlane(attend_visible(a, rq, walk.tile * ROWS, ROWS));
+    const int u = max(1, (visible + UNIT - 1) / UNIT), j0 = walk.j0, j1 = walk.last_unit(a, u);
+    const int count = visible > 0 ? j1 - j0 : 0;
+    ChunkRows<D> rows;
+    rows.begin(a, rq, walk.head, walk.tile * ROWS + 32 * rg);
+    // a lane has the page of one of the next 64 blocks of 32 tokens
+    const int32_t* table = a.table + (size_t)walk.r * a.columns;
+    const auto pages_from = [&](int j) { return table[min(j * UNIT + 32 * lane, max(visible - 1, 0)) >> a.g.page_shift]; };
+    int pages = pages_from(j0);
+    Tile next[KG];
+    const auto load = [&](int k) {
+      const int at = 2 * KG * k & 63;
+      if (at == 0 && k != 0) pages = pages_from(j0 + k);
+#pragma unroll
+      for (int i = 0; i < KG; i++)
+        next[i].load(a, walk.head, (j0 + k) * UNIT + 64 * i, __builtin_amdgcn_readlane(pages, at + 2 * i), __builtin_amdgcn_readlane(pages, at + 2 * i + 1),
+                     visible);
+    };
+    const auto store = [&](int k) {
+      const int set = SETS == 2 ? k & 1 : 0;
+#pragma unroll
+      for (int i = 0; i < KG; i++)
+        next[i].store(lds[set][i], lds[set][i] + HALF, exists[set][i], poison[set][i], &poisoned[set][i], tag + k);
+    };
+    const auto attend = [&](int k) {
+      const int set = SETS == 2 ? k & 1 : 0, t0 = (j0 + k) * UNIT + 64 * kg;
+      if (t0 >= rows.wave_sees) return;
+      const int e0 = exists[set][kg][0], e1 = exists[set][kg][1];
+      v16f s[2];
+      v8bf p[4];
+      rows.logits(lds[set][kg], s);
+      rows.softmax(s, p, t0, e0, e1, a.scale_log2);
+      rows.values(lds[set][kg] + HALF, p);
+      if (poisoned[set][kg] == tag + k) rows.poison(poison[set][kg], GROUP, t0, e0, e1);
+    };
+    if (count > 0) load(0);
+    if (SETS == 2) {
+      for (int k = -1; k < count; k++) {
+        if (k >= 0) attend(k);
+        if (k + 1 < count) {
+          store(k + 1);
+          if (k + 2 < count) load(k + 2);
+        }
+        __syncthreads();
+      }
+    } else {
+      for (int k = 0; k < count; k++) {
+        store(k);
+        if (k + 1 < count) load(k + 1);
+        __syncthreads();
+        attend(k);
+        __syncthreads();
+      }
+    }
+    tag += count;
+    // the sums of the KG waves of a row (of those that had a tile), two at a time
+    const int tiles = count > 1 ? KG : (visible - j0 * UNIT + 63) / 64;
+    float* slots = (float*)&lds[0][0][0];
+    constexpr int SLOT = D * 32 + 128;
+#pragma unroll
+    for (int half = KG / 2; half > 0; half /= 2) {
+      if (half >= tiles) continue;
+      float* slot = slots + ((kg < half ? kg : kg - half) * RG + rg) * SLOT;
+      if (kg >= half && kg < 2 * half) {
+#pragma unroll
+        for (int c = 0; c < ChunkRows<D>::NC; c++)
+#pragma unroll
+          for (int i = 0; i < 4; i++)
+            *(v4f*)(slot + ((4 * c + i) * 64 + lane) * 4) = v4f{rows.o[c][4 * i], rows.o[c][4 * i + 1], rows.o[c][4 * i + 2], rows.o[c][4 * i + 3]};
+        slot[D * 32 + lane] = rows.m;
+        slot[D * 32 + 64 + lane] = rows.l;
+      }
+      __syncthreads();
+      if (kg < half) {
+        const float m = slot[D * 32 + lane], l = slot[D * 32 + 64 + lane], to = fmaxf(rows.m, m), ref = to == -INFINITY ? 0.f : to;
+        const float f = __builtin_amdgcn_exp2f(rows.m - ref), g = __builtin_amdgcn_exp2f(m - ref);
+#pragma unroll
+        for (int c = 0; c < ChunkRows<D>::NC; c++)
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            const v4f x = *(const v4f*)(slot + ((4 * c + i) * 64 + lane) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; e++) rows.o[c][4 * i + e] = rows.o[c][4 * i + e] * f + x[e] * g;
+          }
+        rows.l = rows.l * f + l * g;
+        rows.m = to;
+      }
+      __syncthreads();
+    }
+    if (kg == 0) rows.end(a, rq, walk.head, j0 == 0 && j1 == u, ((size_t)walk.w * 2 + (j0 == 0 ? 1 : 0)) * ROWS + 32 * rg + (lane & 31));
+    more = walk.next(a, u, j1);
+  }
+}
+
 // ---- the same with the keys and values unpacked beforehand ------------------------------------------------------------
 // Where a request's keys meet several row tiles, unpacking them in each costs more vector instructions than the softmax: a launch writes the
 // fragments to the workspace once (as they lie in LDS, 256 d bytes for 64 tokens of a head, request after request, head, tile), and the
@@ -457,7 +592,7 @@ struct WideTile {
 template <int D, int GROUP>
 __global__ __launch_bounds__(512) void cache_unpack_kernel(AttendArgs a) {
   typedef ChunkTile<D, GROUP> Tile;
-  __shared__ ChunkWalk::Scratch s;
+  __shared__ ChunkScratch s;
   __shared__ int exists[2], poisoned;
   const int tid = threadIdx.x, H = a.g.H;
   const int per = (a.R + 511) / 512, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
@@ -512,9 +647,9 @@ template <int D, int GROUP>
 __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache_wide_kernel(AttendArgs a) {
   constexpr int TILE = 256 * D, COPIES = TILE / 8 / 1024;
   __shared__ __attribute__((aligned(16))) char ring[kWideStages][TILE];
-  __shared__ ChunkWalk::Scratch scratch;
+  __shared__ ChunkScratch scratch;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  ChunkWalk walk;
+  ChunkWalk<kChunkRows, kChunkUnit, kChunkCost> walk;
   if (!walk.start(a, scratch)) return;
   const bool late = wave >= 4;
   for (bool more = true; more;) {

@@ -44,11 +44,23 @@ constexpr int kCus = 256;
 // Query rows of a request and head that cache_attend_kernel takes (32 requests of 4096 tokens, 32 rows: 59 us, the kernel for many rows 135; 64 rows in
 // four tiles a wave, which its registers do not hold at d = 128, 206).
 constexpr int kFewRows = 32;
+// Query rows of a request and head at most, keys of a request at most, and the rows of a workgroup of the kernel for many.  cache_span_kernel has 64 or
+// 128 and unpacks 256 or 128 tokens at a time (tiles of 256 rows -> these, us: 32 requests of 4096 tokens, 64 rows 123 -> 87, 128 rows 126 ->
+// 107; 64 of 40 rows, 1000 tokens, 60 -> 46; four requests of 64 tokens 15 -> 19; 65 to 128 rows as two tiles of 64 188, 256 as two of 128, 3000
+// tokens, 79 -> 93).
+int64_t most_rows(const sagebwd_cache_params& p, const sagebwd_cache_call& c) { return (int64_t)(c.max_new < c.T ? c.max_new : c.T) * (c.Hq / p.H); }
+int most_length(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
+  const int64_t all = (int64_t)c.columns * p.page;
+  return (int)(c.max_length > 0 && c.max_length < all ? c.max_length : all);
+}
+int tile_rows_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
+  const int64_t most = most_rows(p, c);
+  return most > 128 || most_length(p, c) <= 256 ? kChunkRows : most > 64 ? 128 : 64;
+}
 // Row tiles of the kernel for many rows, over all heads, at most; 0 where no request goes to it.
 int64_t chunk_tiles_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
-  const int64_t G = c.Hq / p.H;
-  if ((c.max_new < c.T ? c.max_new : c.T) * G <= kFewRows) return 0;
-  return (c.T * G / kChunkRows + c.R) * p.H;
+  if (most_rows(p, c) <= kFewRows) return 0;
+  return ((int64_t)c.T * (c.Hq / p.H) / tile_rows_of(p, c) + c.R) * p.H;
 }
 
 int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c) {
@@ -79,6 +91,7 @@ struct AttendLaunch {
   int rows_from, rows_to;      // of the requests that it has
   int nq;                      // cache_attend_kernel: tiles of 16 rows
   int workgroups, join_rows;
+  int tile_rows;               // of the kernels for many rows
   bool split;
   size_t joins, sums, stats;
   bool wide;                   // the keys and values are unpacked beforehand
@@ -97,9 +110,8 @@ inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
   AttendPlan w;
   const int G = c.Hq / p.H;
-  const int64_t all = (int64_t)c.columns * p.page;
-  w.max_length = (int)(c.max_length > 0 && c.max_length < all ? c.max_length : all);
-  const int64_t most = (int64_t)(c.max_new < c.T ? c.max_new : c.T) * G;      // query rows of a request and head
+  w.max_length = most_length(p, c);
+  const int64_t most = most_rows(p, c);
   const int64_t rows = most > 0 ? most : 1;
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
@@ -133,14 +145,15 @@ AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& 
     l.rows_to = INT32_MAX;
     const int64_t total = (int64_t)c.T * G;
     const int64_t with = w.few ? (total / (l.rows_from + 1) < c.R ? total / (l.rows_from + 1) : c.R) : c.R;      // requests that it may have
-    const int64_t tiles = total / kChunkRows + with, units = tiles * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit + kChunkCost);
+    l.tile_rows = tile_rows_of(p, c);
+    const int unit = l.tile_rows == 64 ? SpanShape<2>::UNIT : l.tile_rows == 128 ? SpanShape<4>::UNIT : kChunkUnit;
+    const int64_t tiles = total / l.tile_rows + with, units = tiles * p.H * ((w.max_length + unit - 1) / unit + kChunkCost);
     const int64_t key_tiles = with * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit);
     l.wide = most >= kWideTiles * kChunkRows && (w.few || total >= kWideTiles * kChunkRows * with) && key_tiles * p.d * 256 <= kMostUnpacked;
-    l.split = total * p.H / kChunkRows < 4 * kCus && units < 1 << 30;
+    l.split = total * p.H / l.tile_rows < 4 * kCus && units < 1 << 30;
     const int64_t slots = l.wide && p.d == 64 ? 2 * kCus : kCus;      // (workgroups that the machine takes at a time)
     l.workgroups = (int)(l.split ? (units < slots ? (units > 0 ? units : 1) : slots) : tiles * p.H);
-    l.join_rows = kChunkRows;
-    lay_out(l, kChunkRows);
+    lay_out(l, l.tile_rows);
     if (l.wide) {
       l.unpack_workgroups = (int)(key_tiles < 4 * kCus ? key_tiles : 4 * kCus);
       l.most_tiles = (int)key_tiles;
@@ -184,12 +197,19 @@ int launch_attend(AttendArgs a, const AttendPlan& w, char* ws, hipStream_t st) {
       cache_unpack_kernel<D, GROUP><<<w.m.unpack_workgroups, 512, 0, st>>>(a);
       SERVE_LAUNCH_CHECK();
       cache_wide_kernel<D, GROUP><<<w.m.workgroups, 512, 0, st>>>(a);
+    } else if (w.m.tile_rows == 64) {
+      cache_span_kernel<D, GROUP, 2><<<w.m.workgroups, 512, 0, st>>>(a);
+    } else if (w.m.tile_rows == 128) {
+      cache_span_kernel<D, GROUP, 4><<<w.m.workgroups, 512, 0, st>>>(a);
     } else {
       cache_chunk_kernel<D, GROUP><<<w.m.workgroups, 512, 0, st>>>(a);
     }
     SERVE_LAUNCH_CHECK();
     if (w.m.split && w.m.workgroups > 1) {
-      cache_join_rows_kernel<D, kChunkRows><<<dim3(w.m.workgroups - 1, kChunkRows / (256 / (D / 4))), 256, 0, st>>>(a);
+      const dim3 grid(w.m.workgroups - 1, w.m.tile_rows / (256 / (D / 4)));
+      if (w.m.tile_rows == 64) cache_join_rows_kernel<D, 64><<<grid, 256, 0, st>>>(a);
+      else if (w.m.tile_rows == 128) cache_join_rows_kernel<D, 128><<<grid, 256, 0, st>>>(a);
+      else cache_join_rows_kernel<D, kChunkRows><<<grid, 256, 0, st>>>(a);
       SERVE_LAUNCH_CHECK();
     }
   }

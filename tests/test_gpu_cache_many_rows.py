@@ -163,3 +163,68 @@ def test_rows_behind_the_last_request_stay():
         cache.sagebwd_cache_attention(q, f.pool, f.table, f.lengths, _i32([0, news[0]]), p, news[0], O=O, LSE=lse)
         assert (O[news[0]:] == 5).all() and (lse[:, news[0]:] == 5).all()
         _check_rows(f, q.cpu(), [0, news[0]], O, lse, True, [0, 127, 128, news[0] - 1])
+
+
+# ---- 33 to 128 rows a request: groups of 32 rows by tiles of 64 tokens in one workgroup ---------------------------------------
+@pytest.mark.parametrize("lens,news,Hq,H,d,group,page", [
+    ([700], [33], 2, 2, 128, 64, 64),                                     # one item, its keys divided over the machine
+    ([257, 64, 65, 1, 0, 1000], [40, 33, 64, 1, 1, 50], 6, 6, 64, 32, 32),
+    ([320, 300, 511, 513], [16, 9, 5, 13], 12, 3, 128, 32, 256),          # 64 rows and fewer, beside requests of few
+    ([300 + 3 * r for r in range(70)], [64] * 70, 8, 8, 64, 64, 64),
+    ([128, 900, 640], [128, 100, 65], 3, 3, 128, 64, 32),                 # up to 128
+    ([3, 600, 20], [100, 127, 31], 4, 4, 64, 32, 128),                    # a request shorter than its new tokens
+    ([290] * 600, [20] * 600, 12, 2, 128, 64, 32),                        # 120 rows; none divided
+    ([270] * 520, [34] * 520, 2, 1, 64, 64, 64),
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_up_to_128_rows_against_64_bits(lens, news, Hq, H, d, group, page, causal):
+    g = torch.Generator().manual_seed(sum(news) + d + 1)
+    f = Filled(lens, CacheParams(H=H, d=d, page=page, group=group), g)
+    v_mean = torch.randn((H, d), generator=g).cuda() if page == 64 else None
+    q, cu, O, lse = _attend(f, news, Hq, g, causal=causal, v_mean=v_mean, max_length=max(max(lens), 257))
+    assert torch.isfinite(O).all()
+    _check_rows(f, q, cu, O, lse, causal, _some(cu, g), v_mean)
+
+
+@pytest.mark.parametrize("n,G,d,group", [(50, 1, 128, 64), (16, 8, 64, 32), (30, 4, 128, 32), (31, 2, 64, 64)])
+def test_up_to_128_rows_every_token_is_weighed_alone(n, G, d, group):
+    g, L = torch.Generator().manual_seed(n), 1000
+    f = Filled([L], CacheParams(H=1, d=d, page=32, group=group), g)
+    for part in range(-(-L // (n * G))):
+        target = ((torch.arange(n * G) + part * n * G) % L).reshape(n, G)
+        q = torch.tensor(f.k[:, 0])[target] * 8
+        _, _, O, _ = _attend(f, [n], G, g, causal=False, sm_scale=1.0, q=q.to(torch.bfloat16))
+        want = torch.tensor(f.v[:, 0])[target]
+        assert (O.double().cpu() - want).abs().max() <= 2.0 ** -7 * want.abs().max()
+
+
+@pytest.mark.parametrize("n", [40, 100])
+@pytest.mark.parametrize("d,group", [(128, 64), (64, 32)])
+def test_up_to_128_rows_what_is_not_a_number_and_pages_that_do_not_exist(n, d, group):
+    """A NaN in one token's V reaches the rows that see it and the group's channels alone; a missing page is left out; every replay the same."""
+    g, L, page = torch.Generator().manual_seed(n + d), 900, 64
+    f = Filled([L], CacheParams(H=1, d=d, page=page, group=group), g)
+    at = L - n // 2                                       # (half of the rows see it)
+    f.V[at, 0, 3] = float("nan")
+    cache.sagebwd_cache_append(f.K.cuda(), f.V.cuda(), f.slots, f.pool, f.p)
+    table = f.table.clone()
+    table[0, 5] = -1
+    kept = np.r_[0:5 * page, 6 * page:L]
+    q = _randn((n, 1, d), g)
+    cu = _i32([0, n])
+    O, lse = cache.sagebwd_cache_attention(q.cuda(), f.pool, table, f.lengths, cu, f.p, n)
+    sees = torch.arange(n) + L - n + 1 > at
+    nan = torch.isnan(O.cpu()).squeeze(1)
+    assert nan[sees][:, :group].all() and not nan[~sees].any() and not nan[:, group:].any() and torch.isfinite(lse).all()
+    v = f.v.copy()
+    v[np.isnan(v)] = 0
+    for i in (0, n // 4, n - 1):
+        keys = kept[kept < L - n + i + 1]
+        want, wl, A = ref.attention(_np(q[i:i + 1]).astype(np.float64), f.k[keys], v[keys], 1, False, d ** -0.5, None)
+        got, ok = _np(O[i]).astype(np.float64), ~nan[i].numpy()
+        # (roundings of O and of the probabilities, 2^-8 of each; logits and sums in FP32 below 2^-14)
+        assert (np.abs(got - want[0]) <= 2.0 ** -8 * np.abs(want[0]) + (2.0 ** -8 + 2.0 ** -13) * A[0] + 1e-5)[:, ok].all(), i
+        assert abs(lse[0, i].item() - wl[0, 0]) <= 2.0 ** -14
+    for _ in range(3):
+        again, _ = cache.sagebwd_cache_attention(q.cuda(), f.pool, table, f.lengths, cu, f.p, n)
+        assert torch.equal(again.view(torch.int16), O.view(torch.int16))

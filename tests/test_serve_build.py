@@ -118,3 +118,10 @@ def test_the_rows_of_a_head_are_taken_from_both_ends():
     for tiles in range(1, 40):
         at = [tiles - 1 - p // 2 if p % 2 else p // 2 for p in range(tiles)]
         assert sorted(at) == list(range(tiles))
+
+
+def test_the_attention_of_up_to_128_rows_fits_a_cu(kernels):
+    for k in _pick(kernels, "cache_span_kernel"):
+        assert k["vgpr"] <= 256 and k["lds"] <= 160 * 1024 and k["scratch"] <= 96, k
+    for k in _pick(kernels, "cache_span_kernel", "ELi4EEEv") + _pick(kernels, "cache_span_kernel", "ILi64E"):
+        assert k["scratch"] == 0, k
