@@ -28,5 +28,6 @@ def sage_rotary(Q, K, positions, inv_freq, sections=None, adjacent: bool = False
     begin on 16 bytes are copied).  inv_freq: float32, one for every pair of channels that turns; the channels behind them pass.
     sections: how many of the frequencies go by each axis of `positions`, int32 or int64 [axes, tokens] (video: time, height, width);
     with one axis (the default) [tokens].  [axes, N] serves every batch.  adjacent: channel 2i turns with 2i + 1, else i with
-    i + len(inv_freq).  inverse: by the negative angles.  Returns (Q, K) as new dense tensors."""
+    i + len(inv_freq).  inverse: by the negative angles.  Returns (Q, K) as new dense tensors.  inv_freq gets no gradient (one that
+    wants it is refused).  A backward captured into a graph wants leaves that no eager graph still holds, as with any operator."""
     return binding._host().rotary(Q, K, positions, inv_freq, sections, adjacent, token_major, inverse)

@@ -228,3 +228,21 @@ def test_up_to_128_rows_what_is_not_a_number_and_pages_that_do_not_exist(n, d, g
     for _ in range(3):
         again, _ = cache.sagebwd_cache_attention(q.cuda(), f.pool, table, f.lengths, cu, f.p, n)
         assert torch.equal(again.view(torch.int16), O.view(torch.int16))
+
+
+# ---- keys and values of 128 channels are unpacked beforehand from 4096 rows on -------------------------------------------------
+@pytest.mark.parametrize("lens,news,Hq,H,group,page", [([1500], [1100], 8, 2, 64, 64), ([1300, 900, 77], [1050, 3, 1], 8, 2, 32, 32),
+                                                       ([4200, 4100], [4200, 4097], 1, 1, 64, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_4096_rows_and_more_of_128_channels(lens, news, Hq, H, group, page, causal):
+    test_rows_against_64_bits(lens, news, Hq, H, 128, group, page, causal)
+
+
+@pytest.mark.parametrize("group", [32, 64])
+def test_4096_rows_every_token_is_weighed_alone(group):
+    test_every_token_is_weighed_alone(4200, 4300, 1, 128, group, 32)
+
+
+def test_4096_rows_masks_and_pages():
+    test_the_mask_hides_what_is_not_a_number(4200, 4400)
+    test_pages_that_do_not_exist(4200)
