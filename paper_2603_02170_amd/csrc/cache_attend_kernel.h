@@ -126,6 +126,20 @@ __device__ __forceinline__ int pack_bf16(float a, float b) {
 }
 __device__ __forceinline__ float low_bf16(int w) { return __uint_as_float((unsigned)w << 16); }
 __device__ __forceinline__ float high_bf16(int w) { return __uint_as_float((unsigned)w & 0xFFFF0000u); }
+// copy_16 and copy_4 of a ring whose reads are counted by hand.  Behind the builtin the compiler lets every read of LDS wait for every copy in
+// flight, as it cannot tell a ring's slots apart, so that a ring is one tile deep; of this it sees no access, only that memory changes: what
+// is read has to have been waited for (vmcnt_only), and its own waits for loads come out early at worst.  (The copies have no register for a
+// result; a kernel with these has nothing else that uses m0.  Wait states: of m0, and of a base that a vector instruction wrote.)
+template <int BYTES>
+__device__ __forceinline__ void ring_copy(gbytes_t base, unsigned lane_offset, const void* lds_base) {
+  const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lptr_t)lds_base);
+  if (BYTES == 16) asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane_offset), "s"(base), "s"(to) : "memory");
+  else asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(lane_offset), "s"(base), "s"(to) : "memory");
+}
+// Waits here for a load, once, and not wherever its result is used: a use that some path reaches with the load under way waits for everything in
+// flight on every path, copies to LDS that were meant to stay there included.
+template <typename T>
+__device__ __forceinline__ void arrived(T& x) { asm volatile("" : "+v"(x)); }
 // max, sum over the four lanes of a column
 __device__ __forceinline__ float column_max(float v) {
   auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -153,17 +167,17 @@ struct CacheTile {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int c = 0; c < CODES / 1024; c++) {
-      copy_16(uniform(p + at * (D / 2) + c * 1024) + lane * 16, slot + c * 1024);
-      copy_16(uniform(p + geo.v_codes() + at * (D / 2) + c * 1024) + lane * 16, slot + CODES + c * 1024);
+      ring_copy<16>(uniform(p + at * (D / 2) + c * 1024), lane * 16, slot + c * 1024);
+      ring_copy<16>(uniform(p + geo.v_codes() + at * (D / 2) + c * 1024), lane * 16, slot + CODES + c * 1024);
     }
     const gbytes_t ps = uniform(p + geo.k_scales() + at * (2 * NG));
     const int apart = geo.v_scales() - geo.k_scales();
     if (NG == 4) {
-      copy_4(ps + lane * 4, slot + 2 * CODES);
-      copy_4(ps + (unsigned)(apart + lane * 4), slot + 2 * CODES + SCALES);
+      ring_copy<4>(ps, lane * 4, slot + 2 * CODES);
+      ring_copy<4>(ps, apart + lane * 4, slot + 2 * CODES + SCALES);
     } else {
       const int l = lane % (32 * NG);        // (with one group the upper half of the lanes copies the same to where nothing is read)
-      copy_4(ps + (unsigned)(l < 16 * NG ? 4 * l : apart + 4 * l - SCALES), slot + 2 * CODES);
+      ring_copy<4>(ps, l < 16 * NG ? 4 * l : apart + 4 * l - SCALES, slot + 2 * CODES);
     }
   }
   __device__ __forceinline__ void take(const char* slot) {
@@ -514,7 +528,10 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
     for (int q = 0; q < NQ; q++) rows[q].fetch(a, piece);
   };
   const auto fetch = [&](int k) {
-    if (k % 64 == 0 && k != 0) pages = pages_from(k);
+    if (k % 64 == 0 && k != 0) {
+      pages = pages_from(k);
+      arrived(pages);
+    }
     const int entry = __builtin_amdgcn_readlane(pages, k % 64);
     const bool ok = (unsigned)entry < (unsigned)a.g.pages;
     const int at = k % kStages;
@@ -523,6 +540,11 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
     Tile::fetch(a.g, p, (first + k * kUnit) & (a.g.page() - 1), ring + at * Tile::SLOT);
   };
   const auto start = [&] {
+    arrived(pages);
+#pragma unroll
+    for (int q = 0; q < NQ; q++)
+#pragma unroll
+      for (int j = 0; j < D / 32; j++) arrived(rows[q].q[j]);
     exists = 0;
     for (int k = 0; k < kStages - 1 && k < count; k++) fetch(k);
   };

@@ -280,6 +280,11 @@ struct ChunkRows {
     m = -INFINITY;
     l = 0.f;
   }
+  // The queries are there.
+  __device__ __forceinline__ void wait() {
+#pragma unroll
+    for (int s = 0; s < NK; s++) arrived(q[s]);
+  }
   // N products whose operand comes from LDS, kAhead reads ahead of each, in this order.  (The compiler by itself reads, waits and multiplies,
   // one after the other, and looks past groups of instructions that it is asked for.)
   static constexpr int kAhead = 4;
@@ -412,6 +417,8 @@ __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
     const int32_t* table = a.table + (size_t)walk.r * a.columns;
     const auto pages_from = [&](int j) { return table[min(j * kChunkUnit + 32 * lane, max(visible - 1, 0)) >> a.g.page_shift]; };
     int pages = pages_from(j0);
+    arrived(pages);
+    rows.wait();
     const auto load = [&](Tile& t, int j) {
       const int k = 2 * (j - j0) & 63;
       if (k == 0 && j != j0) pages = pages_from(j);
@@ -496,6 +503,8 @@ __global__ __launch_bounds__(512, 2) void cache_span_kernel(AttendArgs a) {
     const int32_t* table = a.table + (size_t)walk.r * a.columns;
     const auto pages_from = [&](int j) { return table[min(j * UNIT + 32 * lane, max(visible - 1, 0)) >> a.g.page_shift]; };
     int pages = pages_from(j0);
+    arrived(pages);
+    rows.wait();
     Tile next[KG];
     const auto load = [&](int k) {
       const int at = 2 * KG * k & 63;
@@ -665,7 +674,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache_wide_kernel(Attend
     const auto fetch = [&](int k) {
       const gbytes_t from = uniform(a.unpacked + (tile0 + k) * TILE + wave * (COPIES * 1024));
 #pragma unroll
-      for (int c = 0; c < COPIES; c++) copy_16(from + c * 1024 + lane * 16, ring[k % kWideStages] + wave * (COPIES * 1024) + c * 1024);
+      for (int c = 0; c < COPIES; c++) ring_copy<16>(from, c * 1024 + lane * 16, ring[k % kWideStages] + wave * (COPIES * 1024) + c * 1024);
     };
     // (intervals as in cache_chunk_kernel)
     v16f s[2];
@@ -675,6 +684,8 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache_wide_kernel(Attend
       const int t0 = (j0 + k) * kChunkUnit;
       if (t0 < rows.wave_sees) rows.softmax(s, p, t0, flag & 1, flag >> 1 & 1, a.scale_log2);
     };
+    arrived(flags);
+    rows.wait();
     compiler_fence();
     fetch(0);
     if (count > 1) fetch(1);
@@ -686,7 +697,10 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache_wide_kernel(Attend
       compiler_fence();
       if (k + 2 < count) fetch(k + 2);
       compiler_fence();
-      if (k % 64 == 0 && k != 0) flags = a.tiles[tile0 + min(k + lane, count - 1)].flags;
+      if (k % 64 == 0 && k != 0) {
+        flags = a.tiles[tile0 + min(k + lane, count - 1)].flags;
+        arrived(flags);
+      }
       flag_before = flag;
       flag = __builtin_amdgcn_readlane(flags, k % 64);
       if (late && k > 0) probabilities(k - 1, flag_before);
