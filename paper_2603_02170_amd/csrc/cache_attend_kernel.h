@@ -347,9 +347,18 @@ __device__ __forceinline__ void attend_tile(AttendRows<D, GROUP> (&rows)[NQ], Ca
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Writes channels c .. c + N - 1 of a finished row.
+// V's means of N channels from `at` on, which a finished row gets back.
 template <int N>
-__device__ __forceinline__ void attend_store(const AttendArgs& a, int begin, int head, int row, int D, int c, float m, float l, const float* o) {
+__device__ __forceinline__ auto value_means(const AttendArgs& a, int at) {
+  typedef float vec __attribute__((ext_vector_type(N)));
+  typedef vec vec_dword __attribute__((aligned(4)));
+  vec mean = {};
+  if (a.v_mean != nullptr) mean = *(const vec_dword*)(a.v_mean + at);
+  return mean;
+}
+// Writes channels c .. c + N - 1 of a finished row.
+template <int N, typename Mean>
+__device__ __forceinline__ void attend_store(const AttendArgs& a, int begin, int head, int row, int D, int c, float m, float l, const float* o, const Mean& mean) {
   const int i = row / a.G, hq = head * a.G + row - i * a.G;
   const int64_t token = begin + i;
   const bool any = !(l == 0.f);
@@ -358,7 +367,7 @@ __device__ __forceinline__ void attend_store(const AttendArgs& a, int begin, int
   typedef __bf16 vec __attribute__((ext_vector_type(N)));
   vec x;
 #pragma unroll
-  for (int k = 0; k < N; k++) x[k] = (__bf16)(any ? o[k] * r + (a.v_mean != nullptr ? a.v_mean[head * D + c + k] : 0.f) : 0.f);
+  for (int k = 0; k < N; k++) x[k] = (__bf16)(any ? o[k] * r + mean[k] : 0.f);
   *(vec*)p = x;
   if (c == 0 && a.LSE != nullptr) a.LSE[(int64_t)hq * a.T + token] = any ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
 }
@@ -575,10 +584,15 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
     }
     // Join the waves; the next piece's loads and first copies are on their way meanwhile.
     const AttendPiece done = piece;
+    v4f mean[D / 64];             // (asked for in front of the next piece's copies, which a load behind them would wait for)
+#pragma unroll
+    for (int h = 0; h < D / 64; h++) mean[h] = value_means<4>(a, done.head * D + 64 * h + tid % 16 * 4);
     const bool more = cursor.more(a);
     if (more) {
       piece = cursor.next(a);
       look();
+    } else {
+      count = 0;
     }
     const bool whole = done.j0 == 0 && done.j1 == done.u;
     const size_t part = (size_t)w * 2 + (done.j0 == 0 ? 1 : 0);
@@ -600,7 +614,11 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
         if (q + half > 0) barrier_lds_only();
 #pragma unroll
         for (int v = 0; v < 4; v++) *(v4f*)&stage[wave][lane & 15][16 * v + 4 * (lane >> 4)] = rows[q].o[4 * half + v];
-        if (q + half == 0 && more) start();
+        if (q + half == 0) {
+#pragma unroll
+          for (int h = 0; h < D / 64; h++) arrived(mean[h]);
+          start();
+        }
         barrier_lds_only();
         if (half == 0) {
           M = fmaxf(fmaxf(wave_m[0][k], wave_m[1][k]), fmaxf(wave_m[2][k], wave_m[3][k]));
@@ -616,7 +634,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
         if (k < done.n_rows) {
           const int channel = 64 * half + c;
           if (whole) {
-            attend_store<4>(a, done.begin, done.head, k, D, channel, M, l, (const float*)&o);
+            attend_store<4>(a, done.begin, done.head, k, D, channel, M, l, (const float*)&o, mean[half]);
           } else {
             *(v4f*)(a.sums + (part * ROWS + k) * D + channel) = o;
             if (channel == 0) a.stats[part * ROWS + k] = float2{M, l};
@@ -639,6 +657,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
   const int parts = join.x & 0xFFFF;
   if (k >= join.x >> 16) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const auto mean = value_means<NC>(a, join.z * D + NC * lane);
   const size_t slot0 = (size_t)w * 2;
   const auto at = [&](int p) { return (p == 0 ? slot0 - 1 : slot0 + 2 * (p - 1)) * ROWS + k; };
   float M = -INFINITY;
@@ -675,7 +694,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
   l = (meet[0][D] + meet[1][D]) + (meet[2][D] + meet[3][D]);
 #pragma unroll
   for (int i = 0; i < NC; i++) o[i] = (meet[0][NC * lane + i] + meet[1][NC * lane + i]) + (meet[2][NC * lane + i] + meet[3][NC * lane + i]);
-  attend_store<NC>(a, join.y, join.z, join.w + k, D, NC * lane, M, l, o);
+  attend_store<NC>(a, join.y, join.z, join.w + k, D, NC * lane, M, l, o, mean);
 }
 
 // The same of many rows, with few parts each: D / 4 lanes have a row and take four parts at a time, one trip to memory for up to four.  (A wave a row,
@@ -689,6 +708,7 @@ __global__ __launch_bounds__(256) void cache_join_rows_kernel(AttendArgs a) {
   const int parts = join.x & 0xFFFF;
   if (k >= join.x >> 16) return;
   const int c = threadIdx.x % LANES * 4;
+  const auto mean = value_means<4>(a, join.z * D + c);
   const size_t slot0 = (size_t)w * 2;
   float m = -INFINITY, l = 0.f;
   v4f o = {0.f, 0.f, 0.f, 0.f};
@@ -716,7 +736,7 @@ __global__ __launch_bounds__(256) void cache_join_rows_kernel(AttendArgs a) {
     }
     m = to;
   }
-  attend_store<4>(a, join.y, join.z, join.w + k, D, c, m, l, (const float*)&o);
+  attend_store<4>(a, join.y, join.z, join.w + k, D, c, m, l, (const float*)&o, mean);
 }
 
 }  // namespace sage
