@@ -128,7 +128,7 @@ typedef struct sagebwd_cache_call {
  * request's length reaches nothing.
  * Requests of up to 32 query rows (new tokens x Hq / H) go to a kernel for few rows, the others to one for many; a call that may hold both kinds
  * (max_new tokens are more than 32 rows, T is less than R * max_new, Hq / H at most 32) launches both.  Where a call has few items for
- * the machine their keys are divided over it and the parts joined by a further launch; from 2048 (d = 64) or 4096 rows a request on, keys and values are
+ * the machine their keys are divided over it and the parts joined by a further launch; from 2048 rows a request on, keys and values are
  * unpacked to bf16 in the workspace first (256 d bytes for 64 tokens and head; at most 4 GiB, else each tile unpacks its own).  How
  * work is divided depends on all requests of the call, so that O agrees between calls of different batches to its rounding, and bit
  * for bit between equal calls.

@@ -80,11 +80,11 @@ int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c) {
 // Keys of a request up to this many units are not divided (four requests of 500 tokens 11.0 -> 9.3 us, 256 of 650 56.4 -> 52.0: the joining
 // launch is 4 to 5 us, a unit 0.6 where the machine is empty).
 constexpr int kWholeUnits = 8;
-// Keys and values are unpacked beforehand where a request's meet so many row tiles (us, unpacked by every tile -> beforehand; at d = 128 one request of
-// 512 new tokens x 4 heads of the group against 32768, 8 tiles, 293 -> 299, two of 2048 against 8192, 8 tiles, 151 -> 160; one of 1024
-// x 4 against 16384, 16 tiles, 290 -> 285; 2048 x 4 against 10000, 32 tiles, 335 -> 318; at d = 64, where unpacking is the larger part,
-// the same 228 -> 194, 257 -> 186, 264 -> 204, two of 2048 against 2048 41 -> 44), and the workspace for them is at most this.
-int wide_tiles(int d) { return d == 64 ? 8 : 16; }
+// Keys and values are unpacked beforehand where a request's meet so many row tiles (us, unpacked by every tile -> beforehand: one request of 512 new
+// tokens x 4 heads of the group against 32768, 8 tiles, 288 -> 277, at d = 64 229 -> 180; 2048 x 4 against 10000, 32 tiles, 335 -> 293, at
+// d = 64 264 -> 193; two of 2048 against 8192, 8 tiles, 149 -> 148; 16 ragged ones of at most 600 x 4 140 -> 143; 4 of 256 x 4, 4 tiles,
+// slower by a sixth), and the workspace for them is at most this.
+constexpr int kWideTiles = 8;
 constexpr int64_t kMostUnpacked = (int64_t)4 << 30;
 
 // One of the two kernels' part of a call.
@@ -150,7 +150,7 @@ AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache_call& 
     const int unit = l.tile_rows == 64 ? SpanShape<2>::UNIT : l.tile_rows == 128 ? SpanShape<4>::UNIT : kChunkUnit;
     const int64_t tiles = total / l.tile_rows + with, units = tiles * p.H * ((w.max_length + unit - 1) / unit + kChunkCost);
     const int64_t key_tiles = with * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit);
-    const int64_t wide_rows = wide_tiles(p.d) * kChunkRows;
+    const int64_t wide_rows = kWideTiles * kChunkRows;
     l.wide = most >= wide_rows && (w.few || total >= wide_rows * with) && key_tiles * p.d * 256 <= kMostUnpacked;
     l.split = total * p.H / l.tile_rows < 4 * kCus && units < 1 << 30;
     const int64_t slots = l.wide && p.d == 64 ? 2 * kCus : kCus;      // (workgroups that the machine takes at a time)
