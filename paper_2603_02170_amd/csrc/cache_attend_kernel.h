@@ -574,12 +574,11 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
       else if (behind == 1) __builtin_amdgcn_s_waitcnt(vmcnt_only(Tile::COPIES));
       else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
       compiler_fence();
-      if ((exists >> slot & 1) != 0) {
-        Tile tile;
-        tile.take(ring + slot * Tile::SLOT);
-        const int t0 = first + k * kUnit;
-        attend_tile<D, GROUP, NQ>(rows, tile, t0, t0 + 32 > all_see, a.scale_log2, un);
-      }
+      // (a tile of a page that does not exist is one behind all keys: no branch, which would have the sums in other registers behind it)
+      Tile tile;
+      tile.take(ring + slot * Tile::SLOT);
+      const int t0 = (exists >> slot & 1) != 0 ? first + k * kUnit : 1 << 30;
+      attend_tile<D, GROUP, NQ>(rows, tile, t0, t0 + 32 > all_see, a.scale_log2, un);
       slot = slot == kStages - 1 ? 0 : slot + 1;
     }
     // Join the waves; the next piece's loads and first copies are on their way meanwhile.

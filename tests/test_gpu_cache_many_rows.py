@@ -230,7 +230,7 @@ def test_up_to_128_rows_what_is_not_a_number_and_pages_that_do_not_exist(n, d, g
         assert torch.equal(again.view(torch.int16), O.view(torch.int16))
 
 
-# ---- keys and values of 128 channels are unpacked beforehand from 4096 rows on -------------------------------------------------
+# ---- unpacked beforehand, at 128 channels: 4096 rows and more --------------------------------------------------------------
 @pytest.mark.parametrize("lens,news,Hq,H,group,page", [([1500], [1100], 8, 2, 64, 64), ([1300, 900, 77], [1050, 3, 1], 8, 2, 32, 32),
                                                        ([4200, 4100], [4200, 4097], 1, 1, 64, 128)])
 @pytest.mark.parametrize("causal", [True, False])
