@@ -75,6 +75,7 @@ int sagebwd_cache_page_bytes(const sagebwd_cache_params* params, size_t* bytes);
  *   granted       int32 [R]: 1 or 0
  *   free_left     int32 [1]: free_count less the pages granted; may be `free_count`
  * Everything but block_table is out only, so that the call repeated on the same tensors does the same.
+ * Bounds: R <= 2^20, columns * page < 2^30, rows <= 2^30.
  */
 int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block_table, const int32_t* free_pages,
                        const int32_t* free_count, int32_t R, int32_t columns, int32_t page, int32_t capacity, int32_t rows,

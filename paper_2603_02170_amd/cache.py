@@ -63,7 +63,7 @@ def alloc_cache(p: CacheParams, pages: int, device="cuda"):
 
 def sagebwd_cache_plan(held, added, block_table, free_pages, free_count, p: CacheParams, rows: int, out=None) -> CachePlan:
     """Pages, slots and positions of a step's new tokens (int32 device tensors; `rows` >= all new tokens, or the requests behind
-    are not granted).  block_table [R, columns] gets the granted pages; everything else is in the plan, whose tensors `out` (a
+    are not granted; at most 2^30).  block_table [R, columns] gets the granted pages; everything else is in the plan, whose tensors `out` (a
     CachePlan) may bring: `out.lengths` may be `held` and `out.free_left` may be `free_count`."""
     return CachePlan._make(binding._host().cache_plan(held, added, block_table, free_pages, free_count, p.page, rows, out))
 

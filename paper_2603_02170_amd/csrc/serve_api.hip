@@ -22,6 +22,8 @@ constexpr int64_t kMostElements = (int64_t)1 << 40;
 // A launch's threads are counted in 32 bits, its workgroups along y in 16.
 constexpr int64_t kMostThreads = (int64_t)1 << 31;
 constexpr int kMostInY = 65535;
+// Rows of a plan: its kernels step over them in 32 bits, by as many as a launch has threads (rows rounded up).
+constexpr int kMostRows = 1 << 30;
 
 inline bool aligned(const void* p, size_t to = 16) { return ((uintptr_t)p & (to - 1)) == 0; }
 inline bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s <= kMostElements; }
@@ -250,7 +252,7 @@ int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block
       (capacity > 0 && free_pages == nullptr) || free_count == nullptr || cu_new == nullptr || free_left == nullptr ||
       (rows > 0 && (slots == nullptr || positions == nullptr)))
     return SAGEBWD_INVALID_ARG;
-  if (page_shift_of(page) < 0 || (int64_t)columns * page > INT32_MAX / 2 || R > 1 << 20) return SAGEBWD_UNSUPPORTED_SHAPE;
+  if (page_shift_of(page) < 0 || (int64_t)columns * page > INT32_MAX / 2 || R > 1 << 20 || rows > kMostRows) return SAGEBWD_UNSUPPORTED_SHAPE;
   const PlanArgs a{held, added, free_pages, free_count, block_table, slots, positions, cu_new, lengths, granted, free_left,
                    R, columns, page_shift_of(page), capacity, rows};
   hipStream_t st = (hipStream_t)stream;

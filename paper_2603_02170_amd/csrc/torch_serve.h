@@ -120,6 +120,7 @@ PyObject* py_cache_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !(table = dense(a[2], at::kInt, {held->size(0), -1}, "block_table", dev)) || !(free_pages = dense(a[3], at::kInt, {-1}, "free_pages", dev)) ||
       !(free_count = dense(a[4], at::kInt, {1}, "free_count", dev)) || !size_arg(a[5], "page", 0, &page) || !size_arg(a[6], "rows", 0, &rows))
     return nullptr;
+  if (rows > 1 << 30) return raise_status(SAGEBWD_UNSUPPORTED_SHAPE, "sagebwd_cache_plan");      // (before its outputs are allocated)
   const int64_t R = held->size(0);
   const std::array<int64_t, 6> sizes = {rows, rows, R + 1, R, R, 1};
   const char* names[6] = {"slots", "positions", "cu_new", "lengths", "granted", "free_left"};
