@@ -75,7 +75,7 @@ int sagebwd_cache_page_bytes(const sagebwd_cache_params* params, size_t* bytes);
  *   granted       int32 [R]: 1 or 0
  *   free_left     int32 [1]: free_count less the pages granted; may be `free_count`
  * Everything but block_table is out only, so that the call repeated on the same tensors does the same.
- * Bounds: R <= 2^20, columns * page < 2^30, rows <= 2^30.
+ * Bounds: R <= 2^20, columns * page < 2^30, R * columns < 2^31, rows <= 2^30.
  */
 int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block_table, const int32_t* free_pages,
                        const int32_t* free_count, int32_t R, int32_t columns, int32_t page, int32_t capacity, int32_t rows,
@@ -88,7 +88,7 @@ int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block
  * block_table (freed entries become -1), free_pages and free_count are changed in place.  A keep[r] outside 0 ..
  * lengths[r] leaves the request alone.  Entries that are not pages (negative) give none back.  (Pages beyond `capacity` are lost: the
  * stack has to hold every page.  A page that stands in two requests' rows comes back from each: who shares pages counts them and trims
- * the last one alone.)
+ * the last one alone.)  Bounds as of plan.
  */
 int sagebwd_cache_trim(const int32_t* keep, int32_t* lengths, int32_t* block_table, int32_t* free_pages, int32_t* free_count,
                        int32_t R, int32_t columns, int32_t page, int32_t capacity, void* stream);

@@ -24,6 +24,8 @@ constexpr int64_t kMostThreads = (int64_t)1 << 31;
 constexpr int kMostInY = 65535;
 // Rows of a plan: its kernels step over them in 32 bits, by as many as a launch has threads (rows rounded up).
 constexpr int kMostRows = 1 << 30;
+// Entries of a block table whose pages are counted: what the sums of plan and trim hold (they stop there).
+constexpr int64_t kMostEntries = kFull;
 
 inline bool aligned(const void* p, size_t to = 16) { return ((uintptr_t)p & (to - 1)) == 0; }
 inline bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s <= kMostElements; }
@@ -252,7 +254,7 @@ int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block
       (capacity > 0 && free_pages == nullptr) || free_count == nullptr || cu_new == nullptr || free_left == nullptr ||
       (rows > 0 && (slots == nullptr || positions == nullptr)))
     return SAGEBWD_INVALID_ARG;
-  if (page_shift_of(page) < 0 || (int64_t)columns * page > INT32_MAX / 2 || R > 1 << 20 || rows > kMostRows) return SAGEBWD_UNSUPPORTED_SHAPE;
+  if (page_shift_of(page) < 0 || (int64_t)columns * page > INT32_MAX / 2 || R > 1 << 20 || (int64_t)R * columns > kMostEntries || rows > kMostRows) return SAGEBWD_UNSUPPORTED_SHAPE;
   const PlanArgs a{held, added, free_pages, free_count, block_table, slots, positions, cu_new, lengths, granted, free_left,
                    R, columns, page_shift_of(page), capacity, rows};
   hipStream_t st = (hipStream_t)stream;
@@ -276,7 +278,8 @@ int sagebwd_cache_trim(const int32_t* keep, int32_t* lengths, int32_t* block_tab
   if (R < 0 || columns < 1 || capacity < 0 || free_count == nullptr || (capacity > 0 && free_pages == nullptr) ||
       (R > 0 && (keep == nullptr || lengths == nullptr || block_table == nullptr)))
     return SAGEBWD_INVALID_ARG;
-  if (page_shift_of(page) < 0 || (int64_t)columns * page > INT32_MAX / 2 || R > 1 << 20) return SAGEBWD_UNSUPPORTED_SHAPE;
+  if (page_shift_of(page) < 0 || (int64_t)columns * page > INT32_MAX / 2 || R > 1 << 20 || (int64_t)R * columns > kMostEntries)
+    return SAGEBWD_UNSUPPORTED_SHAPE;
   if (R == 0) return SAGEBWD_OK;
   cache_trim_kernel<<<1, 1024, 0, (hipStream_t)stream>>>(
       TrimArgs{keep, lengths, block_table, free_pages, free_count, R, columns, page_shift_of(page), capacity});

@@ -31,6 +31,15 @@ def test_a_plan_of_more_rows_than_its_steps_hold_is_refused(lib, rows):
         assert _plan(lib, R=R, rows=rows) == -2
 
 
+def test_a_table_of_more_entries_than_the_sums_hold_is_refused(lib):
+    """Pages are counted in sums that stop at 2^31 - 1: more entries than that could be freed in part, or granted beyond the stack."""
+    one, null = ctypes.c_void_p(256), ctypes.c_void_p(None)
+    for R, columns in ((1 << 20, 2048), (1 << 10, 1 << 21), (129, 1 << 24)):
+        assert R * columns > 2 ** 31 - 1 and R <= 1 << 20 and columns * 32 < 2 ** 30
+        assert _plan(lib, R=R, columns=columns) == -2
+        assert lib.sagebwd_cache_trim(one, one, one, one, one, R, columns, 32, 1, null) == -2
+
+
 @pytest.mark.gpu
 def test_a_plan_of_too_many_rows_allocates_nothing(lib):
     i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
