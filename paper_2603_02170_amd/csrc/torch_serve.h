@@ -455,7 +455,9 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
       PyErr_SetString(PyExc_TypeError, "sage_rotary: Q and K are tensors");
       return nullptr;
     }
-    if (is_transformed(THPVariable_Unpack(a[k]))) {
+  }
+  for (int k = 0; k < 4; k++) {       // (the positions and frequencies too: their other checks come later)
+    if (THPVariable_Check(a[k]) && is_transformed(THPVariable_Unpack(a[k]))) {
       PyErr_SetString(PyExc_NotImplementedError,
                       "sage_rotary has no forward-mode derivative and no rule for torch.func transforms (vmap, grad, jvp, ...)");
       return nullptr;
