@@ -1,5 +1,4 @@
-"""What sage_rotary has no derivative or rule for is refused, whichever argument brings it, on the host and before any other check (no GPU
-needed)."""
+"""What sage_rotary has no derivative or rule for is refused, whichever argument brings it, on the host and before any other check."""
 import os
 
 import pytest
@@ -50,3 +49,22 @@ def test_a_functional_derivative_of_the_frequencies_is_refused():
         torch.func.jvp(lambda x: sage_rotary(Q, K, pos, x)[0].float(), (f,), (torch.ones_like(f),))
     with pytest.raises(NotImplementedError):
         torch.func.grad(lambda x: sage_rotary(Q, K, pos, x)[0].float().sum())(f)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", [0, 1])
+def test_a_tangent_of_a_gradient_is_refused(which):
+    Q, K, pos, f = (t.cuda() for t in _inputs())
+    Q.requires_grad_(), K.requires_grad_()
+    out = sage_rotary(Q, K, pos, f)
+    plain = [torch.ones_like(t) for t in out]
+    want = torch.autograd.grad(out, [Q, K], plain, retain_graph=True)
+    with fwAD.dual_level():
+        grads = list(plain)
+        grads[which] = fwAD.make_dual(plain[which], torch.ones_like(plain[which]))
+        with pytest.raises(NotImplementedError, match="forward-mode"):
+            torch.autograd.grad(out, [Q, K], grads, retain_graph=True)
+    # the graph still serves a gradient without one
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, [Q, K], plain, retain_graph=True), want))
+    with pytest.raises(NotImplementedError, match="vmap"):
+        torch.autograd.grad(out, [Q, K], [g.expand(2, *g.shape).contiguous() for g in plain], is_grads_batched=True)
