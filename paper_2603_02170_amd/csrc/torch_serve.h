@@ -356,8 +356,9 @@ int64_t rotary_heads(const Tensor& t, bool token_major) { return t.size(t.dim() 
 // Turned Q and K (either may be undefined) as new dense tensors; no autograd.
 int rotary_launch(const RotaryCall& c, const Tensor& Q, const Tensor& K, bool inverse, Tensor* Qo, Tensor* Ko) {
   const bool both = Q.defined() && K.defined();
-  const Tensor x = rows_fit(Q.defined() ? Q : K) ? (Q.defined() ? Q : K) : (Q.defined() ? Q : K).contiguous();
-  const Tensor z = both ? (rows_fit(K) ? K : K.contiguous()) : Tensor();
+  // (a copy, not contiguous(): a view of a larger buffer may be dense and begin off 16 bytes)
+  const auto fitting = [](const Tensor& t) { return rows_fit(t) ? t : t.clone(at::MemoryFormat::Contiguous); };
+  const Tensor x = fitting(Q.defined() ? Q : K), z = both ? fitting(K) : Tensor();
   Tensor y = at::empty(x.sizes(), x.options()), w;
   if (both) w = at::empty(z.sizes(), z.options());
   sagebwd_rotary_params p;
