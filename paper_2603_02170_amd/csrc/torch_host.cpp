@@ -342,7 +342,7 @@ struct SageAttentionBackward : torch::autograd::Node {
 // A tensor whose data alone is not what the caller asked about: a dual tensor of forward-mode AD (its tangent would be
 // dropped, which reads as a zero derivative), or one wrapped by a torch.func transform.
 bool is_transformed(const Tensor& t) {
-  constexpr c10::DispatchKeySet wrappers({c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::BatchedNestedTensor,
+  constexpr c10::DispatchKeySet wrappers({c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::Batched, c10::DispatchKey::BatchedNestedTensor,
                                           c10::DispatchKey::FuncTorchGradWrapper});
   return torch::autograd::isFwGradDefined(t) || t.key_set().has_any(wrappers);
 }
