@@ -301,6 +301,18 @@ PyObject* py_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   throw err;
 }
 
+// A tensor whose data alone is not what the caller asked about: a dual tensor of forward-mode AD (its tangent would be
+// dropped, which reads as a zero derivative), or one wrapped by a torch.func transform.
+bool is_transformed(const Tensor& t) {
+  constexpr c10::DispatchKeySet wrappers({c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::Batched, c10::DispatchKey::BatchedNestedTensor,
+                                          c10::DispatchKey::FuncTorchGradWrapper});
+  return torch::autograd::isFwGradDefined(t) || t.key_set().has_any(wrappers);
+}
+
+void refuse_transformed(const char* what) {
+  PyErr_Format(PyExc_NotImplementedError, "%s has no forward-mode derivative and no rule for torch.func transforms (vmap, grad, jvp, ...)", what);
+}
+
 struct SageAttentionBackward : torch::autograd::Node {
   torch::autograd::SavedVariable Q, K, V, O, L;
   Params p;
@@ -314,6 +326,7 @@ struct SageAttentionBackward : torch::autograd::Node {
   torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
     std::lock_guard<std::mutex> lock(mutex_);
     at::NoGradGuard no_grad;
+    if (grads[0].defined() && is_transformed(grads[0])) throw_python([] { refuse_transformed("sage_attention"); });
     const Tensor q = Q.unpack(), k = K.unpack(), v = V.unpack(), o = O.unpack(shared_from_this()), l = L.unpack();
     Tensor dO = grads[0].defined() ? grads[0].contiguous() : at::zeros_like(o);
     if (!fits(dO, at::kBFloat16, q.sizes()))
@@ -339,14 +352,6 @@ struct SageAttentionBackward : torch::autograd::Node {
   }
 };
 
-// A tensor whose data alone is not what the caller asked about: a dual tensor of forward-mode AD (its tangent would be
-// dropped, which reads as a zero derivative), or one wrapped by a torch.func transform.
-bool is_transformed(const Tensor& t) {
-  constexpr c10::DispatchKeySet wrappers({c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::Batched, c10::DispatchKey::BatchedNestedTensor,
-                                          c10::DispatchKey::FuncTorchGradWrapper});
-  return torch::autograd::isFwGradDefined(t) || t.key_set().has_any(wrappers);
-}
-
 // attention(Q, K, V, causal, k_smooth, q_smooth, sm_scale, token_major, share_quantized) -> (O, LSE)
 PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -357,8 +362,7 @@ PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       return nullptr;
     }
     if (is_transformed(THPVariable_Unpack(a[k]))) {
-      PyErr_SetString(PyExc_NotImplementedError,
-                      "sage_attention has no forward-mode derivative and no rule for torch.func transforms (vmap, grad, jvp, ...)");
+      refuse_transformed("sage_attention");
       return nullptr;
     }
   }

@@ -394,11 +394,6 @@ int rotary_launch(const RotaryCall& c, const Tensor& Q, const Tensor& K, bool in
 
 int rotary_apply(const RotaryCall& c, const Tensor& Q, const Tensor& K, bool inverse, Tensor* Qo, Tensor* Ko);
 
-void refuse_transformed() {
-  PyErr_SetString(PyExc_NotImplementedError,
-                  "sage_rotary has no forward-mode derivative and no rule for torch.func transforms (vmap, grad, jvp, ...)");
-}
-
 // The turn is linear: its gradient is the turn by the negative angles, and that of a gradient again the turn.
 struct SageRotaryBackward : torch::autograd::Node {
   torch::autograd::SavedVariable positions, inv_freq;
@@ -419,7 +414,7 @@ struct SageRotaryBackward : torch::autograd::Node {
     const Tensor dQ = grads[0], dK = grads.size() > 1 ? grads[1] : Tensor();
     if (!dQ.defined() && !dK.defined()) return out;
     if ((dQ.defined() && is_transformed(dQ)) || (dK.defined() && is_transformed(dK)))       // (double backward has a rule, a tangent of the gradient none)
-      throw_python([] { refuse_transformed(); });
+      throw_python([] { refuse_transformed("sage_rotary"); });
     Tensor q, k;
     const c10::DeviceGuard guard(c.positions.device());
     const int rc = rotary_apply(c, dQ, dK, !inverse, &q, &k);
@@ -466,7 +461,7 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   for (int k = 0; k < 4; k++) {       // (the positions and frequencies too: their other checks come later)
     if (THPVariable_Check(a[k]) && is_transformed(THPVariable_Unpack(a[k]))) {
-      refuse_transformed();
+      refuse_transformed("sage_rotary");
       return nullptr;
     }
   }
