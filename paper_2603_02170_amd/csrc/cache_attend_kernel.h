@@ -14,6 +14,7 @@
 #pragma once
 
 #include "cache_kernels.h"
+#include "cache_shares.h"
 
 namespace sage {
 
@@ -42,10 +43,7 @@ struct AttendArgs {
 };
 
 constexpr int kUnit = 128;          // tokens that a workgroup of four waves takes at a time
-// What an item costs beside its units, in units: its queries, the joining of its waves, its stores.  (Without it a workgroup with many
-// short items ends last: 64 ragged requests 62.7 us, with 1, 2, 3: 58.0, 56.6, 54.0; 32 equal ones of 4 drafted tokens, whose items
-// came out whole by chance, 48.2 and 52.6, 49.4, 51.7.)
-constexpr int kItemCost = 2;
+__device__ __forceinline__ int attend_cut(int offset) { return cut_at<kItemCost>(offset); }
 
 struct AttendRequest {
   int begin, n, rows, len;          // first row, new tokens, query rows computed of each head, keys
@@ -72,27 +70,6 @@ __device__ __forceinline__ int attend_units(const AttendArgs& a, int r) {
   return q.rows == 0 ? 0 : max(1, (attend_visible(a, q, 0, q.rows) + kUnit - 1) / kUnit);     // (rows without a key are an item too: zeros)
 }
 
-// Items are (request, key/value head), request after request, of attend_units units each and kItemCost in front of them; those are dealt to
-// the workgroups in order, total / n each and one more to the first total % n.  (The host bounds the total by 2^30.)  A border inside
-// an item's first kItemCost (or before it) cuts nothing off: attend_cut.
-__device__ __forceinline__ int attend_cut(int offset) { return max(0, offset - kItemCost); }
-struct AttendShares {
-  int each, more, n;
-  __device__ __forceinline__ AttendShares() {}
-  __device__ __forceinline__ AttendShares(int total, int workgroups) {
-    n = min(workgroups, total);
-    each = n > 0 ? total / n : 0;
-    more = total - each * n;
-  }
-  __device__ __forceinline__ int begin(int w) const { return each * w + min(w, more); }
-  // the workgroup that has a unit
-  __device__ __forceinline__ int owner(int unit) const {
-    const int big = (each + 1) * more;
-    return unit < big ? unit / (each + 1) : more + (unit - big) / each;
-  }
-};
-// (at most 512 parts, and 256 rows)
-__device__ __forceinline__ int4 join_word(int parts, int rows, int begin, int head, int row0) { return int4{parts | rows << 16, begin, head, row0}; }
 __device__ __forceinline__ float wave_max_f32(float v) {
   for (int k = 1; k < 64; k <<= 1) v = fmaxf(v, __shfl_xor(v, k));
   return v;
@@ -129,7 +106,8 @@ __device__ __forceinline__ float high_bf16(int w) { return __uint_as_float((unsi
 // copy_16 and copy_4 of a ring whose reads are counted by hand.  Behind the builtin the compiler lets every read of LDS wait for every copy in
 // flight, as it cannot tell a ring's slots apart, so that a ring is one tile deep; of this it sees no access, only that memory changes: what
 // is read has to have been waited for (vmcnt_only), and its own waits for loads come out early at worst.  (The copies have no register for a
-// result; a kernel with these has nothing else that uses m0.  Wait states: of m0, and of a base that a vector instruction wrote.)
+// result; m0 is reserved to the compiler, which does not honour a clobber of it: nothing else of a kernel with these may use it, and the tests look.  Wait
+// states: of m0, and of a base that a vector instruction wrote.)
 template <int BYTES>
 __device__ __forceinline__ void ring_copy(gbytes_t base, unsigned lane_offset, const void* lds_base) {
   const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lptr_t)lds_base);
@@ -515,8 +493,8 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
     cursor.end = shares.begin(w + 1);
   }
   if (!cursor.more(a)) return;
-  if (tid == 0 && cursor.j > 0 && attend_cut(shares.begin(w - 1) - cursor.x) == 0)      // the first border in this item
-    a.joins[w] = join_word(shares.owner(cursor.x + __builtin_amdgcn_readlane(cursor.units, 0) + kItemCost - 1) - w + 2,
+  if (tid == 0 && shares.first_border<kItemCost>(w, cursor.x, cursor.j))
+    a.joins[w] = join_word(shares.parts<kItemCost>(w, cursor.x, __builtin_amdgcn_readlane(cursor.units, 0)),
                            __builtin_amdgcn_readlane(cursor.n_rows, 0), __builtin_amdgcn_readlane(cursor.begin, 0), cursor.head, 0);
 
   AttendRows<D, GROUP> rows[NQ];

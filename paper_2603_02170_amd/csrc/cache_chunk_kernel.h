@@ -13,7 +13,6 @@
 namespace sage {
 
 constexpr int kChunkRows = 256, kChunkUnit = 64;
-constexpr int kChunkCost = 6;        // what an item costs beside its units, in units
 
 // 64 tokens on their way from the pages to bf16 fragments: waves 0 to 3 have K's, the others V's.
 template <int D, int GROUP>
@@ -124,9 +123,6 @@ struct ChunkTile {
 
 // Line of what is dealt out: request, then head, then row tile of 256, each its units + a cost of its own; or (not split) one each,
 // request, then row tile from the last, which sees most, then head.
-// The row tile at a place of a head's line: the last ones see most, so light and heavy take turns and a share of average length cuts every
-// second item instead of each.
-__device__ __forceinline__ int chunk_tile_at(int place, int tiles) { return place & 1 ? tiles - 1 - (place >> 1) : place >> 1; }
 // Tiles of 64 tokens that a head of the request has for the rows to see.
 __device__ __forceinline__ int chunk_key_tiles(const AttendRequest& q) { return q.rows == 0 ? 0 : max(1, (q.len + kChunkUnit - 1) / kChunkUnit); }
 
@@ -141,7 +137,7 @@ struct ChunkWalk {
   static __device__ __forceinline__ int chunk_units(const AttendArgs& a, const AttendRequest& q, int tile) {
     return max(1, (attend_visible(a, q, tile * ROWS, ROWS) + UNIT - 1) / UNIT);
   }
-  static __device__ __forceinline__ int chunk_cut(int offset) { return max(0, offset - COST); }
+  static __device__ __forceinline__ int chunk_cut(int offset) { return cut_at<COST>(offset); }
   // of a request and head
   static __device__ __forceinline__ int chunk_weight(const AttendArgs& a, const AttendRequest& q) {
     const int tiles = chunk_tiles(q.rows);
@@ -230,8 +226,8 @@ struct ChunkWalk {
   }
   // Units j0 .. of the item that are this workgroup's; leaves word for the joining launch at the first border inside it.
   __device__ __forceinline__ int last_unit(const AttendArgs& a, int units) const {
-    if (j0 > 0 && chunk_cut(shares.begin(w - 1) - x) == 0 && threadIdx.x == 0)
-      a.joins[w] = join_word(shares.owner(x + units + COST - 1) - w + 2, min(rq.rows - tile * ROWS, ROWS), rq.begin, head,
+    if (shares.template first_border<COST>(w, x, j0) && threadIdx.x == 0)
+      a.joins[w] = join_word(shares.template parts<COST>(w, x, units), min(rq.rows - tile * ROWS, ROWS), rq.begin, head,
                              tile * ROWS);
     return a.split ? min(units, chunk_cut(end - x)) : units;
   }
@@ -474,10 +470,6 @@ __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
 // are unpacked while slower waves still multiply.  Unpacking is what bounds it: about 1300 vector instructions for 64 tokens of 128 channels.
 // (32 requests of 4096 tokens, 8 heads, 64 rows: 123 -> 87 us, 128 rows 126 -> 107; at d = 64 102 -> 73, 119 -> 91.  With a branch round each tile
 // behind the last token, which a request's last unit may have, the tiles are unpacked one after the other: 108.)
-template <int RG>
-struct SpanShape {
-  static constexpr int KG = 8 / RG, ROWS = 32 * RG, UNIT = 64 * KG, COST = KG == 4 ? 2 : 3;
-};
 template <int D, int GROUP, int RG>
 __global__ __launch_bounds__(512, 2) void cache_span_kernel(AttendArgs a) {
   typedef ChunkTile<D, GROUP> Tile;
