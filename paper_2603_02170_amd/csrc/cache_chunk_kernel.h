@@ -123,6 +123,7 @@ struct ChunkTile {
 
 // Line of what is dealt out: request, then head, then row tile of 256, each its units + a cost of its own; or (not split) one each,
 // request, then row tile from the last, which sees most, then head.
+
 // Tiles of 64 tokens that a head of the request has for the rows to see.
 __device__ __forceinline__ int chunk_key_tiles(const AttendRequest& q) { return q.rows == 0 ? 0 : max(1, (q.len + kChunkUnit - 1) / kChunkUnit); }
 
