@@ -501,39 +501,53 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
 #pragma unroll
   for (int q = 0; q < NQ; q++) rows[q].place(a, 16 * q);
   AttendPiece piece = cursor.next(a);
-  int first, count;           // the wave's tiles: `count`, every 128 tokens from `first`
-  int pages;                  // a lane has the page of one of the wave's next 64 tiles: a tile's address then waits for no load
-  unsigned exists;            // of the tiles in the ring
+  // The wave's tiles: `count`, every 128 tokens from `first`.  Those of pages that do not exist are passed over where tiles are chosen.  (A branch
+  // round a tile's arithmetic has the sums in other registers behind it, 48.4 us for 64 ragged requests in place of 47.5; their arithmetic
+  // under a mask takes as long as that of any other: 64 requests of 8192 tokens of which an eighth is left 94, so 21.)
+  int first, count;
+  int pages, window;          // a lane has the page of one of 64 tiles, from `window` on: a tile's address then waits for no load
+  uint64_t left;              // those of them that exist and are not on their way yet
+  int on_way, to, t0[kStages] = {};      // tiles on their way into the ring, where the next one goes, their first tokens
   const auto pages_from = [&](int k) {
     return a.table[(size_t)piece.r * a.columns + (min(first + (k + lane) * kUnit, max(piece.visible - 1, 0)) >> a.g.page_shift)];
+  };
+  const auto take_pages = [&] {
+    arrived(pages);
+    left = __ballot(window + lane < count && (unsigned)pages < (unsigned)a.g.pages);
   };
   const auto look = [&] {      // loads what the piece's copies wait for, and its queries
     first = piece.j0 * kUnit + wave * 32;
     count = max(0, min(piece.j1 - piece.j0, (piece.visible - first + kUnit - 1) / kUnit));
+    window = 0;
     pages = pages_from(0);
 #pragma unroll
     for (int q = 0; q < NQ; q++) rows[q].fetch(a, piece);
   };
-  const auto fetch = [&](int k) {
-    if (k % 64 == 0 && k != 0) {
-      pages = pages_from(k);
-      arrived(pages);
+  const auto fetch = [&] {      // the next tile's copies, if there is one
+    while (left == 0) {
+      window += 64;
+      if (window >= count) return;
+      pages = pages_from(window);
+      take_pages();
     }
-    const int entry = __builtin_amdgcn_readlane(pages, k % 64);
-    const bool ok = (unsigned)entry < (unsigned)a.g.pages;
-    const int at = k % kStages;
-    exists = ok ? exists | 1u << at : exists & ~(1u << at);
-    const unsigned char* p = a.pool + (size_t)(ok ? entry : 0) * a.g.page_bytes() + (size_t)(piece.head * a.g.head_bytes());
-    Tile::fetch(a.g, p, (first + k * kUnit) & (a.g.page() - 1), ring + at * Tile::SLOT);
+    const int i = __builtin_ctzll(left), k = window + i, entry = __builtin_amdgcn_readlane(pages, i);
+    left &= left - 1;
+    const unsigned char* p = a.pool + (size_t)entry * a.g.page_bytes() + (size_t)(piece.head * a.g.head_bytes());
+    Tile::fetch(a.g, p, (first + k * kUnit) & (a.g.page() - 1), ring + to * Tile::SLOT);
+    to = to == kStages - 1 ? 0 : to + 1;
+#pragma unroll
+    for (int q = 0; q < kStages; q++) t0[q] = q == on_way ? first + k * kUnit : t0[q];
+    on_way++;
   };
   const auto start = [&] {
-    arrived(pages);
+    take_pages();
 #pragma unroll
     for (int q = 0; q < NQ; q++)
 #pragma unroll
       for (int j = 0; j < D / 32; j++) arrived(rows[q].q[j]);
-    exists = 0;
-    for (int k = 0; k < kStages - 1 && k < count; k++) fetch(k);
+    on_way = to = 0;
+#pragma unroll 1
+    for (int k = 0; k < kStages - 1; k++) fetch();       // (one copy of the code: of 4 short requests it is 3 % of the call)
   };
   look();
   start();
@@ -542,22 +556,20 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
     const int all_see = a.causal ? piece.first_sees : piece.len;       // keys that every row sees
 #pragma unroll
     for (int q = 0; q < NQ; q++) rows[q].begin();
-    int slot = 0;
-    for (int k = 0; k < count; k++) {
+    for (int slot = 0; on_way > 0; slot = slot == kStages - 1 ? 0 : slot + 1) {
       compiler_fence();
-      if (k + kStages - 1 < count) fetch(k + kStages - 1);
+      fetch();
       compiler_fence();
-      const int behind = min(count - 1 - k, kStages - 1);                  // tiles on their way behind this one
-      if (behind >= 2) __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * Tile::COPIES));
-      else if (behind == 1) __builtin_amdgcn_s_waitcnt(vmcnt_only(Tile::COPIES));
+      if (on_way >= 3) __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * Tile::COPIES));
+      else if (on_way == 2) __builtin_amdgcn_s_waitcnt(vmcnt_only(Tile::COPIES));
       else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
       compiler_fence();
-      // (a tile of a page that does not exist is one behind all keys: no branch, which would have the sums in other registers behind it)
       Tile tile;
       tile.take(ring + slot * Tile::SLOT);
-      const int t0 = (exists >> slot & 1) != 0 ? first + k * kUnit : 1 << 30;
-      attend_tile<D, GROUP, NQ>(rows, tile, t0, t0 + 32 > all_see, a.scale_log2, un);
-      slot = slot == kStages - 1 ? 0 : slot + 1;
+      attend_tile<D, GROUP, NQ>(rows, tile, t0[0], t0[0] + 32 > all_see, a.scale_log2, un);
+      on_way--;
+#pragma unroll
+      for (int q = 1; q < kStages; q++) t0[q - 1] = t0[q];
     }
     // Join the waves; the next piece's loads and first copies are on their way meanwhile.
     const AttendPiece done = piece;
