@@ -29,10 +29,12 @@
  *   reads as NaN.
  * 5 bits of a scale times the 3 of a code fit the 8 of a bf16 number: what the cache holds is bf16 exactly, and no
  * kernel rounds it again.
- * Means: the token means of K (as sagebwd_export_stats gives them for a prompt) move K's channel offsets out of the
- * codes; the softmax does not see them (paper Sec. 3 "Q and K Smoothing"), so the attention needs them for nothing and
- * its LSE is the log-sum-exp of the smoothed logits, as sagebwd_fwd's is.  V's mean is added back to O, the
- * probabilities of a row summing to 1.  Both are float32 [H, d], or NULL.
+ * Means: token means of K move its channel offsets out of the codes; the softmax does not see them (paper Sec. 3 "Q and K
+ * Smoothing"), so the attention needs them for nothing and its LSE is the log-sum-exp of the smoothed logits, as
+ * sagebwd_fwd's is.  V's mean is added back to O, the probabilities of a row summing to 1.  Both are float32 [H, d], or
+ * NULL, and one for all tokens and requests of a call: a model's, measured once, with which the whole pool is filled.  (All
+ * keys that a row sees need the same mean, whichever it is: means that differ between requests, as sagebwd_export_stats
+ * gives them for one prompt, take an append for each request; V's take an attention for each, too.)
  *
  * Page numbers: a request's pages stand in its row of the block table, int32 [R, columns].  An entry outside
  * 0 .. pages - 1 stands for a page that does not exist: its tokens are not attended to.
@@ -63,7 +65,8 @@ int sagebwd_cache_page_bytes(const sagebwd_cache_params* params, size_t* bytes);
  * It needs need_r = ceil((held + added) / page) - ceil(held / page) new pages and is granted them if held, added >= 0,
  * held + added <= columns * page, its tokens are among the first `rows` of the step, and need_r is 0 or the sum of the
  * needs of the requests up to it is at most free_count.  The k-th page granted (requests in order, a request's pages in
- * order) is free_pages[free_count - 1 - k].
+ * order) is free_pages[free_count - 1 - k].  (Need that is not met counts all the same: behind a request for which there are not enough
+ * pages none is granted a new one, so that a long request is not passed by short ones for ever.)
  *   block_table   int32 [R, columns], in and out: the granted pages go behind those that the request has
  *   free_pages    int32 [capacity], a stack; free_count int32 [1] (read as at most capacity)
  *   slots         int64 [rows]: page * (page number) + offset of every new token, requests in order; -1 for tokens of a
@@ -97,7 +100,7 @@ int sagebwd_cache_trim(const int32_t* keep, int32_t* lengths, int32_t* block_tab
  * New keys and values into the cache, and what it holds out of it.  K, V: bf16 [T, H, d] with strides in elements
  * (multiples of 8; channels are adjacent; 16-byte aligned); slots int64 [T].  A slot outside the pool is skipped by
  * append and read as zeros.  Append wants every slot at most once (of tokens with one slot, any mixture stays).
- * read writes dense bf16 [T, H, d]: the values exactly, or with means their sum rounded once to bf16.
+ * read writes dense bf16 [T, H, d]: the values exactly, or with means value + mean in FP32, rounded to bf16.
  */
 int sagebwd_cache_append(const void* K, const void* V, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
                          int64_t v_head_stride, const int64_t* slots, int32_t T, const float* k_mean, const float* v_mean,
@@ -107,11 +110,13 @@ int sagebwd_cache_read(const int64_t* slots, int32_t T, const float* k_mean, con
 
 typedef struct sagebwd_cache_call {
   int32_t R;          /* requests */
-  int32_t T;          /* rows of Q and O (at least cu[R]; those behind it are left as they are) */
+  int32_t T;          /* rows of Q and O (at least cu[R]; those behind it are left as they are).  From R * max_new on, with max_new * Hq / H
+                         more than 32, the call takes every request to bring max_new tokens: shorter ones are slower than need be */
   int32_t Hq;         /* query heads: a multiple of H, at most 64 H; head h reads key/value head h / (Hq / H) */
   int32_t columns;    /* of the block table */
   int32_t max_new;    /* at least every request's new tokens (1: a decoding step); further tokens are not computed */
-  int32_t max_length; /* at least every length, or 0: columns * page; a longer length is read as this */
+  int32_t max_length; /* at least every length, or 0: columns * page; a longer length is read as this.  Where the table is wider than the
+                         requests are long it saves workspace, and a short batch the joining of parts */
   int32_t causal;     /* 1: new token i of n of a request of length L sees keys 0 .. i + L - n; 0: all L */
   float sm_scale;     /* 0 selects 1 / sqrt(d) */
   int64_t q_token_stride, q_head_stride; /* elements, multiples of 8; channels are adjacent */
@@ -127,9 +132,10 @@ typedef struct sagebwd_cache_call {
  * the matrix instruction.  A row that sees no key (a request of length 0; with the mask the first rows of one shorter
  * than its new tokens; pages that do not exist) gives O = 0, LSE = -infinity.  What stands in the cache behind a
  * request's length reaches nothing.
- * Requests of up to 32 query rows (new tokens x Hq / H) go to a kernel for few rows, the others to one for many; a call that may hold both kinds
- * (max_new tokens are more than 32 rows, T is less than R * max_new, Hq / H at most 32) launches both.  Where a call has few items for
- * the machine their keys are divided over it and the parts joined by a further launch; from 2048 rows a request on, keys and values are
+ * Where max_new tokens are up to 32 query rows (new tokens x Hq / H) all requests go to a kernel for few rows, else to one for many; but where
+ * T is less than R * max_new and Hq / H at most 32 the call launches both, and requests of up to 16 rows (32, where Hq / H is more than 16) go
+ * to the former.  A tile of tokens on a page that does not exist is passed over by the kernel for few rows and masked by the others.
+ * Where a call has few items for the machine their keys are divided over it and the parts joined by a further launch; from 2048 rows a request on, keys and values are
  * unpacked to bf16 in the workspace first (256 d bytes for 64 tokens and head; at most 4 GiB, else each tile unpacks its own).  How
  * work is divided depends on all requests of the call, so that O agrees between calls of different batches to its rounding, and bit
  * for bit between equal calls.

@@ -64,7 +64,10 @@ def alloc_cache(p: CacheParams, pages: int, device="cuda"):
 def sagebwd_cache_plan(held, added, block_table, free_pages, free_count, p: CacheParams, rows: int, out=None) -> CachePlan:
     """Pages, slots and positions of a step's new tokens (int32 device tensors; `rows` >= all new tokens, or the requests behind
     are not granted; at most 2^30).  block_table [R, columns] gets the granted pages; everything else is in the plan, whose tensors `out` (a
-    CachePlan) may bring: `out.lengths` may be `held` and `out.free_left` may be `free_count`."""
+    CachePlan) may bring: `out.lengths` may be `held` and `out.free_left` may be `free_count`.
+
+    Requests are served in order: behind one for which there are not enough pages none that needs a page is granted (trim gives pages
+    back, and the next plan may grant them).  A request that is not granted keeps its length; its rows have slot -1."""
     return CachePlan._make(binding._host().cache_plan(held, added, block_table, free_pages, free_count, p.page, rows, out))
 
 
@@ -74,12 +77,14 @@ def sagebwd_cache_trim(keep, lengths, block_table, free_pages, free_count, p: Ca
 
 
 def sagebwd_cache_append(K, V, slots, cache, p: CacheParams, k_mean=None, v_mean=None) -> None:
-    """New keys and values into the cache; k_mean, v_mean: float32 [H, d], taken off before they are quantised."""
+    """New keys and values into the cache; k_mean, v_mean: float32 [H, d], taken off before they are quantised (one for all tokens: a model's,
+    with which the whole pool is filled)."""
     binding._host().cache_append(K, V, slots, cache, p.H, p.d, p.page, p.group, k_mean, v_mean)
 
 
 def sagebwd_cache_read(slots, cache, p: CacheParams, k_mean=None, v_mean=None, K=None, V=None):
-    """(K, V) bf16 [tokens, H, d]: the values that the cache holds at `slots` (zeros for -1), exactly; with means, their sums rounded."""
+    """(K, V) bf16 [tokens, H, d]: the values that the cache holds at `slots` (zeros for -1), exactly; with means, value + mean in float32,
+    rounded."""
     return binding._host().cache_read(slots, cache, p.H, p.d, p.page, p.group, k_mean, v_mean, K, V)
 
 
@@ -92,7 +97,8 @@ def sagebwd_cache_attention(Q, cache, block_table, lengths, cu, p: CacheParams, 
                             v_mean=None, max_length: int = 0, workspace=None, O=None, LSE=None):
     """O bf16 [tokens, query heads, d] and LSE float32 [query heads, tokens] of every request's new tokens over its cache.
 
-    `max_new` and `max_length` (0: whatever the table holds) bound the requests' new tokens and lengths on the host.  Rows behind the
-    last request are left as they are in O and LSE.  A row that sees no key has O = 0 and LSE = -infinity."""
+    `max_new` and `max_length` (0: whatever the table holds) bound the requests' new tokens and lengths on the host: how the call is laid out and
+    its workspace go by them, so that a table wider than the requests are long wants a `max_length`.  Rows behind the last request are left as
+    they are in O and LSE.  A row that sees no key has O = 0 and LSE = -infinity."""
     return binding._host().cache_attention(Q, cache, block_table, lengths, cu, p.H, p.d, p.page, p.group, max_new, causal, sm_scale, v_mean,
                                            max_length, workspace, O, LSE)
