@@ -257,7 +257,8 @@ int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block
       (capacity > 0 && free_pages == nullptr) || free_count == nullptr || cu_new == nullptr || free_left == nullptr ||
       (rows > 0 && (slots == nullptr || positions == nullptr)))
     return SAGEBWD_INVALID_ARG;
-  if (page_shift_of(page) < 0 || (int64_t)columns * page > INT32_MAX / 2 || R > 1 << 20 || (int64_t)R * columns > kMostEntries || rows > kMostRows) return SAGEBWD_UNSUPPORTED_SHAPE;
+  if (page_shift_of(page) < 0 || (int64_t)columns * page > INT32_MAX / 2 || R > 1 << 20 || (int64_t)R * columns > kMostEntries || rows > kMostRows)
+    return SAGEBWD_UNSUPPORTED_SHAPE;
   const PlanArgs a{held, added, free_pages, free_count, block_table, slots, positions, cu_new, lengths, granted, free_left,
                    R, columns, page_shift_of(page), capacity, rows};
   hipStream_t st = (hipStream_t)stream;
