@@ -1,6 +1,6 @@
 /*
  * sagebwd_serve.h -- C ABI of the operators around the attention of sagebwd.h that training and serving a model
- * need beside it, on one MI355X (gfx950): rotary positions, and a paged key/value cache held in 4 bits with its
+ * need beside it, on one MI355X (gfx950): rotary positions, and a paged key/value cache held in 4 or in 8 bits with its
  * bookkeeping and the attention that reads it.
  *
  * The conventions of sagebwd.h hold: device pointers of the caller, nothing allocated, no memset, no host
@@ -12,7 +12,7 @@
  * The order of a step of serving:  sagebwd_cache_plan (lengths -> pages, slots, positions), sagebwd_rotary (Q, K),
  * sagebwd_cache_append (K, V -> cache), sagebwd_cache_attention (Q, cache -> O).  The four repeat themselves bit for bit.
  *
- * ---- the cache -----------------------------------------------------------------------------------------------
+ * ---- the cache, held in 4 bits (block = 0) -----------------------------------------------------------------------
  * A pool of `pages` pages, bytes [pages, H, page * (d + 4 d / group)], 16-byte aligned.  A page holds `page` tokens of
  * each of the H key/value heads; a head's part holds K's codes (page * d / 2 bytes), V's codes (the same), K's scales
  * and V's scales (page * d / group * 2 bytes each).  A value is (nibble - 8) * scale.
@@ -29,6 +29,24 @@
  *   reads as NaN.
  * 5 bits of a scale times the 3 of a code fit the 8 of a bf16 number: what the cache holds is bf16 exactly, and no
  * kernel rounds it again.
+ * ---- the cache, held in 8 bits (block = 32 or 64) ----------------------------------------------------------------
+ * A pool of `pages` pages, bytes [pages, H, 2 page d + max(16, page / 4)], 16-byte aligned: of a head K's codes (page * d bytes), V's
+ * codes (the same), and for every 32 tokens two floats, a_K and a_V (of a block of 64 tokens the two pairs are alike).  A value is
+ * code * (a / 127), codes -127 .. 127: one scale for `block` tokens of a head, as the INT8 attention has them (paper Sec. 3
+ * "Quantization").
+ *   K's codes    token t = 32 b + 8 o + 4 s + i, channel c = 64 j + 16 g + e: byte 32 d b + 2048 j + 1024 s + 256 g + 64 o + 16 i + e
+ *   V's codes    token t = 32 b + 8 o + i, channel c = 32 j + 16 h + m: byte 32 d b + 1024 j + 256 o + 16 m + 8 h + i
+ * Quantiser, per block of tokens and head, in FP32.  A call brings a run of tokens of a block; in front of its first one the block holds
+ * the tokens that came before (none where the first one is the block's first).
+ *   x = float(k) - mean;  a = max|x| over the run, and a_held where tokens are held;  code = rne(x * (127 / a));
+ *   where a > a_held the codes held become rne(code * (a_held / a)).
+ *   A block that comes whole has the codes of the method's own quantiser; one that comes token by token has its codes rounded once more
+ *   whenever a token is the largest so far (about ln(64 / i) times the i-th token's).
+ *   a < 2^-100: a = 0, codes 0.  a >= 2^127, or an infinity or a NaN: a = NaN, and the block reads as NaN from then on, until its first token is
+ *   stored again.
+ * Tokens dropped from a block's end (sagebwd_cache_trim) leave a_held as it was.
+ *
+ * ---- both --------------------------------------------------------------------------------------------------------
  * Means: token means of K move its channel offsets out of the codes; the softmax does not see them (paper Sec. 3 "Q and K
  * Smoothing"), so the attention needs them for nothing and its LSE is the log-sum-exp of the smoothed logits, as
  * sagebwd_fwd's is.  V's mean is added back to O, the probabilities of a row summing to 1.  Both are float32 [H, d], or
@@ -52,12 +70,12 @@ typedef struct sagebwd_cache_params {
   int32_t H;      /* key/value heads */
   int32_t d;      /* 64 or 128 */
   int32_t page;   /* tokens of a page: 32, 64, 128 or 256 */
-  int32_t group;  /* channels that share a scale: 32 or 64 */
+  int32_t group;  /* channels that share a scale: 32 or 64 (0 where `block` is not 0) */
   int32_t pages;  /* pages of the pool */
-  int32_t reserved; /* must be 0 */
+  int32_t block;  /* 0: held in 4 bits; 32 or 64: in 8 bits, tokens of a head that share a scale (at most a page; `group` is 0 then) */
 } sagebwd_cache_params;
 
-/* Bytes of one page of the pool (all heads): H * page * (d + 4 d / group).  (`pages` is not looked at.) */
+/* Bytes of one page of the pool (all heads).  (`pages` is not looked at.) */
 int sagebwd_cache_page_bytes(const sagebwd_cache_params* params, size_t* bytes);
 
 /*
@@ -100,7 +118,10 @@ int sagebwd_cache_trim(const int32_t* keep, int32_t* lengths, int32_t* block_tab
  * New keys and values into the cache, and what it holds out of it.  K, V: bf16 [T, H, d] with strides in elements
  * (multiples of 8; channels are adjacent; 16-byte aligned); slots int64 [T].  A slot outside the pool is skipped by
  * append and read as zeros.  Append wants every slot at most once (of tokens with one slot, any mixture stays).
- * read writes dense bf16 [T, H, d]: the values exactly, or with means value + mean in FP32, rounded to bf16.
+ * read writes dense bf16 [T, H, d]: the values exactly (held in 8 bits: rounded to bf16), or with means value + mean in FP32, rounded to bf16.
+ * Held in 8 bits, append wants the tokens of a block that it brings one after the other with slots that rise by one, as plan lays them out (of
+ * those that come in several pieces, or of which some are left out, the block may hold anything), and the slots in front of them in the
+ * block to be the tokens held.
  */
 int sagebwd_cache_append(const void* K, const void* V, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
                          int64_t v_head_stride, const int64_t* slots, int32_t T, const float* k_mean, const float* v_mean,
@@ -129,7 +150,7 @@ typedef struct sagebwd_cache_call {
  *               rising from 0 (read as within 0 .. T)
  *   O           bf16 [T, Hq, d] dense; LSE float32 [Hq, T], or NULL
  * Sums, softmax statistics and the joining of parts are FP32; the probabilities times V's scales are rounded to bf16 for
- * the matrix instruction.  A row that sees no key (a request of length 0; with the mask the first rows of one shorter
+ * the matrix instruction (codes, of 4 bits or of 8, are bf16 numbers).  A row that sees no key (a request of length 0; with the mask the first rows of one shorter
  * than its new tokens; pages that do not exist) gives O = 0, LSE = -infinity.  What stands in the cache behind a
  * request's length reaches nothing.
  * Where max_new tokens are up to 32 query rows (new tokens x Hq / H) all requests go to a kernel for few rows, else to one for many; but where

@@ -1,6 +1,6 @@
 """SageBwd hot path for MI355X (gfx950): fused INT8 attention forward and
 backward behind a C-ABI library, with a thin binding, and serving from a paged
-4-bit key/value cache (cache.py)."""
+key/value cache held in 4 or 8 bits (cache.py)."""
 from .binding import (  # noqa: F401
     SageParams,
     lib_path,

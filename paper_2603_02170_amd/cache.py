@@ -1,6 +1,6 @@
-"""Serving from a paged key/value cache held in 4 bits: what a decoding loop calls between the model's projections.
+"""Serving from a paged key/value cache held in 4 or in 8 bits: what a decoding loop calls between the model's projections.
 
-    p = CacheParams(H=8, d=128)                              # key/value heads, head dimension
+    p = CacheParams(H=8, d=128)                              # key/value heads, head dimension; block=64: 8 bits
     cache = alloc_cache(p, pages=4096)
     plan = sagebwd_cache_plan(held, added, block_table, free_pages, free_count, p, rows)   # pages, slots, positions
     Q, K = sage_rotary(Q, K, plan.positions, inv_freq)                                      # (autograd.py)
@@ -28,7 +28,7 @@ EXPORTS = ("sagebwd_cache_page_bytes", "sagebwd_cache_plan", "sagebwd_cache_trim
 
 class _CCacheParams(ctypes.Structure):
     _fields_ = [("H", ctypes.c_int32), ("d", ctypes.c_int32), ("page", ctypes.c_int32), ("group", ctypes.c_int32),
-                ("pages", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+                ("pages", ctypes.c_int32), ("block", ctypes.c_int32)]
 
 
 @dataclass
@@ -37,6 +37,7 @@ class CacheParams:
     d: int              # 64 or 128
     page: int = 64      # tokens of a page: 32, 64, 128 or 256
     group: int = 64     # channels that share a scale: 32 (4.5 bits a value) or 64 (4.25)
+    block: int = 0      # 0: held in 4 bits; 32 or 64: in 8, tokens of a head that share a scale (`group` is not looked at then)
 
 
 class CachePlan(NamedTuple):
@@ -51,7 +52,7 @@ class CachePlan(NamedTuple):
 def cache_page_bytes(p: CacheParams) -> int:
     """Bytes of a page over all heads."""
     n = ctypes.c_size_t(0)
-    cp = _CCacheParams(p.H, p.d, p.page, p.group, 1, 0)
+    cp = _CCacheParams(p.H, p.d, p.page, 0 if p.block else p.group, 1, p.block)
     binding._check(binding.load_library().sagebwd_cache_page_bytes(ctypes.byref(cp), ctypes.byref(n)), "sagebwd_cache_page_bytes")
     return int(n.value)
 
@@ -78,19 +79,20 @@ def sagebwd_cache_trim(keep, lengths, block_table, free_pages, free_count, p: Ca
 
 def sagebwd_cache_append(K, V, slots, cache, p: CacheParams, k_mean=None, v_mean=None) -> None:
     """New keys and values into the cache; k_mean, v_mean: float32 [H, d], taken off before they are quantised (one for all tokens: a model's,
-    with which the whole pool is filled)."""
-    binding._host().cache_append(K, V, slots, cache, p.H, p.d, p.page, p.group, k_mean, v_mean)
+    with which the whole pool is filled).  Held in 8 bits, a block's scale grows with its tokens, whose codes are then written again: the tokens
+    of a block that a call brings stand one after the other, their slots rising by one (as a plan has them)."""
+    binding._host().cache_append(K, V, slots, cache, p.H, p.d, p.page, p.group, p.block, k_mean, v_mean)
 
 
 def sagebwd_cache_read(slots, cache, p: CacheParams, k_mean=None, v_mean=None, K=None, V=None):
-    """(K, V) bf16 [tokens, H, d]: the values that the cache holds at `slots` (zeros for -1), exactly; with means, value + mean in float32,
-    rounded."""
-    return binding._host().cache_read(slots, cache, p.H, p.d, p.page, p.group, k_mean, v_mean, K, V)
+    """(K, V) bf16 [tokens, H, d]: the values that the cache holds at `slots` (zeros for -1), exactly (held in 8 bits: rounded); with means,
+    value + mean in float32, rounded."""
+    return binding._host().cache_read(slots, cache, p.H, p.d, p.page, p.group, p.block, k_mean, v_mean, K, V)
 
 
 def cache_workspace_bytes(p: CacheParams, R: int, T: int, Hq: int, columns: int, max_new: int, max_length: int = 0) -> int:
     """Bytes of workspace of `sagebwd_cache_attention` for R requests, T rows of Hq query heads and that many table columns."""
-    return binding._host().cache_workspace_bytes(p.H, p.d, p.page, p.group, R, T, Hq, columns, max_new, max_length)
+    return binding._host().cache_workspace_bytes(p.H, p.d, p.page, p.group, p.block, R, T, Hq, columns, max_new, max_length)
 
 
 def sagebwd_cache_attention(Q, cache, block_table, lengths, cu, p: CacheParams, max_new: int, causal: bool = True, sm_scale: float = 0.0,
@@ -100,5 +102,5 @@ def sagebwd_cache_attention(Q, cache, block_table, lengths, cu, p: CacheParams, 
     `max_new` and `max_length` (0: whatever the table holds) bound the requests' new tokens and lengths on the host: how the call is laid out and
     its workspace go by them, so that a table wider than the requests are long wants a `max_length`.  Rows behind the last request are left as
     they are in O and LSE.  A row that sees no key has O = 0 and LSE = -infinity."""
-    return binding._host().cache_attention(Q, cache, block_table, lengths, cu, p.H, p.d, p.page, p.group, max_new, causal, sm_scale, v_mean,
+    return binding._host().cache_attention(Q, cache, block_table, lengths, cu, p.H, p.d, p.page, p.group, p.block, max_new, causal, sm_scale, v_mean,
                                            max_length, workspace, O, LSE)

@@ -1,0 +1,324 @@
+// Attention over the cache held in 8 bits (gfx950 only): what is its own beside cache_attend_kernel.h and cache_chunk_kernel.h.
+//
+//   S = q k^T,  k = a_k / 127 n_k;   O = sum_t p_t a_v,t / 127 n_v,t / sum_t p_t,   a: one number for a block of 32 or 64 tokens and head
+//
+// A code -127 .. 127 is a bf16 number, so the matrix instructions multiply the codes themselves and nothing is rounded but the probabilities: K's
+// scale goes with sm_scale into the exponents, V's into the probabilities before they become bf16.  A code takes one and a half vector
+// instructions (a byte to FP32, two of them to a word).
+//
+// Few rows: the codes lie in the page in the order of the operands of 16 x 16 x 32 products (tokens and tiles as in cache_attend_kernel.h),
+// 16 bytes a lane, so that a tile of 32 tokens comes straight to registers, the next one under it.
+#pragma once
+
+#include "cache8_kernels.h"
+#include "cache_chunk_kernel.h"
+
+namespace sage {
+
+// Eight codes to an operand.
+__device__ __forceinline__ v8bf codes_to_bf16(int w0, int w1) {
+  const auto f = [](int w, int i) { return (float)(signed char)(w >> 8 * i); };
+  return as_bf16(v4i{pack_bf16(f(w0, 0), f(w0, 1)), pack_bf16(f(w0, 2), f(w0, 3)), pack_bf16(f(w1, 0), f(w1, 1)), pack_bf16(f(w1, 2), f(w1, 3))});
+}
+
+// 32 tokens of a head.
+template <int D>
+struct ByteTile {
+  static constexpr int SLOT = 0;      // of a ring
+  v4i k[2][D / 64];       // token 8 (m / 4) + m % 4 (+ 4), channels 64 j + 16 g ..
+  v4i v[D / 32];          // octet g, channels 32 j + m and 16 more
+  float ka, va;           // largest magnitudes
+
+  // `p`: the head's part of a page, `at`: a token of it; not `any`: loads from where it is.
+  __device__ __forceinline__ void load(const CacheGeometry& geo, const unsigned char* p, int at, bool any) {
+    const int lane = any ? (threadIdx.x & 63) * 16 : 0;
+    const unsigned char *pk = p + at * D, *pv = pk + geo.page() * D;
+#pragma unroll
+    for (int j = 0; j < D / 64; j++)
+#pragma unroll
+      for (int b = 0; b < 2; b++) k[b][j] = *(const v4i*)(pk + (2 * j + b) * 1024 + lane);
+#pragma unroll
+    for (int j = 0; j < D / 32; j++) v[j] = *(const v4i*)(pv + j * 1024 + lane);
+    const float* a = (const float*)(p + Bytes8<D>::magnitudes(geo) + at / 4);
+    ka = a[0];
+    va = a[1];
+  }
+};
+
+template <int D>
+struct ByteRows : AttendRows<D, D> {
+  typedef AttendRows<D, D> Base;
+  // q[2 j + h]: channels 64 j + 16 g + 8 h ..
+  template <typename Piece>
+  __device__ __forceinline__ void fetch(const AttendArgs& a, const Piece& p) {
+    const int g = (threadIdx.x & 63) >> 4;
+    const bool exists = Base::row < p.n_rows;
+    const __bf16* x =
+        a.Q + (int64_t)(p.begin + (exists ? Base::token : 0)) * a.q_token + (int64_t)(p.head * a.G + (exists ? Base::head_of : 0)) * a.q_head + 16 * g;
+#pragma unroll
+    for (int j = 0; j < Base::NJ; j++) Base::q[j] = exists ? *(const v4i*)(x + 64 * (j / 2) + 8 * (j % 2)) : v4i{0, 0, 0, 0};
+    Base::sees = exists && a.causal ? min(p.len, p.first_sees + Base::token) : p.len;
+  }
+  __device__ __forceinline__ void begin() {
+#pragma unroll
+    for (int v = 0; v < Base::NV; v++) Base::o[v] = v4f{0.f, 0.f, 0.f, 0.f};
+    Base::m = -INFINITY;
+    Base::l = 0.f;
+  }
+};
+
+constexpr float kBy127 = 1.f / 127.f;
+
+template <int D_>
+struct ByteForm {
+  static constexpr int D = D_;
+  typedef ByteTile<D> Tile;
+  typedef ByteRows<D> Rows;
+  struct Unpacking {};
+  static constexpr bool RING = false;
+  static __device__ __forceinline__ const unsigned char* part(const AttendArgs& a, int entry, int head) {
+    return a.pool + ((size_t)entry * a.g.H + head) * Bytes8<D>::head_bytes(a.g);
+  }
+
+  // 32 tokens into NQ tiles of queries.  `masked`: some row does not see all of them.
+  template <int NQ>
+  static __device__ __forceinline__ void attend(Rows (&rows)[NQ], Tile& t, int t0, bool masked, float scale_log2, const Unpacking&) {
+    const int g = (threadIdx.x & 63) >> 4;
+    v4f s[NQ][2];
+#pragma unroll
+    for (int q = 0; q < NQ; q++) s[q][0] = s[q][1] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < 2; b++)
+#pragma unroll
+      for (int j = 0; j < D / 32; j++) {
+        const v8bf k = codes_to_bf16(t.k[b][j / 2][2 * (j % 2)], t.k[b][j / 2][2 * (j % 2) + 1]);
+#pragma unroll
+        for (int q = 0; q < NQ; q++) s[q][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, as_bf16(rows[q].q[j]), s[q][b], 0, 0, 0);
+      }
+    const float k_scale = t.ka * kBy127 * scale_log2, v_scale = t.va * kBy127;
+    v8bf pt[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; q++) {
+      Rows& R = rows[q];
+      const int behind = R.sees - t0 - 8 * g;      // tokens of the octet that the query sees
+      float x[8], c = k_scale;
+#pragma unroll
+      for (int i = 0; i < 8; i++) x[i] = s[q][i / 4][i % 4];
+      if (masked) {
+        asm volatile("");                          // (stays a branch)
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = i < behind ? x[i] * c : -INFINITY;      // (c may be 0)
+        c = 1.f;
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; i++) top = fmaxf(top, x[i]);
+      top *= c;
+      // (the reference need only be near the maximum)
+      if (__any(top > R.m + 8.f)) {
+        const float to = fmaxf(R.m, column_max(top));
+        const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(R.m - to);
+#pragma unroll
+        for (int v = 0; v < D / 16; v++) R.o[v] *= f;
+        R.l *= f;
+        R.m = to;
+      }
+      const float ref = R.m == -INFINITY ? 0.f : R.m;
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -ref));
+        R.l += x[i];
+        x[i] *= v_scale;
+      }
+      if (masked) {
+        asm volatile("");
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = i < behind ? x[i] : 0.f;                // (V's scale may be NaN)
+      }
+      pt[q] = as_bf16(v4i{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])});
+    }
+#pragma unroll
+    for (int v = 0; v < D / 16; v++) {
+      const v8bf w = codes_to_bf16(t.v[v / 2][2 * (v % 2)], t.v[v / 2][2 * (v % 2) + 1]);
+#pragma unroll
+      for (int q = 0; q < NQ; q++) rows[q].o[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, pt[q], rows[q].o[v], 0, 0, 0);
+    }
+  }
+};
+
+template <int D, int NQ>
+__global__ __launch_bounds__(256, 2) void cache8_attend_kernel(AttendArgs a) {
+  attend_items<ByteForm<D>, NQ>(a);
+}
+
+// ---- many rows ---------------------------------------------------------------------------------------------------------
+struct ByteKnown {
+  int exists[2];
+  float k[2], v[2];       // scales of the halves
+};
+
+// 64 tokens on their way from the pages to bf16 fragments of codes: waves 0 to 3 have K's, the others V's, 16 bytes at a time as they lie
+// in the page (one of which is two lanes' octets of channels, or of tokens).
+template <int D_>
+struct ByteChunk {
+  static constexpr int D = D_, FRAG = D / 16 * 1024, N = D / 64, NG = 0;
+  typedef ByteKnown Known;
+  v4i code[N];
+  float k, v;             // of the half with the same number as (u & 127) / 64
+  int valid;
+
+  __device__ __forceinline__ void load(const AttendArgs& a, int head, int from, int page0, int page1, int visible) {
+    const int tid = threadIdx.x, u = tid & 255;
+    const auto of = [&](int b) {
+      const int entry = __builtin_amdgcn_readfirstlane(b ? page1 : page0);
+      return a.pool + ((size_t)((unsigned)entry < (unsigned)a.g.pages ? entry : 0) * a.g.H + head) * Bytes8<D>::head_bytes(a.g);
+    };
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const int b = N == 2 ? i : u >> 7, at = (from + 32 * b) & (a.g.page() - 1);
+      const int q = N == 2 ? u : u & 127;
+      code[i] = *(const v4i*)(of(b) + (tid < 256 ? 0 : a.g.page() * D) + at * D + q * 16);
+    }
+    const int b = u >> 6 & 1, at = (from + 32 * b) & (a.g.page() - 1);
+    const float* s = (const float*)(of(b) + Bytes8<D>::magnitudes(a.g) + at / 4);
+    k = s[0];
+    v = s[1];
+    valid = (unsigned)(b ? page1 : page0) < (unsigned)a.g.pages;
+  }
+  __device__ __forceinline__ void store(char* K, char* V, Known& known, unsigned char*, int*, int) const {
+    const int tid = threadIdx.x, u = tid & 255;
+    if (tid < 128 && (tid & 63) == 0) {
+      known.exists[tid >> 6] = valid;
+      known.k[tid >> 6] = k * kBy127;
+      known.v[tid >> 6] = fabsf(v) < INFINITY ? v * kBy127 : __builtin_nanf("");      // (where nothing was stored any bits may be)
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const int b = N == 2 ? i : u >> 7, q = N == 2 ? u : u & 127;
+      const v8bf x = codes_to_bf16(code[i][0], code[i][1]), y = codes_to_bf16(code[i][2], code[i][3]);
+      if (tid < 256) {      // j = q / 128, s = q / 64 % 2, g = q / 16 % 4, m = q % 16: token 8 (m / 4) + 4 s + m % 4, channels 64 j + 16 g ..
+        const int m = q & 15, rho = 16 * (m >> 3) + 8 * (q >> 6 & 1) + 4 * (m >> 2 & 1) + (m & 3);
+        char* to = K + b * FRAG + ((4 * (q >> 7) + (q >> 4 & 3)) * 64 + rho) * 16;
+        *(v8bf*)to = x;
+        *(v8bf*)(to + 512) = y;
+      } else {              // j = q / 64, octet q / 16 % 4, channels 32 j + q % 16 and 16 more
+        const int o = 4 * b + (q >> 4 & 3);
+        char* to = V + ((q >> 6) * 4 + (o >> 1)) * 1024 + ((o & 1) * 32 + (q & 15)) * 16;
+        *(v8bf*)to = x;
+        *(v8bf*)(to + 256) = y;
+      }
+    }
+  }
+};
+
+template <int D>
+struct ByteChunkRows : ChunkRows<D> {
+  typedef ChunkRows<D> Base;
+  __device__ __forceinline__ void softmax(v16f (&s)[2], v8bf (&p)[4], int t0, const ByteKnown& known, float scale_log2) {
+    float c[2] = {known.k[0] * scale_log2, known.k[1] * scale_log2};
+    if (t0 + kChunkUnit > Base::all_see || known.exists[0] + known.exists[1] != 2) {
+      const int h = threadIdx.x >> 5 & 1;
+#pragma unroll
+      for (int b = 0; b < 2; b++) {
+        const int behind = known.exists[b] ? Base::sees - t0 - 32 * b - 8 * h : 0;
+#pragma unroll
+        for (int i = 0; i < 16; i++) s[b][i] = 16 * (i / 8) + i % 8 < behind ? s[b][i] * c[b] : -INFINITY;      // (c may be 0)
+        c[b] = 1.f;
+      }
+    }
+    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int b = 0; b < 2; b++) {
+#pragma unroll
+      for (int i = 0; i < 16; i++) top[b] = fmaxf(top[b], s[b][i]);
+      top[b] *= c[b];
+    }
+    if (__any(fmaxf(top[0], top[1]) > Base::m + 8.f)) {
+      const float to = fmaxf(Base::m, half_swap_max_f32(fmaxf(top[0], top[1])));
+      const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(Base::m - to);
+#pragma unroll
+      for (int i = 0; i < Base::NC; i++) Base::o[i] *= f;
+      Base::l *= f;
+      Base::m = to;
+    }
+    const float ref = Base::m == -INFINITY ? 0.f : Base::m;
+#pragma unroll
+    for (int b = 0; b < 2; b++) {
+      const float w = known.v[b] == known.v[b] ? known.v[b] : 0.f;      // (NaN: poison() has it)
+#pragma unroll
+      for (int i = 0; i < 16; i++) {
+        s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c[b], -ref));
+        Base::l += s[b][i];
+        s[b][i] *= w;
+      }
+#pragma unroll
+      for (int k = 0; k < 2; k++)
+        p[2 * b + k] = as_bf16(v4i{pack_bf16(s[b][8 * k], s[b][8 * k + 1]), pack_bf16(s[b][8 * k + 2], s[b][8 * k + 3]),
+                                   pack_bf16(s[b][8 * k + 4], s[b][8 * k + 5]), pack_bf16(s[b][8 * k + 6], s[b][8 * k + 7])});
+    }
+  }
+  // A block whose values are not numbers, to the rows that see some of it.
+  __device__ __forceinline__ void poison(const ByteKnown& known, int t0) {
+#pragma unroll
+    for (int b = 0; b < 2; b++)
+      if (known.v[b] != known.v[b] && known.exists[b] && Base::sees > t0 + 32 * b)
+#pragma unroll
+        for (int c = 0; c < Base::NC; c++) Base::o[c] += __builtin_nanf("");
+  }
+};
+
+template <int D_>
+struct ByteChunks {
+  static constexpr int D = D_;
+  typedef ByteChunk<D> Tile;
+  typedef ByteChunkRows<D> Rows;
+  typedef ByteKnown Known;
+  static __device__ __forceinline__ void poison(Rows& rows, bool, const unsigned char*, const Known& known, int t0) {
+    if (__builtin_expect(known.v[0] != known.v[0] || known.v[1] != known.v[1], 0)) rows.poison(known, t0);
+  }
+  typedef ByteKnown Word;
+  static __device__ __forceinline__ Word word(const Known& known, bool) { return known; }
+  struct Words {
+    ByteKnown of_lane;
+    __device__ __forceinline__ void take(const AttendArgs& a, size_t tile) { of_lane = ((const ByteKnown*)a.tiles)[tile]; }
+    __device__ __forceinline__ void wait() {
+#pragma unroll
+      for (int b = 0; b < 2; b++) {
+        arrived(of_lane.exists[b]);
+        arrived(of_lane.k[b]);
+        arrived(of_lane.v[b]);
+      }
+    }
+    __device__ __forceinline__ Word of(int lane) const {
+      Word w;
+#pragma unroll
+      for (int b = 0; b < 2; b++) {
+        w.exists[b] = __builtin_amdgcn_readlane(of_lane.exists[b], lane);
+        w.k[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(of_lane.k[b]), lane));
+        w.v[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(of_lane.v[b]), lane));
+      }
+      return w;
+    }
+  };
+  static __device__ __forceinline__ const Known& known(const Word& w) { return w; }
+  static __device__ __forceinline__ bool any_bad(const Word&) { return false; }
+};
+
+template <int D>
+__global__ __launch_bounds__(512, 2) void cache8_chunk_kernel(AttendArgs a) {
+  chunk_items<ByteChunks<D>>(a);
+}
+template <int D, int RG>
+__global__ __launch_bounds__(512, 2) void cache8_span_kernel(AttendArgs a) {
+  span_items<ByteChunks<D>, RG>(a);
+}
+template <int D>
+__global__ __launch_bounds__(512) void cache8_unpack_kernel(AttendArgs a) {
+  unpack_items<ByteChunks<D>>(a);
+}
+template <int D>
+__global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache8_wide_kernel(AttendArgs a) {
+  wide_items<ByteChunks<D>>(a);
+}
+
+}  // namespace sage

@@ -422,10 +422,27 @@ struct AttendCursor {
   }
 };
 
-template <int D, int GROUP, int NQ>
-__global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
+// What the walk over items needs of a cache's format: where a head's part of a page is, a tile of 32 tokens, a tile of queries, their meeting.
+template <int D_, int GROUP>
+struct NibbleForm {
+  static constexpr int D = D_;
   typedef CacheTile<D, GROUP> Tile;
-  constexpr int ROWS = 16 * NQ, PITCH = 64 + 4, RING = kStages * Tile::SLOT;
+  typedef AttendRows<D, GROUP> Rows;
+  typedef Unpack Unpacking;
+  static constexpr bool RING = true;      // tiles come through LDS, else to registers
+  static __device__ __forceinline__ const unsigned char* part(const AttendArgs& a, int entry, int head) {
+    return a.pool + (size_t)entry * a.g.page_bytes() + (size_t)(head * a.g.head_bytes());
+  }
+  template <int NQ>
+  static __device__ __forceinline__ void attend(Rows (&rows)[NQ], Tile& t, int t0, bool masked, float scale_log2, const Unpack& un) {
+    attend_tile<D, GROUP, NQ>(rows, t, t0, masked, scale_log2, un);
+  }
+};
+
+template <typename Form, int NQ>
+__device__ __forceinline__ void attend_items(AttendArgs a) {
+  typedef typename Form::Tile Tile;
+  constexpr int D = Form::D, ROWS = 16 * NQ, PITCH = 64 + 4, RING = Form::RING ? kStages * Tile::SLOT : 4;
   __shared__ __attribute__((aligned(16))) char lds[4 * RING];          // the ring of every wave
   __shared__ __attribute__((aligned(16))) float stage[4][16][PITCH];   // their sums for 16 rows and 64 channels
   __shared__ float wave_m[4][ROWS], wave_l[4][ROWS];
@@ -433,7 +450,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int H = a.g.H;
   char* ring = lds + wave * RING;
-  const Unpack un;
+  const typename Form::Unpacking un;
   const auto shared_units = [&](int u) { return u == 0 ? 0 : a.split ? u + kItemCost : 1; };      // what is dealt out of an item
 
   // units up to every thread's requests (R / 256 each; where that is one it is kept)
@@ -497,7 +514,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
     a.joins[w] = join_word(shares.parts<kItemCost>(w, cursor.x, __builtin_amdgcn_readlane(cursor.units, 0)),
                            __builtin_amdgcn_readlane(cursor.n_rows, 0), __builtin_amdgcn_readlane(cursor.begin, 0), cursor.head, 0);
 
-  AttendRows<D, GROUP> rows[NQ];
+  typename Form::Rows rows[NQ];
 #pragma unroll
   for (int q = 0; q < NQ; q++) rows[q].place(a, 16 * q);
   AttendPiece piece = cursor.next(a);
@@ -523,21 +540,40 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
 #pragma unroll
     for (int q = 0; q < NQ; q++) rows[q].fetch(a, piece);
   };
-  const auto fetch = [&] {      // the next tile's copies, if there is one
+  const auto some_left = [&] {      // the window is on a tile that is not on its way yet, if there is one
     while (left == 0) {
       window += 64;
-      if (window >= count) return;
+      if (window >= count) return false;
       pages = pages_from(window);
       take_pages();
     }
+    return true;
+  };
+  const auto fetch = [&] {      // the next tile's copies, if there is one
+    if (!some_left()) return;
     const int i = __builtin_ctzll(left), k = window + i, entry = __builtin_amdgcn_readlane(pages, i);
     left &= left - 1;
-    const unsigned char* p = a.pool + (size_t)entry * a.g.page_bytes() + (size_t)(piece.head * a.g.head_bytes());
-    Tile::fetch(a.g, p, (first + k * kUnit) & (a.g.page() - 1), ring + to * Tile::SLOT);
+    if constexpr (Form::RING) Tile::fetch(a.g, Form::part(a, entry, piece.head), (first + k * kUnit) & (a.g.page() - 1), ring + to * Tile::SLOT);
     to = to == kStages - 1 ? 0 : to + 1;
 #pragma unroll
     for (int q = 0; q < kStages; q++) t0[q] = q == on_way ? first + k * kUnit : t0[q];
     on_way++;
+  };
+  // To registers: loads every time, of one address where there is no tile left, so that how many loads are under way does not depend on it.
+  Tile tiles[Form::RING ? 1 : 2];
+  bool has = false;
+  const auto load = [&](Tile& t, int& from) {
+    const bool any = some_left();
+    int entry = 0, k = 0;
+    if (any) {
+      const int i = __builtin_ctzll(left);
+      k = window + i;
+      entry = __builtin_amdgcn_readlane(pages, i);
+      left &= left - 1;
+    }
+    from = first + k * kUnit;
+    if constexpr (!Form::RING) t.load(a.g, Form::part(a, entry, piece.head), from & (a.g.page() - 1), any);
+    return any;
   };
   const auto start = [&] {
     take_pages();
@@ -545,9 +581,13 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
     for (int q = 0; q < NQ; q++)
 #pragma unroll
       for (int j = 0; j < D / 32; j++) arrived(rows[q].q[j]);
-    on_way = to = 0;
+    if constexpr (Form::RING) {
+      on_way = to = 0;
 #pragma unroll 1
-    for (int k = 0; k < kStages - 1; k++) fetch();       // (one copy of the code: of 4 short requests it is 3 % of the call)
+      for (int k = 0; k < kStages - 1; k++) fetch();       // (one copy of the code: of 4 short requests it is 3 % of the call)
+    } else {
+      has = load(tiles[0], t0[0]);
+    }
   };
   look();
   start();
@@ -556,7 +596,16 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
     const int all_see = a.causal ? piece.first_sees : piece.len;       // keys that every row sees
 #pragma unroll
     for (int q = 0; q < NQ; q++) rows[q].begin();
-    for (int slot = 0; on_way > 0; slot = slot == kStages - 1 ? 0 : slot + 1) {
+    if constexpr (!Form::RING) {
+      while (has) {
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+          const bool more = load(tiles[1 - x], t0[1 - x]);
+          if (has) Form::template attend<NQ>(rows, tiles[x], t0[x], t0[x] + 32 > all_see, a.scale_log2, un);
+          has = more;
+        }
+      }
+    } else for (int slot = 0; on_way > 0; slot = slot == kStages - 1 ? 0 : slot + 1) {
       compiler_fence();
       fetch();
       compiler_fence();
@@ -566,7 +615,7 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
       compiler_fence();
       Tile tile;
       tile.take(ring + slot * Tile::SLOT);
-      attend_tile<D, GROUP, NQ>(rows, tile, t0[0], t0[0] + 32 > all_see, a.scale_log2, un);
+      Form::template attend<NQ>(rows, tile, t0[0], t0[0] + 32 > all_see, a.scale_log2, un);
       on_way--;
 #pragma unroll
       for (int q = 1; q < kStages; q++) t0[q - 1] = t0[q];
@@ -634,12 +683,16 @@ __global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
     if (!more) break;
   }
 }
+template <int D, int GROUP, int NQ>
+__global__ __launch_bounds__(256, 2) void cache_attend_kernel(AttendArgs a) {
+  attend_items<NibbleForm<D, GROUP>, NQ>(a);
+}
 
 // Joins the parts of an item that several workgroups had, in the order of the keys: the workgroup at the first border inside it has left word
 // (AttendArgs::joins).  Of few rows, with many parts: a workgroup has a row, every lane weighs a part, then each wave takes every fourth part,
 // several loads in flight, and they meet in LDS (one wave and one part after the other took 97 us for the 128 parts of a request alone, now 7).
 template <int D, int ROWS>
-__global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
+__device__ __forceinline__ void join_few(AttendArgs a) {
   constexpr int NC = D / 64, MOST = 256;
   const int w = blockIdx.x + 1, k = blockIdx.y;
   const int4 join = a.joins[w];
@@ -685,12 +738,16 @@ __global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
   for (int i = 0; i < NC; i++) o[i] = (meet[0][NC * lane + i] + meet[1][NC * lane + i]) + (meet[2][NC * lane + i] + meet[3][NC * lane + i]);
   attend_store<NC>(a, join.y, join.z, join.w + k, D, NC * lane, M, l, o, mean);
 }
+template <int D, int ROWS>
+__global__ __launch_bounds__(256) void cache_join_kernel(AttendArgs a) {
+  join_few<D, ROWS>(a);
+}
 
 // The same of many rows, with few parts each: D / 4 lanes have a row and take four parts at a time, one trip to memory for up to four.  (A wave a row,
 // two channels a lane, the maxima asked for first: vector instructions were 83 % of its cycles; 255 divided tiles of 256 rows of 128
 // channels 20 us, the call 327 -> 319; 511 borders of a mixed batch, 64 channels, 72.5 -> 67.5.)
 template <int D, int ROWS>
-__global__ __launch_bounds__(256) void cache_join_rows_kernel(AttendArgs a) {
+__device__ __forceinline__ void join_many(AttendArgs a) {
   constexpr int LANES = D / 4, HERE = 256 / LANES, BATCH = 4;
   const int w = blockIdx.x + 1, k = blockIdx.y * HERE + threadIdx.x / LANES;
   const int4 join = a.joins[w];
@@ -726,6 +783,10 @@ __global__ __launch_bounds__(256) void cache_join_rows_kernel(AttendArgs a) {
     m = to;
   }
   attend_store<4>(a, join.y, join.z, join.w + k, D, c, m, l, (const float*)&o, mean);
+}
+template <int D, int ROWS>
+__global__ __launch_bounds__(256) void cache_join_rows_kernel(AttendArgs a) {
+  join_many<D, ROWS>(a);
 }
 
 }  // namespace sage

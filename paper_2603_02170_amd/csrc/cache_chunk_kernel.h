@@ -14,10 +14,16 @@ namespace sage {
 
 constexpr int kChunkRows = 256, kChunkUnit = 64;
 
+// What the rows have to know of 64 tokens that lie in LDS or in the workspace: whether the pages of its halves exist.
+struct ChunkKnown {
+  int exists[2];
+};
+
 // 64 tokens on their way from the pages to bf16 fragments: waves 0 to 3 have K's, the others V's.
-template <int D, int GROUP>
+template <int D_, int GROUP_>
 struct ChunkTile {
-  static constexpr int NG = D / GROUP, FRAG = D / 16 * 1024;     // bytes of 32 tokens of K, of 32 tokens' worth of V
+  static constexpr int D = D_, GROUP = GROUP_, NG = D / GROUP, FRAG = D / 16 * 1024;     // bytes of 32 tokens of K, of 32 tokens' worth of V
+  typedef ChunkKnown Known;
   v4i code, s0, s1;
   int valid;               // tokens of the thread's own that exist, counted from its first
 
@@ -57,11 +63,11 @@ struct ChunkTile {
 
   // Writes the fragments.  `poison`: tokens whose scale of V is not a number (bit s: of the group s), which the product may not meet
   // (0 times NaN in the rows that do not see the token); `poisoned` says that there is one.
-  __device__ __forceinline__ void store(char* K, char* V, int* exists, unsigned char* poison, int* poisoned, int tag) const {
+  __device__ __forceinline__ void store(char* K, char* V, Known& known, unsigned char* poison, int* poisoned, int tag) const {
     const int tid = threadIdx.x, u = tid & 255;
     if (tid < 256) {
       const int rho = u & 31, q = (u >> 5) & 3, b = u >> 7;
-      if ((u & 127) == 0) exists[b] = valid;
+      if ((u & 127) == 0) known.exists[b] = valid;
 #pragma unroll
       for (int j = 0; j < D / 32; j++) {
         const float s = bf16_bits_to_float((unsigned short)s0[32 * j / GROUP]), s8 = -8.f * s;
@@ -306,8 +312,9 @@ struct ChunkRows {
     products<2 * NK>([&](int i) { return *(const v4i*)(K + ((i & 1) * NK + (i >> 1)) * 1024); },
                      [&](int i, const v8bf& f) { s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, as_bf16(q[i >> 1]), s[i & 1], 0, 0, 0); });
   }
-  // Logits of the tokens t0 .. t0 + 63 to probabilities; e0, e1: whether its halves' pages exist.
-  __device__ __forceinline__ void softmax(v16f (&s)[2], v8bf (&p)[4], int t0, int e0, int e1, float scale_log2) {
+  // Logits of the tokens t0 .. t0 + 63 to probabilities.
+  __device__ __forceinline__ void softmax(v16f (&s)[2], v8bf (&p)[4], int t0, const ChunkKnown& known, float scale_log2) {
+    const int e0 = known.exists[0], e1 = known.exists[1];
     if (t0 + kChunkUnit > all_see || e0 + e1 != 2) {
       const int h = threadIdx.x >> 5 & 1;
 #pragma unroll
@@ -350,7 +357,8 @@ struct ChunkRows {
                      [&](int i, const v8bf& f) { o[i % NC] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p[i / NC], o[i % NC], 0, 0, 0); });
   }
   // Tokens whose values are not numbers, to the rows that see them.
-  __device__ __forceinline__ void poison(const unsigned char* bad, int group, int t0, int e0, int e1) {
+  __device__ __forceinline__ void poison(const unsigned char* bad, int group, int t0, const ChunkKnown& known) {
+    const int e0 = known.exists[0], e1 = known.exists[1];
     for (int t = 0; t < kChunkUnit; t++)
 #pragma unroll
       for (int c = 0; c < NC; c++)
@@ -390,13 +398,42 @@ struct ChunkRows {
   }
 };
 
-template <int D, int GROUP>
-__global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
+struct WideTile {
+  int flags;        // bit 0, 1: the pages of its halves exist; bit 2: some value is not a number
+};
+
+// What the kernels need of a cache's format.
+template <int D_, int GROUP>
+struct NibbleChunks {
+  static constexpr int D = D_;
   typedef ChunkTile<D, GROUP> Tile;
+  typedef ChunkRows<D> Rows;
+  typedef ChunkKnown Known;
+  // Of 64 tokens: `bad` has those that are not numbers, if there are any.
+  static __device__ __forceinline__ void poison(Rows& rows, bool any, const unsigned char* bad, const Known& known, int t0) {
+    if (any) rows.poison(bad, GROUP, t0, known);
+  }
+  // What is known of tiles unpacked beforehand, of 64 of them, one a lane.
+  typedef WideTile Word;
+  static __device__ __forceinline__ Word word(const Known& known, bool any) { return Word{(known.exists[0] != 0) | (known.exists[1] != 0) << 1 | any << 2}; }
+  struct Words {
+    int flags;
+    __device__ __forceinline__ void take(const AttendArgs& a, size_t tile) { flags = a.tiles[tile].flags; }
+    __device__ __forceinline__ void wait() { arrived(flags); }
+    __device__ __forceinline__ Word of(int lane) const { return Word{__builtin_amdgcn_readlane(flags, lane)}; }
+  };
+  static __device__ __forceinline__ Known known(const Word& w) { return Known{{w.flags & 1, w.flags >> 1 & 1}}; }
+  static __device__ __forceinline__ bool any_bad(const Word& w) { return w.flags & 4; }
+};
+
+template <typename Form>
+__device__ __forceinline__ void chunk_items(AttendArgs a) {
+  typedef typename Form::Tile Tile;
   constexpr int HALF = 2 * Tile::FRAG;
   __shared__ __attribute__((aligned(16))) char Ks[2][HALF], Vs[3][HALF];
   __shared__ __attribute__((aligned(8))) unsigned char poison[4][Tile::NG * 64];
-  __shared__ int exists[4][2], poisoned[4];
+  __shared__ typename Form::Known known[4];
+  __shared__ int poisoned[4];
   __shared__ ChunkScratch scratch;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (tid < 4) poisoned[tid] = -1;
@@ -408,7 +445,7 @@ __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
     const AttendRequest& rq = walk.rq;
     const int visible = __builtin_amdgcn_readfirstlane(attend_visible(a, rq, walk.tile * kChunkRows, kChunkRows));
     const int u = max(1, (visible + kChunkUnit - 1) / kChunkUnit), j0 = walk.j0, j1 = walk.last_unit(a, u);
-    ChunkRows<D> rows;
+    typename Form::Rows rows;
     rows.begin(a, rq, walk.head, walk.tile * kChunkRows + 32 * wave);
     // a lane has the page of one of the next 64 blocks of 32 tokens
     const int32_t* table = a.table + (size_t)walk.r * a.columns;
@@ -425,7 +462,7 @@ __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
     const int count = visible > 0 ? j1 - j0 : 0;
     int v_at = 0;      // (k + 1) % 3 of the tile that is stored next
     const auto store = [&](int k) {
-      next.store(Ks[k & 1], Vs[v_at], exists[k & 3], poison[k & 3], &poisoned[k & 3], tag + k);
+      next.store(Ks[k & 1], Vs[v_at], known[k & 3], poison[k & 3], &poisoned[k & 3], tag + k);
       v_at = v_at == 2 ? 0 : v_at + 1;
     };
     if (count > 0) {
@@ -441,14 +478,13 @@ __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
     v8bf p[4];
     const auto probabilities = [&](int k) {
       const int t0 = (j0 + k) * kChunkUnit;
-      if (t0 < rows.wave_sees) rows.softmax(s, p, t0, exists[k & 3][0], exists[k & 3][1], a.scale_log2);
+      if (t0 < rows.wave_sees) rows.softmax(s, p, t0, known[k & 3], a.scale_log2);
     };
     for (int k = 0, v = 2; k <= count; k++, v = v == 2 ? 0 : v + 1) {      // v = (k + 2) % 3
       if (late && k > 0) probabilities(k - 1);
       if (k > 0 && (j0 + k - 1) * kChunkUnit < rows.wave_sees) {
         rows.values(Vs[v], p);
-        if (poisoned[k - 1 & 3] == tag + k - 1)
-          rows.poison(poison[k - 1 & 3], GROUP, (j0 + k - 1) * kChunkUnit, exists[k - 1 & 3][0], exists[k - 1 & 3][1]);
+        Form::poison(rows, poisoned[k - 1 & 3] == tag + k - 1, poison[k - 1 & 3], known[k - 1 & 3], (j0 + k - 1) * kChunkUnit);
       }
       if (k < count && (j0 + k) * kChunkUnit < rows.wave_sees) rows.logits(Ks[k & 1], s);
       if (!late && k < count) probabilities(k);
@@ -463,6 +499,10 @@ __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
     more = walk.next(a, u, j1);
   }
 }
+template <int D, int GROUP>
+__global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
+  chunk_items<NibbleChunks<D, GROUP>>(a);
+}
 
 // ---- up to 128 query rows a request ---------------------------------------------------------------------------------
 // Of the 256 rows of cache_chunk_kernel's tile most do not exist then, and their waves wait.  Here a workgroup's eight waves are RG groups
@@ -471,14 +511,16 @@ __global__ __launch_bounds__(512, 2) void cache_chunk_kernel(AttendArgs a) {
 // are unpacked while slower waves still multiply.  Unpacking is what bounds it: about 1300 vector instructions for 64 tokens of 128 channels.
 // (32 requests of 4096 tokens, 8 heads, 64 rows: 123 -> 87 us, 128 rows 126 -> 107; at d = 64 102 -> 73, 119 -> 91.  With a branch round each tile
 // behind the last token, which a request's last unit may have, the tiles are unpacked one after the other: 108.)
-template <int D, int GROUP, int RG>
-__global__ __launch_bounds__(512, 2) void cache_span_kernel(AttendArgs a) {
-  typedef ChunkTile<D, GROUP> Tile;
+template <typename Form, int RG>
+__device__ __forceinline__ void span_items(AttendArgs a) {
+  typedef typename Form::Tile Tile;
   typedef SpanShape<RG> Shape;
+  constexpr int D = Form::D;
   constexpr int KG = Shape::KG, ROWS = Shape::ROWS, UNIT = Shape::UNIT, HALF = 2 * Tile::FRAG, SETS = KG * 4 * HALF <= 131072 ? 2 : 1;
   __shared__ __attribute__((aligned(16))) char lds[SETS][KG][2 * HALF];
   __shared__ __attribute__((aligned(8))) unsigned char poison[SETS][KG][Tile::NG * 64];
-  __shared__ int exists[SETS][KG][2], poisoned[SETS][KG];
+  __shared__ typename Form::Known known[SETS][KG];
+  __shared__ int poisoned[SETS][KG];
   __shared__ ChunkScratch scratch;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wave % RG, kg = wave / RG;
   if (tid < SETS * KG) (&poisoned[0][0])[tid] = -1;
@@ -490,7 +532,7 @@ __global__ __launch_bounds__(512, 2) void cache_span_kernel(AttendArgs a) {
     const int visible = __builtin_amdgcn_readfirstlane(attend_visible(a, rq, walk.tile * ROWS, ROWS));
     const int u = max(1, (visible + UNIT - 1) / UNIT), j0 = walk.j0, j1 = walk.last_unit(a, u);
     const int count = visible > 0 ? j1 - j0 : 0;
-    ChunkRows<D> rows;
+    typename Form::Rows rows;
     rows.begin(a, rq, walk.head, walk.tile * ROWS + 32 * rg);
     // a lane has the page of one of the next 64 blocks of 32 tokens
     const int32_t* table = a.table + (size_t)walk.r * a.columns;
@@ -511,18 +553,18 @@ __global__ __launch_bounds__(512, 2) void cache_span_kernel(AttendArgs a) {
       const int set = SETS == 2 ? k & 1 : 0;
 #pragma unroll
       for (int i = 0; i < KG; i++)
-        next[i].store(lds[set][i], lds[set][i] + HALF, exists[set][i], poison[set][i], &poisoned[set][i], tag + k);
+        next[i].store(lds[set][i], lds[set][i] + HALF, known[set][i], poison[set][i], &poisoned[set][i], tag + k);
     };
     const auto attend = [&](int k) {
       const int set = SETS == 2 ? k & 1 : 0, t0 = (j0 + k) * UNIT + 64 * kg;
       if (t0 >= rows.wave_sees) return;
-      const int e0 = exists[set][kg][0], e1 = exists[set][kg][1];
+      const typename Form::Known of = known[set][kg];
       v16f s[2];
       v8bf p[4];
       rows.logits(lds[set][kg], s);
-      rows.softmax(s, p, t0, e0, e1, a.scale_log2);
+      rows.softmax(s, p, t0, of, a.scale_log2);
       rows.values(lds[set][kg] + HALF, p);
-      if (poisoned[set][kg] == tag + k) rows.poison(poison[set][kg], GROUP, t0, e0, e1);
+      Form::poison(rows, poisoned[set][kg] == tag + k, poison[set][kg], of, t0);
     };
     if (count > 0) load(0);
     if (SETS == 2) {
@@ -582,20 +624,22 @@ __global__ __launch_bounds__(512, 2) void cache_span_kernel(AttendArgs a) {
     more = walk.next(a, u, j1);
   }
 }
+template <int D, int GROUP, int RG>
+__global__ __launch_bounds__(512, 2) void cache_span_kernel(AttendArgs a) {
+  span_items<NibbleChunks<D, GROUP>, RG>(a);
+}
 
 // ---- the same with the keys and values unpacked beforehand ------------------------------------------------------------
 // Where a request's keys meet several row tiles, unpacking them in each costs more vector instructions than the softmax: a launch writes the
 // fragments to the workspace once (as they lie in LDS, 256 d bytes for 64 tokens of a head, request after request, head, tile), and the
 // attention copies them into a ring past the registers.
-struct WideTile {
-  int flags;        // bit 0, 1: the pages of its halves exist; bit 2: some value is not a number
-};
-
-template <int D, int GROUP>
-__global__ __launch_bounds__(512) void cache_unpack_kernel(AttendArgs a) {
-  typedef ChunkTile<D, GROUP> Tile;
+template <typename Form>
+__device__ __forceinline__ void unpack_items(AttendArgs a) {
+  typedef typename Form::Tile Tile;
+  constexpr int D = Form::D;
   __shared__ ChunkScratch s;
-  __shared__ int exists[2], poisoned;
+  __shared__ typename Form::Known known;
+  __shared__ int poisoned;
   const int tid = threadIdx.x, H = a.g.H;
   const int per = (a.R + 511) / 512, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
   unsigned tiles = 0;
@@ -636,17 +680,22 @@ __global__ __launch_bounds__(512) void cache_unpack_kernel(AttendArgs a) {
     Tile t;
     t.load(a, head, t0, table[min(t0, last) >> a.g.page_shift], table[min(t0 + 32, last) >> a.g.page_shift], rq.len);
     char* to = a.unpacked + (size_t)y * (256 * D);
-    t.store(to, to + 128 * D, exists, a.poison + (size_t)y * (Tile::NG * 64), &poisoned, y);
+    t.store(to, to + 128 * D, known, a.poison + (size_t)y * (Tile::NG * 64), &poisoned, y);
     __syncthreads();
-    if (tid == 0) a.tiles[y].flags = (exists[0] != 0) | (exists[1] != 0) << 1 | (poisoned == y) << 2;
+    if (tid == 0) ((typename Form::Word*)a.tiles)[y] = Form::word(known, poisoned == y);
     __syncthreads();
   }
+}
+template <int D, int GROUP>
+__global__ __launch_bounds__(512) void cache_unpack_kernel(AttendArgs a) {
+  unpack_items<NibbleChunks<D, GROUP>>(a);
 }
 
 constexpr int kWideStages = 4;
 
-template <int D, int GROUP>
-__global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache_wide_kernel(AttendArgs a) {
+template <typename Form>
+__device__ __forceinline__ void wide_items(AttendArgs a) {
+  constexpr int D = Form::D;
   constexpr int TILE = 256 * D, COPIES = TILE / 8 / 1024;
   __shared__ __attribute__((aligned(16))) char ring[kWideStages][TILE];
   __shared__ ChunkScratch scratch;
@@ -661,9 +710,10 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache_wide_kernel(Attend
     int count = visible > 0 ? j1 - j0 : 0;
     size_t tile0 = (size_t)walk.before * a.g.H + (size_t)walk.head * chunk_key_tiles(rq) + j0;      // of the unpacked ones
     if (tile0 + max(count, 1) > (size_t)a.most_tiles) tile0 = count = 0;
-    ChunkRows<D> rows;
+    typename Form::Rows rows;
     rows.begin(a, rq, walk.head, walk.tile * kChunkRows + 32 * wave);
-    int flags = a.tiles[tile0 + min(lane, max(count - 1, 0))].flags;        // of the next 64 tiles, one a lane
+    typename Form::Words words;        // of the next 64 tiles, one a lane
+    words.take(a, tile0 + min(lane, max(count - 1, 0)));
     const auto fetch = [&](int k) {
       const gbytes_t from = uniform(a.unpacked + (tile0 + k) * TILE + wave * (COPIES * 1024));
 #pragma unroll
@@ -672,12 +722,12 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache_wide_kernel(Attend
     // (intervals as in cache_chunk_kernel)
     v16f s[2];
     v8bf p[4];
-    int flag = 0, flag_before = 0;
-    const auto probabilities = [&](int k, int flag) {
+    typename Form::Word word = {}, word_before = {};
+    const auto probabilities = [&](int k, const typename Form::Word& word) {
       const int t0 = (j0 + k) * kChunkUnit;
-      if (t0 < rows.wave_sees) rows.softmax(s, p, t0, flag & 1, flag >> 1 & 1, a.scale_log2);
+      if (t0 < rows.wave_sees) rows.softmax(s, p, t0, Form::known(word), a.scale_log2);
     };
-    arrived(flags);
+    words.wait();
     rows.wait();
     compiler_fence();
     fetch(0);
@@ -691,26 +741,29 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache_wide_kernel(Attend
       if (k + 2 < count) fetch(k + 2);
       compiler_fence();
       if (k % 64 == 0 && k != 0) {
-        flags = a.tiles[tile0 + min(k + lane, count - 1)].flags;
-        arrived(flags);
+        words.take(a, tile0 + min(k + lane, count - 1));
+        words.wait();
       }
-      flag_before = flag;
-      flag = __builtin_amdgcn_readlane(flags, k % 64);
-      if (late && k > 0) probabilities(k - 1, flag_before);
+      word_before = word;
+      word = words.of(k % 64);
+      if (late && k > 0) probabilities(k - 1, word_before);
       if (k > 0 && (j0 + k - 1) * kChunkUnit < rows.wave_sees) {
         rows.values(ring[(k - 1) % kWideStages] + TILE / 2, p);
-        if (flag_before & 4)
-          rows.poison(a.poison + (tile0 + k - 1) * (D / GROUP * 64), GROUP, (j0 + k - 1) * kChunkUnit, flag_before & 1, flag_before >> 1 & 1);
+        Form::poison(rows, Form::any_bad(word_before), a.poison + (tile0 + k - 1) * (Form::Tile::NG * 64), Form::known(word_before), (j0 + k - 1) * kChunkUnit);
       }
       if (k < count) {
         if ((j0 + k) * kChunkUnit < rows.wave_sees) rows.logits(ring[k % kWideStages], s);
-        if (!late) probabilities(k, flag);
+        if (!late) probabilities(k, word);
       }
     }
     rows.end(a, rq, walk.head, j0 == 0 && j1 == u, ((size_t)walk.w * 2 + (j0 == 0 ? 1 : 0)) * kChunkRows + 32 * wave + (lane & 31));
     more = walk.next(a, u, j1);
     barrier_all_memory();                  // (the ring is the next item's)
   }
+}
+template <int D, int GROUP>
+__global__ __launch_bounds__(512, D == 64 ? 4 : 2) void cache_wide_kernel(AttendArgs a) {
+  wide_items<NibbleChunks<D, GROUP>>(a);
 }
 
 }  // namespace sage

@@ -90,13 +90,13 @@ bool size_arg(PyObject* o, const char* name, int64_t least, int64_t* out) {
   *out = x;
   return true;
 }
-// (H, d, page, group) as four arguments
+// (H, d, page, group, block) as five arguments
 bool cache_params(PyObject* const* a, sagebwd_cache_params& p) {
-  int64_t x[4];
-  const char* names[4] = {"H", "d", "page", "group"};
-  for (int k = 0; k < 4; k++)
+  int64_t x[5];
+  const char* names[5] = {"H", "d", "page", "group", "block"};
+  for (int k = 0; k < 5; k++)
     if (!size_arg(a[k], names[k], 0, &x[k])) return false;
-  p = sagebwd_cache_params{(int32_t)x[0], (int32_t)x[1], (int32_t)x[2], (int32_t)x[3], 0, 0};
+  p = sagebwd_cache_params{(int32_t)x[0], (int32_t)x[1], (int32_t)x[2], x[4] == 0 ? (int32_t)x[3] : 0, 0, (int32_t)x[4]};
   return true;
 }
 
@@ -195,17 +195,17 @@ PyObject* py_cache_trim(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 const float* data_or_null(const Tensor& t) { return t.defined() ? (const float*)t.data_ptr() : nullptr; }
 
-// append(K, V, slots, cache, H, d, page, group, k_mean | None, v_mean | None)
+// append(K, V, slots, cache, H, d, page, group, block, k_mean | None, v_mean | None)
 PyObject* py_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   DeviceOf dev;
   sagebwd_cache_params p;
   const Tensor *K, *V, *slots, *pool;
   Tensor km, vm;
-  if (!arg_count(n, 10, "cache_append") || !cache_params(a + 4, p) || !(pool = pool_arg(a[3], p, dev)) ||
+  if (!arg_count(n, 11, "cache_append") || !cache_params(a + 4, p) || !(pool = pool_arg(a[3], p, dev)) ||
       !(K = token_rows(a[0], -1, p.H, p.d, "K", dev)) || !(V = token_rows(a[1], K->size(0), p.H, p.d, "V", dev)) ||
-      !(slots = dense(a[2], at::kLong, {K->size(0)}, "slots", dev)) || !dense_or_none(a[8], at::kFloat, {p.H, p.d}, "k_mean", dev, &km) ||
-      !dense_or_none(a[9], at::kFloat, {p.H, p.d}, "v_mean", dev, &vm))
+      !(slots = dense(a[2], at::kLong, {K->size(0)}, "slots", dev)) || !dense_or_none(a[9], at::kFloat, {p.H, p.d}, "k_mean", dev, &km) ||
+      !dense_or_none(a[10], at::kFloat, {p.H, p.d}, "v_mean", dev, &vm))
     return nullptr;
   if (K->size(0) > INT32_MAX) {
     value_error("K", "too many tokens");
@@ -223,19 +223,19 @@ PyObject* py_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// read(slots, cache, H, d, page, group, k_mean | None, v_mean | None, K | None, V | None) -> (K, V)
+// read(slots, cache, H, d, page, group, block, k_mean | None, v_mean | None, K | None, V | None) -> (K, V)
 PyObject* py_cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   DeviceOf dev;
   sagebwd_cache_params p;
   const Tensor *slots, *pool;
   Tensor km, vm, K, V;
-  if (!arg_count(n, 10, "cache_read") || !cache_params(a + 2, p) || !(pool = pool_arg(a[1], p, dev)) ||
-      !(slots = dense(a[0], at::kLong, {-1}, "slots", dev)) || !dense_or_none(a[6], at::kFloat, {p.H, p.d}, "k_mean", dev, &km) ||
-      !dense_or_none(a[7], at::kFloat, {p.H, p.d}, "v_mean", dev, &vm))
+  if (!arg_count(n, 11, "cache_read") || !cache_params(a + 2, p) || !(pool = pool_arg(a[1], p, dev)) ||
+      !(slots = dense(a[0], at::kLong, {-1}, "slots", dev)) || !dense_or_none(a[7], at::kFloat, {p.H, p.d}, "k_mean", dev, &km) ||
+      !dense_or_none(a[8], at::kFloat, {p.H, p.d}, "v_mean", dev, &vm))
     return nullptr;
   const std::array<int64_t, 3> shape = {slots->size(0), p.H, p.d};
-  if (!dense_or_none(a[8], at::kBFloat16, shape, "K", dev, &K) || !dense_or_none(a[9], at::kBFloat16, shape, "V", dev, &V)) return nullptr;
+  if (!dense_or_none(a[9], at::kBFloat16, shape, "K", dev, &K) || !dense_or_none(a[10], at::kBFloat16, shape, "V", dev, &V)) return nullptr;
   if (shape[0] > INT32_MAX) {
     value_error("slots", "too many tokens");
     return nullptr;
@@ -253,7 +253,7 @@ PyObject* py_cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// attention(Q, cache, table, lengths, cu, H, d, page, group, max_new, causal, sm_scale, v_mean | None, max_length, workspace | None, O | None,
+// attention(Q, cache, table, lengths, cu, H, d, page, group, block, max_new, causal, sm_scale, v_mean | None, max_length, workspace | None, O | None,
 //           LSE | None) -> (O, LSE)
 PyObject* py_cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -262,20 +262,20 @@ PyObject* py_cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const Tensor *Q, *pool, *table, *lengths, *cu;
   Tensor vm, ws, O, L;
   int64_t max_new, max_length;
-  if (!arg_count(n, 17, "cache_attention") || !cache_params(a + 5, p) || !(pool = pool_arg(a[1], p, dev)) ||
+  if (!arg_count(n, 18, "cache_attention") || !cache_params(a + 5, p) || !(pool = pool_arg(a[1], p, dev)) ||
       !(Q = token_rows(a[0], -1, -1, p.d, "Q", dev)) || !(lengths = dense(a[3], at::kInt, {-1}, "lengths", dev)) ||
       !(table = dense(a[2], at::kInt, {lengths->size(0), -1}, "block_table", dev)) ||
-      !(cu = dense(a[4], at::kInt, {lengths->size(0) + 1}, "cu", dev)) || !size_arg(a[9], "max_new", 1, &max_new) ||
-      !dense_or_none(a[12], at::kFloat, {p.H, p.d}, "v_mean", dev, &vm) || !size_arg(a[13], "max_length", 0, &max_length) ||
-      !dense_or_none(a[14], at::kByte, {-1}, "workspace", dev, &ws))
+      !(cu = dense(a[4], at::kInt, {lengths->size(0) + 1}, "cu", dev)) || !size_arg(a[10], "max_new", 1, &max_new) ||
+      !dense_or_none(a[13], at::kFloat, {p.H, p.d}, "v_mean", dev, &vm) || !size_arg(a[14], "max_length", 0, &max_length) ||
+      !dense_or_none(a[15], at::kByte, {-1}, "workspace", dev, &ws))
     return nullptr;
-  const int causal = PyObject_IsTrue(a[10]);
-  const double sm_scale = PyFloat_AsDouble(a[11]);
+  const int causal = PyObject_IsTrue(a[11]);
+  const double sm_scale = PyFloat_AsDouble(a[12]);
   if (causal < 0 || (sm_scale == -1.0 && PyErr_Occurred())) return nullptr;
   const int64_t T = Q->size(0), Hq = Q->size(1);
   const std::array<int64_t, 3> oshape = {T, Hq, p.d};
   const std::array<int64_t, 2> lshape = {Hq, T};
-  if (!dense_or_none(a[15], at::kBFloat16, oshape, "O", dev, &O) || !dense_or_none(a[16], at::kFloat, lshape, "LSE", dev, &L)) return nullptr;
+  if (!dense_or_none(a[16], at::kBFloat16, oshape, "O", dev, &O) || !dense_or_none(a[17], at::kFloat, lshape, "LSE", dev, &L)) return nullptr;
   if (T > INT32_MAX || Hq > INT32_MAX || table->size(1) < 1 || table->size(1) > INT32_MAX || lengths->size(0) > INT32_MAX) {
     value_error("block_table", "sizes are out of range");
     return nullptr;
@@ -314,16 +314,16 @@ PyObject* py_cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// workspace_bytes(H, d, page, group, R, T, Hq, columns, max_new, max_length) -> bytes
+// workspace_bytes(H, d, page, group, block, R, T, Hq, columns, max_new, max_length) -> bytes
 PyObject* py_cache_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   sagebwd_cache_params p;
-  if (!arg_count(n, 10, "cache_workspace_bytes") || !cache_params(a, p)) return nullptr;
+  if (!arg_count(n, 11, "cache_workspace_bytes") || !cache_params(a, p)) return nullptr;
   p.pages = 1;
   int64_t x[6];
   const char* names[6] = {"R", "T", "Hq", "columns", "max_new", "max_length"};
   for (int k = 0; k < 6; k++)
-    if (!size_arg(a[4 + k], names[k], 0, &x[k])) return nullptr;
+    if (!size_arg(a[5 + k], names[k], 0, &x[k])) return nullptr;
   const sagebwd_cache_call c = {(int32_t)x[0], (int32_t)x[1], (int32_t)x[2], (int32_t)x[3], (int32_t)x[4], (int32_t)x[5], 1, 0.f, 0, 0};
   size_t bytes = 0;
   const int rc = sagebwd_cache_workspace_bytes(&p, &c, &bytes);

@@ -1,0 +1,539 @@
+"""The cache held in 8 bits against plain implementations: storing, reading, and attention over it in every form."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import serve8_ref as ref8
+import serve_ref as ref
+from paper_2603_02170_amd import binding, cache
+from paper_2603_02170_amd.autograd import sage_rotary
+from paper_2603_02170_amd.cache import CacheParams
+
+pytestmark = pytest.mark.gpu
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy()
+
+
+def _randn(shape, g, scale=1.0):
+    return (scale * torch.randn(shape, generator=g)).to(torch.bfloat16)
+
+
+def _slots(x):
+    return torch.tensor(x, dtype=torch.int64, device="cuda")
+
+
+# ---- storing and reading ----------------------------------------------------------------------------------------
+
+def _same(pool, model, p, heads, before=None, stored=()):
+    """The pool's bytes are the model's wherever tokens are held; elsewhere, and behind a block's last token, `before`'s."""
+    for n in range(pool.shape[0]):
+        for h in heads:
+            k, v, ka, va = ref8.decode(pool[n, h].cpu().numpy(), p.d, p.page)
+            k0, v0, ka0, va0 = ref8.decode(before[n, h].cpu().numpy(), p.d, p.page)
+            for first in range(0, p.page, p.block):
+                here = slice(first, first + p.block)
+                for which, codes, a, codes0, a0 in ((0, k, ka, k0, ka0), (1, v, va, v0, va0)):
+                    b = model.blocks.get(((n * p.page + first) // p.block, h, which))
+                    held = b.held if b else 0
+                    if b:
+                        assert np.array_equal(a[here].view(np.uint32) & 0x7FFFFFFF, np.full(p.block, b.a).view(np.uint32) & 0x7FFFFFFF)
+                        if not np.isnan(b.a):
+                            assert np.array_equal(codes[here][:held], b.codes[:held]), (n, h, first, which)
+                    else:
+                        assert np.array_equal(a[here].view(np.uint32), a0[here].view(np.uint32))
+                    assert np.array_equal(codes[here][held:], codes0[here][held:])
+
+
+@pytest.mark.parametrize("d,block,page,H,T", [(64, 32, 32, 1, 1), (64, 64, 64, 3, 37), (128, 32, 128, 2, 100), (128, 64, 256, 4, 700), (128, 64, 64, 5, 65),
+                                              (64, 32, 64, 40, 200)])
+@pytest.mark.parametrize("mean", [False, True])
+def test_what_is_stored_in_pieces_is_read_back_as_the_quantiser_says(d, block, page, H, T, mean):
+    """Two requests' tokens in pieces of every size, side by side in a call: codes and magnitudes bit for bit, and nothing else changes."""
+    g, rng = torch.Generator().manual_seed(d + T), np.random.default_rng(T)
+    p = CacheParams(H=H, d=d, page=page, block=block)
+    per = -(-T // page)
+    pages = 2 * per + 2
+    pool = torch.randint(0, 256, tuple(cache.alloc_cache(p, pages).shape), generator=g, dtype=torch.uint8).cuda()
+    assert cache.cache_page_bytes(p) == H * (2 * page * d + max(16, page // 4))
+    before, model = pool.clone(), ref8.Pages(H, d, page, block)
+    order = rng.permutation(pages)
+    km, vm = (torch.randn((H, d), generator=g).cuda(), torch.randn((H, d), generator=g).cuda()) if mean else (None, None)
+    held = [0, 0]
+    while min(held) < T:
+        slots = []
+        for r in range(2):
+            n = min(T - held[r], int(rng.choice([0, 1, 1, 3, 40, 300])))
+            slots += [int(order[r * per + t // page]) * page + t % page for t in range(held[r], held[r] + n)]
+            held[r] += n
+        qkv = (_randn((len(slots), 2 * H + 1, d), g).float() * torch.exp(torch.randn((len(slots), 1, 1), generator=g))).to(torch.bfloat16).cuda()
+        K, V = qkv[:, 1:1 + H], qkv[:, 1 + H:]          # slices of one tensor
+        cache.sagebwd_cache_append(K, V, _slots(slots), pool, p, k_mean=km, v_mean=vm)
+        model.append(_np(K) - (_np(km) if mean else F0), _np(V) - (_np(vm) if mean else F0), slots)
+    _same(pool, model, p, range(min(H, 3)), before)
+    slots = [int(order[r * per + t // page]) * page + t % page for r in range(2) for t in range(T)]
+    Kr, Vr = cache.sagebwd_cache_read(_slots(slots), pool, p)
+    for got, which in ((Kr, 0), (Vr, 1)):
+        assert np.array_equal(_np(got), ref.bf16_round(model.gather(slots, which, "read")))
+    if mean:
+        Km, Vm = cache.sagebwd_cache_read(_slots(slots), pool, p, k_mean=km, v_mean=vm)
+        assert np.array_equal(_np(Km), ref.bf16_round(model.gather(slots, 0, "read") + _np(km)))
+        assert np.array_equal(_np(Vm), ref.bf16_round(model.gather(slots, 1, "read") + _np(vm)))
+
+
+F0 = np.float32(0)
+
+
+@pytest.mark.parametrize("H,T,news", [(8, 9000, 1), (3, 5000, 7), (1, 4096, 64), (2, 130, 130)])
+def test_many_runs_in_a_call(H, T, news):
+    """More rows than there are workgroups, in runs of one token, of some, of whole blocks: each block once."""
+    g = torch.Generator().manual_seed(T)
+    p = CacheParams(H=H, d=64, page=64, block=64)
+    runs = -(-T // news)
+    pool = torch.zeros(tuple(cache.alloc_cache(p, runs * (1 + (news - 1) // 64) + 1).shape), dtype=torch.uint8, device="cuda")
+    per = 1 + (news - 1) // 64
+    slots = torch.cat([torch.arange(min(news, T - news * r)) + r * 64 * per for r in range(runs)]).cuda()
+    K, V = _randn((T, H, 64), g).cuda(), _randn((T, H, 64), g).cuda()
+    cache.sagebwd_cache_append(K, V, slots, pool, p)
+    Kr, Vr = cache.sagebwd_cache_read(slots, pool, p)
+    block = slots // 64
+    for got, x in ((Kr, K), (Vr, V)):
+        top = torch.zeros((int(block.max()) + 1, H), device="cuda").scatter_reduce_(0, block[:, None].expand(-1, H), x.float().abs().amax(-1), "amax")[block]
+        code = (x.float() * (torch.full_like(top, 127.0) / top)[..., None]).round()
+        assert torch.equal(got, (code * (top / torch.full_like(top, 127.0))[..., None]).to(torch.bfloat16))
+
+
+def test_a_block_that_comes_whole_has_the_codes_of_the_int8_attention():
+    """Of 64 tokens at once the codes and scales are those that the INT8 forward's pre-pass makes of the same block, bit for bit."""
+    g = torch.Generator().manual_seed(3)
+    H, N, d = 2, 256, 128
+    p = CacheParams(H=H, d=d, block=64)
+    Q, K, V = (_randn((1, H, N, d), g).cuda() for _ in range(3))
+    sp = binding.SageParams(1, H, N, d, k_smooth=False)
+    ws = binding.alloc_workspace(sp)
+    binding.sagebwd_fwd(Q, K, V, sp, ws)
+    pool = cache.alloc_cache(p, N // 64)
+    cache.sagebwd_cache_append(K[0].transpose(0, 1), V[0].transpose(0, 1), torch.arange(N, device="cuda"), pool, p)
+    parts = [[ref8.decode(pool[n, h].cpu().numpy(), d, 64) for n in range(N // 64)] for h in range(H)]
+    for which, tensor in ((0, binding.TENSOR_K), (1, binding.TENSOR_V)):
+        codes, scales = binding.sagebwd_export_quantized(sp, ws, tensor)
+        for h in range(H):
+            for n in range(N // 64):
+                assert np.array_equal(parts[h][n][which], codes[0, h, 64 * n:64 * n + 64].cpu().numpy())
+                assert np.float32(parts[h][n][2 + which][0] / np.float32(127)) == scales[0, h, n].item()
+
+
+def test_blocks_of_every_magnitude_and_what_is_not_a_number():
+    """Zeros, ties, the ends of the range; infinities and NaN make their block of their head NaN until it begins anew, and no other."""
+    p, model = CacheParams(H=2, d=64, page=32, block=32), ref8.Pages(2, 64, 32, 32)
+    pool = torch.full(tuple(cache.alloc_cache(p, 24).shape), 0xFF, dtype=torch.uint8, device="cuda")
+    before = pool.clone()
+
+    def store(x, slots):
+        x = torch.tensor(np.array(x, np.float32)).to(torch.bfloat16)
+        K = torch.stack([x, x.flip(-1) * 0.5], dim=1).cuda()
+        cache.sagebwd_cache_append(K, K, _slots(slots), pool, p)
+        model.append(_np(K), _np(K), slots)
+
+    line = np.linspace(-1, 1, 64)
+    for n, e in enumerate((-133, -101, -100, -99, -60, 0, 60, 126, 127)):
+        for t in range(3):                    # (growing token by token)
+            store([line * 2.0 ** (e + t - 2 if e > 0 else e + t)], [32 * n + t])
+    store([np.zeros(64), np.full(64, 3.5), np.where(np.arange(64) % 2 == 0, 127.0, np.arange(64) % 41 / 2)], [320, 321, 322])      # scale 1: ties
+    for n, bad in ((11, np.inf), (12, -np.inf), (13, np.nan)):
+        x = np.array(line)
+        x[40] = bad
+        store([line, x, line], [32 * n, 32 * n + 1, 32 * n + 2])
+        store([line], [32 * n + 3])
+    _same(pool, model, p, range(2), before)
+    slots = [s for n in range(14) for s in range(32 * n, 32 * n + 3) if (s // 32, 0, 0) in model.blocks and s % 32 < model.blocks[s // 32, 0, 0].held]
+    Kr, Vr = cache.sagebwd_cache_read(_slots(slots), pool, p)
+    want = ref.bf16_round(model.gather(slots, 0, "read"))
+    assert np.array_equal(_np(Kr), want, equal_nan=True) and np.array_equal(_np(Vr), want, equal_nan=True)
+    assert np.isnan(want[-9:]).all() and np.isfinite(want[:-9]).any()
+    store([line, line], [32 * 11, 32 * 11 + 1])          # begins anew
+    Kr, _ = cache.sagebwd_cache_read(_slots([32 * 11, 32 * 11 + 1]), pool, p)
+    assert torch.isfinite(Kr).all()
+
+
+def test_slots_outside_the_pool_are_skipped_and_read_as_zeros():
+    p = CacheParams(H=2, d=128, page=32, block=32)
+    g = torch.Generator().manual_seed(3)
+    pool = torch.full(tuple(cache.alloc_cache(p, 2).shape), 0x77, dtype=torch.uint8, device="cuda")
+    K = _randn((8, 2, 128), g).cuda()
+    slots = _slots([-1, 64, 1 << 40, -(1 << 50), 0, 63, 64, (1 << 63) - 1])
+    before = pool.clone()
+    cache.sagebwd_cache_append(K, K, slots, pool, p)
+    Kr, Vr = cache.sagebwd_cache_read(slots, pool, p)
+    out = [0, 1, 2, 3, 6, 7]
+    assert (Kr[out] == 0).all() and (Vr[out] == 0).all() and (Kr[4] != 0).any()
+    assert (pool[0] != before[0]).sum().item() <= 2 * (2 * 128 + 8)
+    cache.sagebwd_cache_append(K[:0], K[:0], slots[:0], pool, p)
+
+
+def test_dropped_tokens_are_written_over():
+    """Drafted tokens that were taken back: the block keeps its magnitude, the tokens before them theirs codes."""
+    g = torch.Generator().manual_seed(4)
+    p, model = CacheParams(H=1, d=64, page=64, block=64), ref8.Pages(1, 64, 64, 64)
+    pool = torch.zeros(tuple(cache.alloc_cache(p, 1).shape), dtype=torch.uint8, device="cuda")
+    for at, n in ((0, 10), (10, 5), (12, 2), (14, 30), (20, 1), (0, 3)):
+        K, V = _randn((n, 1, 64), g, 1 + at), _randn((n, 1, 64), g)
+        cache.sagebwd_cache_append(K.cuda(), V.cuda(), torch.arange(at, at + n, device="cuda"), pool, p)
+        model.append(_np(K), _np(V), list(range(at, at + n)))
+        k, v, ka, va = ref8.decode(pool[0, 0].cpu().numpy(), 64, 64)
+        for which, codes, a in ((0, k, ka), (1, v, va)):
+            b = model.blocks[0, 0, which]
+            assert np.array_equal(codes[:at + n], b.codes[:at + n]) and a[0] == b.a == a[63]
+
+
+# ---- attention --------------------------------------------------------------------------------------------------
+
+class Filled:
+    """A cache of random tokens for requests of given lengths: pages in random order, every other byte of the pool 0xFF (magnitudes NaN)."""
+
+    def __init__(self, lens, p, g, extra=3, sigma=1.0, spare_columns=1, fill=0xFF):
+        self.p, self.lens = p, lens
+        used = [-(-n // p.page) for n in lens]
+        columns = max(used + [1]) + spare_columns
+        order = torch.randperm(sum(used) + extra, generator=g).tolist()
+        self.pool = torch.full(tuple(cache.alloc_cache(p, sum(used) + extra).shape), fill, dtype=torch.uint8, device="cuda")
+        table, slots = [], []
+        for n, u in zip(lens, used):
+            pages = [order.pop() for _ in range(u)]
+            table.append(pages + [-1] * (columns - u))
+            slots += [pages[t // p.page] * p.page + t % p.page for t in range(n)]
+        self.table, self.lengths = _i32(table).reshape(len(lens), columns), _i32(lens)
+        T = len(slots)
+        self.K, self.V = _randn((T, p.H, p.d), g, sigma), _randn((T, p.H, p.d), g)
+        self.slots = slots
+        self.at = np.concatenate([[0], np.cumsum(lens)]).astype(int)
+        self.store()
+
+    def store(self):
+        p = self.p
+        if self.slots:
+            cache.sagebwd_cache_append(self.K.cuda(), self.V.cuda(), _slots(self.slots), self.pool, p)
+        model = ref8.Pages(p.H, p.d, p.page, p.block)
+        model.append(_np(self.K), _np(self.V), self.slots)
+        self.k, self.v = model.gather(self.slots, 0), model.gather(self.slots, 1)
+
+
+def _attend(f, news, Hq, g, causal=True, sm_scale=0.0, v_mean=None, q=None, **kw):
+    T = sum(news)
+    q = _randn((T, Hq, f.p.d), g) if q is None else q
+    cu = np.concatenate([[0], np.cumsum(news)]).astype(int).tolist()
+    O, lse = cache.sagebwd_cache_attention(q.cuda(), f.pool, f.table, f.lengths, _i32(cu), f.p, max(news + [1]), causal=causal, sm_scale=sm_scale,
+                                           v_mean=v_mean, **kw)
+    return q, cu, O, lse
+
+
+def _check(f, q, cu, O, lse, causal, sm_scale=0.0, v_mean=None, requests=None):
+    """Tolerances, from the roundings: O is rounded to bf16 (2^-8 of it), every probability times its scale too (2^-8 of sum p |v|); a logit
+    is a sum of d products in FP32, each at most a |q| / 127 times a code of 127 (d roundings of 2^-24 of the whole, and six of its
+    scales), which moves a probability by as much; hardware exp2, log2: 2^-18.  The sums over the keys round once a product of 32 tokens."""
+    scale = sm_scale or f.p.d ** -0.5
+    O, lse = O.float().cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64)
+    for r in range(len(f.lens)) if requests is None else requests:
+        a, b = cu[r], cu[r + 1]
+        qs = _np(q[a:b]).astype(np.float64)
+        k, v = f.k[f.at[r]:f.at[r + 1]], f.v[f.at[r]:f.at[r + 1]]
+        want, wlse, A = ref.attention(qs, k, v, b - a, causal, scale, None if v_mean is None else _np(v_mean))
+        top = np.abs(k).max() if k.size else 0.0
+        e = scale * (f.p.d + 6) * 2.0 ** -24 * top * np.abs(qs).sum(-1) + 2.0 ** -18
+        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2 * e[..., None] + 2.0 ** -24 * (f.lens[r] / 32 + 40)) * A + 1e-30
+        err = np.abs(O[a:b] - want)
+        assert (err <= tol).all(), (r, f.lens[r], b - a, float((err / tol).max()), np.argwhere(err > tol)[:4].tolist())
+        none = np.isinf(wlse)
+        assert np.array_equal(lse[:, a:b][none], wlse[none]) and (O[a:b].transpose(1, 0, 2)[none] == 0).all()
+        le = np.abs(lse[:, a:b][~none] - wlse[~none])
+        assert (le <= (e.T + 2.0 ** -22 * (1 + np.abs(wlse)) + 2.0 ** -24 * (f.lens[r] / 32 + 40))[~none]).all(), (r, float(le.max()))
+
+
+LENGTHS = [
+    ([1], [1]), ([0], [1]), ([33], [1]), ([500, 1, 130, 31], [1, 1, 1, 1]),
+    ([3, 0, 40, 700, 64, 128], [2, 3, 5, 1, 4, 0]),       # a request shorter than its new tokens, an empty one, one without new tokens
+    ([260, 90], [17, 3]), ([200, 1000], [1, 70]), ([300], [300]), ([70, 1, 513, 129], [70, 1, 200, 129]),
+]
+
+
+@pytest.mark.parametrize("lens,news", LENGTHS)
+@pytest.mark.parametrize("d,block,page,Hq,H", [(64, 32, 32, 1, 1), (64, 64, 128, 6, 2), (128, 32, 64, 8, 1), (128, 64, 256, 10, 5), (128, 32, 32, 17, 1)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_against_64_bits(lens, news, d, block, page, Hq, H, causal):
+    g = torch.Generator().manual_seed(sum(lens) + d + Hq)
+    f = Filled(lens, CacheParams(H=H, d=d, page=page, block=block), g)
+    v_mean = torch.randn((H, d), generator=g).cuda() if page == 64 else None
+    sm = 0.3 if page == 32 else 0.0
+    q, cu, O, lse = _attend(f, news, Hq, g, causal=causal, sm_scale=sm, v_mean=v_mean)
+    _check(f, q, cu, O, lse, causal, sm, v_mean)
+
+
+@pytest.mark.parametrize("lens,news,d,block,Hq,H,causal", [
+    ([3000], [530], 128, 64, 8, 2, True), ([700], [520], 64, 32, 4, 1, False), ([2100, 60], [1024, 3], 128, 32, 4, 2, True),        # unpacked beforehand
+    ([20000], [1], 128, 64, 4, 1, True), ([9000, 30], [5, 1], 64, 64, 8, 2, True), ([9000], [7], 128, 32, 4, 1, False),            # few rows, divided
+    ([3000, 400, 2999], [12, 9, 1], 128, 64, 4, 1, True), ([2600, 700], [30, 25], 64, 32, 8, 2, False), ([1500], [100], 128, 32, 2, 2, True),      # span
+    ([5000], [60], 64, 64, 16, 2, True), ([1200], [200], 128, 64, 6, 2, True),
+])
+def test_long_requests_in_every_form(lens, news, d, block, Hq, H, causal):
+    g = torch.Generator().manual_seed(sum(lens) + d)
+    f = Filled(lens, CacheParams(H=H, d=d, page=64, block=block), g)
+    q, cu, O, lse = _attend(f, news, Hq, g, causal=causal)
+    _check(f, q, cu, O, lse, causal)
+    # and under a table much wider than the requests are long, with another workspace
+    f.table = torch.nn.functional.pad(f.table, (0, 300), value=-1)
+    q, cu, O, lse = _attend(f, news, Hq, g, causal=causal, q=q)
+    _check(f, q, cu, O, lse, causal)
+
+
+@pytest.mark.parametrize("d,block,page,Hq,H,n,L", [(64, 32, 32, 4, 4, 1, 777), (128, 64, 64, 4, 1, 1, 1025), (128, 32, 64, 32, 2, 3, 300), (64, 64, 256, 16, 2, 40, 333),
+                                                   (128, 64, 128, 8, 2, 150, 400), (128, 32, 64, 4, 1, 520, 600)])
+def test_every_token_is_weighed_alone(d, block, page, Hq, H, n, L):
+    """One query row in turn points at one key so sharply that its value alone comes out: a token left out, read twice or given another's
+    scale shows whole."""
+    g = torch.Generator().manual_seed(L)
+    f = Filled([L], CacheParams(H=H, d=d, page=page, block=block), g)
+    G = Hq // H
+    for start in range(0, L, n * G):
+        q = torch.zeros((n, Hq, d))
+        target = np.zeros((n, Hq), int)
+        for i in range(n):
+            for h in range(Hq):
+                t = (start + i * G + h % G) % L
+                target[i, h] = t
+                q[i, h] = torch.tensor(f.k[t, h // G] * 8)
+        _, _, O, lse = _attend(f, [n], Hq, g, causal=False, sm_scale=1.0, q=q.to(torch.bfloat16))
+        O = _np(O)
+        for h in range(Hq):
+            want = f.v[target[:, h], h // G]
+            # (another key's logit is 8 |k|^2 less 8 k.k' below: hundreds; P times the scale and O are rounded to bf16)
+            assert np.abs(O[:, h] - want).max() <= 2.0 ** -7 * np.abs(want).max()
+        if start > 6 * n * G:
+            break
+
+
+@pytest.mark.parametrize("L,n,d,Hq,block", [(100, 9, 128, 2, 32), (100, 40, 64, 4, 32), (700, 60, 128, 4, 64), (600, 300, 128, 2, 32), (900, 600, 64, 8, 64), (700, 400, 64, 2, 64)])
+def test_the_mask_hides_blocks_that_are_not_numbers(L, n, d, Hq, block):
+    """A block of keys, and one of values, that are NaN are seen by the rows whose mask lets them see some of it, and by no other."""
+    g = torch.Generator().manual_seed(8)
+    f = Filled([L], CacheParams(H=2, d=d, page=64, block=block), g)
+    first = (L - 2) // block * block
+    f.K[first + 1, 0, 3], f.V[first + 1, 1, 5] = math.nan, math.inf
+    f.store()
+    q, cu, O, lse = _attend(f, [n], Hq, g)
+    O, lse = _np(O), _np(lse)
+    G = Hq // 2
+    for i in range(n):
+        sees = L - n + i + 1
+        assert np.isnan(O[i]).all() if sees > first else np.isfinite(O[i]).all(), (i, sees)
+        assert np.isnan(lse[:G, i]).all() == (sees > first) and np.isfinite(lse[G:, i]).all()
+
+
+@pytest.mark.parametrize("fill", [0xFF, 0x7F, 0x80])
+def test_what_stands_behind_a_length_reaches_nothing(fill):
+    """Codes of -128, magnitudes that are NaN, infinite or negative in every place that holds no token."""
+    for lens, news, Hq in (([70, 5, 129], [1, 1, 1], 4), ([70, 65, 300], [20, 9, 40], 4), ([290, 33], [290, 33], 2), ([650], [600], 8)):
+        out = []
+        for value in (fill, 0):
+            g = torch.Generator().manual_seed(1)
+            f = Filled(lens, CacheParams(H=2, d=128, page=128, block=32), g, fill=value)
+            if value:
+                part = f.pool.view(torch.uint8)[:, :, 2 * 128 * 128:].reshape(f.pool.shape[0], 2, 4, 8)
+                inf = torch.tensor([0, 0, 0x80, 0x7F] * 2, dtype=torch.uint8, device="cuda")
+                if fill == 0x7F:
+                    part[(part == fill).all(-1)] = inf
+                    f.pool[:, :, 2 * 128 * 128:] = part.reshape(f.pool.shape[0], 2, 32)
+            out.append(_attend(f, news, Hq, g)[2:])
+        assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+
+
+@pytest.mark.parametrize("n,Hq", [(1, 4), (30, 4), (100, 4), (530, 8)])
+def test_pages_that_do_not_exist_are_not_attended_to(n, Hq):
+    g = torch.Generator().manual_seed(9)
+    f = Filled([640, 96], CacheParams(H=2, d=128, page=32, block=32), g)
+    q = _randn((n + 1, Hq, 128), g)
+    f.table[0, 3], f.table[0, 7], f.table[1, :3] = -1, f.pool.shape[0], _i32([-7, 1 << 30, -(1 << 31)])
+    keep = np.array([t for t in range(640) if t // 32 not in (3, 7)])
+    _, cu, O, lse = _attend(f, [n, 1], Hq, g, causal=False, q=q)
+    f.k, f.v, f.at = np.concatenate([f.k[keep], f.k[640:]]), np.concatenate([f.v[keep], f.v[640:]]), np.array([0, 576, 672])
+    _check(f, q, cu, O, lse, False, requests=[0])
+    assert (O[n] == 0).all() and torch.isinf(lse[:, n]).all()
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_batches(seed):
+    rng = np.random.default_rng(seed)
+    g = torch.Generator().manual_seed(seed)
+    d, block = int(rng.choice([64, 128])), int(rng.choice([32, 64]))
+    page = max(block, int(rng.choice([32, 64, 128, 256])))
+    H = int(rng.integers(1, 6))
+    Hq = H * int(rng.choice([1, 2, 3, 4, 7, 8, 16, 33, 64]))
+    R = int(rng.integers(1, 40))
+    lens = [int(x) for x in np.exp(rng.uniform(0, math.log(1500), R))]
+    kind = rng.choice(["decode", "few", "mixed"])
+    news = [1 if kind == "decode" or (kind == "mixed" and rng.random() < 0.8) else int(rng.integers(0, 7 if kind == "few" else 200)) for _ in range(R)]
+    if Hq * sum(n * a for n, a in zip(news, lens)) > 4e7:
+        news = [min(n, 2) for n in news]
+    if sum(news) == 0:
+        news[0] = 1
+    f = Filled(lens, CacheParams(H=H, d=d, page=page, block=block), g, sigma=float(rng.choice([0.1, 1.0, 4.0])))
+    causal = bool(rng.integers(2))
+    v_mean = torch.randn((H, d), generator=g).cuda() if rng.integers(2) else None
+    q, cu, O, lse = _attend(f, news, Hq, g, causal=causal, v_mean=v_mean)
+    check = rng.permutation(R)[:6].tolist()
+    _check(f, q, cu, O, lse, causal, 0.0, v_mean, requests=check)
+
+
+def test_blocks_of_zeros_and_of_very_different_scales():
+    """Keys of zeros (scale 0) beside others, behind the mask too; values from 2^-90 to 2^90 in neighbouring blocks."""
+    for n, Hq in ((1, 2), (40, 2), (300, 2), (520, 8)):
+        g = torch.Generator().manual_seed(n)
+        f = Filled([700], CacheParams(H=2, d=128, page=64, block=32), g)
+        f.K[32:64], f.K[640:], f.V[96:128] = 0, 0, 0
+        f.K[:, 1] *= 30
+        for b in range(4, 20):
+            f.V[32 * b:32 * b + 32] = (f.V[32 * b:32 * b + 32].float() * 2.0 ** (9 * (b - 12))).to(torch.bfloat16)
+        f.store()
+        q, cu, O, lse = _attend(f, [n], Hq, g)
+        _check(f, q, cu, O, lse, True)
+
+
+def test_strided_queries_rows_behind_the_last_request_and_a_dirty_workspace():
+    g = torch.Generator().manual_seed(6)
+    p = CacheParams(H=2, d=128, page=64, block=64)
+    for lens, news in (([200, 1500, 64], [1, 1, 1]), ([200, 900, 64], [30, 1, 64]), ([700, 64], [520, 1])):
+        f = Filled(lens, p, g)
+        T, R = sum(news), len(lens)
+        qkv = _randn((T + 5, 8 + 4, 128), g).cuda()
+        q = qkv[:, 2:10]
+        q[T:] = math.nan
+        cu = _i32(np.concatenate([[0], np.cumsum(news)]).tolist())
+        O, lse = torch.full((T + 5, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((8, T + 5), 7.0, device="cuda")
+        n = cache.cache_workspace_bytes(p, R, T + 5, 8, f.table.shape[1], max(news))
+        for fill in (0xFF, 0x00):
+            ws = torch.full((n,), fill, dtype=torch.uint8, device="cuda")
+            O.fill_(7.0), lse.fill_(7.0)
+            cache.sagebwd_cache_attention(q, f.pool, f.table, f.lengths, cu, p, max(news), O=O, LSE=lse, workspace=ws)
+            assert (O[T:] == 7).all() and (lse[:, T:] == 7).all()
+            _check(f, q[:T].cpu(), cu.tolist(), O[:T], lse[:, :T], True)
+        if n > 256:
+            with pytest.raises(binding.SageError) as e:
+                cache.sagebwd_cache_attention(q, f.pool, f.table, f.lengths, cu, p, max(news), workspace=ws[:-256])
+            assert e.value.status == -3
+
+
+def test_offsets_beyond_32_bits():
+    p = CacheParams(H=8, d=128, page=64, block=32)
+    page_bytes = cache.cache_page_bytes(p)
+    pages = (5 << 30) // page_bytes
+    g = torch.Generator().manual_seed(2)
+    small = Filled([300, 40], p, g)
+    big = torch.empty((pages, p.H, page_bytes // p.H), dtype=torch.uint8, device="cuda")
+    shift = pages - small.pool.shape[0]
+    big[shift:] = 0xFF
+    table = torch.where(small.table >= 0, small.table + shift, small.table)
+    slots = _slots(small.slots) + shift * p.page
+    cache.sagebwd_cache_append(small.K.cuda(), small.V.cuda(), slots, big, p)
+    assert torch.equal(big[shift:], small.pool)
+    a, b = cache.sagebwd_cache_read(slots, big, p), cache.sagebwd_cache_read(_slots(small.slots), small.pool, p)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    for news in ([1, 1], [20, 3], [100, 3], [260, 40]):
+        q, cu, O, lse = _attend(small, news, 16, g)
+        O2, lse2 = cache.sagebwd_cache_attention(q.cuda(), big, table, small.lengths, _i32(cu), p, max(news))
+        assert torch.equal(O, O2) and torch.equal(lse, lse2)
+
+
+def test_streams_repeats_and_two_calls_at_once():
+    g = torch.Generator().manual_seed(12)
+    p = CacheParams(H=2, d=128, block=64)
+    f1, f2 = Filled([900, 3000, 20], p, g), Filled([2500], p, g)
+    q1, cu1, O1, l1 = _attend(f1, [1, 2, 1], 8, g)
+    q2, cu2, O2, l2 = _attend(f2, [70], 8, g)
+    d1, d2, c1, c2 = q1.cuda(), q2.cuda(), _i32(cu1), _i32(cu2)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(4):
+        with torch.cuda.stream(s1):
+            a = cache.sagebwd_cache_attention(d1, f1.pool, f1.table, f1.lengths, c1, p, 2)
+        with torch.cuda.stream(s2):
+            b = cache.sagebwd_cache_attention(d2, f2.pool, f2.table, f2.lengths, c2, p, 70)
+        torch.cuda.synchronize()
+        assert torch.equal(a[0], O1) and torch.equal(a[1], l1) and torch.equal(b[0], O2) and torch.equal(b[1], l2)
+
+
+# ---- a decoding loop --------------------------------------------------------------------------------------------
+
+class Loop:
+    def __init__(self, R, p, Hq, columns, pages):
+        self.R, self.p, self.Hq = R, p, Hq
+        self.lengths, self.table = _i32([0] * R), torch.full((R, columns), -1, dtype=torch.int32, device="cuda")
+        self.free_pages, self.free_count = _i32(list(range(pages))), _i32([pages])
+        self.pool = torch.full(tuple(cache.alloc_cache(p, pages).shape), 0xFF, dtype=torch.uint8, device="cuda")
+        self.inv_freq = (10000.0 ** (-torch.arange(p.d // 2, dtype=torch.float64) / (p.d // 2))).float().cuda()
+
+    def step(self, qkv, added, rows, max_new):
+        p, H, Hq = self.p, self.p.H, self.Hq
+        plan = cache.sagebwd_cache_plan(self.lengths, added, self.table, self.free_pages, self.free_count, p, rows)
+        Q, K = sage_rotary(qkv[:, :Hq], qkv[:, Hq:Hq + H], plan.positions, self.inv_freq)
+        V = qkv[:, Hq + H:]
+        cache.sagebwd_cache_append(K, V, plan.slots, self.pool, p)
+        O, lse = cache.sagebwd_cache_attention(Q, self.pool, self.table, plan.lengths, plan.cu_new, p, max_new)
+        self.lengths.copy_(plan.lengths)
+        self.free_count.copy_(plan.free_left)
+        return O, lse, Q, K, V, plan
+
+
+def test_prompts_and_decoding_over_blocks_that_grow():
+    """Whole steps of the operators; what the cache holds at every step is the quantiser's, token by token."""
+    g = torch.Generator().manual_seed(21)
+    p = CacheParams(H=2, d=128, page=64, block=64)
+    loop, model = Loop(3, p, 4, 8, 20), ref8.Pages(2, 128, 64, 64)
+    slots = [[], [], []]
+    for added in [[70, 0, 5], [1, 130, 1]] + [[1, 1, 1]] * 4 + [[0, 9, 62], [2, 1, 1]]:
+        rows = sum(added)
+        qkv = _randn((rows, 4 + 4, 128), g).cuda()
+        O, lse, Q, K, V, plan = loop.step(qkv, _i32(added), rows, max(added))
+        new = plan.slots.tolist()
+        model.append(_np(K), _np(V), new)
+        at = 0
+        for r, n in enumerate(added):
+            slots[r] += new[at:at + n]
+            one = type("One", (), dict(p=p, lens=[len(slots[r])], k=model.gather(slots[r], 0), v=model.gather(slots[r], 1), at=[0, len(slots[r])]))
+            _check(one, Q[at:at + n], [0, n], O[at:at + n], lse[:, at:at + n], True)
+            at += n
+
+
+def test_a_captured_step_replayed_against_the_eager_one():
+    g = torch.Generator().manual_seed(5)
+    R, Hq, p = 4, 8, CacheParams(H=2, d=128, page=32, block=32)
+    loops = [Loop(R, p, Hq, columns=40, pages=120) for _ in range(2)]
+    prompt = [100, 31, 700, 64]
+    qkv = _randn((sum(prompt), Hq + 4, 128), g).cuda()
+    for loop in loops:
+        loop.step(qkv, _i32(prompt), sum(prompt), max(prompt))
+    one = _i32([1] * R)
+    new = _randn((R, Hq + 4, 128), g).cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for loop in loops:                       # (the first warms up; both have the token that is taken back, so that blocks hold the same)
+        with torch.cuda.stream(side):
+            loop.step(new, one, R, 1)
+            cache.sagebwd_cache_trim(_i32(prompt), loop.lengths, loop.table, loop.free_pages, loop.free_count, p)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        O, lse, *_ = loops[0].step(new, one, R, 1)
+    for step in range(40):                   # (across the ends of pages)
+        new.copy_(_randn((R, Hq + 4, 128), g))
+        graph.replay()
+        want, wl, *_ = loops[1].step(new, one, R, 1)
+        torch.cuda.synchronize()
+        assert torch.equal(O, want) and torch.equal(lse, wl), step
+        assert torch.equal(loops[0].lengths, loops[1].lengths) and torch.equal(loops[0].table, loops[1].table)
