@@ -108,11 +108,49 @@ int sagebwd_cache_plan(const int32_t* held, const int32_t* added, int32_t* block
  * stack; the first request's first page is on top, so that trim after plan leaves the stack as it was.  lengths,
  * block_table (freed entries become -1), free_pages and free_count are changed in place.  A keep[r] outside 0 ..
  * lengths[r] leaves the request alone.  Entries that are not pages (negative) give none back.  (Pages beyond `capacity` are lost: the
- * stack has to hold every page.  A page that stands in two requests' rows comes back from each: who shares pages counts them and trims
- * the last one alone.)  Bounds as of plan.
+ * stack has to hold every page.  A page that stands in two requests' rows comes back from each: who shares pages calls free, below.)  Bounds as of plan.
  */
 int sagebwd_cache_trim(const int32_t* keep, int32_t* lengths, int32_t* block_table, int32_t* free_pages, int32_t* free_count,
                        int32_t R, int32_t columns, int32_t page, int32_t capacity, void* stream);
+
+/*
+ * Pages that requests share: several rows of the table may name one page, of whichever format.  `shares`, int32 [3, pages], counts them: row 0
+ * has the holders of a page beyond its first (0 for a page of one request and for a free one, so that plan needs no shares); the other
+ * rows are the calls' own and hold zeros between them.  All zeros at the start; who shares pages gives them back with free, not with trim.
+ * A call's lengths, table, stack and shares belong together; two calls on them are not in flight at a time.  An entry of the table outside
+ * 0 .. pages - 1 has no holders.  `pages` is at most 2^28; the other bounds are those of plan.  Every call repeats itself bit for bit.
+ *
+ * free: as trim (request r keeps its first keep[r] tokens; outside 0 .. lengths[r] it is left alone), but a page goes on the stack when
+ * its last holder gives it up.  Of the pages that a call (or fork) frees the one with the lowest number ends on top.
+ *
+ * fork: request r goes on from what parents[r] holds at the call (a prompt's samples, the beams of a search): its length and its row
+ * become its parent's, whose pages it then shares; what it held before is given up as by free.  parents[r] = r, or outside 0 .. R - 1:
+ * the request goes on as it is.  A parent may itself be forked by the call.  Nothing is copied.
+ *
+ * own: before tokens are added (before plan).  A request with added[r] > 0 whose last page is not full and has other holders gets a page of
+ * its own with the same bytes, from the stack, and the table names that; if all holders of a page are such requests the last of them
+ * keeps it.  Requests are served in order: behind one for which no page is left none gets one.  added_out int32 [R] (may be `added`): added[r], or 0
+ * where a page was wanted and not got: that request must not add tokens, and plan then grants it none.
+ *
+ * compact: moves the pages in use (those that a request's row names for its length) to 0 .. used - 1: pages from used on are copied to
+ * unused ones below, in the order of their numbers, the others stay.  Out: table_out (may be `block_table`; entries behind a
+ * request's length and such as are no pages become -1), free_pages (pages - 1 first, `used` on top, -1 behind; capacity >= pages),
+ * free_count, shares (row 0 out; the other rows zeros as ever), used int32 [1].  A page that no row names is free afterwards, whoever
+ * meant to keep it.  What the pages from `used` on hold is left as it was.
+ */
+int sagebwd_cache_free(const int32_t* keep, int32_t* lengths, int32_t* block_table, int32_t* free_pages, int32_t* free_count, int32_t* shares, int32_t R,
+                       int32_t columns, int32_t page, int32_t capacity, int32_t pages, void* stream);
+int sagebwd_cache_fork_workspace_bytes(int32_t R, int32_t columns, size_t* bytes);
+int sagebwd_cache_fork(const int32_t* parents, int32_t* lengths, int32_t* block_table, int32_t* free_pages, int32_t* free_count, int32_t* shares, int32_t R,
+                       int32_t columns, int32_t page, int32_t capacity, int32_t pages, void* workspace, size_t workspace_bytes, void* stream);
+/* (the workspace of own: 8 R bytes, 16-byte aligned) */
+int sagebwd_cache_own(const int32_t* added, const int32_t* lengths, int32_t* block_table, const int32_t* free_pages, int32_t* free_count, int32_t* shares,
+                      int32_t R, int32_t columns, int32_t capacity, const sagebwd_cache_params* params, void* pool, int32_t* added_out, void* workspace,
+                      size_t workspace_bytes, void* stream);
+int sagebwd_cache_compact_workspace_bytes(int32_t pages, size_t* bytes);
+int sagebwd_cache_compact(const int32_t* lengths, const int32_t* block_table, int32_t R, int32_t columns, const sagebwd_cache_params* params, void* pool,
+                          int32_t* table_out, int32_t* free_pages, int32_t capacity, int32_t* free_count, int32_t* shares, int32_t* used, void* workspace,
+                          size_t workspace_bytes, void* stream);
 
 /*
  * New keys and values into the cache, and what it holds out of it.  K, V: bf16 [T, H, d] with strides in elements

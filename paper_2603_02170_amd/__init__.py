@@ -12,13 +12,19 @@ from .binding import (  # noqa: F401
     sagebwd_strerror,
 )
 from .cache import (  # noqa: F401
+    CacheCompaction,
     CacheParams,
     CachePlan,
     alloc_cache,
+    alloc_shares,
     cache_page_bytes,
     cache_workspace_bytes,
     sagebwd_cache_append,
     sagebwd_cache_attention,
+    sagebwd_cache_compact,
+    sagebwd_cache_fork,
+    sagebwd_cache_free,
+    sagebwd_cache_own,
     sagebwd_cache_plan,
     sagebwd_cache_read,
     sagebwd_cache_trim,

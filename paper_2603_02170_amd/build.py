@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libsagebwd.so")
 HOST = os.path.join(HERE, "_sage_host.so")
-SOURCES = ("sagebwd_api", "serve_api", "serve8_api")
+SOURCES = ("sagebwd_api", "serve_api", "serve8_api", "pages_api")
 
 
 def hipcc_path() -> str:
@@ -34,7 +34,7 @@ def _run(cmd, verbose: bool) -> None:
 
 
 def build(verbose: bool = True) -> str:
-    """Compile csrc/sagebwd_api.hip, csrc/serve_api.hip and csrc/serve8_api.hip (which include every kernel) into libsagebwd.so, and csrc/torch_host.cpp
+    """Compile csrc/sagebwd_api.hip, serve_api.hip, serve8_api.hip and pages_api.hip (which include every kernel) into libsagebwd.so, and csrc/torch_host.cpp
     (host code only: what stands between Python's tensors and that library) into _sage_host.so."""
     common = [
         hipcc_path(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -7,6 +7,13 @@
     sagebwd_cache_append(K, V, plan.slots, cache, p)
     O, LSE = sagebwd_cache_attention(Q, cache, block_table, plan.lengths, plan.cu_new, p, max_new=1)
 
+Requests that share pages (samples of one prompt, the beams of a search):
+
+    shares = alloc_shares(pages=4096)                        # holders of each page
+    sagebwd_cache_fork(parents, lengths, block_table, free_pages, free_count, shares, p)    # go on from another request's tokens
+    added = sagebwd_cache_own(added, lengths, block_table, free_pages, free_count, shares, cache, p)    # before each plan
+    sagebwd_cache_free(keep, lengths, block_table, free_pages, free_count, shares, p)       # in place of trim
+
 Tensors are packed: Q is bf16 [tokens, query heads, d], K and V are bf16 [tokens, H, d], the requests' new tokens one after the other.
 They may be slices of one projection's output (adjacent channels, strides that are multiples of 8, rows that begin on 16 bytes).
 Formats, arithmetic and bounds of device data: include/sagebwd_serve.h.  Like the calls of `binding`, these are not differentiable,
@@ -23,7 +30,8 @@ import torch
 from . import binding
 
 EXPORTS = ("sagebwd_cache_page_bytes", "sagebwd_cache_plan", "sagebwd_cache_trim", "sagebwd_cache_append", "sagebwd_cache_read",
-           "sagebwd_cache_workspace_bytes", "sagebwd_cache_attention", "sagebwd_rotary")
+           "sagebwd_cache_workspace_bytes", "sagebwd_cache_attention", "sagebwd_rotary", "sagebwd_cache_free", "sagebwd_cache_fork",
+           "sagebwd_cache_fork_workspace_bytes", "sagebwd_cache_own", "sagebwd_cache_compact", "sagebwd_cache_compact_workspace_bytes")
 
 
 class _CCacheParams(ctypes.Structure):
@@ -75,6 +83,42 @@ def sagebwd_cache_plan(held, added, block_table, free_pages, free_count, p: Cach
 def sagebwd_cache_trim(keep, lengths, block_table, free_pages, free_count, p: CacheParams) -> None:
     """Requests keep their first keep[r] tokens (0: done); freed pages go back on the stack.  In place."""
     binding._host().cache_trim(keep, lengths, block_table, free_pages, free_count, p.page)
+
+
+class CacheCompaction(NamedTuple):
+    block_table: torch.Tensor  # int32 [R, columns]: the pages' new numbers
+    free_pages: torch.Tensor   # int32 [pages]: the stack, the lowest on top
+    free_count: torch.Tensor   # int32 [1]
+    shares: torch.Tensor       # int32 [3, pages]
+    used: torch.Tensor         # int32 [1]: pages in use, which are 0 .. used - 1
+
+
+def alloc_shares(pages: int, device="cuda"):
+    """The holders of a pool's pages, int32 [3, pages]: row 0 has those beyond a page's first, the others are the calls' own.  Zeros at the start."""
+    return torch.zeros((3, pages), dtype=torch.int32, device=device)
+
+
+def sagebwd_cache_free(keep, lengths, block_table, free_pages, free_count, shares, p: CacheParams) -> None:
+    """`sagebwd_cache_trim` where requests share pages: a page goes back on the stack when its last holder gives it up.  In place."""
+    binding._host().cache_free(keep, lengths, block_table, free_pages, free_count, shares, p.page)
+
+
+def sagebwd_cache_fork(parents, lengths, block_table, free_pages, free_count, shares, p: CacheParams) -> None:
+    """Request r goes on from what request parents[r] holds (int32; itself, or any number that is no request's: as it is) and gives up what it
+    held.  The pages are shared and nothing is copied: `sagebwd_cache_own` does that where a request writes.  In place."""
+    binding._host().cache_fork(parents, lengths, block_table, free_pages, free_count, shares, p.page)
+
+
+def sagebwd_cache_own(added, lengths, block_table, free_pages, free_count, shares, cache, p: CacheParams, out=None):
+    """Before a step's plan: a request that is about to add tokens to a page which others hold gets a copy of it from the stack.  Returns added
+    (int32 [R]), with 0 for a request that wanted a page when none was left: what the plan is given.  Everything else in place."""
+    return binding._host().cache_own(added, lengths, block_table, free_pages, free_count, shares, cache, p.H, p.d, p.page, p.group, p.block, out)
+
+
+def sagebwd_cache_compact(lengths, block_table, cache, p: CacheParams, out=None) -> CacheCompaction:
+    """Moves the pages in use to the front of the pool (in place) and returns the table that names them there, with the stack and shares that go
+    with it.  `out` (a CacheCompaction) may bring their tensors, the inputs' own among them; what no row of the table names is free afterwards."""
+    return CacheCompaction._make(binding._host().cache_compact(lengths, block_table, cache, p.H, p.d, p.page, p.group, p.block, out))
 
 
 def sagebwd_cache_append(K, V, slots, cache, p: CacheParams, k_mean=None, v_mean=None) -> None:

@@ -1,0 +1,344 @@
+// Pages that requests share: freeing, forking, owning, compacting (gfx950 only).  What the calls do is in sagebwd_serve.h.
+//
+// shares [3, pages]: the holders of a page beyond its first; a bit for each page that lost one; nothing (own: who asks).  Holders are
+// counted with integer atomics, whose order changes nothing; what depends on an order (the stack of free pages, who keeps a page) is decided
+// by page numbers or request numbers afterwards.
+//
+// Steps: a wave has a request's row of the table; one workgroup settles the stack.  Small calls are one launch of one workgroup.
+#pragma once
+
+#include "cache_kernels.h"
+
+namespace sage {
+
+struct PagesArgs {
+  const int32_t* asked;            // keep, parents or added
+  int32_t *lengths, *table, *free_pages, *free_count, *shares;
+  int32_t *rows, *new_lengths;     // fork: the new rows of the table
+  int32_t* granted;                // own: added, or 0
+  int2* moves;                     // own, compact: page from, page to (own: -1 for none)
+  int R, columns, page_shift, capacity, pages;
+  __device__ __forceinline__ uint32_t* bits() const { return (uint32_t*)shares + pages; }
+  __device__ __forceinline__ int pages_of(int length) const {
+    return (int)min(((int64_t)length + (1 << page_shift) - 1) >> page_shift, (int64_t)columns);
+  }
+  __device__ __forceinline__ bool is_page(int entry) const { return (unsigned)entry < (unsigned)pages; }
+};
+
+// What another step of the same workgroup, or another workgroup's atomic, wrote.
+__device__ __forceinline__ int now_in(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+__device__ __forceinline__ void lose_page(const PagesArgs& a, int entry) {
+  atomicSub(a.shares + entry, 1);
+  atomicOr(a.bits() + (entry >> 5), 1u << (entry & 31));
+}
+
+// Pages whose last holder went go on the stack, the lowest last.  1024 threads; 65536 pages at a time, from the highest: each wave finds the ones
+// among 64, a lane a page, then their places are summed.
+struct SettleScratch {
+  uint64_t freed[1024];
+  unsigned sums[16][1], total;
+};
+__device__ __forceinline__ void settle_pages(const PagesArgs& a, SettleScratch& s) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int groups = (a.pages + 63) >> 6, words = (a.pages + 31) >> 5;
+  int64_t count = max(0, min(now_in(a.free_count), a.capacity));
+  for (int end = groups; end > 0; end -= 1024) {
+    const int here = min(end, 1024);
+    for (int i = wave; i < here; i += 16) {
+      const int group = end - 1 - i, page = 64 * group + lane;
+      const uint32_t word = 2 * group + (lane >> 5) < words ? (uint32_t)now_in((const int32_t*)a.bits() + 2 * group + (lane >> 5)) : 0;
+      const bool lost = word >> (lane & 31) & 1;
+      if ((lane & 31) == 0 && word != 0) a.bits()[2 * group + (lane >> 5)] = 0;
+      const bool freed = lost && page < a.pages && now_in(a.shares + page) < 0;
+      if (freed) a.shares[page] = 0;
+      const uint64_t mask = __ballot(freed);
+      if (lane == 0) s.freed[i] = mask;
+    }
+    __syncthreads();
+    unsigned to[1] = {tid < here ? (unsigned)__popcll(s.freed[tid]) : 0};
+    block_scan<16>(to, s.sums);
+    if (tid == 1023) s.total = to[0];
+    if (tid < here) {
+      uint64_t mask = s.freed[tid];
+      int64_t at = count + to[0] - __popcll(mask);
+      while (mask != 0) {
+        const int bit = 63 - __builtin_clzll(mask);
+        mask ^= 1ull << bit;
+        if (at < a.capacity) a.free_pages[at] = 64 * (end - 1 - tid) + bit;
+        at++;
+      }
+    }
+    __syncthreads();
+    count += s.total;
+    __syncthreads();
+  }
+  if (tid == 0) a.free_count[0] = (int)min(count, (int64_t)a.capacity);
+}
+
+// ---- free ----------------------------------------------------------------------------------------------------------
+// A wave: what a request gives up.
+__device__ __forceinline__ void free_row(const PagesArgs& a, int r) {
+  const int lane = threadIdx.x & 63, length = a.lengths[r], keep = a.asked[r];
+  if (keep < 0 || keep > length) return;
+  int32_t* row = a.table + (size_t)r * a.columns;
+  const int end = a.pages_of(length);
+  for (int c = a.pages_of(keep) + lane; c < end; c += 64) {
+    const int entry = row[c];
+    if (a.is_page(entry)) lose_page(a, entry);
+    row[c] = -1;
+  }
+  if (lane == 0) a.lengths[r] = keep;
+}
+__global__ __launch_bounds__(256) void cache_free_rows_kernel(PagesArgs a) {
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r < a.R) free_row(a, r);
+}
+__global__ __launch_bounds__(1024) void cache_settle_kernel(PagesArgs a) {
+  __shared__ SettleScratch s;
+  settle_pages(a, s);
+}
+__global__ __launch_bounds__(1024) void cache_free_kernel(PagesArgs a) {
+  __shared__ SettleScratch s;
+  for (int r = threadIdx.x >> 6; r < a.R; r += 16) free_row(a, r);
+  __threadfence_block();
+  __syncthreads();
+  settle_pages(a, s);
+}
+
+// ---- fork ----------------------------------------------------------------------------------------------------------
+// A wave: the row that a request goes on with, to `rows`, as a row may be another one's parent; pages that stay where they are count for nothing.
+__device__ __forceinline__ bool forked(const PagesArgs& a, int r) {
+  const int p = a.asked[r];
+  return p >= 0 && p < a.R && p != r;
+}
+__device__ __forceinline__ void fork_row(const PagesArgs& a, int r) {
+  if (!forked(a, r)) return;
+  const int lane = threadIdx.x & 63, p = a.asked[r], length = a.lengths[p];
+  const int32_t *from = a.table + (size_t)p * a.columns, *old = a.table + (size_t)r * a.columns;
+  int32_t* to = a.rows + (size_t)r * a.columns;
+  const int n = a.pages_of(length), had = a.pages_of(a.lengths[r]);
+  for (int c = lane; c < a.columns; c += 64) {
+    const int entry = c < n ? from[c] : -1, before = c < had ? old[c] : -1;
+    to[c] = entry;
+    if (entry == before) continue;
+    if (a.is_page(entry)) atomicAdd(a.shares + entry, 1);
+    if (a.is_page(before)) lose_page(a, before);
+  }
+  if (lane == 0) a.new_lengths[r] = length;
+}
+__device__ __forceinline__ void forked_row(const PagesArgs& a, int r) {
+  if (!forked(a, r)) return;
+  const int lane = threadIdx.x & 63;
+  for (int c = lane; c < a.columns; c += 64) a.table[(size_t)r * a.columns + c] = a.rows[(size_t)r * a.columns + c];
+  if (lane == 0) a.lengths[r] = a.new_lengths[r];
+}
+__global__ __launch_bounds__(256) void cache_fork_rows_kernel(PagesArgs a) {
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r < a.R) fork_row(a, r);
+}
+// the first workgroup settles, the others have 16 rows each
+__global__ __launch_bounds__(1024) void cache_forked_kernel(PagesArgs a) {
+  __shared__ SettleScratch s;
+  if (blockIdx.x == 0) {
+    settle_pages(a, s);
+    return;
+  }
+  const int r = (blockIdx.x - 1) * 16 + (threadIdx.x >> 6);
+  if (r < a.R) forked_row(a, r);
+}
+__global__ __launch_bounds__(1024) void cache_fork_kernel(PagesArgs a) {
+  __shared__ SettleScratch s;
+  for (int r = threadIdx.x >> 6; r < a.R; r += 16) fork_row(a, r);
+  __threadfence_block();
+  __syncthreads();
+  for (int r = threadIdx.x >> 6; r < a.R; r += 16) forked_row(a, r);
+  settle_pages(a, s);
+}
+
+// ---- own -----------------------------------------------------------------------------------------------------------
+// Who writes into a page that others hold gets a copy of it; if all its holders are about to write, the last of them keeps it.  One
+// workgroup; the copies are a launch of their own.
+__global__ __launch_bounds__(1024) void cache_own_kernel(PagesArgs a) {
+  __shared__ unsigned sums[16][1], total;
+  const int tid = threadIdx.x;
+  int32_t *asks = a.shares + a.pages, *last = asks + a.pages;      // of a page: how many are about to write, and 1 + the last of them
+  // the page that a request's next token goes into, if that has tokens
+  const auto page_of = [&](int r) {
+    const int length = a.lengths[r];
+    if (a.asked[r] <= 0 || length <= 0 || (length & ((1 << a.page_shift) - 1)) == 0 || length >> a.page_shift >= a.columns) return -1;
+    const int entry = a.table[(size_t)r * a.columns + (length >> a.page_shift)];
+    return a.is_page(entry) ? entry : -1;
+  };
+  for (int r = tid; r < a.R; r += 1024) {
+    const int entry = page_of(r);
+    if (entry < 0 || a.shares[entry] <= 0) continue;
+    atomicAdd(asks + entry, 1);
+    atomicMax(last + entry, r + 1);
+  }
+  __threadfence_block();
+  __syncthreads();
+  const unsigned count = (unsigned)max(0, min(a.free_count[0], a.capacity));
+  unsigned before = 0, taken = 0;
+  for (int base = 0; base < a.R; base += 1024) {
+    const int r = base + tid, entry = r < a.R ? page_of(r) : -1;
+    const bool wants = entry >= 0 && a.shares[entry] > 0;
+    const bool copies = wants && !(now_in(asks + entry) == a.shares[entry] + 1 && now_in(last + entry) == r + 1);
+    unsigned need[1] = {copies ? 1u : 0u};
+    block_scan<16>(need, sums);
+    if (tid == 1023) total = need[0];
+    const unsigned needs = min(before + need[0], kFull);
+    const bool granted = !wants || needs <= count;
+    if (r < a.R) {
+      a.granted[r] = granted ? a.asked[r] : 0;
+      int2 move = {entry, -1};
+      if (copies && granted) {
+        const int to = a.free_pages[count - needs];
+        a.table[(size_t)r * a.columns + (a.lengths[r] >> a.page_shift)] = to;
+        move.y = a.is_page(to) ? to : -2;      // (a stack of something else: nothing is copied there)
+      }
+      a.moves[r] = move;
+    }
+    __syncthreads();
+    before = min(before + total, kFull);
+    taken = min(before, count);
+    __syncthreads();
+  }
+  for (int r = tid; r < a.R; r += 1024) {
+    const int2 move = a.moves[r];
+    if (move.x < 0) continue;
+    asks[move.x] = 0;
+    last[move.x] = 0;
+    if (move.y != -1) atomicSub(a.shares + move.x, 1);
+  }
+  if (tid == 0) a.free_count[0] = (int)(count - taken);
+}
+
+// Pages are copied in pieces of 16 KiB, four loads of a thread in flight.
+constexpr int kCopyPiece = 16384;
+__device__ __forceinline__ void copy_piece(unsigned char* pool, size_t page_bytes, const int2& move, int piece) {
+  const unsigned char* from = pool + (size_t)move.x * page_bytes;
+  unsigned char* to = pool + (size_t)move.y * page_bytes;
+  const size_t at0 = (size_t)piece * kCopyPiece + threadIdx.x * 16;
+  v4i x[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    if (at0 + i * 4096 < page_bytes) x[i] = *(const v4i*)(from + at0 + i * 4096);
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    if (at0 + i * 4096 < page_bytes) *(v4i*)(to + at0 + i * 4096) = x[i];
+}
+__global__ __launch_bounds__(256) void cache_copy_pages_kernel(const int2* moves, unsigned char* pool, size_t page_bytes) {
+  const int2 move = moves[blockIdx.x];
+  if (move.y >= 0) copy_piece(pool, page_bytes, move, blockIdx.y);
+}
+
+// ---- compact -------------------------------------------------------------------------------------------------------
+struct CompactArgs {
+  PagesArgs p;               // its shares, free_pages and free_count are written; `moves` has room for half of the pages
+  int32_t* table_out;
+  int32_t* used;
+  uint64_t* masks;           // of every 64 pages, which are in use,
+  int32_t* before;           // and how many in front of them
+  int32_t* sizes;            // pages in use, those of them that have to move
+  unsigned char* pool;
+  size_t page_bytes;
+  int pieces;
+};
+// A wave: the holders of a request's pages, in the second row of shares.
+__device__ __forceinline__ void count_row(const PagesArgs& a, int r) {
+  const int32_t* row = a.table + (size_t)r * a.columns;
+  const int n = a.pages_of(max(a.lengths[r], 0));
+  for (int c = threadIdx.x & 63; c < n; c += 64)
+    if (a.is_page(row[c])) atomicAdd(a.shares + a.pages + row[c], 1);
+}
+// 1024 threads: which pages are in use, and which of them go where.
+struct CompactScratch {
+  unsigned sums[16][1], total, below;
+};
+__device__ __forceinline__ void choose_moves(const CompactArgs& c, CompactScratch& s) {
+  const PagesArgs& a = c.p;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int groups = (a.pages + 63) >> 6;
+  for (int g = wave; g < groups; g += 16) {
+    const int page = 64 * g + lane;
+    const uint64_t mask = __ballot(page < a.pages && now_in(a.shares + a.pages + page) > 0);
+    if (lane == 0) c.masks[g] = mask;
+  }
+  __threadfence_block();
+  __syncthreads();
+  unsigned n = 0;
+  for (int base = 0; base < groups; base += 1024) {
+    const int g = base + tid;
+    const unsigned mine = g < groups ? (unsigned)__popcll(c.masks[g]) : 0;
+    unsigned to[1] = {mine};
+    block_scan<16>(to, s.sums);
+    if (g < groups) c.before[g] = (int)(n + to[0] - mine);
+    if (tid == 1023) s.total = to[0];
+    __syncthreads();
+    n += s.total;
+    __syncthreads();
+  }
+  if (tid == 0) s.below = (int)n == a.pages ? n : (unsigned)c.before[n >> 6] + __popcll(c.masks[n >> 6] & ((1ull << (n & 63)) - 1));
+  __syncthreads();
+  const int below = (int)s.below;      // in use among the first n: the others of those are where the rest goes
+  for (int g = wave; g < groups; g += 16) {
+    const int page = 64 * g + lane;
+    const uint64_t mask = c.masks[g];
+    const bool in_use = mask >> lane & 1;
+    const int upto = c.before[g] + __popcll(mask & ((1ull << lane) - 1));
+    if (page < (int)n && !in_use) a.moves[page - upto].y = page;
+    if (page >= (int)n && in_use) a.moves[upto - below].x = page;
+  }
+  if (tid == 0) {
+    c.sizes[0] = (int)n;
+    c.sizes[1] = (int)n - below;
+    c.used[0] = (int)n;
+    a.free_count[0] = a.pages - (int)n;
+  }
+}
+__global__ __launch_bounds__(256) void cache_count_kernel(CompactArgs c) {
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r < c.p.R) count_row(c.p, r);
+}
+__global__ __launch_bounds__(1024) void cache_choose_kernel(CompactArgs c) {
+  __shared__ CompactScratch s;
+  choose_moves(c, s);
+}
+__global__ __launch_bounds__(1024) void cache_count_and_choose_kernel(CompactArgs c) {
+  __shared__ CompactScratch s;
+  for (int r = threadIdx.x >> 6; r < c.p.R; r += 16) count_row(c.p, r);
+  __threadfence_block();
+  __syncthreads();
+  choose_moves(c, s);
+}
+// The new table, stack and shares, and the copies: every workgroup has some of each.
+__global__ __launch_bounds__(256) void cache_compact_kernel(CompactArgs c) {
+  const PagesArgs& a = c.p;
+  const int n = c.sizes[0], moves = c.sizes[1];
+  const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  const int below = n - moves;
+  const auto place_of = [&](int page) {      // of a page in use
+    if (page < n) return page;
+    const int g = page >> 6;
+    return a.moves[c.before[g] + __popcll(c.masks[g] & ((1ull << (page & 63)) - 1)) - below].y;
+  };
+  for (int64_t i = first; i < (int64_t)a.R * a.columns; i += step) {
+    const int r = (int)(i / a.columns), at = (int)(i - (int64_t)r * a.columns);
+    const int entry = at < a.pages_of(max(a.lengths[r], 0)) ? a.table[i] : -1;
+    c.table_out[i] = a.is_page(entry) ? place_of(entry) : -1;
+  }
+  for (int64_t i = first; i < a.capacity; i += step) a.free_pages[i] = i < a.pages - n ? (int)(a.pages - 1 - i) : -1;
+  for (int64_t i = first; i < a.pages; i += step) {
+    const int holders = a.shares[a.pages + i];
+    if (holders > 0) a.shares[place_of((int)i)] = holders - 1;
+    if (i >= n) a.shares[i] = 0;
+    a.shares[a.pages + i] = 0;
+  }
+  for (int64_t i = blockIdx.x; i < (int64_t)moves * c.pieces; i += gridDim.x) {
+    const int k = (int)(i / c.pieces);
+    copy_piece(c.pool, c.page_bytes, a.moves[k], (int)(i - (int64_t)k * c.pieces));
+  }
+}
+
+}  // namespace sage

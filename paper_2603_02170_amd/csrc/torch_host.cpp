@@ -449,6 +449,10 @@ PyMethodDef g_methods[] = {
     {"attention", (PyCFunction)(void (*)(void))py_attention, METH_FASTCALL, nullptr},
     {"cache_plan", (PyCFunction)(void (*)(void))py_cache_plan, METH_FASTCALL, nullptr},
     {"cache_trim", (PyCFunction)(void (*)(void))py_cache_trim, METH_FASTCALL, nullptr},
+    {"cache_free", (PyCFunction)(void (*)(void))py_cache_free, METH_FASTCALL, nullptr},
+    {"cache_fork", (PyCFunction)(void (*)(void))py_cache_fork, METH_FASTCALL, nullptr},
+    {"cache_own", (PyCFunction)(void (*)(void))py_cache_own, METH_FASTCALL, nullptr},
+    {"cache_compact", (PyCFunction)(void (*)(void))py_cache_compact, METH_FASTCALL, nullptr},
     {"cache_append", (PyCFunction)(void (*)(void))py_cache_append, METH_FASTCALL, nullptr},
     {"cache_read", (PyCFunction)(void (*)(void))py_cache_read, METH_FASTCALL, nullptr},
     {"cache_attention", (PyCFunction)(void (*)(void))py_cache_attention, METH_FASTCALL, nullptr},

@@ -193,6 +193,163 @@ PyObject* py_cache_trim(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// lengths, table, free_pages, free_count, shares: what the calls on shared pages change, five arguments from `a` on, of R requests.
+struct SharedPages {
+  const Tensor *lengths, *table, *free_pages, *free_count, *shares;
+  int32_t R, columns, capacity, pages;
+  bool take(PyObject* const* a, int64_t requests, DeviceOf& dev) {
+    if (!(lengths = dense(a[0], at::kInt, {requests}, "lengths", dev)) || !(table = dense(a[1], at::kInt, {requests, -1}, "block_table", dev)) ||
+        !(free_pages = dense(a[2], at::kInt, {-1}, "free_pages", dev)) || !(free_count = dense(a[3], at::kInt, {1}, "free_count", dev)) ||
+        !(shares = dense(a[4], at::kInt, {3, -1}, "shares", dev)))
+      return false;
+    if (table->size(1) < 1 || table->size(1) > INT32_MAX || requests > INT32_MAX || free_pages->size(0) > INT32_MAX || shares->size(1) > INT32_MAX)
+      return value_error("block_table", "sizes are out of range");
+    R = (int32_t)requests;
+    columns = (int32_t)table->size(1);
+    capacity = (int32_t)free_pages->size(0);
+    pages = (int32_t)shares->size(1);
+    return true;
+  }
+};
+
+// free(keep, lengths, table, free_pages, free_count, shares, page)
+PyObject* py_cache_free(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  DeviceOf dev;
+  const Tensor* keep;
+  SharedPages s;
+  int64_t page;
+  if (!arg_count(n, 7, "cache_free") || !(keep = dense(a[0], at::kInt, {-1}, "keep", dev)) || !s.take(a + 1, keep->size(0), dev) ||
+      !size_arg(a[6], "page", 0, &page))
+    return nullptr;
+  int rc;
+  WITHOUT_GIL({
+    const c10::DeviceGuard guard(keep->device());
+    rc = sagebwd_cache_free((const int32_t*)keep->data_ptr(), (int32_t*)s.lengths->data_ptr(), (int32_t*)s.table->data_ptr(),
+                            (int32_t*)s.free_pages->data_ptr(), (int32_t*)s.free_count->data_ptr(), (int32_t*)s.shares->data_ptr(), s.R, s.columns,
+                            (int32_t)page, s.capacity, s.pages, (void*)current_stream());
+  })
+  if (rc != SAGEBWD_OK) return raise_status(rc, "sagebwd_cache_free");
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+// fork(parents, lengths, table, free_pages, free_count, shares, page)
+PyObject* py_cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  DeviceOf dev;
+  const Tensor* parents;
+  SharedPages s;
+  int64_t page;
+  if (!arg_count(n, 7, "cache_fork") || !(parents = dense(a[0], at::kInt, {-1}, "parents", dev)) || !s.take(a + 1, parents->size(0), dev) ||
+      !size_arg(a[6], "page", 0, &page))
+    return nullptr;
+  int rc;
+  WITHOUT_GIL({
+    const c10::DeviceGuard guard(parents->device());
+    size_t bytes = 0;
+    rc = sagebwd_cache_fork_workspace_bytes(s.R, s.columns, &bytes);
+    if (rc == SAGEBWD_OK) {
+      const Tensor ws = at::empty({(int64_t)bytes}, parents->options().dtype(at::kByte));
+      rc = sagebwd_cache_fork((const int32_t*)parents->data_ptr(), (int32_t*)s.lengths->data_ptr(), (int32_t*)s.table->data_ptr(),
+                              (int32_t*)s.free_pages->data_ptr(), (int32_t*)s.free_count->data_ptr(), (int32_t*)s.shares->data_ptr(), s.R, s.columns,
+                              (int32_t)page, s.capacity, s.pages, ws.data_ptr(), bytes, (void*)current_stream());
+    }
+  })
+  if (rc != SAGEBWD_OK) return raise_status(rc, "sagebwd_cache_fork");
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+bool shares_fit(const SharedPages& s, const sagebwd_cache_params& p) {
+  return s.pages == p.pages || value_error("shares", "has another number of pages than the cache");
+}
+
+// own(added, lengths, table, free_pages, free_count, shares, cache, H, d, page, group, block, out | None) -> added
+PyObject* py_cache_own(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  DeviceOf dev;
+  sagebwd_cache_params p;
+  const Tensor *added, *pool;
+  Tensor out;
+  SharedPages s;
+  if (!arg_count(n, 13, "cache_own") || !cache_params(a + 7, p) || !(pool = pool_arg(a[6], p, dev)) || !(added = dense(a[0], at::kInt, {-1}, "added", dev)) ||
+      !s.take(a + 1, added->size(0), dev) || !shares_fit(s, p) || !dense_or_none(a[12], at::kInt, {added->size(0)}, "out", dev, &out))
+    return nullptr;
+  int rc;
+  WITHOUT_GIL({
+    const c10::DeviceGuard guard(added->device());
+    if (!out.defined()) out = at::empty({s.R}, added->options());
+    const Tensor ws = at::empty({8 * (int64_t)s.R + 16}, added->options().dtype(at::kByte));
+    rc = sagebwd_cache_own((const int32_t*)added->data_ptr(), (const int32_t*)s.lengths->data_ptr(), (int32_t*)s.table->data_ptr(),
+                           (const int32_t*)s.free_pages->data_ptr(), (int32_t*)s.free_count->data_ptr(), (int32_t*)s.shares->data_ptr(), s.R, s.columns,
+                           s.capacity, &p, pool->data_ptr(), (int32_t*)out.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), (void*)current_stream());
+  })
+  if (rc != SAGEBWD_OK) return raise_status(rc, "sagebwd_cache_own");
+  return THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// compact(lengths, table, cache, H, d, page, group, block, out | None) -> (table, free_pages, free_count, shares, used)
+PyObject* py_cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  DeviceOf dev;
+  sagebwd_cache_params p;
+  const Tensor *lengths, *table, *pool;
+  if (!arg_count(n, 9, "cache_compact") || !cache_params(a + 3, p) || !(pool = pool_arg(a[2], p, dev)) ||
+      !(lengths = dense(a[0], at::kInt, {-1}, "lengths", dev)) || !(table = dense(a[1], at::kInt, {lengths->size(0), -1}, "block_table", dev)))
+    return nullptr;
+  const int64_t R = lengths->size(0);
+  if (table->size(1) < 1 || table->size(1) > INT32_MAX || R > INT32_MAX) {
+    value_error("block_table", "sizes are out of range");
+    return nullptr;
+  }
+  Tensor out[5];
+  if (a[8] != Py_None) {
+    THPObjectPtr seq(PySequence_Fast(a[8], "out: need the five tensors of a compaction"));
+    if (!seq) return nullptr;
+    if (PySequence_Fast_GET_SIZE(seq.get()) != 5) {
+      PyErr_SetString(PyExc_ValueError, "out: need the five tensors of a compaction");
+      return nullptr;
+    }
+    const char* names[5] = {"block_table", "free_pages", "free_count", "shares", "used"};
+    const std::vector<int64_t> shapes[5] = {{R, table->size(1)}, {-1}, {1}, {3, p.pages}, {1}};
+    for (int k = 0; k < 5; k++) {
+      const Tensor* t = dense(PySequence_Fast_GET_ITEM(seq.get(), k), at::kInt, shapes[k], names[k], dev);
+      if (t == nullptr) return nullptr;
+      out[k] = *t;
+    }
+    if (out[1].size(0) < p.pages || out[1].size(0) > INT32_MAX) {
+      value_error("free_pages", "has no room for every page");
+      return nullptr;
+    }
+  }
+  int rc;
+  WITHOUT_GIL({
+    const c10::DeviceGuard guard(lengths->device());
+    size_t bytes = 0;
+    rc = sagebwd_cache_compact_workspace_bytes(p.pages, &bytes);
+    if (rc == SAGEBWD_OK) {
+      if (!out[0].defined()) {
+        out[0] = at::empty(table->sizes(), lengths->options());
+        out[1] = at::empty({p.pages}, lengths->options());
+        out[2] = at::empty({1}, lengths->options());
+        out[3] = at::zeros({3, p.pages}, lengths->options());
+        out[4] = at::empty({1}, lengths->options());
+      }
+      const Tensor ws = at::empty({(int64_t)bytes}, lengths->options().dtype(at::kByte));
+      rc = sagebwd_cache_compact((const int32_t*)lengths->data_ptr(), (const int32_t*)table->data_ptr(), (int32_t)R, (int32_t)table->size(1), &p,
+                                 pool->data_ptr(), (int32_t*)out[0].data_ptr(), (int32_t*)out[1].data_ptr(), (int32_t)out[1].size(0),
+                                 (int32_t*)out[2].data_ptr(), (int32_t*)out[3].data_ptr(), (int32_t*)out[4].data_ptr(), ws.data_ptr(), bytes,
+                                 (void*)current_stream());
+    }
+  })
+  if (rc != SAGEBWD_OK) return raise_status(rc, "sagebwd_cache_compact");
+  return Py_BuildValue("(NNNNN)", THPVariable_Wrap(out[0]), THPVariable_Wrap(out[1]), THPVariable_Wrap(out[2]), THPVariable_Wrap(out[3]),
+                       THPVariable_Wrap(out[4]));
+  END_HANDLE_TH_ERRORS
+}
+
 const float* data_or_null(const Tensor& t) { return t.defined() ? (const float*)t.data_ptr() : nullptr; }
 
 // append(K, V, slots, cache, H, d, page, group, block, k_mean | None, v_mean | None)
