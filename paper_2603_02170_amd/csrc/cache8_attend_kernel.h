@@ -75,7 +75,7 @@ struct ByteForm {
   typedef ByteTile<D> Tile;
   typedef ByteRows<D> Rows;
   struct Unpacking {};
-  static constexpr bool RING = false;
+  static constexpr bool RING = false, TILED = true;
   static __device__ __forceinline__ const unsigned char* part(const AttendArgs& a, int entry, int head) {
     return a.pool + ((size_t)entry * a.g.H + head) * Bytes8<D>::head_bytes(a.g);
   }

@@ -352,18 +352,21 @@ __device__ __forceinline__ void attend_store(const AttendArgs& a, int begin, int
 
 constexpr int kStages = 3;          // tiles of a wave's ring
 
-// What a workgroup does with one item: units j0 .. j1 - 1 of the u of (request, head).  All of it is the same in every lane.
+// What a workgroup does with one item: units j0 .. j1 - 1 of the u of (request, head, tile of rows).  All of it is the same in every lane.
 struct AttendPiece {
   int r, head, j0, j1, u;
+  int row0;                   // the tile's first row
   int begin, n_rows, len, first_sees, visible;
 };
 
 constexpr int kKnown = 256;
-// 64 requests at a time, one a lane: where one ends the next one's sizes are at hand.
+// 64 requests at a time, one a lane: where one ends the next one's sizes are at hand.  ROWS: of a tile, where requests may have several (each of them an
+// item, those of a head one after the other), else 0.
+template <int ROWS>
 struct AttendCursor {
   int base;                                                // request of lane 0
   int begin, n_rows, len, first_sees, visible, units;      // of request base + lane
-  int r, head, j;                                          // the next piece begins here: request, head, unit
+  int r, head, j;                                          // the next piece begins here: request, head (of several tiles: and tile), unit
   int (*known)[kKnown];                                    // the same of all requests in LDS, if they are few
   int x, end;                                              // where its item begins in what is dealt out, and where the share ends
   __device__ __forceinline__ bool more(const AttendArgs& a) const { return a.split ? attend_cut(end - x) > j : x < end; }
@@ -390,6 +393,9 @@ struct AttendCursor {
       take(a, attend_request(a, i));
     }
   }
+  static __device__ __forceinline__ int tiles_of(int rows) { return ROWS > 0 ? (rows + ROWS - 1) / ROWS : 1; }
+  __device__ __forceinline__ int head_of(int item, int rows) const { return ROWS > 0 ? item / tiles_of(rows) : item; }
+  __device__ __forceinline__ int row0_of(int item, int rows) const { return ROWS > 0 ? item % tiles_of(rows) * ROWS : 0; }
   // (more)
   __device__ __forceinline__ AttendPiece next(const AttendArgs& a) {
     AttendPiece p;
@@ -401,9 +407,10 @@ struct AttendCursor {
       if (p.u == 0) r++;
     } while (p.u == 0);
     p.r = r;
-    p.head = head;
     p.begin = __builtin_amdgcn_readlane(begin, at);
     p.n_rows = __builtin_amdgcn_readlane(n_rows, at);
+    p.head = head_of(head, p.n_rows);
+    p.row0 = row0_of(head, p.n_rows);
     p.len = __builtin_amdgcn_readlane(len, at);
     p.first_sees = __builtin_amdgcn_readlane(first_sees, at);
     p.visible = __builtin_amdgcn_readlane(visible, at);
@@ -413,7 +420,7 @@ struct AttendCursor {
     if (j == p.u) {
       x += a.split ? p.u + kItemCost : 1;
       j = 0;
-      if (++head == a.g.H) {
+      if (++head == a.g.H * tiles_of(p.n_rows)) {
         head = 0;
         r++;
       }
@@ -430,6 +437,7 @@ struct NibbleForm {
   typedef AttendRows<D, GROUP> Rows;
   typedef Unpack Unpacking;
   static constexpr bool RING = true;      // tiles come through LDS, else to registers
+  static constexpr bool TILED = false;    // requests may have more rows than a workgroup
   static __device__ __forceinline__ const unsigned char* part(const AttendArgs& a, int entry, int head) {
     return a.pool + (size_t)entry * a.g.page_bytes() + (size_t)(head * a.g.head_bytes());
   }
@@ -451,11 +459,13 @@ __device__ __forceinline__ void attend_items(AttendArgs a) {
   const int H = a.g.H;
   char* ring = lds + wave * RING;
   const typename Form::Unpacking un;
-  const auto shared_units = [&](int u) { return u == 0 ? 0 : a.split ? u + kItemCost : 1; };      // what is dealt out of an item
+  typedef AttendCursor<Form::TILED ? ROWS : 0> Cursor;
+  // what is dealt out of a request's items of a head
+  const auto shared_units = [&](int u, int rows) { return u == 0 ? 0 : (a.split ? u + kItemCost : 1) * Cursor::tiles_of(rows); };
 
   // units up to every thread's requests (R / 256 each; where that is one it is kept)
   const int per = (a.R + 255) / 256, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
-  AttendCursor cursor;
+  Cursor cursor;
   cursor.known = known;
   int mine = 0;
   if (a.R <= kKnown) {
@@ -464,10 +474,10 @@ __device__ __forceinline__ void attend_items(AttendArgs a) {
       const int x[6] = {cursor.begin, cursor.n_rows, cursor.len, cursor.first_sees, cursor.visible, cursor.units};
 #pragma unroll
       for (int i = 0; i < 6; i++) known[i][tid] = x[i];
-      mine = shared_units(cursor.units);
+      mine = shared_units(cursor.units, cursor.n_rows);
     }
   } else {
-    for (int r = r0; r < r1; r++) mine += shared_units(attend_units(a, r));
+    for (int r = r0; r < r1; r++) mine += shared_units(attend_units(a, r), attend_request(a, r).rows);
   }
   int upto = mine;
   for (int k = 1; k < 64; k <<= 1) {
@@ -490,7 +500,7 @@ __device__ __forceinline__ void attend_items(AttendArgs a) {
   if ((upto - mine) * H <= begin && begin < upto * H) {
     int at = upto - mine;
     for (int r = r0; r < r1; r++) {
-      const int u = shared_units(a.R <= kKnown ? known[5][r] : attend_units(a, r));
+      const int u = a.R <= kKnown ? shared_units(known[5][r], known[1][r]) : shared_units(attend_units(a, r), attend_request(a, r).rows);
       if (begin < (at + u) * H) {
         found[0] = r;
         found[1] = begin - at * H;
@@ -510,13 +520,17 @@ __device__ __forceinline__ void attend_items(AttendArgs a) {
     cursor.end = shares.begin(w + 1);
   }
   if (!cursor.more(a)) return;
+  const int row0 = cursor.row0_of(cursor.head, __builtin_amdgcn_readlane(cursor.n_rows, 0));
   if (tid == 0 && shares.first_border<kItemCost>(w, cursor.x, cursor.j))
     a.joins[w] = join_word(shares.parts<kItemCost>(w, cursor.x, __builtin_amdgcn_readlane(cursor.units, 0)),
-                           __builtin_amdgcn_readlane(cursor.n_rows, 0), __builtin_amdgcn_readlane(cursor.begin, 0), cursor.head, 0);
+                           Form::TILED ? min(__builtin_amdgcn_readlane(cursor.n_rows, 0) - row0, ROWS) : __builtin_amdgcn_readlane(cursor.n_rows, 0),
+                           __builtin_amdgcn_readlane(cursor.begin, 0), cursor.head_of(cursor.head, __builtin_amdgcn_readlane(cursor.n_rows, 0)), row0);
 
   typename Form::Rows rows[NQ];
+  if constexpr (!Form::TILED) {
 #pragma unroll
-  for (int q = 0; q < NQ; q++) rows[q].place(a, 16 * q);
+    for (int q = 0; q < NQ; q++) rows[q].place(a, 16 * q);
+  }
   AttendPiece piece = cursor.next(a);
   // The wave's tiles: `count`, every 128 tokens from `first`.  Those of pages that do not exist are passed over where tiles are chosen.  (A branch
   // round a tile's arithmetic has the sums in other registers behind it, 48.4 us for 64 ragged requests in place of 47.5; their arithmetic
@@ -538,7 +552,10 @@ __device__ __forceinline__ void attend_items(AttendArgs a) {
     window = 0;
     pages = pages_from(0);
 #pragma unroll
-    for (int q = 0; q < NQ; q++) rows[q].fetch(a, piece);
+    for (int q = 0; q < NQ; q++) {
+      if constexpr (Form::TILED) rows[q].place(a, piece.row0 + 16 * q);
+      rows[q].fetch(a, piece);
+    }
   };
   const auto some_left = [&] {      // the window is on a tile that is not on its way yet, if there is one
     while (left == 0) {
@@ -593,7 +610,7 @@ __device__ __forceinline__ void attend_items(AttendArgs a) {
   start();
 
   for (;;) {
-    const int all_see = a.causal ? piece.first_sees : piece.len;       // keys that every row sees
+    const int all_see = a.causal ? piece.first_sees + (Form::TILED ? piece.row0 / a.G : 0) : piece.len;       // keys that every row sees
 #pragma unroll
     for (int q = 0; q < NQ; q++) rows[q].begin();
     if constexpr (!Form::RING) {
@@ -669,10 +686,10 @@ __device__ __forceinline__ void attend_items(AttendArgs a) {
         v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < 4; w++) o += *(const v4f*)&stage[w][row][c] * f[w];
-        if (k < done.n_rows) {
+        if (k + done.row0 < done.n_rows) {
           const int channel = 64 * half + c;
           if (whole) {
-            attend_store<4>(a, done.begin, done.head, k, D, channel, M, l, (const float*)&o, mean[half]);
+            attend_store<4>(a, done.begin, done.head, k + done.row0, D, channel, M, l, (const float*)&o, mean[half]);
           } else {
             *(v4f*)(a.sums + (part * ROWS + k) * D + channel) = o;
             if (channel == 0) a.stats[part * ROWS + k] = float2{M, l};

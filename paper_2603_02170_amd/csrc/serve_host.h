@@ -49,10 +49,16 @@ constexpr int kFewRows = 32;
 // 128 and unpacks 256 or 128 tokens at a time (tiles of 256 rows -> these, us: 32 requests of 4096 tokens, 64 rows 123 -> 87, 128 rows 126 ->
 // 107; 64 of 40 rows, 1000 tokens, 60 -> 46; four requests of 64 tokens 15 -> 19; 65 to 128 rows as two tiles of 64 188, 256 as two of 128, 3000
 // tokens, 79 -> 93).
+// Of a cache held in 8 bits: rows in several tiles of 32, each a pass over the keys, while the line that they are dealt out on holds them.
+constexpr int kTiledRows = 128;
 inline int64_t most_rows(const sagebwd_cache_params& p, const sagebwd_cache_call& c) { return (int64_t)(c.max_new < c.T ? c.max_new : c.T) * (c.Hq / p.H); }
 inline int most_length(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
   const int64_t all = (int64_t)c.columns * p.page;
   return (int)(c.max_length > 0 && c.max_length < all ? c.max_length : all);
+}
+inline int few_rows_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
+  const int64_t line = (int64_t)c.R * p.H * (kTiledRows / 32) * ((most_length(p, c) + kUnit - 1) / kUnit + kItemCost);
+  return p.block > 0 && line <= 1 << 29 ? kTiledRows : kFewRows;
 }
 inline int tile_rows_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
   const int64_t most = most_rows(p, c);
@@ -60,7 +66,7 @@ inline int tile_rows_of(const sagebwd_cache_params& p, const sagebwd_cache_call&
 }
 // Row tiles of the kernel for many rows, over all heads, at most; 0 where no request goes to it.
 inline int64_t chunk_tiles_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
-  if (most_rows(p, c) <= kFewRows) return 0;
+  if (most_rows(p, c) <= few_rows_of(p, c)) return 0;
   return ((int64_t)c.T * (c.Hq / p.H) / tile_rows_of(p, c) + c.R) * p.H;
 }
 
@@ -128,18 +134,19 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
   // padded to it, with requests of one token among them, is served by the kernel for many: 32 of 4096 tokens, 4 heads a group, T = 512: 82 us, T = 511
   // 38.  And 17 to 32 rows beside a prompt go to it too: the same 32 with 8 tokens each 52 us, a prompt of 2048 129, together 356; with 4 tokens each
   // together 170.)
-  w.many = rows > kFewRows;
-  w.few = !w.many || (G <= kFewRows && (int64_t)c.T < (int64_t)c.R * c.max_new);
+  const int few_rows = few_rows_of(p, c);
+  w.many = rows > few_rows;
+  w.few = !w.many || (G <= few_rows && (int64_t)c.T < (int64_t)c.R * c.max_new);
   if (w.few) {
     AttendLaunch& l = w.f;
-    const int64_t here = w.many ? (G > 16 ? G : 16) : rows;
+    const int64_t here = !w.many ? rows : few_rows > kFewRows ? few_rows : G > 16 ? G : 16;
     l.nq = here <= 16 ? 1 : 2;
     l.rows_from = 0;
-    l.rows_to = 16 * l.nq;
-    l.join_rows = (int)(here < l.rows_to ? here : l.rows_to);
+    l.rows_to = here > 32 ? few_rows : 16 * l.nq;
+    l.join_rows = (int)(here < 16 * l.nq ? here : 16 * l.nq);
     const int most_units = (w.max_length + kUnit - 1) / kUnit;
     l.split = most_units > kWholeUnits;
-    const int64_t units = (int64_t)c.R * p.H * (l.split ? most_units + kItemCost : 1);
+    const int64_t units = (int64_t)c.R * p.H * ((here + 31) / 32) * (l.split ? most_units + kItemCost : 1);
     const int64_t slots = 2 * kCus;
     l.workgroups = (int)(units < slots ? (units > 0 ? units : 1) : slots);
     lay_out(l, 16 * l.nq);
