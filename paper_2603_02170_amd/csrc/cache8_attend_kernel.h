@@ -152,9 +152,28 @@ __global__ __launch_bounds__(256, 2) void cache8_attend_kernel(AttendArgs a) {
 }
 
 // ---- many rows ---------------------------------------------------------------------------------------------------------
+// V's scale of a half goes into its exponents (log2 of it), so that they give the probabilities times it, and out of their sum.  (Of a scale of zero, whose
+// codes are zeros, any other will do, and for one that is no number poison() stands in.)  32 products of a lane and tile less: 2048 rows x 4 against 10000 tokens 300.4 -> WIDE us.
 struct ByteKnown {
-  int exists[2];
-  float k[2], v[2];       // scales of the halves
+  int flags[2];           // bit 0: the half's page exists; bit 1: and its values are not numbers; bit 2: and its keys
+  float k[2], log_v[2];
+  __device__ __forceinline__ void set(int half, bool is_page, float ka, float va) {
+    const auto number = [](float x) { return x >= 0.f && x < INFINITY; };      // (where nothing was stored any bits may be)
+    flags[half] = is_page ? 1 | (number(va) ? 0 : 2) | (number(ka) ? 0 : 4) : 0;
+    k[half] = number(ka) ? ka * kBy127 : 0.f;
+    log_v[half] = number(va) && va > 0.f ? __builtin_amdgcn_logf(va * kBy127) : 0.f;
+  }
+  // Of all lanes the same: to scalar registers.
+  __device__ __forceinline__ ByteKnown uniform(int lane) const {
+    ByteKnown w;
+#pragma unroll
+    for (int b = 0; b < 2; b++) {
+      w.flags[b] = __builtin_amdgcn_readlane(flags[b], lane);
+      w.k[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k[b]), lane));
+      w.log_v[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(log_v[b]), lane));
+    }
+    return w;
+  }
 };
 
 // 64 tokens on their way from the pages to bf16 fragments of codes: waves 0 to 3 have K's, the others V's, 16 bytes at a time as they lie
@@ -188,9 +207,7 @@ struct ByteChunk {
   __device__ __forceinline__ void store(char* K, char* V, Known& known, unsigned char*, int*, int) const {
     const int tid = threadIdx.x, u = tid & 255;
     if (tid < 128 && (tid & 63) == 0) {
-      known.exists[tid >> 6] = valid;
-      known.k[tid >> 6] = k * kBy127;
-      known.v[tid >> 6] = fabsf(v) < INFINITY ? v * kBy127 : __builtin_nanf("");      // (where nothing was stored any bits may be)
+      known.set(tid >> 6, valid, k, v);
     }
 #pragma unroll
     for (int i = 0; i < N; i++) {
@@ -214,16 +231,18 @@ struct ByteChunk {
 template <int D>
 struct ByteChunkRows : ChunkRows<D> {
   typedef ChunkRows<D> Base;
-  __device__ __forceinline__ void softmax(v16f (&s)[2], v8bf (&p)[4], int t0, const ByteKnown& known, float scale_log2) {
-    float c[2] = {known.k[0] * scale_log2, known.k[1] * scale_log2};
-    if (t0 + kChunkUnit > Base::all_see || known.exists[0] + known.exists[1] != 2) {
+  __device__ __forceinline__ void softmax(v16f (&s)[2], v8bf (&p)[4], int t0, const ByteKnown& of_tile, float scale_log2) {
+    const ByteKnown known = of_tile.uniform(0);
+    // (above zero, as a hidden logit is -infinity times it; a scale of zero has codes of zeros)
+    const auto scalar = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
+    const float c[2] = {scalar(fmaxf(known.k[0] * scale_log2, 1e-37f)), scalar(fmaxf(known.k[1] * scale_log2, 1e-37f))};
+    if (t0 + kChunkUnit > Base::all_see || !known.flags[0] || !known.flags[1]) {
       const int h = threadIdx.x >> 5 & 1;
 #pragma unroll
       for (int b = 0; b < 2; b++) {
-        const int behind = known.exists[b] ? Base::sees - t0 - 32 * b - 8 * h : 0;
+        const int behind = known.flags[b] ? Base::sees - t0 - 32 * b - 8 * h : 0;
 #pragma unroll
-        for (int i = 0; i < 16; i++) s[b][i] = 16 * (i / 8) + i % 8 < behind ? s[b][i] * c[b] : -INFINITY;      // (c may be 0)
-        c[b] = 1.f;
+        for (int i = 0; i < 16; i++) s[b][i] = 16 * (i / 8) + i % 8 < behind ? s[b][i] : -INFINITY;
       }
     }
     float top[2] = {-INFINITY, -INFINITY};
@@ -244,26 +263,29 @@ struct ByteChunkRows : ChunkRows<D> {
     const float ref = Base::m == -INFINITY ? 0.f : Base::m;
 #pragma unroll
     for (int b = 0; b < 2; b++) {
-      const float w = known.v[b] == known.v[b] ? known.v[b] : 0.f;      // (NaN: poison() has it)
+      const float off = known.log_v[b] - ref;
+      float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; i++) {
-        s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c[b], -ref));
-        Base::l += s[b][i];
-        s[b][i] *= w;
+        s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c[b], off));
+        sum += s[b][i];
       }
+      Base::l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(-known.log_v[b]), Base::l);
 #pragma unroll
       for (int k = 0; k < 2; k++)
         p[2 * b + k] = as_bf16(v4i{pack_bf16(s[b][8 * k], s[b][8 * k + 1]), pack_bf16(s[b][8 * k + 2], s[b][8 * k + 3]),
                                    pack_bf16(s[b][8 * k + 4], s[b][8 * k + 5]), pack_bf16(s[b][8 * k + 6], s[b][8 * k + 7])});
     }
   }
-  // A block whose values are not numbers, to the rows that see some of it.
+  // A block whose keys or values are not numbers, to the rows that see some of it.
   __device__ __forceinline__ void poison(const ByteKnown& known, int t0) {
 #pragma unroll
     for (int b = 0; b < 2; b++)
-      if (known.v[b] != known.v[b] && known.exists[b] && Base::sees > t0 + 32 * b)
+      if ((known.flags[b] & 6) != 0 && Base::sees > t0 + 32 * b) {
 #pragma unroll
         for (int c = 0; c < Base::NC; c++) Base::o[c] += __builtin_nanf("");
+        if (known.flags[b] & 4) Base::l = __builtin_nanf("");
+      }
   }
 };
 
@@ -274,32 +296,12 @@ struct ByteChunks {
   typedef ByteChunkRows<D> Rows;
   typedef ByteKnown Known;
   static __device__ __forceinline__ void poison(Rows& rows, bool, const unsigned char*, const Known& known, int t0) {
-    if (__builtin_expect(known.v[0] != known.v[0] || known.v[1] != known.v[1], 0)) rows.poison(known, t0);
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(known.flags[0] | known.flags[1]) & 6, 0)) rows.poison(known, t0);
   }
+  static constexpr bool WORDS_IN_RING = true;      // (six registers of them are more than the kernel for heads of 64 has)
   typedef ByteKnown Word;
   static __device__ __forceinline__ Word word(const Known& known, bool) { return known; }
-  struct Words {
-    ByteKnown of_lane;
-    __device__ __forceinline__ void take(const AttendArgs& a, size_t tile) { of_lane = ((const ByteKnown*)a.tiles)[tile]; }
-    __device__ __forceinline__ void wait() {
-#pragma unroll
-      for (int b = 0; b < 2; b++) {
-        arrived(of_lane.exists[b]);
-        arrived(of_lane.k[b]);
-        arrived(of_lane.v[b]);
-      }
-    }
-    __device__ __forceinline__ Word of(int lane) const {
-      Word w;
-#pragma unroll
-      for (int b = 0; b < 2; b++) {
-        w.exists[b] = __builtin_amdgcn_readlane(of_lane.exists[b], lane);
-        w.k[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(of_lane.k[b]), lane));
-        w.v[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(of_lane.v[b]), lane));
-      }
-      return w;
-    }
-  };
+  struct Words {};
   static __device__ __forceinline__ const Known& known(const Word& w) { return w; }
   static __device__ __forceinline__ bool any_bad(const Word&) { return false; }
 };

@@ -414,6 +414,7 @@ struct NibbleChunks {
     if (any) rows.poison(bad, GROUP, t0, known);
   }
   // What is known of tiles unpacked beforehand, of 64 of them, one a lane.
+  static constexpr bool WORDS_IN_RING = false;      // (else it comes with each tile)
   typedef WideTile Word;
   static __device__ __forceinline__ Word word(const Known& known, bool any) { return Word{(known.exists[0] != 0) | (known.exists[1] != 0) << 1 | any << 2}; }
   struct Words {
@@ -696,8 +697,9 @@ constexpr int kWideStages = 4;
 template <typename Form>
 __device__ __forceinline__ void wide_items(AttendArgs a) {
   constexpr int D = Form::D;
-  constexpr int TILE = 256 * D, COPIES = TILE / 8 / 1024;
+  constexpr int TILE = 256 * D, COPIES = TILE / 8 / 1024, LOADS = COPIES + (Form::WORDS_IN_RING ? 1 : 0);
   __shared__ __attribute__((aligned(16))) char ring[kWideStages][TILE];
+  __shared__ __attribute__((aligned(16))) char word_ring[kWideStages][Form::WORDS_IN_RING ? 256 : 0];      // (all waves copy them, to the same place)
   __shared__ ChunkScratch scratch;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   ChunkWalk<kChunkRows, kChunkUnit, kChunkCost> walk;
@@ -713,11 +715,12 @@ __device__ __forceinline__ void wide_items(AttendArgs a) {
     typename Form::Rows rows;
     rows.begin(a, rq, walk.head, walk.tile * kChunkRows + 32 * wave);
     typename Form::Words words;        // of the next 64 tiles, one a lane
-    words.take(a, tile0 + min(lane, max(count - 1, 0)));
+    if constexpr (!Form::WORDS_IN_RING) words.take(a, tile0 + min(lane, max(count - 1, 0)));
     const auto fetch = [&](int k) {
       const gbytes_t from = uniform(a.unpacked + (tile0 + k) * TILE + wave * (COPIES * 1024));
 #pragma unroll
       for (int c = 0; c < COPIES; c++) ring_copy<16>(from, c * 1024 + lane * 16, ring[k % kWideStages] + wave * (COPIES * 1024) + c * 1024);
+      if constexpr (Form::WORDS_IN_RING) ring_copy<4>(uniform((const typename Form::Word*)a.tiles + tile0 + k), lane * 4, word_ring[k % kWideStages]);
     };
     // (intervals as in cache_chunk_kernel)
     v16f s[2];
@@ -727,25 +730,28 @@ __device__ __forceinline__ void wide_items(AttendArgs a) {
       const int t0 = (j0 + k) * kChunkUnit;
       if (t0 < rows.wave_sees) rows.softmax(s, p, t0, Form::known(word), a.scale_log2);
     };
-    words.wait();
+    if constexpr (!Form::WORDS_IN_RING) words.wait();
     rows.wait();
     compiler_fence();
     fetch(0);
     if (count > 1) fetch(1);
     for (int k = 0; k <= count; k++) {
       compiler_fence();
-      if (k + 1 < count) __builtin_amdgcn_s_waitcnt(vmcnt_only(COPIES));
+      if (k + 1 < count) __builtin_amdgcn_s_waitcnt(vmcnt_only(LOADS));
       else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
       barrier_lds_only();                  // the tile has landed, and every wave is through with the one two before it
       compiler_fence();
       if (k + 2 < count) fetch(k + 2);
       compiler_fence();
-      if (k % 64 == 0 && k != 0) {
-        words.take(a, tile0 + min(k + lane, count - 1));
-        words.wait();
+      if constexpr (!Form::WORDS_IN_RING) {
+        if (k % 64 == 0 && k != 0) {
+          words.take(a, tile0 + min(k + lane, count - 1));
+          words.wait();
+        }
       }
       word_before = word;
-      word = words.of(k % 64);
+      if constexpr (Form::WORDS_IN_RING) word = ((const typename Form::Word*)word_ring[k % kWideStages])->uniform(0);
+      else word = words.of(k % 64);
       if (late && k > 0) probabilities(k - 1, word_before);
       if (k > 0 && (j0 + k - 1) * kChunkUnit < rows.wave_sees) {
         rows.values(ring[(k - 1) % kWideStages] + TILE / 2, p);

@@ -99,6 +99,7 @@ struct AttendLaunch {
   int rows_from, rows_to;      // of the requests that it has
   int nq;                      // cache_attend_kernel: tiles of 16 rows
   int workgroups, join_rows;
+  bool join_wide;              // items have few parts: several rows a workgroup
   int tile_rows;               // of the kernels for many rows
   bool split;
   size_t joins, sums, stats;
@@ -149,6 +150,7 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
     const int64_t units = (int64_t)c.R * p.H * ((here + 31) / 32) * (l.split ? most_units + kItemCost : 1);
     const int64_t slots = 2 * kCus;
     l.workgroups = (int)(units < slots ? (units > 0 ? units : 1) : slots);
+    l.join_wide = p.block > 0 && (int64_t)c.R * p.H * ((here + 31) / 32) >= 64;
     lay_out(l, 16 * l.nq);
   }
   if (w.many) {
@@ -171,7 +173,7 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
       l.unpack_workgroups = (int)(key_tiles < 4 * kCus ? key_tiles : 4 * kCus);
       l.most_tiles = (int)key_tiles;
       l.unpacked = take((size_t)key_tiles * p.d * 256);
-      l.tiles = take((size_t)key_tiles * (p.block ? sizeof(ByteKnown) : sizeof(WideTile)));
+      l.tiles = take((size_t)key_tiles * (p.block ? sizeof(ByteKnown) : sizeof(WideTile)) + (p.block ? 256 : 0));      // (the last one's copy reads 256 bytes)
       l.poison = take(p.block ? 0 : (size_t)key_tiles * (p.d / p.group) * 64);
     }
   }
@@ -185,7 +187,8 @@ int launch_few(const AttendArgs& a, const AttendLaunch& l, hipStream_t st) {
   Kernels::template few<NQ>(l.workgroups, a, st);
   SERVE_LAUNCH_CHECK();
   if (l.split && l.workgroups > 1) {
-    Kernels::template join_few<16 * NQ>(dim3(l.workgroups - 1, l.join_rows), a, st);
+    if (l.join_wide) Kernels::template join_many<16 * NQ>(dim3(l.workgroups - 1, (l.join_rows * (Kernels::D / 4) + 255) / 256), a, st);
+    else Kernels::template join_few<16 * NQ>(dim3(l.workgroups - 1, l.join_rows), a, st);
     SERVE_LAUNCH_CHECK();
   }
   return SAGEBWD_OK;
