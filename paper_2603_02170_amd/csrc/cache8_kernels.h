@@ -25,189 +25,281 @@ __device__ __forceinline__ float magnitude8(unsigned top) {
 }
 // What turns a block's numbers into codes, and codes held into codes of a larger magnitude.
 __device__ __forceinline__ float to_codes8(float a) { return a > 0.f ? __fdiv_rn(127.f, a) : 0.f; }
-__device__ __forceinline__ unsigned code8(float x, float r) { return (unsigned)(int)rintf(x * r) & 255u; }
-__device__ __forceinline__ unsigned recode8(unsigned w, float f) {      // four of them
-  unsigned y = 0;
+// Four numbers times r, rounded to nearest: the sum with 1.5 * 2^23 has the integer in its low bits.  (The product is rounded first, as the header has it:
+// half of the magnitude is a tie in it, not in an fma.)
+__device__ __forceinline__ unsigned codes8(const float* x, float r) {
+#pragma clang fp contract(off)
+  unsigned u[4];
 #pragma unroll
-  for (int i = 0; i < 4; i++) y |= ((unsigned)(int)rintf((float)(signed char)(w >> 8 * i) * f) & 255u) << 8 * i;
-  return y;
+  for (int i = 0; i < 4; i++) u[i] = __float_as_uint(x[i] * r + 12582912.f);
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0C0C0400u), __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0400u), 0x05040100u);
+}
+__device__ __forceinline__ unsigned recode8(unsigned w, float f) {      // four codes of another scale
+  float x[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[i] = (float)(signed char)(w >> 8 * i);
+  return codes8(x, f);
 }
 
-// A run is what a call brings of one block: tokens one after the other with slots that rise by one.  Its first row finds it, and one workgroup
-// has it for a head: the block's largest magnitude has to be known before the first code is written, and where it grows the codes held are
-// written again.  A workgroup looks through `window` rows for first ones.
+// 8 tokens (an octet) of a head are the work of D / 2 lanes, and a wave has EACH at a time.  K: a lane has 16 channels of a token, as they lie in
+// the page.  V: lane (j, q, i) has 16 bytes of channels c = 32 j + 4 q + i and c + 16, which turned are channels 32 j + 4 q .. and 16 more of tokens i
+// and 4 + i.  (A byte at a time, of V in LDS or in the page, storing 7700 tokens of 8 heads of 128 took 19.1 us and
+// reading them 22.8, so 16.8 and 13.1.)
 template <int D>
-__global__ __launch_bounds__(256) void cache8_append_kernel(StoreArgs a, int block_shift, int window) {
-  constexpr int PIECES = D / 8, MOST = 64 * PIECES / 256;      // 8 channels of a token each, and those of a thread
-  __shared__ __attribute__((aligned(16))) unsigned char codes[64][D + 8];
-  __shared__ unsigned tops[4][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = blockIdx.y;
-  const int row0 = blockIdx.x * window;
-  const int block = 1 << block_shift;
-  const int64_t end = (int64_t)a.g.pages << a.g.page_shift;
-  uint64_t firsts;
-  {
-    const int row = row0 + lane;
-    const bool in = lane < window && row < a.T;
-    const int64_t slot = in ? a.slots[row] : -1, before = in && row > 0 ? a.slots[row - 1] : -2;
-    firsts = __ballot(slot >= 0 && slot < end && (slot - before != 1 || (slot & (block - 1)) == 0));
+struct Octet8 {
+  static constexpr int LANES = D / 2, EACH = 64 / LANES;
+  int k_token, k_channel;                 // of the octet
+  int v_token, v_channel, v_byte;         // (and 4 more; and 16 more); of the bytes, from the octet's first
+  __device__ __forceinline__ Octet8() {
+    const int l = threadIdx.x % LANES;
+    k_token = l / (D / 16);
+    k_channel = l % (D / 16) * 16;
+    v_token = l & 3;
+    v_channel = (l >> 4) * 32 + (l >> 2 & 3) * 4;
+    v_byte = (l >> 4) * 1024 + (l & 15) * 16;
   }
-  for (; firsts != 0; firsts &= firsts - 1) {
-    const int first = row0 + __builtin_ctzll(firsts);
-    const int64_t slot0 = a.slots[first];
-    const int o = (int)(slot0 & (block - 1));
-    int n;
-    {
-      const int64_t row = (int64_t)first + lane;
-      const bool in = lane < block - o && row < a.T && a.slots[row] == slot0 + lane;
-      const uint64_t others = ~__ballot(in);
-      n = others == 0 ? 64 : __builtin_ctzll(others);
-    }
+  // of the octet's first token
+  static __device__ __forceinline__ int v_at(const CacheGeometry& g, int token) { return g.page() * D + (token >> 5) * (32 * D) + (token >> 3 & 3) * 256; }
+};
+
+// 4 x 4 bytes over the four lanes of a quad: byte k of lane i to byte i of lane k.
+struct Turn8 {
+  unsigned one, two;
+  __device__ __forceinline__ Turn8() : one(threadIdx.x & 1 ? 0x03070105u : 0x06020400u), two(threadIdx.x & 2 ? 0x03020706u : 0x05040100u) {}
+  __device__ __forceinline__ unsigned operator()(unsigned w) const {
+    w = __builtin_amdgcn_perm((unsigned)__builtin_amdgcn_mov_dpp((int)w, 0xB1, 0xF, 0xF, true), w, one);      // (lanes 1, 0, 3, 2)
+    return __builtin_amdgcn_perm((unsigned)__builtin_amdgcn_mov_dpp((int)w, 0x4E, 0xF, 0xF, true), w, two);   // (lanes 2, 3, 0, 1)
+  }
+};
+
+typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
+
+// Rows of a call whose slots rise by one inside a unit of tokens (a block, an octet) are a run, which its first row finds.  A wave looks at
+// 64 rows and the 64 behind them with one trip to memory: the runs that begin in the first `window` of them.
+struct Runs8 {
+  int64_t slot;                     // of the lane's row
+  uint64_t firsts, on, on_behind;   // rows that begin a run; that go on with the one before
+  __device__ __forceinline__ Runs8(const StoreArgs& a, int row0, int window, int unit, bool all) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)row0 + lane, end = (int64_t)a.g.pages << a.g.page_shift;
+    const auto at = [&](int64_t r) { return r >= 0 && r < a.T ? a.slots[r] : -1; };
+    const int64_t before = at(row - 1), before_behind = at(row + 63), behind = at(row + 64);
+    slot = at(row);
+    const auto valid = [&](int64_t x) { return x >= 0 && x < end; };
+    const auto goes_on = [&](int64_t x, int64_t y) { return valid(x) && y >= 0 && x - 1 == y && (x & (unit - 1)) != 0; };
+    on = __ballot(goes_on(slot, before));
+    on_behind = __ballot(goes_on(behind, before_behind));
+    firsts = __ballot(lane < window && row < a.T && (all || valid(slot))) & ~on;      // (all: rows without a slot, each by itself)
+  }
+  __device__ __forceinline__ int length(int i) const {      // of the run that begins at row i
+    const uint64_t rest = i == 63 ? on_behind : on >> (i + 1) | on_behind << (63 - i);
+    return rest == ~0ull ? 64 : 1 + __builtin_ctzll(~rest);
+  }
+};
+
+// One workgroup has a run of a block, for a head: the block's largest magnitude has to be known before the first code is written, and where it
+// grows the codes held are written again.  Of the tokens that the block can have each thread has 16 values of K and 16 of V.  (With a thread having two such
+// in turn, and the slots asked for once more for each run, 20.0 us in place of 16.8.)
+template <int D, int BLOCK>
+__global__ __launch_bounds__(BLOCK * D / 16) void cache8_append_kernel(StoreArgs a, int window) {
+  typedef Octet8<D> Octet;
+  constexpr int THREADS = BLOCK * D / 16, WAVES = THREADS / 64;
+  __shared__ unsigned tops[2][WAVES][2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = blockIdx.y;
+  const Octet me;
+  const Turn8 turn;
+  const int row0 = blockIdx.x * window;
+  const Runs8 runs(a, row0, window, BLOCK, false);
+  int side = 0;
+  for (uint64_t firsts = runs.firsts; firsts != 0; firsts &= firsts - 1, side ^= 1) {
+    const int index = __builtin_ctzll(firsts), first = row0 + index, n = runs.length(index);
+    const int64_t slot0 = (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(runs.slot >> 32), index) << 32 |
+                                    (unsigned)__builtin_amdgcn_readlane((int)runs.slot, index));
+    const int o = (int)(slot0 & (BLOCK - 1));
     const int at = (int)(slot0 & (a.g.page() - 1)) - o;          // the block's first token in its page
     unsigned char* p = a.pool + ((size_t)(slot0 >> a.g.page_shift) * a.g.H + h) * Bytes8<D>::head_bytes(a.g);
     float* magnitudes = (float*)(p + Bytes8<D>::magnitudes(a.g) + at / 4);
     const float held[2] = {o > 0 ? magnitudes[0] : 0.f, o > 0 ? magnitudes[1] : 0.f};
-    v8bf x[2][MOST];
-    unsigned top[2] = {0, 0};
-    const auto numbers = [&](float* f, int which, int i) {      // of the thread's i-th piece
-      const int c = tid % PIECES * 8;
-#pragma unroll
-      for (int e = 0; e < 8; e++) f[e] = (float)x[which][i][e];
-      subtract_mean(f, which == 0 ? a.k_mean : a.v_mean, h * D + c);
-    };
-#pragma unroll
-    for (int i = 0; i < MOST; i++) {
-      const int t = tid / PIECES + i * (256 / PIECES), c = tid % PIECES * 8;
-      if (t >= n) continue;
-      x[0][i] = *(const v8bf*)(a.K + (int64_t)(first + t) * a.ks[0] + h * a.ks[1] + c);
-      x[1][i] = *(const v8bf*)(a.V + (int64_t)(first + t) * a.vs[0] + h * a.vs[1] + c);
+    const int t0 = 8 * ((o >> 3) + tid / Octet::LANES);      // the thread's octet of the block
+    const auto is_new = [&](int t) { return t >= o && t < o + n; };
+    v8bf k[2] = {};
+    v4bf v[2][2] = {};      // token i or 4 + i, channels c or c + 16
+    if (is_new(t0 + me.k_token)) {
+      const __bf16* x = a.K + (int64_t)(first + t0 + me.k_token - o) * a.ks[0] + h * a.ks[1] + me.k_channel;
+      k[0] = *(const v8bf*)x;
+      k[1] = *(const v8bf*)(x + 8);
     }
 #pragma unroll
-    for (int i = 0; i < MOST; i++) {
-      const int t = tid / PIECES + i * (256 / PIECES);
-      if (t >= n) continue;
+    for (int half = 0; half < 2; half++) {
+      const int t = t0 + me.v_token + 4 * half;
+      if (!is_new(t)) continue;
+      const __bf16* x = a.V + (int64_t)(first + t - o) * a.vs[0] + h * a.vs[1] + me.v_channel;
+      v[half][0] = *(const v4bf*)x;
+      v[half][1] = *(const v4bf*)(x + 16);
+    }
+    const auto keys = [&](float* f) {
 #pragma unroll
-      for (int which = 0; which < 2; which++) {
-        float f[8];
-        numbers(f, which, i);
+      for (int e = 0; e < 16; e++) f[e] = (float)k[e / 8][e % 8];
+      subtract_mean(f, a.k_mean, h * D + me.k_channel);
+      subtract_mean(f + 8, a.k_mean, h * D + me.k_channel + 8);
+    };
+    const auto values = [&](int half, int more, float* f) {
+      typedef v4f v4f_dword __attribute__((aligned(4)));
 #pragma unroll
-        for (int e = 0; e < 8; e++) top[which] = max(top[which], __float_as_uint(f[e]) & 0x7FFFFFFFu);
+      for (int e = 0; e < 4; e++) f[e] = (float)v[half][more][e];
+      if (a.v_mean == nullptr) return;
+      const v4f mean = *(const v4f_dword*)(a.v_mean + h * D + me.v_channel + 16 * more);
+#pragma unroll
+      for (int e = 0; e < 4; e++) f[e] -= mean[e];
+    };
+    unsigned top[2] = {0, 0};      // (tokens that are not the call's are zeros, but for a mean taken off)
+    float f[16];
+    if (is_new(t0 + me.k_token)) {
+      keys(f);
+#pragma unroll
+      for (int e = 0; e < 16; e++) top[0] = max(top[0], __float_as_uint(f[e]) & 0x7FFFFFFFu);
+    }
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+      if (!is_new(t0 + me.v_token + 4 * half)) continue;
+#pragma unroll
+      for (int more = 0; more < 2; more++) {
+        values(half, more, f);
+#pragma unroll
+        for (int e = 0; e < 4; e++) top[1] = max(top[1], __float_as_uint(f[e]) & 0x7FFFFFFFu);
       }
     }
 #pragma unroll
     for (int which = 0; which < 2; which++) {
 #pragma unroll
-      for (int k = 1; k < 64; k <<= 1) top[which] = max(top[which], (unsigned)__shfl_xor((int)top[which], k));
-      if (lane == 0) tops[wave][which] = top[which];
+      for (int x = 1; x < 64; x <<= 1) top[which] = max(top[which], (unsigned)__shfl_xor((int)top[which], x));
+      if (lane == 0) tops[side][wave][which] = top[which];
     }
-    __syncthreads();
+    __syncthreads();               // (the next run has the other side of them)
     float now[2], r[2], again[2];
     bool grown[2];
 #pragma unroll
     for (int which = 0; which < 2; which++) {
-      unsigned t = max(max(tops[0][which], tops[1][which]), max(tops[2][which], tops[3][which]));
-      t = max(t, __float_as_uint(held[which]) & 0x7FFFFFFFu);
+      unsigned t = __float_as_uint(held[which]) & 0x7FFFFFFFu;
+#pragma unroll
+      for (int w = 0; w < WAVES; w++) t = max(t, tops[side][w][which]);
       now[which] = magnitude8(t);
       r[which] = to_codes8(now[which]);
       grown[which] = o > 0 && now[which] > held[which];
       again[which] = grown[which] ? __fdiv_rn(held[which], now[which]) : 1.f;
     }
-    // new codes: K's to the page, V's to LDS, where 8 tokens of a channel meet
+    if (is_new(t0 + me.k_token)) {
+      keys(f);
+      *(uint4*)(p + Bytes8<D>::k(at + t0 + me.k_token, me.k_channel)) = uint4{codes8(f, r[0]), codes8(f + 4, r[0]), codes8(f + 8, r[0]), codes8(f + 12, r[0])};
+    }
+    unsigned w[2][2];      // channel c or c + 16; tokens 0 .. 3 or 4 .. 7
 #pragma unroll
-    for (int i = 0; i < MOST; i++) {
-      const int t = tid / PIECES + i * (256 / PIECES), c = tid % PIECES * 8;
-      if (t >= n) continue;
+    for (int more = 0; more < 2; more++)
 #pragma unroll
-      for (int which = 0; which < 2; which++) {
-        float f[8];
-        numbers(f, which, i);
-        uint2 w = {0, 0};
-        if (r[which] > 0.f) {
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            w.x |= code8(f[e], r[which]) << 8 * e;
-            w.y |= code8(f[4 + e], r[which]) << 8 * e;
-          }
-        }
-        if (which == 0) *(uint2*)(p + Bytes8<D>::k(at + o + t, c)) = w;
-        else *(uint2*)&codes[o + t][c] = w;
+      for (int half = 0; half < 2; half++) {
+        values(half, more, f);
+        w[more][half] = turn(codes8(f, r[1]));
       }
+    const int from = max(o - t0, 0), upto = min(o + n - t0, 8);      // new tokens of the octet
+    if (upto > 0) {
+      uint4* to = (uint4*)(p + Octet::v_at(a.g, at + t0) + me.v_byte);
+      if (from > 0 || upto < 8) {
+        const uint4 y = *to;
+        const unsigned old[2][2] = {{y.x, y.y}, {y.z, y.w}};
+        const uint64_t below = (1ull << 8 * from) - 1, fresh = (upto == 8 ? ~0ull : (1ull << 8 * upto) - 1) & ~below;
+#pragma unroll
+        for (int more = 0; more < 2; more++)
+#pragma unroll
+          for (int half = 0; half < 2; half++) {
+            const unsigned is_fresh = (unsigned)(fresh >> 32 * half), is_below = (unsigned)(below >> 32 * half), x = old[more][half];
+            const unsigned kept = grown[1] ? (recode8(x, again[1]) & is_below) | (x & ~is_below) : x;      // (behind the new tokens nothing is the call's)
+            w[more][half] = (w[more][half] & is_fresh) | (kept & ~is_fresh);
+          }
+      }
+      *to = uint4{w[0][0], w[0][1], w[1][0], w[1][1]};
     }
     if (grown[0]) {
-      for (int i = tid; i < o * PIECES; i += 256) {
-        uint2* q = (uint2*)(p + Bytes8<D>::k(at + i / PIECES, i % PIECES * 8));
-        const uint2 w = *q;
-        *q = uint2{recode8(w.x, again[0]), recode8(w.y, again[0])};
+#pragma unroll 1
+      for (int i = tid; i < o * (D / 16); i += THREADS) {
+        uint4* q = (uint4*)(p + Bytes8<D>::k(at + i / (D / 16), i % (D / 16) * 16));
+        const uint4 w = *q;
+        *q = uint4{recode8(w.x, again[0]), recode8(w.y, again[0]), recode8(w.z, again[0]), recode8(w.w, again[0])};
       }
     }
-    __syncthreads();
-    {
-      const int octet0 = grown[1] ? 0 : o >> 3, octets = ((o + n + 7) >> 3) - octet0;
-      for (int i = tid; i < octets * (D / 2); i += 256) {
-        const int octet = octet0 + i / (D / 2), q = i % (D / 2), c = q / 16 * 32 + q % 16;
-        uint4* to = (uint4*)(p + Bytes8<D>::v(a.g, at / 8 + octet, c));
-        const int from = min(max(o - 8 * octet, 0), 8), upto = min(o + n - 8 * octet, 8);      // new tokens of the octet
-        uint4 w = {0, 0, 0, 0};
-        if (from > 0 || upto < 8) {
-          w = *to;
-          if (grown[1]) {
-            const uint4 y = {recode8(w.x, again[1]), recode8(w.y, again[1]), recode8(w.z, again[1]), recode8(w.w, again[1])};
-            // (tokens behind the new ones are not the call's)
-            const uint64_t mask = from == 8 ? ~0ull : (1ull << 8 * from) - 1;
-            const unsigned lo = (unsigned)mask, hi = (unsigned)(mask >> 32);
-            w = uint4{(w.x & ~lo) | (y.x & lo), (w.y & ~hi) | (y.y & hi), (w.z & ~lo) | (y.z & lo), (w.w & ~hi) | (y.w & hi)};
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < 8; t++) {
-          if (t < from || t >= upto) continue;
-          const unsigned mask = 255u << 8 * (t & 3), u = (unsigned)codes[8 * octet + t][c] << 8 * (t & 3),
-                         v = (unsigned)codes[8 * octet + t][c + 16] << 8 * (t & 3);
-          if (t < 4) {
-            w.x = (w.x & ~mask) | u;
-            w.z = (w.z & ~mask) | v;
-          } else {
-            w.y = (w.y & ~mask) | u;
-            w.w = (w.w & ~mask) | v;
-          }
-        }
-        *to = w;
+    if (grown[1]) {
+#pragma unroll 1
+      for (int i = tid; i < (o >> 3) * Octet::LANES; i += THREADS) {
+        uint4* q = (uint4*)(p + Octet::v_at(a.g, at + i / Octet::LANES * 8) + (i % Octet::LANES >> 4) * 1024 + (i & 15) * 16);
+        const uint4 w = *q;
+        *q = uint4{recode8(w.x, again[1]), recode8(w.y, again[1]), recode8(w.z, again[1]), recode8(w.w, again[1])};
       }
     }
-    if (tid < block >> 5) *(float2*)(magnitudes + 2 * tid) = float2{now[0], now[1]};
-    __syncthreads();
+    if (tid < BLOCK / 32) *(float2*)(magnitudes + 2 * tid) = float2{now[0], now[1]};
   }
 }
 
-// d / 8 lanes have a token of a head, 8 channels each.
+// The tokens of an octet that stand one after the other are read together; a wave has some of those that begin in the workgroup's `window` rows.
 template <int D>
-__global__ __launch_bounds__(256) void cache8_read_kernel(StoreArgs a) {
-  constexpr int LANES = D / 8, ROWS = 256 / LANES;
-  const int l = threadIdx.x % LANES, c = 8 * l;
-  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
-  if (row >= a.T) return;
-  const int h = blockIdx.y, t = (int)row;
-  const int64_t slot = a.slots[t];
-  const bool stored = slot >= 0 && slot < ((int64_t)a.g.pages << a.g.page_shift);
-  const int at = stored ? (int)(slot & (a.g.page() - 1)) : 0;
-  const unsigned char* p = a.pool + ((size_t)(stored ? slot >> a.g.page_shift : 0) * a.g.H + h) * Bytes8<D>::head_bytes(a.g);
-  const uint2 w = *(const uint2*)(p + Bytes8<D>::k(at, c));
-  const float2 top = *(const float2*)(p + Bytes8<D>::magnitudes(a.g) + at / 32 * 8);
-  const unsigned char* pv = p + Bytes8<D>::v(a.g, at / 8, c) + at % 8;
-  const float ks = __fdiv_rn(top.x, 127.f), vs = __fdiv_rn(top.y, 127.f);
-  v8bf k, v;
+__global__ __launch_bounds__(256) void cache8_read_kernel(StoreArgs a, int window) {
+  typedef Octet8<D> Octet;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = blockIdx.y;
+  const Octet me;
+  const Turn8 turn;
+  const int row0 = blockIdx.x * window;
+  const int64_t end = (int64_t)a.g.pages << a.g.page_shift;
+  const Runs8 runs(a, row0, window, 8, true);
+  uint64_t firsts = runs.firsts;
+  for (int skip = wave * Octet::EACH; skip > 0; skip--) firsts &= firsts - 1;
+  while (firsts != 0) {
+    uint64_t mine = firsts;
+    if (lane >= Octet::LANES && (mine & (mine - 1)) != 0) mine &= mine - 1;      // (of two octets the second; where there is none both are the first)
+    for (int skip = 4 * Octet::EACH; skip > 0; skip--) firsts &= firsts - 1;
+    const int index = __builtin_ctzll(mine), first = row0 + index, n = runs.length(index);
+    const int64_t slot0 = __shfl(runs.slot, index);
+    const bool stored = slot0 >= 0 && slot0 < end;
+    const int at = stored ? (int)(slot0 & (a.g.page() - 1)) : 0, t0 = at & ~7, o = at & 7;
+    const unsigned char* p = a.pool + ((size_t)(stored ? slot0 >> a.g.page_shift : 0) * a.g.H + h) * Bytes8<D>::head_bytes(a.g);
+    const uint4 kw = *(const uint4*)(p + Bytes8<D>::k(t0 + me.k_token, me.k_channel));
+    const uint4 vw = *(const uint4*)(p + Octet::v_at(a.g, t0) + me.v_byte);
+    const float2 top = *(const float2*)(p + Bytes8<D>::magnitudes(a.g) + t0 / 32 * 8);
+    const float ks = stored ? __fdiv_rn(top.x, 127.f) : 0.f, vs = stored ? __fdiv_rn(top.y, 127.f) : 0.f;
+    const auto row_of = [&](int t) { return t >= o && t < o + n ? first + t - o : -1; };      // of the octet's token t, if the call asks for it here
+    const auto numbers = [&](unsigned w, float s, const float* mean, int c, __bf16* to) {      // four of them
+#pragma clang fp contract(off)
+      typedef v4f v4f_dword __attribute__((aligned(4)));
+      v4f m = {0.f, 0.f, 0.f, 0.f};
+      if (mean != nullptr && stored) m = *(const v4f_dword*)(mean + h * D + c);
 #pragma unroll
-  for (int e = 0; e < 8; e++) {
-    float x = (float)(signed char)((e < 4 ? w.x : w.y) >> 8 * (e % 4)) * ks;
-    float y = (float)(signed char)pv[16 * e] * vs;
-    if (a.k_mean != nullptr) x += a.k_mean[h * D + c + e];
-    if (a.v_mean != nullptr) y += a.v_mean[h * D + c + e];
-    k[e] = (__bf16)(stored ? x : 0.f);
-    v[e] = (__bf16)(stored ? y : 0.f);
+      for (int e = 0; e < 4; e++) to[e] = (__bf16)(stored ? (float)(signed char)(w >> 8 * e) * s + m[e] : 0.f);
+    };
+    const int row = row_of(me.k_token);
+    if (row >= 0) {
+      v8bf x[2];
+      const unsigned w[4] = {kw.x, kw.y, kw.z, kw.w};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        __bf16 f[4];
+        numbers(w[i], ks, a.k_mean, me.k_channel + 4 * i, f);
+#pragma unroll
+        for (int e = 0; e < 4; e++) x[i / 2][4 * (i % 2) + e] = f[e];
+      }
+      __bf16* to = a.Ko + ((size_t)row * a.g.H + h) * D + me.k_channel;
+      *(v8bf*)to = x[0];
+      *(v8bf*)(to + 8) = x[1];
+    }
+    const unsigned w[2][2] = {{turn(vw.x), turn(vw.y)}, {turn(vw.z), turn(vw.w)}};
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+      const int row = row_of(me.v_token + 4 * half);
+      if (row < 0) continue;
+#pragma unroll
+      for (int more = 0; more < 2; more++) {
+        __bf16 f[4];
+        numbers(w[more][half], vs, a.v_mean, me.v_channel + 16 * more, f);
+        *(v4bf*)(a.Vo + ((size_t)row * a.g.H + h) * D + me.v_channel + 16 * more) = v4bf{f[0], f[1], f[2], f[3]};
+      }
+    }
   }
-  const size_t to = ((size_t)t * a.g.H + h) * D + c;
-  *(v8bf*)(a.Ko + to) = k;
-  *(v8bf*)(a.Vo + to) = v;
 }
 
 }  // namespace sage
