@@ -147,7 +147,7 @@ struct ByteForm {
 };
 
 template <int D, int NQ>
-__global__ __launch_bounds__(256, 2) void cache8_attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, NQ > 2 ? 1 : 2) void cache8_attend_kernel(AttendArgs a) {
   attend_items<ByteForm<D>, NQ>(a);
 }
 
@@ -309,10 +309,6 @@ struct ByteChunks {
 template <int D>
 __global__ __launch_bounds__(512, 2) void cache8_chunk_kernel(AttendArgs a) {
   chunk_items<ByteChunks<D>>(a);
-}
-template <int D, int RG>
-__global__ __launch_bounds__(512, 2) void cache8_span_kernel(AttendArgs a) {
-  span_items<ByteChunks<D>, RG>(a);
 }
 template <int D>
 __global__ __launch_bounds__(512) void cache8_unpack_kernel(AttendArgs a) {

@@ -19,7 +19,8 @@ __global__ __launch_bounds__(256) void cache8_join_rows_kernel(AttendArgs a) {
 
 template <int DIM>
 struct ByteKernels {
-  static constexpr int D = DIM;
+  static constexpr int D = DIM, MOST_TILES = DIM == 128 ? 4 : 2;      // of 16 rows, of the kernel for few
+  static constexpr bool BYTES = true;      // held in 8 bits: no kernel for tiles of 64 and 128 rows
   template <int NQ>
   static void few(int grid, const AttendArgs& a, hipStream_t st) { cache8_attend_kernel<D, NQ><<<grid, 256, 0, st>>>(a); }
   template <int ROWS>
@@ -27,8 +28,6 @@ struct ByteKernels {
   template <int ROWS>
   static void join_many(dim3 grid, const AttendArgs& a, hipStream_t st) { cache8_join_rows_kernel<D, ROWS><<<grid, 256, 0, st>>>(a); }
   static void chunk(int grid, const AttendArgs& a, hipStream_t st) { cache8_chunk_kernel<D><<<grid, 512, 0, st>>>(a); }
-  template <int RG>
-  static void span(int grid, const AttendArgs& a, hipStream_t st) { cache8_span_kernel<D, RG><<<grid, 512, 0, st>>>(a); }
   static void unpack(int grid, const AttendArgs& a, hipStream_t st) { cache8_unpack_kernel<D><<<grid, 512, 0, st>>>(a); }
   static void wide(int grid, const AttendArgs& a, hipStream_t st) { cache8_wide_kernel<D><<<grid, 512, 0, st>>>(a); }
 };

@@ -19,7 +19,8 @@ using namespace sage;
 
 template <int DIM, int GROUP>
 struct NibbleKernels {
-  static constexpr int D = DIM;
+  static constexpr int D = DIM, MOST_TILES = 2;      // of 16 rows, of the kernel for few
+  static constexpr bool BYTES = false;      // held in 8 bits: no kernel for tiles of 64 and 128 rows
   template <int NQ>
   static void few(int grid, const AttendArgs& a, hipStream_t st) { cache_attend_kernel<D, GROUP, NQ><<<grid, 256, 0, st>>>(a); }
   template <int ROWS>

@@ -56,13 +56,21 @@ inline int most_length(const sagebwd_cache_params& p, const sagebwd_cache_call& 
   const int64_t all = (int64_t)c.columns * p.page;
   return (int)(c.max_length > 0 && c.max_length < all ? c.max_length : all);
 }
+// Where every request brings so many rows and a CU has much to do, tiles of 48 or 64 rows by one wave a SIMD, with all its registers, unpack less often
+// than those of 32 by two; in short calls the latter end sooner.  (us, 32 -> 48 or 64 rows a tile, 8 heads of 128 in the cache: 32 requests of 4096
+// tokens, 48 rows 90 -> 67, 64 rows 88 -> 81, 128 rows 166 -> 147; 24 ragged ones of up to 3000 of 4 heads, 48 rows 19.0 -> 20.4; heads of 64, 64 rows 48 -> 54.)
+inline int tile_tiles_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c, int64_t rows) {      // of 16 rows
+  const int64_t units = (int64_t)c.R * p.H * ((most_length(p, c) + kUnit - 1) / kUnit);
+  if (p.block == 0 || p.d != 128 || rows <= 32 || units < 16 * kCus || 5 * (int64_t)c.T < 3 * (int64_t)c.R * c.max_new) return rows <= 16 ? 1 : 2;
+  return rows <= 48 || (rows > 64 && rows <= 96) ? 3 : 4;
+}
 inline int few_rows_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
   const int64_t line = (int64_t)c.R * p.H * (kTiledRows / 32) * ((most_length(p, c) + kUnit - 1) / kUnit + kItemCost);
   return p.block > 0 && line <= 1 << 29 ? kTiledRows : kFewRows;
 }
 inline int tile_rows_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
   const int64_t most = most_rows(p, c);
-  return most > 128 || most_length(p, c) <= 256 ? kChunkRows : most > 64 ? 128 : 64;
+  return p.block > 0 || most > 128 || most_length(p, c) <= 256 ? kChunkRows : most > 64 ? 128 : 64;
 }
 // Row tiles of the kernel for many rows, over all heads, at most; 0 where no request goes to it.
 inline int64_t chunk_tiles_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
@@ -141,16 +149,19 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
   if (w.few) {
     AttendLaunch& l = w.f;
     const int64_t here = !w.many ? rows : few_rows > kFewRows ? few_rows : G > 16 ? G : 16;
-    l.nq = here <= 16 ? 1 : 2;
+    l.nq = w.many ? (here <= 16 ? 1 : 2) : tile_tiles_of(p, c, here);
+    const int64_t tiles = (here + 16 * l.nq - 1) / (16 * l.nq);
     l.rows_from = 0;
     l.rows_to = here > 32 ? few_rows : 16 * l.nq;
     l.join_rows = (int)(here < 16 * l.nq ? here : 16 * l.nq);
     const int most_units = (w.max_length + kUnit - 1) / kUnit;
     l.split = most_units > kWholeUnits;
-    const int64_t units = (int64_t)c.R * p.H * ((here + 31) / 32) * (l.split ? most_units + kItemCost : 1);
-    const int64_t slots = 2 * kCus;
+    const int64_t units = (int64_t)c.R * p.H * tiles * (l.split ? most_units + kItemCost : 1);
+    // (Held in 8 bits the keys alone bound a call of one tile, and a workgroup a CU has enough of them under way: 32 requests of 4096 tokens, 16 rows
+    // 59.4 -> 55.1 us, 32 rows 63.2 -> 57.0, one of 131000 57.4 -> 55.2.  Of several tiles two: heads of 64, up to 100 rows 19.6 -> 18.4.)
+    const int64_t slots = (p.block > 0 && (tiles == 1 || l.nq > 2) ? 1 : 2) * kCus;
     l.workgroups = (int)(units < slots ? (units > 0 ? units : 1) : slots);
-    l.join_wide = p.block > 0 && (int64_t)c.R * p.H * ((here + 31) / 32) >= 64;
+    l.join_wide = p.block > 0 && (int64_t)c.R * p.H * tiles >= 64;
     lay_out(l, 16 * l.nq);
   }
   if (w.many) {
@@ -187,8 +198,9 @@ int launch_few(const AttendArgs& a, const AttendLaunch& l, hipStream_t st) {
   Kernels::template few<NQ>(l.workgroups, a, st);
   SERVE_LAUNCH_CHECK();
   if (l.split && l.workgroups > 1) {
-    if (l.join_wide) Kernels::template join_many<16 * NQ>(dim3(l.workgroups - 1, (l.join_rows * (Kernels::D / 4) + 255) / 256), a, st);
-    else Kernels::template join_few<16 * NQ>(dim3(l.workgroups - 1, l.join_rows), a, st);
+    if (!Kernels::BYTES || !l.join_wide) Kernels::template join_few<16 * NQ>(dim3(l.workgroups - 1, l.join_rows), a, st);
+    if constexpr (Kernels::BYTES)
+      if (l.join_wide) Kernels::template join_many<16 * NQ>(dim3(l.workgroups - 1, (l.join_rows * (Kernels::D / 4) + 255) / 256), a, st);
     SERVE_LAUNCH_CHECK();
   }
   return SAGEBWD_OK;
@@ -214,24 +226,28 @@ int launch_attend(AttendArgs a, const AttendPlan& w, char* ws, hipStream_t st) {
       Kernels::unpack(w.m.unpack_workgroups, a, st);
       SERVE_LAUNCH_CHECK();
       Kernels::wide(w.m.workgroups, a, st);
-    } else if (w.m.tile_rows == 64) {
-      Kernels::template span<2>(w.m.workgroups, a, st);
-    } else if (w.m.tile_rows == 128) {
-      Kernels::template span<4>(w.m.workgroups, a, st);
-    } else {
+    } else if (w.m.tile_rows == kChunkRows) {
       Kernels::chunk(w.m.workgroups, a, st);
+    } else {
+      if constexpr (!Kernels::BYTES) w.m.tile_rows == 64 ? Kernels::template span<2>(w.m.workgroups, a, st) : Kernels::template span<4>(w.m.workgroups, a, st);
     }
     SERVE_LAUNCH_CHECK();
     if (w.m.split && w.m.workgroups > 1) {
       const dim3 grid(w.m.workgroups - 1, w.m.tile_rows / (256 / (Kernels::D / 4)));
-      if (w.m.tile_rows == 64) Kernels::template join_many<64>(grid, a, st);
-      else if (w.m.tile_rows == 128) Kernels::template join_many<128>(grid, a, st);
-      else Kernels::template join_many<kChunkRows>(grid, a, st);
+      if (w.m.tile_rows == kChunkRows) Kernels::template join_many<kChunkRows>(grid, a, st);
+      if constexpr (!Kernels::BYTES) {
+        if (w.m.tile_rows == 64) Kernels::template join_many<64>(grid, a, st);
+        if (w.m.tile_rows == 128) Kernels::template join_many<128>(grid, a, st);
+      }
       SERVE_LAUNCH_CHECK();
     }
   }
   if (w.few) {
     with(w.f);
+    if constexpr (Kernels::MOST_TILES > 2) {
+      if (w.f.nq == 3) return launch_few<Kernels, 3>(a, w.f, st);
+      if (w.f.nq == 4) return launch_few<Kernels, 4>(a, w.f, st);
+    }
     return w.f.nq == 1 ? launch_few<Kernels, 1>(a, w.f, st) : launch_few<Kernels, 2>(a, w.f, st);
   }
   return SAGEBWD_OK;

@@ -292,6 +292,43 @@ def test_long_requests_in_every_form(lens, news, d, block, Hq, H, causal):
     _check(f, q, cu, O, lse, causal)
 
 
+@pytest.mark.parametrize("R,L,n,G,H,block", [(20, 4100, 12, 4, 8, 64), (24, 4000, 16, 4, 6, 32), (20, 4000, 23, 4, 7, 64), (20, 4000, 32, 4, 7, 64), (1, 40000, 16, 3, 16, 64),
+                                             (20, 4100, 4, 8, 8, 32)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_much_work_in_tiles_of_48_and_64_rows(R, L, n, G, H, block, causal):
+    """Requests of other lengths and new tokens than the longest, too; of each form some requests and heads are looked at."""
+    g, rng = torch.Generator().manual_seed(R + n), np.random.default_rng(n)
+    p = CacheParams(H=H, d=128, page=64, block=block)
+    base = Filled([L], p, g, spare_columns=0)          # (its pages are every request's)
+    lens = [L - int(x) for x in rng.integers(0, L // 3, R)]
+    news = [n - int(x) if r % 3 == 1 else n for r, x in enumerate(rng.integers(0, n, R))]
+    lens[0], news[-1] = L, n
+    q = _randn((sum(news), H * G, 128), g)
+    cu = np.concatenate([[0], np.cumsum(news)]).astype(int).tolist()
+    O, lse = cache.sagebwd_cache_attention(q.cuda(), base.pool, base.table.expand(R, -1).contiguous(), _i32(lens), _i32(cu), p, n, causal=causal)
+    again = cache.sagebwd_cache_attention(q.cuda(), base.pool, base.table.expand(R, -1).contiguous(), _i32(lens), _i32(cu), p, n, causal=causal)
+    assert torch.equal(O, again[0]) and torch.equal(lse, again[1])
+    for r in sorted({0, min(1, R - 1), R - 1, int(rng.integers(0, R))}):
+        a, b = cu[r], cu[r + 1]
+        for h in (0, H - 1):
+            one = type("One", (), dict(p=p, lens=[lens[r]], k=base.k[:lens[r], h:h + 1], v=base.v[:lens[r], h:h + 1], at=[0, lens[r]]))
+            heads = slice(h * G, h * G + G)
+            _check(one, q[a:b, heads], [0, b - a], O[a:b, heads], lse[heads, a:b], causal)
+
+
+def test_more_keys_and_heads_than_a_line_of_row_tiles_holds():
+    """33 to 128 rows under tables so wide that they go to the kernel for 256 rows."""
+    g = torch.Generator().manual_seed(3)
+    f = Filled([300, 70], CacheParams(H=512, d=64, page=32, block=32), g)
+    wide = torch.nn.functional.pad(f.table, (0, 1_200_000), value=-1)
+    assert 2 * 512 * 4 * (wide.shape[1] // 4) > 1 << 29
+    q = _randn((80, 512, 64), g)
+    O, lse = cache.sagebwd_cache_attention(q.cuda(), f.pool, wide, f.lengths, _i32([0, 40, 80]), f.p, 40)
+    want, wl = cache.sagebwd_cache_attention(q.cuda(), f.pool, f.table, f.lengths, _i32([0, 40, 80]), f.p, 40)
+    _check(f, q, [0, 40, 80], O, lse, True)
+    _check(f, q, [0, 40, 80], want, wl, True)
+
+
 @pytest.mark.parametrize("d,block,page,Hq,H,n,L", [(64, 32, 32, 4, 4, 1, 777), (128, 64, 64, 4, 1, 1, 1025), (128, 32, 64, 32, 2, 3, 300), (64, 64, 256, 16, 2, 40, 333),
                                                    (128, 64, 128, 8, 2, 150, 400), (128, 32, 64, 4, 1, 520, 600)])
 def test_every_token_is_weighed_alone(d, block, page, Hq, H, n, L):

@@ -42,12 +42,16 @@ def _pick(kernels, stem, *bits):
 
 
 def test_two_workgroups_of_the_attention_of_few_rows_share_a_cu(kernels):
-    for k in _pick(kernels, "cache8_attend_kernel"):
-        assert k["vgpr"] <= 256 and k["scratch"] == 0 and 2 * k["lds"] <= 160 * 1024, k
+    for bits in ("ELi1EEEv", "ELi2EEEv"):
+        for k in _pick(kernels, "cache8_attend_kernel", bits):
+            assert k["vgpr"] <= 256 and k["scratch"] == 0 and 2 * k["lds"] <= 160 * 1024, k
+    for bits in ("ELi3EEEv", "ELi4EEEv"):              # (one)
+        for k in _pick(kernels, "cache8_attend_kernel", "ILi128", bits):
+            assert k["vgpr"] <= 512 and k["scratch"] <= 64, k
 
 
 def test_the_attention_of_many_rows_fits_a_cu(kernels):
-    for stem in ("cache8_chunk_kernel", "cache8_span_kernel", "cache8_wide_kernel"):
+    for stem in ("cache8_chunk_kernel", "cache8_wide_kernel"):
         for k in _pick(kernels, stem):
             assert k["vgpr"] <= 256 and k["lds"] <= 160 * 1024, (stem, k)
     for k in _pick(kernels, "cache8_chunk_kernel") + _pick(kernels, "cache8_wide_kernel", "ILi128E"):
