@@ -198,7 +198,7 @@ typedef struct sagebwd_cache_call {
  * unpacked to bf16 in the workspace first (256 d bytes for 64 tokens and head; at most 4 GiB, else each tile unpacks its own).  How
  * work is divided depends on all requests of the call, so that O agrees between calls of different batches to its rounding, and bit
  * for bit between equal calls.
- * Range: with |Q| < 2^117, and V's largest magnitude (less its mean) times the request's length < 2^117, no sum overflows where the result does
+ * Range: with |Q| < 2^117 (held in 8 bits 2^112, as codes are whole numbers up to 127), and V's largest magnitude (less its mean) times the request's length < 2^117, no sum overflows where the result does
  * not.  (Logits: nibbles are read as 16 .. 31 and 24 sum(Q) taken off.  Values: a row's sum is formed before it is divided, of probabilities
  * relative to a reference up to 2^8 below the largest, times nibbles of 31.)  Beyond it rows may be infinite or NaN.
  * The workspace depends on the host's sizes alone; its contents before the call do not matter, and calls in flight at a time (on two

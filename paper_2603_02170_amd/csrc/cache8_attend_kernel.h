@@ -166,7 +166,8 @@ __global__ __launch_bounds__(256, NQ > 2 ? 1 : 2) void cache8_attend_kernel(Atte
 
 // ---- many rows ---------------------------------------------------------------------------------------------------------
 // V's scale of a half goes into its exponents (log2 of it), so that they give the probabilities times it, and out of their sum.  (Of a scale of zero, whose
-// codes are zeros, any other will do, and for one that is no number poison() stands in.)  32 products of a lane and tile less: 2048 rows x 4 against 10000 tokens 300.4 -> WIDE us.
+// codes are zeros, any other will do, and for one that is no number poison() stands in.)  It saves 32 products of a lane and tile: 2048 new tokens of
+// 4 heads of a group against 10000 313 -> 304 us.
 struct ByteKnown {
   int flags[2];           // bit 0: the half's page exists; bit 1: and its values are not numbers; bit 2: and its keys
   float k[2], log_v[2];

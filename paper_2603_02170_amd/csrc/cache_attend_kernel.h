@@ -40,6 +40,7 @@ struct AttendArgs {
   int workgroups;
   int split;            // 1: an item's units may go to several workgroups
   int rows_from, rows_to;   // the launch has the requests of rows_from < rows (new tokens times G) <= rows_to
+  int direct;           // not 0: every request has so many workgroups, one an item, whether it has as many items or not
 };
 
 constexpr int kUnit = 128;          // tokens that a workgroup of four waves takes at a time
@@ -463,68 +464,80 @@ __device__ __forceinline__ void attend_items(AttendArgs a) {
   // what is dealt out of a request's items of a head
   const auto shared_units = [&](int u, int rows) { return u == 0 ? 0 : (a.split ? u + kItemCost : 1) * Cursor::tiles_of(rows); };
 
-  // units up to every thread's requests (R / 256 each; where that is one it is kept)
-  const int per = (a.R + 255) / 256, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
   Cursor cursor;
   cursor.known = known;
-  int mine = 0;
-  if (a.R <= kKnown) {
-    if (tid < a.R) {
-      cursor.take(a, attend_request(a, tid));
-      const int x[6] = {cursor.begin, cursor.n_rows, cursor.len, cursor.first_sees, cursor.visible, cursor.units};
-#pragma unroll
-      for (int i = 0; i < 6; i++) known[i][tid] = x[i];
-      mine = shared_units(cursor.units, cursor.n_rows);
-    }
-  } else {
-    for (int r = r0; r < r1; r++) mine += shared_units(attend_units(a, r), attend_request(a, r).rows);
-  }
-  int upto = mine;
-  for (int k = 1; k < 64; k <<= 1) {
-    const int u = __shfl_up(upto, k);
-    if (lane >= k) upto += u;
-  }
-  if (lane == 63) wave_units[wave] = upto;
-  __syncthreads();
-  int units = 0;
-#pragma unroll
-  for (int k = 0; k < 4; k++) {
-    if (k < wave) upto += wave_units[k];
-    units += wave_units[k];
-  }
-  const AttendShares shares(__builtin_amdgcn_readfirstlane(units) * H, a.workgroups);
   const int w = blockIdx.x;
-  if (a.split && tid == 0) a.joins[w] = int4{0, 0, 0, 0};
-  if (w >= shares.n) return;
-  const int begin = shares.begin(w);
-  if ((upto - mine) * H <= begin && begin < upto * H) {
-    int at = upto - mine;
-    for (int r = r0; r < r1; r++) {
-      const int u = a.R <= kKnown ? shared_units(known[5][r], known[1][r]) : shared_units(attend_units(a, r), attend_request(a, r).rows);
-      if (begin < (at + u) * H) {
-        found[0] = r;
-        found[1] = begin - at * H;
-        break;
+  // (Where nothing is divided and items are few: no sum over the requests, four of up to 500 tokens 8.4 -> 7.4 us.)
+  bool dealt = true;
+  if constexpr (Form::TILED) dealt = a.direct == 0;
+  if (!dealt) {
+    cursor.r = cursor.base = w / a.direct;
+    cursor.head = w - cursor.r * a.direct;
+    cursor.take(a, attend_request(a, cursor.r));
+    cursor.j = cursor.x = 0;
+    cursor.end = 1;
+    if (cursor.head >= a.g.H * Cursor::tiles_of(cursor.n_rows) || cursor.n_rows == 0) return;
+  } else {
+    // units up to every thread's requests (R / 256 each; where that is one it is kept)
+    const int per = (a.R + 255) / 256, r0 = min(tid * per, a.R), r1 = min(r0 + per, a.R);
+    int mine = 0;
+    if (a.R <= kKnown) {
+      if (tid < a.R) {
+        cursor.take(a, attend_request(a, tid));
+        const int x[6] = {cursor.begin, cursor.n_rows, cursor.len, cursor.first_sees, cursor.visible, cursor.units};
+#pragma unroll
+        for (int i = 0; i < 6; i++) known[i][tid] = x[i];
+        mine = shared_units(cursor.units, cursor.n_rows);
       }
-      at += u;
+    } else {
+      for (int r = r0; r < r1; r++) mine += shared_units(attend_units(a, r), attend_request(a, r).rows);
     }
+    int upto = mine;
+    for (int k = 1; k < 64; k <<= 1) {
+      const int u = __shfl_up(upto, k);
+      if (lane >= k) upto += u;
+    }
+    if (lane == 63) wave_units[wave] = upto;
+    __syncthreads();
+    int units = 0;
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      if (k < wave) upto += wave_units[k];
+      units += wave_units[k];
+    }
+    const AttendShares shares(__builtin_amdgcn_readfirstlane(units) * H, a.workgroups);
+    if (a.split && tid == 0) a.joins[w] = int4{0, 0, 0, 0};
+    if (w >= shares.n) return;
+    const int begin = shares.begin(w);
+    if ((upto - mine) * H <= begin && begin < upto * H) {
+      int at = upto - mine;
+      for (int r = r0; r < r1; r++) {
+        const int u = a.R <= kKnown ? shared_units(known[5][r], known[1][r]) : shared_units(attend_units(a, r), attend_request(a, r).rows);
+        if (begin < (at + u) * H) {
+          found[0] = r;
+          found[1] = begin - at * H;
+          break;
+        }
+        at += u;
+      }
+    }
+    __syncthreads();
+    cursor.r = __builtin_amdgcn_readfirstlane(found[0]);
+    cursor.look(a, cursor.r);
+    {
+      const int rel = __builtin_amdgcn_readfirstlane(found[1]), u = a.split ? __builtin_amdgcn_readlane(cursor.units, 0) + kItemCost : 1;
+      cursor.head = rel / u;
+      cursor.j = attend_cut(rel - cursor.head * u);
+      cursor.x = begin - (rel - cursor.head * u);
+      cursor.end = shares.begin(w + 1);
+    }
+    if (!cursor.more(a)) return;
+    const int row0 = cursor.row0_of(cursor.head, __builtin_amdgcn_readlane(cursor.n_rows, 0));
+    if (tid == 0 && shares.first_border<kItemCost>(w, cursor.x, cursor.j))
+      a.joins[w] = join_word(shares.parts<kItemCost>(w, cursor.x, __builtin_amdgcn_readlane(cursor.units, 0)),
+                             Form::TILED ? min(__builtin_amdgcn_readlane(cursor.n_rows, 0) - row0, ROWS) : __builtin_amdgcn_readlane(cursor.n_rows, 0),
+                             __builtin_amdgcn_readlane(cursor.begin, 0), cursor.head_of(cursor.head, __builtin_amdgcn_readlane(cursor.n_rows, 0)), row0);
   }
-  __syncthreads();
-  cursor.r = __builtin_amdgcn_readfirstlane(found[0]);
-  cursor.look(a, cursor.r);
-  {
-    const int rel = __builtin_amdgcn_readfirstlane(found[1]), u = a.split ? __builtin_amdgcn_readlane(cursor.units, 0) + kItemCost : 1;
-    cursor.head = rel / u;
-    cursor.j = attend_cut(rel - cursor.head * u);
-    cursor.x = begin - (rel - cursor.head * u);
-    cursor.end = shares.begin(w + 1);
-  }
-  if (!cursor.more(a)) return;
-  const int row0 = cursor.row0_of(cursor.head, __builtin_amdgcn_readlane(cursor.n_rows, 0));
-  if (tid == 0 && shares.first_border<kItemCost>(w, cursor.x, cursor.j))
-    a.joins[w] = join_word(shares.parts<kItemCost>(w, cursor.x, __builtin_amdgcn_readlane(cursor.units, 0)),
-                           Form::TILED ? min(__builtin_amdgcn_readlane(cursor.n_rows, 0) - row0, ROWS) : __builtin_amdgcn_readlane(cursor.n_rows, 0),
-                           __builtin_amdgcn_readlane(cursor.begin, 0), cursor.head_of(cursor.head, __builtin_amdgcn_readlane(cursor.n_rows, 0)), row0);
 
   typename Form::Rows rows[NQ];
   if constexpr (!Form::TILED) {

@@ -35,6 +35,7 @@ __device__ __forceinline__ void lose_page(const PagesArgs& a, int entry) {
 
 // Pages whose last holder went go on the stack, the lowest last.  1024 threads; 65536 pages at a time, from the highest: each wave finds the ones
 // among 64, a lane a page, then their places are summed.
+constexpr int kAtOnce = 4;      // loads of a lane under way
 struct SettleScratch {
   uint64_t freed[1024];
   unsigned sums[16][1], total;
@@ -45,15 +46,25 @@ __device__ __forceinline__ void settle_pages(const PagesArgs& a, SettleScratch& 
   int64_t count = max(0, min(now_in(a.free_count), a.capacity));
   for (int end = groups; end > 0; end -= 1024) {
     const int here = min(end, 1024);
-    for (int i = wave; i < here; i += 16) {
-      const int group = end - 1 - i, page = 64 * group + lane;
-      const uint32_t word = 2 * group + (lane >> 5) < words ? (uint32_t)now_in((const int32_t*)a.bits() + 2 * group + (lane >> 5)) : 0;
-      const bool lost = word >> (lane & 31) & 1;
-      if ((lane & 31) == 0 && word != 0) a.bits()[2 * group + (lane >> 5)] = 0;
-      const bool freed = lost && page < a.pages && now_in(a.shares + page) < 0;
-      if (freed) a.shares[page] = 0;
-      const uint64_t mask = __ballot(freed);
-      if (lane == 0) s.freed[i] = mask;
+    for (int i0 = wave; i0 < here; i0 += 16 * kAtOnce) {
+      uint32_t word[kAtOnce];
+      int holders[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; k++) {
+        const int i = i0 + 16 * k, group = end - 1 - i, at = 2 * group + (lane >> 5), page = 64 * group + lane;
+        word[k] = i < here && at < words ? (uint32_t)now_in((const int32_t*)a.bits() + at) : 0;
+        holders[k] = i < here && page < a.pages ? now_in(a.shares + page) : 0;
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; k++) {
+        const int i = i0 + 16 * k, group = end - 1 - i;
+        if (i >= here) break;
+        if ((lane & 31) == 0 && word[k] != 0) a.bits()[2 * group + (lane >> 5)] = 0;
+        const bool freed = (word[k] >> (lane & 31) & 1) && holders[k] < 0;
+        if (freed) a.shares[64 * group + lane] = 0;
+        const uint64_t mask = __ballot(freed);
+        if (lane == 0) s.freed[i] = mask;
+      }
     }
     __syncthreads();
     unsigned to[1] = {tid < here ? (unsigned)__popcll(s.freed[tid]) : 0};
@@ -170,28 +181,33 @@ __global__ __launch_bounds__(1024) void cache_own_kernel(PagesArgs a) {
     const int entry = a.table[(size_t)r * a.columns + (length >> a.page_shift)];
     return a.is_page(entry) ? entry : -1;
   };
+  // (the thread's first request stays in registers from step to step)
+  const auto holders_of = [&](int entry) { return entry >= 0 ? a.shares[entry] : 0; };
+  const int entry0 = tid < a.R ? page_of(tid) : -1, holders0 = holders_of(entry0);
   for (int r = tid; r < a.R; r += 1024) {
-    const int entry = page_of(r);
-    if (entry < 0 || a.shares[entry] <= 0) continue;
+    const int entry = r == tid ? entry0 : page_of(r), holders = r == tid ? holders0 : holders_of(entry);
+    if (holders <= 0) continue;
     atomicAdd(asks + entry, 1);
     atomicMax(last + entry, r + 1);
   }
+  const unsigned count = (unsigned)max(0, min(a.free_count[0], a.capacity));
   __threadfence_block();
   __syncthreads();
-  const unsigned count = (unsigned)max(0, min(a.free_count[0], a.capacity));
-  unsigned before = 0, taken = 0;
+  unsigned before = 0;
+  int2 move0 = {-1, -1};
   for (int base = 0; base < a.R; base += 1024) {
-    const int r = base + tid, entry = r < a.R ? page_of(r) : -1;
-    const bool wants = entry >= 0 && a.shares[entry] > 0;
-    const bool copies = wants && !(now_in(asks + entry) == a.shares[entry] + 1 && now_in(last + entry) == r + 1);
+    const int r = base + tid;
+    const int entry = base == 0 ? entry0 : r < a.R ? page_of(r) : -1, holders = base == 0 ? holders0 : holders_of(entry);
+    const bool wants = holders > 0;
+    const bool copies = wants && !(now_in(asks + entry) == holders + 1 && now_in(last + entry) == r + 1);
     unsigned need[1] = {copies ? 1u : 0u};
     block_scan<16>(need, sums);
     if (tid == 1023) total = need[0];
     const unsigned needs = min(before + need[0], kFull);
     const bool granted = !wants || needs <= count;
+    int2 move = {entry, -1};
     if (r < a.R) {
       a.granted[r] = granted ? a.asked[r] : 0;
-      int2 move = {entry, -1};
       if (copies && granted) {
         const int to = a.free_pages[count - needs];
         a.table[(size_t)r * a.columns + (a.lengths[r] >> a.page_shift)] = to;
@@ -199,19 +215,19 @@ __global__ __launch_bounds__(1024) void cache_own_kernel(PagesArgs a) {
       }
       a.moves[r] = move;
     }
+    if (base == 0) move0 = move;
     __syncthreads();
     before = min(before + total, kFull);
-    taken = min(before, count);
     __syncthreads();
   }
   for (int r = tid; r < a.R; r += 1024) {
-    const int2 move = a.moves[r];
+    const int2 move = r == tid ? move0 : a.moves[r];
     if (move.x < 0) continue;
     asks[move.x] = 0;
     last[move.x] = 0;
     if (move.y != -1) atomicSub(a.shares + move.x, 1);
   }
-  if (tid == 0) a.free_count[0] = (int)(count - taken);
+  if (tid == 0) a.free_count[0] = (int)(count - min(before, count));
 }
 
 // Pages are copied in pieces of 16 KiB, four loads of a thread in flight.
@@ -260,10 +276,18 @@ __device__ __forceinline__ void choose_moves(const CompactArgs& c, CompactScratc
   const PagesArgs& a = c.p;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int groups = (a.pages + 63) >> 6;
-  for (int g = wave; g < groups; g += 16) {
-    const int page = 64 * g + lane;
-    const uint64_t mask = __ballot(page < a.pages && now_in(a.shares + a.pages + page) > 0);
-    if (lane == 0) c.masks[g] = mask;
+  for (int g0 = wave; g0 < groups; g0 += 16 * kAtOnce) {
+    int holders[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; k++) {
+      const int page = 64 * (g0 + 16 * k) + lane;
+      holders[k] = page < a.pages ? now_in(a.shares + a.pages + page) : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; k++) {
+      const uint64_t mask = __ballot(holders[k] > 0);
+      if (lane == 0 && g0 + 16 * k < groups) c.masks[g0 + 16 * k] = mask;
+    }
   }
   __threadfence_block();
   __syncthreads();

@@ -108,6 +108,7 @@ struct AttendLaunch {
   int nq;                      // cache_attend_kernel: tiles of 16 rows
   int workgroups, join_rows;
   bool join_wide;              // items have few parts: several rows a workgroup
+  int direct;                  // workgroups of each request, or 0: items are dealt out
   int tile_rows;               // of the kernels for many rows
   bool split;
   size_t joins, sums, stats;
@@ -161,11 +162,14 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
     // 59.4 -> 55.1 us, 32 rows 63.2 -> 57.0, one of 131000 57.4 -> 55.2.  Of several tiles two: heads of 64, up to 100 rows 19.6 -> 18.4.)
     const int64_t slots = (p.block > 0 && (tiles == 1 || l.nq > 2) ? 1 : 2) * kCus;
     l.workgroups = (int)(units < slots ? (units > 0 ? units : 1) : slots);
+    l.direct = p.block > 0 && !l.split && units <= 4 * kCus ? (int)(p.H * tiles) : 0;
+    if (l.direct) l.workgroups = (int)(units > 0 ? units : 1);
     l.join_wide = p.block > 0 && (int64_t)c.R * p.H * tiles >= 64;
     lay_out(l, 16 * l.nq);
   }
   if (w.many) {
     AttendLaunch& l = w.m;
+    l.direct = 0;
     l.rows_from = w.few ? w.f.rows_to : 0;
     l.rows_to = INT32_MAX;
     const int64_t total = (int64_t)c.T * G;
@@ -215,6 +219,7 @@ int launch_attend(AttendArgs a, const AttendPlan& w, char* ws, hipStream_t st) {
     a.split = l.split;
     a.rows_from = l.rows_from;
     a.rows_to = l.rows_to;
+    a.direct = l.direct;
   };
   if (w.many) {
     with(w.m);
