@@ -164,6 +164,74 @@ __global__ __launch_bounds__(256, NQ > 2 ? 1 : 2) void cache8_attend_kernel(Atte
   attend_items<ByteForm<D>, NQ>(a);
 }
 
+// Short requests, a wave each of their items: no sum over the requests, nothing to join, no LDS.  (Four waves an item, dealt out to a workgroup a CU: 405
+// requests of 3 tokens, 14 heads, 73 us; so SHORT.)
+template <int D, int NQ>
+__global__ __launch_bounds__(256, 2) void cache8_short_kernel(AttendArgs a) {
+  typedef ByteForm<D> Form;
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), r = item / a.direct;
+  if (r >= a.R) return;
+  const AttendRequest rq = attend_request(a, r);
+  const int tiles = (rq.rows + 16 * NQ - 1) / (16 * NQ), index = item - r * a.direct;
+  if (index >= a.g.H * tiles) return;
+  struct {
+    int begin, n_rows, head, len, first_sees;
+  } piece;
+  piece.begin = rq.begin;
+  piece.n_rows = rq.rows;
+  piece.head = index / tiles;
+  piece.len = rq.len;
+  piece.first_sees = rq.first_sees;
+  const int row0 = (index - piece.head * tiles) * 16 * NQ, visible = attend_visible(a, rq, row0, 16 * NQ);
+  const int all_see = a.causal ? rq.first_sees + row0 / a.G : rq.len, last = max(visible - 1, 0);
+  const int32_t* table = a.table + (size_t)r * a.columns;
+  ByteRows<D> rows[NQ];
+#pragma unroll
+  for (int q = 0; q < NQ; q++) {
+    rows[q].place(a, row0 + 16 * q);
+    rows[q].fetch(a, piece);
+    rows[q].begin();
+  }
+  const typename Form::Unpacking un;
+  ByteTile<D> t[2];
+  bool there[2];
+  const auto load = [&](int x, int t0) {      // (as in attend_items: loads every time)
+    const int entry = __builtin_amdgcn_readfirstlane(table[min(t0, last) >> a.g.page_shift]);
+    there[x] = t0 < visible && (unsigned)entry < (unsigned)a.g.pages;
+    t[x].load(a.g, Form::part(a, there[x] ? entry : 0, piece.head), t0 & (a.g.page() - 1), there[x]);
+  };
+  load(0, 0);
+  for (int t0 = 0; t0 < visible; t0 += 64) {
+#pragma unroll
+    for (int x = 0; x < 2; x++) {
+      const int at = t0 + 32 * x;
+      load(1 - x, at + 32);
+      if (there[x]) Form::template attend<NQ>(rows, t[x], at, at + 32 > all_see, a.scale_log2, un);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < NQ; q++) {
+    const ByteRows<D>& R = rows[q];
+    const float l = column_sum(R.l);
+    const bool any = !(l == 0.f);
+    const float f = any ? 1.f / l : 0.f;
+    if (R.row >= rq.rows) continue;
+    const int64_t token = rq.begin + R.token;
+    const int hq = piece.head * a.G + R.head_of;
+    __bf16* p = a.O + (token * a.Hq + hq) * D + 4 * g;
+#pragma unroll
+    for (int v = 0; v < D / 16; v++) {
+      const auto mean = value_means<4>(a, piece.head * D + 16 * v + 4 * g);
+      float y[4];
+#pragma unroll
+      for (int i = 0; i < 4; i++) y[i] = any ? R.o[v][i] * f + mean[i] : 0.f;
+      *(v2i*)(p + 16 * v) = v2i{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+    }
+    if (g == 0 && a.LSE != nullptr) a.LSE[(int64_t)hq * a.T + token] = any ? (R.m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+  }
+}
+
 // ---- many rows ---------------------------------------------------------------------------------------------------------
 // V's scale of a half goes into its exponents (log2 of it), so that they give the probabilities times it, and out of their sum.  (Of a scale of zero, whose
 // codes are zeros, any other will do, and for one that is no number poison() stands in.)  It saves 32 products of a lane and tile: 2048 new tokens of

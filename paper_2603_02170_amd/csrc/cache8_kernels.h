@@ -100,10 +100,11 @@ struct Runs8 {
 // One workgroup has a run of a block, for a head: the block's largest magnitude has to be known before the first code is written, and where it
 // grows the codes held are written again.  Of the tokens that the block can have each thread has 16 values of K and 16 of V.  (With a thread having two such
 // in turn, and the slots asked for once more for each run, 20.0 us in place of 16.8.)
-template <int D, int BLOCK>
-__global__ __launch_bounds__(BLOCK * D / 16) void cache8_append_kernel(StoreArgs a, int window) {
+template <int D, int BLOCK, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void cache8_append_kernel(StoreArgs a, int window) {
   typedef Octet8<D> Octet;
-  constexpr int THREADS = BLOCK * D / 16, WAVES = THREADS / 64;
+  constexpr int THREADS = 64 * WAVES, AT_ONCE = WAVES * Octet::EACH;      // octets
+  constexpr bool ONCE = AT_ONCE >= BLOCK / 8;
   __shared__ unsigned tops[2][WAVES][2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = blockIdx.y;
   const Octet me;
@@ -120,23 +121,29 @@ __global__ __launch_bounds__(BLOCK * D / 16) void cache8_append_kernel(StoreArgs
     unsigned char* p = a.pool + ((size_t)(slot0 >> a.g.page_shift) * a.g.H + h) * Bytes8<D>::head_bytes(a.g);
     float* magnitudes = (float*)(p + Bytes8<D>::magnitudes(a.g) + at / 4);
     const float held[2] = {o > 0 ? magnitudes[0] : 0.f, o > 0 ? magnitudes[1] : 0.f};
-    const int t0 = 8 * ((o >> 3) + tid / Octet::LANES);      // the thread's octet of the block
+    const int octets = ((o + n + 7) >> 3) - (o >> 3), rounds = ONCE ? 1 : (octets + AT_ONCE - 1) / AT_ONCE;      // with new tokens
+    int t0 = 8 * ((o >> 3) + tid / Octet::LANES);      // the thread's octet of the block, in the first round
     const auto is_new = [&](int t) { return t >= o && t < o + n; };
-    v8bf k[2] = {};
-    v4bf v[2][2] = {};      // token i or 4 + i, channels c or c + 16
-    if (is_new(t0 + me.k_token)) {
-      const __bf16* x = a.K + (int64_t)(first + t0 + me.k_token - o) * a.ks[0] + h * a.ks[1] + me.k_channel;
-      k[0] = *(const v8bf*)x;
-      k[1] = *(const v8bf*)(x + 8);
-    }
+    v8bf k[2];
+    v4bf v[2][2];      // token i or 4 + i, channels c or c + 16
+    const auto fetch = [&] {
+      k[0] = k[1] = v8bf{};
 #pragma unroll
-    for (int half = 0; half < 2; half++) {
-      const int t = t0 + me.v_token + 4 * half;
-      if (!is_new(t)) continue;
-      const __bf16* x = a.V + (int64_t)(first + t - o) * a.vs[0] + h * a.vs[1] + me.v_channel;
-      v[half][0] = *(const v4bf*)x;
-      v[half][1] = *(const v4bf*)(x + 16);
-    }
+      for (int half = 0; half < 2; half++) v[half][0] = v[half][1] = v4bf{};
+      if (is_new(t0 + me.k_token)) {
+        const __bf16* x = a.K + (int64_t)(first + t0 + me.k_token - o) * a.ks[0] + h * a.ks[1] + me.k_channel;
+        k[0] = *(const v8bf*)x;
+        k[1] = *(const v8bf*)(x + 8);
+      }
+#pragma unroll
+      for (int half = 0; half < 2; half++) {
+        const int t = t0 + me.v_token + 4 * half;
+        if (!is_new(t)) continue;
+        const __bf16* x = a.V + (int64_t)(first + t - o) * a.vs[0] + h * a.vs[1] + me.v_channel;
+        v[half][0] = *(const v4bf*)x;
+        v[half][1] = *(const v4bf*)(x + 16);
+      }
+    };
     const auto keys = [&](float* f) {
 #pragma unroll
       for (int e = 0; e < 16; e++) f[e] = (float)k[e / 8][e % 8];
@@ -154,21 +161,26 @@ __global__ __launch_bounds__(BLOCK * D / 16) void cache8_append_kernel(StoreArgs
     };
     unsigned top[2] = {0, 0};      // (tokens that are not the call's are zeros, but for a mean taken off)
     float f[16];
-    if (is_new(t0 + me.k_token)) {
-      keys(f);
+#pragma unroll 1
+    for (int round = 0; round < rounds; round++, t0 += 8 * AT_ONCE) {
+      fetch();
+      if (is_new(t0 + me.k_token)) {
+        keys(f);
 #pragma unroll
-      for (int e = 0; e < 16; e++) top[0] = max(top[0], __float_as_uint(f[e]) & 0x7FFFFFFFu);
-    }
+        for (int e = 0; e < 16; e++) top[0] = max(top[0], __float_as_uint(f[e]) & 0x7FFFFFFFu);
+      }
 #pragma unroll
-    for (int half = 0; half < 2; half++) {
-      if (!is_new(t0 + me.v_token + 4 * half)) continue;
+      for (int half = 0; half < 2; half++) {
+        if (!is_new(t0 + me.v_token + 4 * half)) continue;
 #pragma unroll
-      for (int more = 0; more < 2; more++) {
-        values(half, more, f);
+        for (int more = 0; more < 2; more++) {
+          values(half, more, f);
 #pragma unroll
-        for (int e = 0; e < 4; e++) top[1] = max(top[1], __float_as_uint(f[e]) & 0x7FFFFFFFu);
+          for (int e = 0; e < 4; e++) top[1] = max(top[1], __float_as_uint(f[e]) & 0x7FFFFFFFu);
+        }
       }
     }
+    t0 -= 8 * AT_ONCE * rounds;
 #pragma unroll
     for (int which = 0; which < 2; which++) {
 #pragma unroll
@@ -188,35 +200,39 @@ __global__ __launch_bounds__(BLOCK * D / 16) void cache8_append_kernel(StoreArgs
       grown[which] = o > 0 && now[which] > held[which];
       again[which] = grown[which] ? __fdiv_rn(held[which], now[which]) : 1.f;
     }
-    if (is_new(t0 + me.k_token)) {
-      keys(f);
-      *(uint4*)(p + Bytes8<D>::k(at + t0 + me.k_token, me.k_channel)) = uint4{codes8(f, r[0]), codes8(f + 4, r[0]), codes8(f + 8, r[0]), codes8(f + 12, r[0])};
-    }
-    unsigned w[2][2];      // channel c or c + 16; tokens 0 .. 3 or 4 .. 7
-#pragma unroll
-    for (int more = 0; more < 2; more++)
-#pragma unroll
-      for (int half = 0; half < 2; half++) {
-        values(half, more, f);
-        w[more][half] = turn(codes8(f, r[1]));
+#pragma unroll 1
+    for (int round = 0; round < rounds; round++, t0 += 8 * AT_ONCE) {
+      if (!ONCE && rounds > 1) fetch();      // (once more)
+      if (is_new(t0 + me.k_token)) {
+        keys(f);
+        *(uint4*)(p + Bytes8<D>::k(at + t0 + me.k_token, me.k_channel)) = uint4{codes8(f, r[0]), codes8(f + 4, r[0]), codes8(f + 8, r[0]), codes8(f + 12, r[0])};
       }
-    const int from = max(o - t0, 0), upto = min(o + n - t0, 8);      // new tokens of the octet
-    if (upto > 0) {
-      uint4* to = (uint4*)(p + Octet::v_at(a.g, at + t0) + me.v_byte);
-      if (from > 0 || upto < 8) {
-        const uint4 y = *to;
-        const unsigned old[2][2] = {{y.x, y.y}, {y.z, y.w}};
-        const uint64_t below = (1ull << 8 * from) - 1, fresh = (upto == 8 ? ~0ull : (1ull << 8 * upto) - 1) & ~below;
+      unsigned w[2][2];      // channel c or c + 16; tokens 0 .. 3 or 4 .. 7
 #pragma unroll
-        for (int more = 0; more < 2; more++)
+      for (int more = 0; more < 2; more++)
 #pragma unroll
-          for (int half = 0; half < 2; half++) {
-            const unsigned is_fresh = (unsigned)(fresh >> 32 * half), is_below = (unsigned)(below >> 32 * half), x = old[more][half];
-            const unsigned kept = grown[1] ? (recode8(x, again[1]) & is_below) | (x & ~is_below) : x;      // (behind the new tokens nothing is the call's)
-            w[more][half] = (w[more][half] & is_fresh) | (kept & ~is_fresh);
-          }
+        for (int half = 0; half < 2; half++) {
+          values(half, more, f);
+          w[more][half] = turn(codes8(f, r[1]));
+        }
+      const int from = max(o - t0, 0), upto = min(o + n - t0, 8);      // new tokens of the octet
+      if (upto > 0) {
+        uint4* to = (uint4*)(p + Octet::v_at(a.g, at + t0) + me.v_byte);
+        if (from > 0 || upto < 8) {
+          const uint4 y = *to;
+          const unsigned old[2][2] = {{y.x, y.y}, {y.z, y.w}};
+          const uint64_t below = (1ull << 8 * from) - 1, fresh = (upto == 8 ? ~0ull : (1ull << 8 * upto) - 1) & ~below;
+#pragma unroll
+          for (int more = 0; more < 2; more++)
+#pragma unroll
+            for (int half = 0; half < 2; half++) {
+              const unsigned is_fresh = (unsigned)(fresh >> 32 * half), is_below = (unsigned)(below >> 32 * half), x = old[more][half];
+              const unsigned kept = grown[1] ? (recode8(x, again[1]) & is_below) | (x & ~is_below) : x;      // (behind the new tokens nothing is the call's)
+              w[more][half] = (w[more][half] & is_fresh) | (kept & ~is_fresh);
+            }
+        }
+        *to = uint4{w[0][0], w[0][1], w[1][0], w[1][1]};
       }
-      *to = uint4{w[0][0], w[0][1], w[1][0], w[1][1]};
     }
     if (grown[0]) {
 #pragma unroll 1

@@ -4,7 +4,9 @@
 // counted with integer atomics, whose order changes nothing; what depends on an order (the stack of free pages, who keeps a page) is decided
 // by page numbers or request numbers afterwards.
 //
-// Steps: a wave has a request's row of the table; one workgroup settles the stack.  Small calls are one launch of one workgroup.
+// Steps: a workgroup has kColumns columns of a request's row of the table, a thread four of them, whose loads are under way together; one workgroup
+// settles the stack.  Small calls are one launch of one workgroup.  (A wave a row, one trip to memory after the other: 25 requests of 530 pages 55 us
+// for free, fork and own; so LONGROWS.)
 #pragma once
 
 #include "cache_kernels.h"
@@ -87,83 +89,119 @@ __device__ __forceinline__ void settle_pages(const PagesArgs& a, SettleScratch& 
   if (tid == 0) a.free_count[0] = (int)min(count, (int64_t)a.capacity);
 }
 
+constexpr int kColumns = 1024;
+template <typename F>
+__device__ __forceinline__ void each_column(const PagesArgs& a, F f) {
+  const int chunks = (a.columns + kColumns - 1) / kColumns, r = blockIdx.x / chunks;
+  f(r, (int)(blockIdx.x - r * chunks) * kColumns + (int)threadIdx.x);
+}
+template <typename F>
+__device__ __forceinline__ void each_entry(const PagesArgs& a, F f) {      // of a small call
+  for (int i = threadIdx.x; i < a.R * a.columns; i += 1024) f(i / a.columns, i % a.columns);
+}
+
 // ---- free ----------------------------------------------------------------------------------------------------------
-// A wave: what a request gives up.
-__device__ __forceinline__ void free_row(const PagesArgs& a, int r) {
-  const int lane = threadIdx.x & 63, length = a.lengths[r], keep = a.asked[r];
+__device__ __forceinline__ bool keeps(const PagesArgs& a, int r) { return a.asked[r] >= 0 && a.asked[r] <= a.lengths[r]; }
+// What a request gives up of N columns, `step` apart.
+template <int N>
+__device__ __forceinline__ void free_columns(const PagesArgs& a, int r, int c0, int step) {
+  const int length = a.lengths[r], keep = a.asked[r];
   if (keep < 0 || keep > length) return;
+  const int first = a.pages_of(keep), end = a.pages_of(length);
   int32_t* row = a.table + (size_t)r * a.columns;
-  const int end = a.pages_of(length);
-  for (int c = a.pages_of(keep) + lane; c < end; c += 64) {
-    const int entry = row[c];
-    if (a.is_page(entry)) lose_page(a, entry);
-    row[c] = -1;
+  int entry[N];
+#pragma unroll
+  for (int k = 0; k < N; k++) {
+    const int c = c0 + k * step;
+    entry[k] = c >= first && c < end ? row[c] : -1;
   }
-  if (lane == 0) a.lengths[r] = keep;
+#pragma unroll
+  for (int k = 0; k < N; k++) {
+    const int c = c0 + k * step;
+    if (a.is_page(entry[k])) lose_page(a, entry[k]);
+    if (c >= first && c < end) row[c] = -1;
+  }
 }
 __global__ __launch_bounds__(256) void cache_free_rows_kernel(PagesArgs a) {
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r < a.R) free_row(a, r);
+  each_column(a, [&](int r, int c) { free_columns<4>(a, r, c, 256); });
 }
-__global__ __launch_bounds__(1024) void cache_settle_kernel(PagesArgs a) {
+// the first workgroup settles, the others have the lengths
+__global__ __launch_bounds__(1024) void cache_freed_kernel(PagesArgs a) {
   __shared__ SettleScratch s;
-  settle_pages(a, s);
+  if (blockIdx.x == 0) {
+    settle_pages(a, s);
+    return;
+  }
+  const int r = (blockIdx.x - 1) * 1024 + threadIdx.x;
+  if (r < a.R && keeps(a, r)) a.lengths[r] = a.asked[r];
 }
 __global__ __launch_bounds__(1024) void cache_free_kernel(PagesArgs a) {
   __shared__ SettleScratch s;
-  for (int r = threadIdx.x >> 6; r < a.R; r += 16) free_row(a, r);
+  each_entry(a, [&](int r, int c) { free_columns<1>(a, r, c, 0); });
   __threadfence_block();
   __syncthreads();
+  for (int r = threadIdx.x; r < a.R; r += 1024)
+    if (keeps(a, r)) a.lengths[r] = a.asked[r];
   settle_pages(a, s);
 }
 
 // ---- fork ----------------------------------------------------------------------------------------------------------
-// A wave: the row that a request goes on with, to `rows`, as a row may be another one's parent; pages that stay where they are count for nothing.
 __device__ __forceinline__ bool forked(const PagesArgs& a, int r) {
   const int p = a.asked[r];
   return p >= 0 && p < a.R && p != r;
 }
-__device__ __forceinline__ void fork_row(const PagesArgs& a, int r) {
+// N columns of the row that a request goes on with, to `rows`, as a row may be another one's parent; pages that stay where they are count for nothing.
+template <int N>
+__device__ __forceinline__ void fork_columns(const PagesArgs& a, int r, int c0, int step) {
   if (!forked(a, r)) return;
-  const int lane = threadIdx.x & 63, p = a.asked[r], length = a.lengths[p];
+  const int p = a.asked[r], length = a.lengths[p], n = a.pages_of(length), had = a.pages_of(a.lengths[r]);
   const int32_t *from = a.table + (size_t)p * a.columns, *old = a.table + (size_t)r * a.columns;
-  int32_t* to = a.rows + (size_t)r * a.columns;
-  const int n = a.pages_of(length), had = a.pages_of(a.lengths[r]);
-  for (int c = lane; c < a.columns; c += 64) {
-    const int entry = c < n ? from[c] : -1, before = c < had ? old[c] : -1;
-    to[c] = entry;
-    if (entry == before) continue;
-    if (a.is_page(entry)) atomicAdd(a.shares + entry, 1);
-    if (a.is_page(before)) lose_page(a, before);
+  int entry[N], before[N];
+#pragma unroll
+  for (int k = 0; k < N; k++) {
+    const int c = c0 + k * step;
+    entry[k] = c < n ? from[c] : -1;
+    before[k] = c < had ? old[c] : -1;
   }
-  if (lane == 0) a.new_lengths[r] = length;
+#pragma unroll
+  for (int k = 0; k < N; k++) {
+    const int c = c0 + k * step;
+    if (c < a.columns) a.rows[(size_t)r * a.columns + c] = entry[k];
+    if (entry[k] == before[k]) continue;
+    if (a.is_page(entry[k])) atomicAdd(a.shares + entry[k], 1);
+    if (a.is_page(before[k])) lose_page(a, before[k]);
+  }
+  if (c0 == 0) a.new_lengths[r] = length;
 }
-__device__ __forceinline__ void forked_row(const PagesArgs& a, int r) {
+template <int N>
+__device__ __forceinline__ void forked_columns(const PagesArgs& a, int r, int c0, int step) {
   if (!forked(a, r)) return;
-  const int lane = threadIdx.x & 63;
-  for (int c = lane; c < a.columns; c += 64) a.table[(size_t)r * a.columns + c] = a.rows[(size_t)r * a.columns + c];
-  if (lane == 0) a.lengths[r] = a.new_lengths[r];
+#pragma unroll
+  for (int k = 0; k < N; k++) {
+    const int c = c0 + k * step;
+    if (c < a.columns) a.table[(size_t)r * a.columns + c] = a.rows[(size_t)r * a.columns + c];
+  }
+  if (c0 == 0) a.lengths[r] = a.new_lengths[r];
 }
 __global__ __launch_bounds__(256) void cache_fork_rows_kernel(PagesArgs a) {
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r < a.R) fork_row(a, r);
+  each_column(a, [&](int r, int c) { fork_columns<4>(a, r, c, 256); });
 }
-// the first workgroup settles, the others have 16 rows each
+// the first workgroup settles, the others have kColumns of a row each
 __global__ __launch_bounds__(1024) void cache_forked_kernel(PagesArgs a) {
   __shared__ SettleScratch s;
   if (blockIdx.x == 0) {
     settle_pages(a, s);
     return;
   }
-  const int r = (blockIdx.x - 1) * 16 + (threadIdx.x >> 6);
-  if (r < a.R) forked_row(a, r);
+  const int chunks = (a.columns + kColumns - 1) / kColumns, i = blockIdx.x - 1, r = i / chunks;
+  forked_columns<1>(a, r, (i - r * chunks) * kColumns + (int)threadIdx.x, 0);
 }
 __global__ __launch_bounds__(1024) void cache_fork_kernel(PagesArgs a) {
   __shared__ SettleScratch s;
-  for (int r = threadIdx.x >> 6; r < a.R; r += 16) fork_row(a, r);
+  each_entry(a, [&](int r, int c) { fork_columns<1>(a, r, c, 0); });
   __threadfence_block();
   __syncthreads();
-  for (int r = threadIdx.x >> 6; r < a.R; r += 16) forked_row(a, r);
+  each_entry(a, [&](int r, int c) { forked_columns<1>(a, r, c, 0); });
   settle_pages(a, s);
 }
 
@@ -261,12 +299,16 @@ struct CompactArgs {
   size_t page_bytes;
   int pieces;
 };
-// A wave: the holders of a request's pages, in the second row of shares.
-__device__ __forceinline__ void count_row(const PagesArgs& a, int r) {
-  const int32_t* row = a.table + (size_t)r * a.columns;
+// The holders of a request's pages, in the second row of shares.
+template <int N>
+__device__ __forceinline__ void count_columns(const PagesArgs& a, int r, int c0, int step) {
   const int n = a.pages_of(max(a.lengths[r], 0));
-  for (int c = threadIdx.x & 63; c < n; c += 64)
-    if (a.is_page(row[c])) atomicAdd(a.shares + a.pages + row[c], 1);
+  int entry[N];
+#pragma unroll
+  for (int k = 0; k < N; k++) entry[k] = c0 + k * step < n ? a.table[(size_t)r * a.columns + c0 + k * step] : -1;
+#pragma unroll
+  for (int k = 0; k < N; k++)
+    if (a.is_page(entry[k])) atomicAdd(a.shares + a.pages + entry[k], 1);
 }
 // 1024 threads: which pages are in use, and which of them go where.
 struct CompactScratch {
@@ -322,8 +364,7 @@ __device__ __forceinline__ void choose_moves(const CompactArgs& c, CompactScratc
   }
 }
 __global__ __launch_bounds__(256) void cache_count_kernel(CompactArgs c) {
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r < c.p.R) count_row(c.p, r);
+  each_column(c.p, [&](int r, int at) { count_columns<4>(c.p, r, at, 256); });
 }
 __global__ __launch_bounds__(1024) void cache_choose_kernel(CompactArgs c) {
   __shared__ CompactScratch s;
@@ -331,7 +372,7 @@ __global__ __launch_bounds__(1024) void cache_choose_kernel(CompactArgs c) {
 }
 __global__ __launch_bounds__(1024) void cache_count_and_choose_kernel(CompactArgs c) {
   __shared__ CompactScratch s;
-  for (int r = threadIdx.x >> 6; r < c.p.R; r += 16) count_row(c.p, r);
+  each_entry(c.p, [&](int r, int at) { count_columns<1>(c.p, r, at, 0); });
   __threadfence_block();
   __syncthreads();
   choose_moves(c, s);

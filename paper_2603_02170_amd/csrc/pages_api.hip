@@ -7,10 +7,11 @@ namespace {
 
 using namespace sage;
 
-// Rows, and entries of the table, up to which a call is one launch of one workgroup, sixteen rows at a time.
-constexpr int kSmallRows = 64;
-constexpr int64_t kSmallEntries = 1 << 15;
-bool small(int R, int columns) { return R <= kSmallRows && (int64_t)R * columns <= kSmallEntries; }
+// Entries of the table up to which a call is one launch of one workgroup.
+constexpr int64_t kSmallEntries = 2048;
+bool small(int R, int columns) { return (int64_t)R * columns <= kSmallEntries; }
+// Workgroups of a launch that has kColumns columns of a row each.
+unsigned row_chunks(int R, int columns) { return (unsigned)(R * (int64_t)((columns + kColumns - 1) / kColumns)); }
 
 int check_pages(const void* asked, const void* lengths, const void* table, const void* free_pages, const void* free_count, const void* shares, int32_t R,
                 int32_t columns, int32_t page, int32_t capacity, int32_t pages) {
@@ -70,9 +71,9 @@ int sagebwd_cache_free(const int32_t* keep, int32_t* lengths, int32_t* block_tab
   if (small(R, columns)) {
     cache_free_kernel<<<1, 1024, 0, st>>>(a);
   } else {
-    cache_free_rows_kernel<<<(R + 3) / 4, 256, 0, st>>>(a);
+    cache_free_rows_kernel<<<row_chunks(R, columns), 256, 0, st>>>(a);
     SERVE_LAUNCH_CHECK();
-    cache_settle_kernel<<<1, 1024, 0, st>>>(a);
+    cache_freed_kernel<<<1 + (R + 1023) / 1024, 1024, 0, st>>>(a);
   }
   SERVE_LAUNCH_CHECK();
   return SAGEBWD_OK;
@@ -111,9 +112,9 @@ int sagebwd_cache_fork(const int32_t* parents, int32_t* lengths, int32_t* block_
   if (small(R, columns)) {
     cache_fork_kernel<<<1, 1024, 0, st>>>(a);
   } else {
-    cache_fork_rows_kernel<<<(R + 3) / 4, 256, 0, st>>>(a);
+    cache_fork_rows_kernel<<<row_chunks(R, columns), 256, 0, st>>>(a);
     SERVE_LAUNCH_CHECK();
-    cache_forked_kernel<<<1 + (R + 15) / 16, 1024, 0, st>>>(a);
+    cache_forked_kernel<<<1 + row_chunks(R, columns), 1024, 0, st>>>(a);
   }
   SERVE_LAUNCH_CHECK();
   return SAGEBWD_OK;
@@ -197,7 +198,7 @@ int sagebwd_cache_compact(const int32_t* lengths, const int32_t* block_table, in
   if (small(R, columns)) {
     cache_count_and_choose_kernel<<<1, 1024, 0, st>>>(c);
   } else {
-    cache_count_kernel<<<(R + 3) / 4, 256, 0, st>>>(c);
+    cache_count_kernel<<<row_chunks(R, columns), 256, 0, st>>>(c);
     SERVE_LAUNCH_CHECK();
     cache_choose_kernel<<<1, 1024, 0, st>>>(c);
   }

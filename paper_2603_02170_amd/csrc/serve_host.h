@@ -95,6 +95,8 @@ inline int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c
 // Keys of a request up to this many units are not divided (four requests of 500 tokens 11.0 -> 9.3 us, 256 of 650 56.4 -> 52.0: the joining
 // launch is 4 to 5 us, a unit 0.6 where the machine is empty).
 constexpr int kWholeUnits = 8;
+// Held in 8 bits, items of so many keys have a wave each, whatever their number.
+constexpr int kShortLength = 128;
 // Keys and values are unpacked beforehand where a request's meet so many row tiles (us, unpacked by every tile -> beforehand: one request of 512 new
 // tokens x 4 heads of the group against 32768, 8 tiles, 288 -> 277, at d = 64 229 -> 180; 2048 x 4 against 10000, 32 tiles, 335 -> 293, at
 // d = 64 264 -> 193; two of 2048 against 8192, 8 tiles, 149 -> 148; 16 ragged ones of at most 600 x 4 140 -> 143; 4 of 256 x 4, 4 tiles,
@@ -108,7 +110,8 @@ struct AttendLaunch {
   int nq;                      // cache_attend_kernel: tiles of 16 rows
   int workgroups, join_rows;
   bool join_wide;              // items have few parts: several rows a workgroup
-  int direct;                  // workgroups of each request, or 0: items are dealt out
+  int direct;                  // workgroups of each request (short_items: waves), or 0: items are dealt out
+  bool short_items;
   int tile_rows;               // of the kernels for many rows
   bool split;
   size_t joins, sums, stats;
@@ -147,6 +150,8 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
   const int few_rows = few_rows_of(p, c);
   w.many = rows > few_rows;
   w.few = !w.many || (G <= few_rows && (int64_t)c.T < (int64_t)c.R * c.max_new);
+  // (Held in 8 bits and small, two launches more cost more than tiles half empty: eight ragged requests of 1380 tokens with up to 915 rows 45 -> MANYONLY us.)
+  if (w.many && p.block > 0 && (int64_t)c.R * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit) <= 2 * kCus) w.few = false;
   if (w.few) {
     AttendLaunch& l = w.f;
     const int64_t here = !w.many ? rows : few_rows > kFewRows ? few_rows : G > 16 ? G : 16;
@@ -162,7 +167,9 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
     // 59.4 -> 55.1 us, 32 rows 63.2 -> 57.0, one of 131000 57.4 -> 55.2.  Of several tiles two: heads of 64, up to 100 rows 19.6 -> 18.4.)
     const int64_t slots = (p.block > 0 && (tiles == 1 || l.nq > 2) ? 1 : 2) * kCus;
     l.workgroups = (int)(units < slots ? (units > 0 ? units : 1) : slots);
-    l.direct = p.block > 0 && !l.split && units <= 4 * kCus ? (int)(p.H * tiles) : 0;
+    // a wave an item where they are short, or many
+    l.short_items = p.block > 0 && !l.split && l.nq <= 2 && (w.max_length <= kShortLength || units > 4 * kCus) && units < 1 << 22;
+    l.direct = p.block > 0 && !l.split && (l.short_items || units <= 4 * kCus) ? (int)(p.H * tiles) : 0;
     if (l.direct) l.workgroups = (int)(units > 0 ? units : 1);
     l.join_wide = p.block > 0 && (int64_t)c.R * p.H * tiles >= 64;
     lay_out(l, 16 * l.nq);
@@ -170,6 +177,7 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
   if (w.many) {
     AttendLaunch& l = w.m;
     l.direct = 0;
+    l.short_items = false;
     l.rows_from = w.few ? w.f.rows_to : 0;
     l.rows_to = INT32_MAX;
     const int64_t total = (int64_t)c.T * G;
@@ -199,7 +207,12 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
 // The launches of a call, `Kernels` those of a format.
 template <typename Kernels, int NQ>
 int launch_few(const AttendArgs& a, const AttendLaunch& l, hipStream_t st) {
-  Kernels::template few<NQ>(l.workgroups, a, st);
+  if constexpr (Kernels::BYTES && NQ <= 2) {
+    if (l.short_items) Kernels::template few_short<NQ>((l.workgroups + 3) / 4, a, st);
+    else Kernels::template few<NQ>(l.workgroups, a, st);
+  } else {
+    Kernels::template few<NQ>(l.workgroups, a, st);
+  }
   SERVE_LAUNCH_CHECK();
   if (l.split && l.workgroups > 1) {
     if (!Kernels::BYTES || !l.join_wide) Kernels::template join_few<16 * NQ>(dim3(l.workgroups - 1, l.join_rows), a, st);
