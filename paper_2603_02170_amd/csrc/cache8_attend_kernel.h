@@ -210,25 +210,36 @@ __global__ __launch_bounds__(256, 2) void cache8_short_kernel(AttendArgs a) {
       if (there[x]) Form::template attend<NQ>(rows, t[x], at, at + 32 > all_see, a.scale_log2, un);
     }
   }
+  // A tile's rows, turned in the wave's part of LDS so that 16 lanes write a row.
+  __shared__ __attribute__((aligned(16))) char turned[4][16][2 * D + 16];
+  char(*out)[2 * D + 16] = turned[threadIdx.x >> 6];
 #pragma unroll
   for (int q = 0; q < NQ; q++) {
     const ByteRows<D>& R = rows[q];
     const float l = column_sum(R.l);
     const bool any = !(l == 0.f);
     const float f = any ? 1.f / l : 0.f;
-    if (R.row >= rq.rows) continue;
-    const int64_t token = rq.begin + R.token;
-    const int hq = piece.head * a.G + R.head_of;
-    __bf16* p = a.O + (token * a.Hq + hq) * D + 4 * g;
 #pragma unroll
     for (int v = 0; v < D / 16; v++) {
       const auto mean = value_means<4>(a, piece.head * D + 16 * v + 4 * g);
       float y[4];
 #pragma unroll
       for (int i = 0; i < 4; i++) y[i] = any ? R.o[v][i] * f + mean[i] : 0.f;
-      *(v2i*)(p + 16 * v) = v2i{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+      *(v2i*)(out[lane & 15] + 32 * v + 8 * g) = v2i{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
     }
-    if (g == 0 && a.LSE != nullptr) a.LSE[(int64_t)hq * a.T + token] = any ? (R.m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+    if (g == 0 && R.row < rq.rows && a.LSE != nullptr)
+      a.LSE[(int64_t)(piece.head * a.G + R.head_of) * a.T + rq.begin + R.token] = any ? (R.m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+    __builtin_amdgcn_wave_barrier();
+    constexpr int LANES = D / 8, AT_ONCE = 64 / LANES;      // of a row, rows
+#pragma unroll
+    for (int k = 0; k < 16 / AT_ONCE; k++) {
+      const int i = k * AT_ONCE + lane / LANES, row = row0 + 16 * q + i;
+      const v4i x = *(const v4i*)(out[i] + lane % LANES * 16);
+      if (row >= rq.rows) continue;
+      const int token = row / a.G, hq = piece.head * a.G + row - token * a.G;
+      *(v4i*)(a.O + ((int64_t)(rq.begin + token) * a.Hq + hq) * D + lane % LANES * 8) = x;
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 

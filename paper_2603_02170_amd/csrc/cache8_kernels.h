@@ -122,7 +122,13 @@ __global__ __launch_bounds__(64 * WAVES) void cache8_append_kernel(StoreArgs a, 
     float* magnitudes = (float*)(p + Bytes8<D>::magnitudes(a.g) + at / 4);
     const float held[2] = {o > 0 ? magnitudes[0] : 0.f, o > 0 ? magnitudes[1] : 0.f};
     const int octets = ((o + n + 7) >> 3) - (o >> 3), rounds = ONCE ? 1 : (octets + AT_ONCE - 1) / AT_ONCE;      // with new tokens
-    int t0 = 8 * ((o >> 3) + tid / Octet::LANES);      // the thread's octet of the block, in the first round
+    // The thread's octet of the block: all of them at once, so that the codes held are on their way with the new numbers; or, in rounds, those with new tokens.
+    int t0 = 8 * ((ONCE ? 0 : o >> 3) + tid / Octet::LANES);
+    uint4 held_k = {0, 0, 0, 0}, held_v = {0, 0, 0, 0};
+    if (ONCE) {
+      if (t0 + me.k_token < o) held_k = *(const uint4*)(p + Bytes8<D>::k(at + t0 + me.k_token, me.k_channel));
+      if (t0 < o || (t0 < o + n && o + n < t0 + 8)) held_v = *(const uint4*)(p + Octet::v_at(a.g, at + t0) + me.v_byte);
+    }
     const auto is_new = [&](int t) { return t >= o && t < o + n; };
     v8bf k[2];
     v4bf v[2][2];      // token i or 4 + i, channels c or c + 16
@@ -215,13 +221,17 @@ __global__ __launch_bounds__(64 * WAVES) void cache8_append_kernel(StoreArgs a, 
           values(half, more, f);
           w[more][half] = turn(codes8(f, r[1]));
         }
-      const int from = max(o - t0, 0), upto = min(o + n - t0, 8);      // new tokens of the octet
-      if (upto > 0) {
+      if (ONCE && grown[0] && t0 + me.k_token < o)
+        *(uint4*)(p + Bytes8<D>::k(at + t0 + me.k_token, me.k_channel)) =
+            uint4{recode8(held_k.x, again[0]), recode8(held_k.y, again[0]), recode8(held_k.z, again[0]), recode8(held_k.w, again[0])};
+      const int from = min(max(o - t0, 0), 8), upto = min(max(o + n - t0, 0), 8);      // new tokens of the octet
+      if (upto > from || (ONCE && grown[1] && from > 0)) {
         uint4* to = (uint4*)(p + Octet::v_at(a.g, at + t0) + me.v_byte);
         if (from > 0 || upto < 8) {
-          const uint4 y = *to;
+          const uint4 y = ONCE ? held_v : *to;
           const unsigned old[2][2] = {{y.x, y.y}, {y.z, y.w}};
-          const uint64_t below = (1ull << 8 * from) - 1, fresh = (upto == 8 ? ~0ull : (1ull << 8 * upto) - 1) & ~below;
+          const auto bytes = [](int n) { return n == 8 ? ~0ull : (1ull << 8 * n) - 1; };
+          const uint64_t below = bytes(from), fresh = bytes(upto) & ~below;
 #pragma unroll
           for (int more = 0; more < 2; more++)
 #pragma unroll
@@ -234,7 +244,7 @@ __global__ __launch_bounds__(64 * WAVES) void cache8_append_kernel(StoreArgs a, 
         *to = uint4{w[0][0], w[0][1], w[1][0], w[1][1]};
       }
     }
-    if (grown[0]) {
+    if (!ONCE && grown[0]) {
 #pragma unroll 1
       for (int i = tid; i < o * (D / 16); i += THREADS) {
         uint4* q = (uint4*)(p + Bytes8<D>::k(at + i / (D / 16), i % (D / 16) * 16));
@@ -242,7 +252,7 @@ __global__ __launch_bounds__(64 * WAVES) void cache8_append_kernel(StoreArgs a, 
         *q = uint4{recode8(w.x, again[0]), recode8(w.y, again[0]), recode8(w.z, again[0]), recode8(w.w, again[0])};
       }
     }
-    if (grown[1]) {
+    if (!ONCE && grown[1]) {
 #pragma unroll 1
       for (int i = tid; i < (o >> 3) * Octet::LANES; i += THREADS) {
         uint4* q = (uint4*)(p + Octet::v_at(a.g, at + i / Octet::LANES * 8) + (i % Octet::LANES >> 4) * 1024 + (i & 15) * 16);
