@@ -97,18 +97,20 @@ struct Runs8 {
   }
 };
 
-// One workgroup has a run of a block, for a head: the block's largest magnitude has to be known before the first code is written, and where it
-// grows the codes held are written again.  Of the tokens that the block can have each thread has 16 values of K and 16 of V.  (With a thread having two such
-// in turn, and the slots asked for once more for each run, 20.0 us in place of 16.8.)
-template <int D, int BLOCK, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void cache8_append_kernel(StoreArgs a, int window) {
+// One workgroup has a run of a block's keys or values (blockIdx.z), for a head: the block's largest magnitude has to be known before the first code is written,
+// and where it grows the codes held are written again.  A thread has 16 numbers at a time.  (With 16 of K and 16 of V registers halve the waves of a CU:
+// APPENDBOTH; a thread having two such in turn, and the slots asked for once more for each run, 20.0 in place of 16.8.)
+template <int D, int BLOCK, int WAVES, bool VALUES>
+__device__ __forceinline__ void store_runs(const StoreArgs& a, int window, unsigned (*tops)[WAVES]) {
   typedef Octet8<D> Octet;
   constexpr int THREADS = 64 * WAVES, AT_ONCE = WAVES * Octet::EACH;      // octets
   constexpr bool ONCE = AT_ONCE >= BLOCK / 8;
-  __shared__ unsigned tops[2][WAVES][2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = blockIdx.y;
   const Octet me;
   const Turn8 turn;
+  const float* mean = VALUES ? a.v_mean : a.k_mean;
+  const __bf16* from_head = VALUES ? a.V + h * a.vs[1] + me.v_channel : a.K + h * a.ks[1] + me.k_channel;
+  const int64_t stride = VALUES ? a.vs[0] : a.ks[0];
   const int row0 = blockIdx.x * window;
   const Runs8 runs(a, row0, window, BLOCK, false);
   int side = 0;
@@ -119,149 +121,119 @@ __global__ __launch_bounds__(64 * WAVES) void cache8_append_kernel(StoreArgs a, 
     const int o = (int)(slot0 & (BLOCK - 1));
     const int at = (int)(slot0 & (a.g.page() - 1)) - o;          // the block's first token in its page
     unsigned char* p = a.pool + ((size_t)(slot0 >> a.g.page_shift) * a.g.H + h) * Bytes8<D>::head_bytes(a.g);
-    float* magnitudes = (float*)(p + Bytes8<D>::magnitudes(a.g) + at / 4);
-    const float held[2] = {o > 0 ? magnitudes[0] : 0.f, o > 0 ? magnitudes[1] : 0.f};
+    float* magnitude = (float*)(p + Bytes8<D>::magnitudes(a.g) + at / 4) + (VALUES ? 1 : 0);
+    const float held = o > 0 ? *magnitude : 0.f;
     const int octets = ((o + n + 7) >> 3) - (o >> 3), rounds = ONCE ? 1 : (octets + AT_ONCE - 1) / AT_ONCE;      // with new tokens
     // The thread's octet of the block: all of them at once, so that the codes held are on their way with the new numbers; or, in rounds, those with new tokens.
     int t0 = 8 * ((ONCE ? 0 : o >> 3) + tid / Octet::LANES);
-    uint4 held_k = {0, 0, 0, 0}, held_v = {0, 0, 0, 0};
-    if (ONCE) {
-      if (t0 + me.k_token < o) held_k = *(const uint4*)(p + Bytes8<D>::k(at + t0 + me.k_token, me.k_channel));
-      if (t0 < o || (t0 < o + n && o + n < t0 + 8)) held_v = *(const uint4*)(p + Octet::v_at(a.g, at + t0) + me.v_byte);
-    }
+    const auto bytes_of = [&](int t0) { return (uint4*)(p + (VALUES ? Octet::v_at(a.g, at + t0) + me.v_byte : Bytes8<D>::k(at + t0 + me.k_token, me.k_channel))); };
+    uint4 codes = {0, 0, 0, 0};      // held
+    if (ONCE && (VALUES ? t0 < o || (t0 < o + n && o + n < t0 + 8) : t0 + me.k_token < o)) codes = *bytes_of(t0);
     const auto is_new = [&](int t) { return t >= o && t < o + n; };
-    v8bf k[2];
-    v4bf v[2][2];      // token i or 4 + i, channels c or c + 16
+    v4bf x[4];      // K: 16 channels of a token; V: [2 * (token i or 4 + i) + (channels c or c + 16)]
     const auto fetch = [&] {
-      k[0] = k[1] = v8bf{};
 #pragma unroll
-      for (int half = 0; half < 2; half++) v[half][0] = v[half][1] = v4bf{};
-      if (is_new(t0 + me.k_token)) {
-        const __bf16* x = a.K + (int64_t)(first + t0 + me.k_token - o) * a.ks[0] + h * a.ks[1] + me.k_channel;
-        k[0] = *(const v8bf*)x;
-        k[1] = *(const v8bf*)(x + 8);
-      }
+      for (int i = 0; i < 4; i++) x[i] = v4bf{};
+      if (VALUES) {
 #pragma unroll
-      for (int half = 0; half < 2; half++) {
-        const int t = t0 + me.v_token + 4 * half;
-        if (!is_new(t)) continue;
-        const __bf16* x = a.V + (int64_t)(first + t - o) * a.vs[0] + h * a.vs[1] + me.v_channel;
-        v[half][0] = *(const v4bf*)x;
-        v[half][1] = *(const v4bf*)(x + 16);
+        for (int half = 0; half < 2; half++) {
+          const int t = t0 + me.v_token + 4 * half;
+          if (!is_new(t)) continue;
+          const __bf16* y = from_head + (int64_t)(first + t - o) * stride;
+          x[2 * half] = *(const v4bf*)y;
+          x[2 * half + 1] = *(const v4bf*)(y + 16);
+        }
+      } else if (is_new(t0 + me.k_token)) {
+        const __bf16* y = from_head + (int64_t)(first + t0 + me.k_token - o) * stride;
+        const v8bf lo = *(const v8bf*)y, hi = *(const v8bf*)(y + 8);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          x[0][e] = lo[e];
+          x[1][e] = lo[4 + e];
+          x[2][e] = hi[e];
+          x[3][e] = hi[4 + e];
+        }
       }
     };
-    const auto keys = [&](float* f) {
-#pragma unroll
-      for (int e = 0; e < 16; e++) f[e] = (float)k[e / 8][e % 8];
-      subtract_mean(f, a.k_mean, h * D + me.k_channel);
-      subtract_mean(f + 8, a.k_mean, h * D + me.k_channel + 8);
-    };
-    const auto values = [&](int half, int more, float* f) {
+    const auto numbers = [&](int i, float* f) {
       typedef v4f v4f_dword __attribute__((aligned(4)));
 #pragma unroll
-      for (int e = 0; e < 4; e++) f[e] = (float)v[half][more][e];
-      if (a.v_mean == nullptr) return;
-      const v4f mean = *(const v4f_dword*)(a.v_mean + h * D + me.v_channel + 16 * more);
+      for (int e = 0; e < 4; e++) f[e] = (float)x[i][e];
+      if (mean == nullptr) return;
+      const v4f m = *(const v4f_dword*)(mean + h * D + (VALUES ? me.v_channel + 16 * (i & 1) : me.k_channel + 4 * i));
 #pragma unroll
-      for (int e = 0; e < 4; e++) f[e] -= mean[e];
+      for (int e = 0; e < 4; e++) f[e] -= m[e];
     };
-    unsigned top[2] = {0, 0};      // (tokens that are not the call's are zeros, but for a mean taken off)
-    float f[16];
+    unsigned top = 0;
+    float f[4];
 #pragma unroll 1
     for (int round = 0; round < rounds; round++, t0 += 8 * AT_ONCE) {
       fetch();
-      if (is_new(t0 + me.k_token)) {
-        keys(f);
 #pragma unroll
-        for (int e = 0; e < 16; e++) top[0] = max(top[0], __float_as_uint(f[e]) & 0x7FFFFFFFu);
-      }
+      for (int i = 0; i < 4; i++) {
+        if (!is_new(t0 + (VALUES ? me.v_token + 4 * (i >> 1) : me.k_token))) continue;
+        numbers(i, f);
 #pragma unroll
-      for (int half = 0; half < 2; half++) {
-        if (!is_new(t0 + me.v_token + 4 * half)) continue;
-#pragma unroll
-        for (int more = 0; more < 2; more++) {
-          values(half, more, f);
-#pragma unroll
-          for (int e = 0; e < 4; e++) top[1] = max(top[1], __float_as_uint(f[e]) & 0x7FFFFFFFu);
-        }
+        for (int e = 0; e < 4; e++) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
       }
     }
     t0 -= 8 * AT_ONCE * rounds;
 #pragma unroll
-    for (int which = 0; which < 2; which++) {
-#pragma unroll
-      for (int x = 1; x < 64; x <<= 1) top[which] = max(top[which], (unsigned)__shfl_xor((int)top[which], x));
-      if (lane == 0) tops[side][wave][which] = top[which];
-    }
+    for (int k = 1; k < 64; k <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, k));
+    if (lane == 0) tops[side][wave] = top;
     __syncthreads();               // (the next run has the other side of them)
-    float now[2], r[2], again[2];
-    bool grown[2];
+    top = __float_as_uint(held) & 0x7FFFFFFFu;
 #pragma unroll
-    for (int which = 0; which < 2; which++) {
-      unsigned t = __float_as_uint(held[which]) & 0x7FFFFFFFu;
-#pragma unroll
-      for (int w = 0; w < WAVES; w++) t = max(t, tops[side][w][which]);
-      now[which] = magnitude8(t);
-      r[which] = to_codes8(now[which]);
-      grown[which] = o > 0 && now[which] > held[which];
-      again[which] = grown[which] ? __fdiv_rn(held[which], now[which]) : 1.f;
-    }
+    for (int w = 0; w < WAVES; w++) top = max(top, tops[side][w]);
+    const float now = magnitude8(top), r = to_codes8(now);
+    const bool grown = o > 0 && now > held;
+    const float again = grown ? __fdiv_rn(held, now) : 1.f;
+    const auto recode = [&](const uint4& w) { return uint4{recode8(w.x, again), recode8(w.y, again), recode8(w.z, again), recode8(w.w, again)}; };
 #pragma unroll 1
     for (int round = 0; round < rounds; round++, t0 += 8 * AT_ONCE) {
       if (!ONCE && rounds > 1) fetch();      // (once more)
-      if (is_new(t0 + me.k_token)) {
-        keys(f);
-        *(uint4*)(p + Bytes8<D>::k(at + t0 + me.k_token, me.k_channel)) = uint4{codes8(f, r[0]), codes8(f + 4, r[0]), codes8(f + 8, r[0]), codes8(f + 12, r[0])};
+      unsigned w[4];
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        numbers(i, f);
+        w[i] = codes8(f, r);
       }
-      unsigned w[2][2];      // channel c or c + 16; tokens 0 .. 3 or 4 .. 7
-#pragma unroll
-      for (int more = 0; more < 2; more++)
-#pragma unroll
-        for (int half = 0; half < 2; half++) {
-          values(half, more, f);
-          w[more][half] = turn(codes8(f, r[1]));
-        }
-      if (ONCE && grown[0] && t0 + me.k_token < o)
-        *(uint4*)(p + Bytes8<D>::k(at + t0 + me.k_token, me.k_channel)) =
-            uint4{recode8(held_k.x, again[0]), recode8(held_k.y, again[0]), recode8(held_k.z, again[0]), recode8(held_k.w, again[0])};
+      if (!VALUES) {
+        if (is_new(t0 + me.k_token)) *bytes_of(t0) = uint4{w[0], w[1], w[2], w[3]};
+        else if (ONCE && grown && t0 + me.k_token < o) *bytes_of(t0) = recode(codes);
+        continue;
+      }
       const int from = min(max(o - t0, 0), 8), upto = min(max(o + n - t0, 0), 8);      // new tokens of the octet
-      if (upto > from || (ONCE && grown[1] && from > 0)) {
-        uint4* to = (uint4*)(p + Octet::v_at(a.g, at + t0) + me.v_byte);
+      uint4 z = {turn(w[0]), turn(w[2]), turn(w[1]), turn(w[3])};                      // channel c, tokens 0 .. 3 and 4 .. 7; channel c + 16
+      if (upto > from || (ONCE && grown && from > 0)) {
         if (from > 0 || upto < 8) {
-          const uint4 y = ONCE ? held_v : *to;
-          const unsigned old[2][2] = {{y.x, y.y}, {y.z, y.w}};
+          const uint4 old = ONCE ? codes : *bytes_of(t0), y = grown ? recode(old) : old;
           const auto bytes = [](int n) { return n == 8 ? ~0ull : (1ull << 8 * n) - 1; };
-          const uint64_t below = bytes(from), fresh = bytes(upto) & ~below;
-#pragma unroll
-          for (int more = 0; more < 2; more++)
-#pragma unroll
-            for (int half = 0; half < 2; half++) {
-              const unsigned is_fresh = (unsigned)(fresh >> 32 * half), is_below = (unsigned)(below >> 32 * half), x = old[more][half];
-              const unsigned kept = grown[1] ? (recode8(x, again[1]) & is_below) | (x & ~is_below) : x;      // (behind the new tokens nothing is the call's)
-              w[more][half] = (w[more][half] & is_fresh) | (kept & ~is_fresh);
-            }
+          const uint64_t below = bytes(from), fresh = bytes(upto) & ~below, behind = ~(below | fresh);      // (behind the new tokens nothing is the call's)
+          const auto merge = [&](unsigned z, unsigned y, unsigned old, int half) {
+            return (z & (unsigned)(fresh >> half)) | (y & (unsigned)(below >> half)) | (old & (unsigned)(behind >> half));
+          };
+          z = uint4{merge(z.x, y.x, old.x, 0), merge(z.y, y.y, old.y, 32), merge(z.z, y.z, old.z, 0), merge(z.w, y.w, old.w, 32)};
         }
-        *to = uint4{w[0][0], w[0][1], w[1][0], w[1][1]};
+        *bytes_of(t0) = z;
       }
     }
-    if (!ONCE && grown[0]) {
+    if (!ONCE && grown) {      // octets of tokens held (of K up to the last of them)
+      constexpr int EACH = VALUES ? Octet::LANES : D / 16;
 #pragma unroll 1
-      for (int i = tid; i < o * (D / 16); i += THREADS) {
-        uint4* q = (uint4*)(p + Bytes8<D>::k(at + i / (D / 16), i % (D / 16) * 16));
-        const uint4 w = *q;
-        *q = uint4{recode8(w.x, again[0]), recode8(w.y, again[0]), recode8(w.z, again[0]), recode8(w.w, again[0])};
+      for (int i = tid; i < (VALUES ? o >> 3 : o) * EACH; i += THREADS) {
+        uint4* q = (uint4*)(p + (VALUES ? Octet::v_at(a.g, at + i / EACH * 8) + (i % EACH >> 4) * 1024 + (i & 15) * 16 : Bytes8<D>::k(at + i / EACH, i % EACH * 16)));
+        *q = recode(*q);
       }
     }
-    if (!ONCE && grown[1]) {
-#pragma unroll 1
-      for (int i = tid; i < (o >> 3) * Octet::LANES; i += THREADS) {
-        uint4* q = (uint4*)(p + Octet::v_at(a.g, at + i / Octet::LANES * 8) + (i % Octet::LANES >> 4) * 1024 + (i & 15) * 16);
-        const uint4 w = *q;
-        *q = uint4{recode8(w.x, again[1]), recode8(w.y, again[1]), recode8(w.z, again[1]), recode8(w.w, again[1])};
-      }
-    }
-    if (tid < BLOCK / 32) *(float2*)(magnitudes + 2 * tid) = float2{now[0], now[1]};
+    if (tid < BLOCK / 32) magnitude[2 * tid] = now;
   }
+}
+template <int D, int BLOCK, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void cache8_append_kernel(StoreArgs a, int window) {
+  __shared__ unsigned tops[2][WAVES];
+  if (blockIdx.z == 0) store_runs<D, BLOCK, WAVES, false>(a, window, tops);
+  else store_runs<D, BLOCK, WAVES, true>(a, window, tops);
 }
 
 // The tokens of an octet that stand one after the other are read together; a wave has some of those that begin in the workgroup's `window` rows.

@@ -52,9 +52,9 @@ int cache8_append(const StoreArgs& a, const sagebwd_cache_params& p, hipStream_t
   // Few tokens are mostly one of each request: two waves, which go through a whole block in up to four rounds, where else a wave has no more than one.
   // (TWOWAVES)
   const bool few = a.T <= 256;
-  const int waves = few ? 2 : p.block * p.d / 1024, window = window_of(a, p, waves);
-  const dim3 grid((unsigned)((a.T + (int64_t)window - 1) / window), p.H);
-  if ((int64_t)grid.x * p.H * 512 > kMostThreads) return SAGEBWD_UNSUPPORTED_SHAPE;
+  const int waves = few ? 2 : p.block * p.d / 1024, window = window_of(a, p, 2 * waves);
+  const dim3 grid((unsigned)((a.T + (int64_t)window - 1) / window), p.H, 2);
+  if ((int64_t)grid.x * p.H * 1024 > kMostThreads) return SAGEBWD_UNSUPPORTED_SHAPE;
   if (p.d == 64 && p.block == 32) launch_append<64, 32, 2>(a, grid, window, st);
   else if (p.d == 64) few ? launch_append<64, 64, 2>(a, grid, window, st) : launch_append<64, 64, 4>(a, grid, window, st);
   else if (p.block == 32) few ? launch_append<128, 32, 2>(a, grid, window, st) : launch_append<128, 32, 4>(a, grid, window, st);
