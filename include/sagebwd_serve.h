@@ -170,7 +170,7 @@ int sagebwd_cache_read(const int64_t* slots, int32_t T, const float* k_mean, con
 typedef struct sagebwd_cache_call {
   int32_t R;          /* requests */
   int32_t T;          /* rows of Q and O (at least cu[R]; those behind it are left as they are).  From R * max_new on, with max_new * Hq / H
-                         more than 32, the call takes every request to bring max_new tokens: shorter ones are slower than need be */
+                         more than 32 (held in 8 bits 128), the call takes every request to bring max_new tokens: shorter ones are slower than need be */
   int32_t Hq;         /* query heads: a multiple of H, at most 64 H; head h reads key/value head h / (Hq / H) */
   int32_t columns;    /* of the block table */
   int32_t max_new;    /* at least every request's new tokens (1: a decoding step); further tokens are not computed */
@@ -188,12 +188,14 @@ typedef struct sagebwd_cache_call {
  *               rising from 0 (read as within 0 .. T)
  *   O           bf16 [T, Hq, d] dense; LSE float32 [Hq, T], or NULL
  * Sums, softmax statistics and the joining of parts are FP32; the probabilities times V's scales are rounded to bf16 for
- * the matrix instruction (codes, of 4 bits or of 8, are bf16 numbers).  A row that sees no key (a request of length 0; with the mask the first rows of one shorter
+ * the matrix instruction (codes, of 4 bits or of 8, are bf16 numbers; held in 8 bits, in tiles of up to 32 rows, what that rounding leaves has a
+ * product of its own).  A row that sees no key (a request of length 0; with the mask the first rows of one shorter
  * than its new tokens; pages that do not exist) gives O = 0, LSE = -infinity.  What stands in the cache behind a
  * request's length reaches nothing.
  * Where max_new tokens are up to 32 query rows (new tokens x Hq / H) all requests go to a kernel for few rows, else to one for many; but where
  * T is less than R * max_new and Hq / H at most 32 the call launches both, and requests of up to 16 rows (32, where Hq / H is more than 16) go
- * to the former.  A tile of tokens on a page that does not exist is passed over by the kernel for few rows and masked by the others.
+ * to the former.  Held in 8 bits the kernel for few rows takes up to 128, in tiles of 16 to 64 rows with a pass over the keys each (32 where R * H *
+ * (max_length / 128 + 3) passes 2^27), beside requests of more rows too; short requests have a wave each.  A tile of tokens on a page that does not exist is passed over by the kernel for few rows and masked by the others.
  * Where a call has few items for the machine their keys are divided over it and the parts joined by a further launch; from 2048 rows a request on, keys and values are
  * unpacked to bf16 in the workspace first (256 d bytes for 64 tokens and head; at most 4 GiB, else each tile unpacks its own).  How
  * work is divided depends on all requests of the call, so that O agrees between calls of different batches to its rounding, and bit

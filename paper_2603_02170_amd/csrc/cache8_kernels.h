@@ -44,7 +44,7 @@ __device__ __forceinline__ unsigned recode8(unsigned w, float f) {      // four 
 // 8 tokens (an octet) of a head are the work of D / 2 lanes, and a wave has EACH at a time.  K: a lane has 16 channels of a token, as they lie in
 // the page.  V: lane (j, q, i) has 16 bytes of channels c = 32 j + 4 q + i and c + 16, which turned are channels 32 j + 4 q .. and 16 more of tokens i
 // and 4 + i.  (A byte at a time, of V in LDS or in the page, storing 7700 tokens of 8 heads of 128 took 19.1 us and
-// reading them 22.8, so 16.8 and 13.1.)
+// reading them 22.8, now 14.5 and 13.9.)
 template <int D>
 struct Octet8 {
   static constexpr int LANES = D / 2, EACH = 64 / LANES;
@@ -99,7 +99,8 @@ struct Runs8 {
 
 // One workgroup has a run of a block's keys or values (blockIdx.z), for a head: the block's largest magnitude has to be known before the first code is written,
 // and where it grows the codes held are written again.  A thread has 16 numbers at a time.  (With 16 of K and 16 of V registers halve the waves of a CU:
-// APPENDBOTH; a thread having two such in turn, and the slots asked for once more for each run, 20.0 in place of 16.8.)
+// 7700 tokens of 8 heads
+// 15.8 us, so 14.5; a thread having two such in turn, and the slots asked for once more for each run, 20.0.)
 template <int D, int BLOCK, int WAVES, bool VALUES>
 __device__ __forceinline__ void store_runs(const StoreArgs& a, int window, unsigned (*tops)[WAVES]) {
   typedef Octet8<D> Octet;

@@ -6,7 +6,7 @@
 //
 // Steps: a workgroup has kColumns columns of a request's row of the table, a thread four of them, whose loads are under way together; one workgroup
 // settles the stack.  Small calls are one launch of one workgroup.  (A wave a row, one trip to memory after the other: 25 requests of 530 pages 55 us
-// for free, fork and own; so LONGROWS.)
+// for free, fork and own; so 24.)
 #pragma once
 
 #include "cache_kernels.h"
@@ -31,7 +31,7 @@ struct PagesArgs {
 __device__ __forceinline__ int now_in(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // (Whoever takes the count below zero says so: of a page that ends there someone does, also where others count it up meanwhile.  With a bit from each of five holders
-// of 530 pages free took 14.3 us, so FREEBITS.)
+// of 530 pages free took 14.3 us, so 4.2.)
 __device__ __forceinline__ void lose_page(const PagesArgs& a, int entry) {
   if (atomicSub(a.shares + entry, 1) <= 0) atomicOr(a.bits() + (entry >> 5), 1u << (entry & 31));
 }

@@ -150,7 +150,7 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
   const int few_rows = few_rows_of(p, c);
   w.many = rows > few_rows;
   w.few = !w.many || (G <= few_rows && (int64_t)c.T < (int64_t)c.R * c.max_new);
-  // (Held in 8 bits and small, two launches more cost more than tiles half empty: eight ragged requests of 1380 tokens with up to 915 rows 45 -> MANYONLY us.)
+  // (Held in 8 bits and small, two launches more cost more than tiles half empty: eight ragged requests of 1380 tokens with up to 915 rows 45 -> 30 us.)
   if (w.many && p.block > 0 && (int64_t)c.R * p.H * ((w.max_length + kChunkUnit - 1) / kChunkUnit) <= 2 * kCus) w.few = false;
   if (w.few) {
     AttendLaunch& l = w.f;
