@@ -36,31 +36,34 @@ __device__ __forceinline__ void lose_page(const PagesArgs& a, int entry) {
   if (atomicSub(a.shares + entry, 1) <= 0) atomicOr(a.bits() + (entry >> 5), 1u << (entry & 31));
 }
 
-// Pages whose last holder went go on the stack, the lowest last.  1024 threads; 65536 pages at a time, from the highest: each wave finds the ones
+// Pages whose last holder went go on the stack, the lowest last.  One workgroup; 64 pages a thread at a time, from the highest: each wave finds the ones
 // among 64, a lane a page, then their places are summed.
 constexpr int kAtOnce = 4;      // loads of a lane under way
+template <int WAVES>
 struct SettleScratch {
-  uint64_t freed[1024];
-  unsigned sums[16][1], total;
+  uint64_t freed[64 * WAVES];
+  unsigned sums[WAVES][1], total;
 };
-__device__ __forceinline__ void settle_pages(const PagesArgs& a, SettleScratch& s) {
+template <int WAVES>
+__device__ __forceinline__ void settle_pages(const PagesArgs& a, SettleScratch<WAVES>& s) {
+  constexpr int THREADS = 64 * WAVES;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int groups = (a.pages + 63) >> 6, words = (a.pages + 31) >> 5;
   int64_t count = max(0, min(now_in(a.free_count), a.capacity));
-  for (int end = groups; end > 0; end -= 1024) {
-    const int here = min(end, 1024);
-    for (int i0 = wave; i0 < here; i0 += 16 * kAtOnce) {
+  for (int end = groups; end > 0; end -= THREADS) {
+    const int here = min(end, THREADS);
+    for (int i0 = wave; i0 < here; i0 += WAVES * kAtOnce) {
       uint32_t word[kAtOnce];
       int holders[kAtOnce];
 #pragma unroll
       for (int k = 0; k < kAtOnce; k++) {
-        const int i = i0 + 16 * k, group = end - 1 - i, at = 2 * group + (lane >> 5), page = 64 * group + lane;
+        const int i = i0 + WAVES * k, group = end - 1 - i, at = 2 * group + (lane >> 5), page = 64 * group + lane;
         word[k] = i < here && at < words ? (uint32_t)now_in((const int32_t*)a.bits() + at) : 0;
         holders[k] = i < here && page < a.pages ? now_in(a.shares + page) : 0;
       }
 #pragma unroll
       for (int k = 0; k < kAtOnce; k++) {
-        const int i = i0 + 16 * k, group = end - 1 - i;
+        const int i = i0 + WAVES * k, group = end - 1 - i;
         if (i >= here) break;
         if ((lane & 31) == 0 && word[k] != 0) a.bits()[2 * group + (lane >> 5)] = 0;
         const bool freed = (word[k] >> (lane & 31) & 1) && holders[k] < 0;
@@ -71,8 +74,8 @@ __device__ __forceinline__ void settle_pages(const PagesArgs& a, SettleScratch& 
     }
     __syncthreads();
     unsigned to[1] = {tid < here ? (unsigned)__popcll(s.freed[tid]) : 0};
-    block_scan<16>(to, s.sums);
-    if (tid == 1023) s.total = to[0];
+    block_scan<WAVES>(to, s.sums);
+    if (tid == THREADS - 1) s.total = to[0];
     if (tid < here) {
       uint64_t mask = s.freed[tid];
       int64_t at = count + to[0] - __popcll(mask);
@@ -96,9 +99,9 @@ __device__ __forceinline__ void each_column(const PagesArgs& a, F f) {
   const int chunks = (a.columns + kColumns - 1) / kColumns, r = blockIdx.x / chunks;
   f(r, (int)(blockIdx.x - r * chunks) * kColumns + (int)threadIdx.x);
 }
-template <typename F>
+template <int THREADS, typename F>
 __device__ __forceinline__ void each_entry(const PagesArgs& a, F f) {      // of a small call
-  for (int i = threadIdx.x; i < a.R * a.columns; i += 1024) f(i / a.columns, i % a.columns);
+  for (int i = threadIdx.x; i < a.R * a.columns; i += THREADS) f(i / a.columns, i % a.columns);
 }
 
 // ---- free ----------------------------------------------------------------------------------------------------------
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(256) void cache_free_rows_kernel(PagesArgs a) {
 }
 // the first workgroup settles, the others have the lengths
 __global__ __launch_bounds__(1024) void cache_freed_kernel(PagesArgs a) {
-  __shared__ SettleScratch s;
+  __shared__ SettleScratch<16> s;
   if (blockIdx.x == 0) {
     settle_pages(a, s);
     return;
@@ -136,12 +139,13 @@ __global__ __launch_bounds__(1024) void cache_freed_kernel(PagesArgs a) {
   const int r = (blockIdx.x - 1) * 1024 + threadIdx.x;
   if (r < a.R && keeps(a, r)) a.lengths[r] = a.asked[r];
 }
-__global__ __launch_bounds__(1024) void cache_free_kernel(PagesArgs a) {
-  __shared__ SettleScratch s;
-  each_entry(a, [&](int r, int c) { free_columns<1>(a, r, c, 0); });
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void cache_free_kernel(PagesArgs a) {
+  __shared__ SettleScratch<WAVES> s;
+  each_entry<64 * WAVES>(a, [&](int r, int c) { free_columns<1>(a, r, c, 0); });
   __threadfence_block();
   __syncthreads();
-  for (int r = threadIdx.x; r < a.R; r += 1024)
+  for (int r = threadIdx.x; r < a.R; r += 64 * WAVES)
     if (keeps(a, r)) a.lengths[r] = a.asked[r];
   settle_pages(a, s);
 }
@@ -189,7 +193,7 @@ __global__ __launch_bounds__(256) void cache_fork_rows_kernel(PagesArgs a) {
 }
 // the first workgroup settles, the others have kColumns of a row each
 __global__ __launch_bounds__(1024) void cache_forked_kernel(PagesArgs a) {
-  __shared__ SettleScratch s;
+  __shared__ SettleScratch<16> s;
   if (blockIdx.x == 0) {
     settle_pages(a, s);
     return;
@@ -197,20 +201,23 @@ __global__ __launch_bounds__(1024) void cache_forked_kernel(PagesArgs a) {
   const int chunks = (a.columns + kColumns - 1) / kColumns, i = blockIdx.x - 1, r = i / chunks;
   forked_columns<1>(a, r, (i - r * chunks) * kColumns + (int)threadIdx.x, 0);
 }
-__global__ __launch_bounds__(1024) void cache_fork_kernel(PagesArgs a) {
-  __shared__ SettleScratch s;
-  each_entry(a, [&](int r, int c) { fork_columns<1>(a, r, c, 0); });
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void cache_fork_kernel(PagesArgs a) {
+  __shared__ SettleScratch<WAVES> s;
+  each_entry<64 * WAVES>(a, [&](int r, int c) { fork_columns<1>(a, r, c, 0); });
   __threadfence_block();
   __syncthreads();
-  each_entry(a, [&](int r, int c) { forked_columns<1>(a, r, c, 0); });
+  each_entry<64 * WAVES>(a, [&](int r, int c) { forked_columns<1>(a, r, c, 0); });
   settle_pages(a, s);
 }
 
 // ---- own -----------------------------------------------------------------------------------------------------------
 // Who writes into a page that others hold gets a copy of it; if all its holders are about to write, the last of them keeps it.  One
 // workgroup; the copies are a launch of their own.
-__global__ __launch_bounds__(1024) void cache_own_kernel(PagesArgs a) {
-  __shared__ unsigned sums[16][1], total;
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void cache_own_kernel(PagesArgs a) {
+  constexpr int THREADS = 64 * WAVES;
+  __shared__ unsigned sums[WAVES][1], total;
   const int tid = threadIdx.x;
   int32_t *asks = a.shares + a.pages, *last = asks + a.pages;      // of a page: how many are about to write, and 1 + the last of them
   // the page that a request's next token goes into, if that has tokens
@@ -223,7 +230,7 @@ __global__ __launch_bounds__(1024) void cache_own_kernel(PagesArgs a) {
   // (the thread's first request stays in registers from step to step)
   const auto holders_of = [&](int entry) { return entry >= 0 ? a.shares[entry] : 0; };
   const int entry0 = tid < a.R ? page_of(tid) : -1, holders0 = holders_of(entry0);
-  for (int r = tid; r < a.R; r += 1024) {
+  for (int r = tid; r < a.R; r += THREADS) {
     const int entry = r == tid ? entry0 : page_of(r), holders = r == tid ? holders0 : holders_of(entry);
     if (holders <= 0) continue;
     atomicAdd(asks + entry, 1);
@@ -234,14 +241,14 @@ __global__ __launch_bounds__(1024) void cache_own_kernel(PagesArgs a) {
   __syncthreads();
   unsigned before = 0;
   int2 move0 = {-1, -1};
-  for (int base = 0; base < a.R; base += 1024) {
+  for (int base = 0; base < a.R; base += THREADS) {
     const int r = base + tid;
     const int entry = base == 0 ? entry0 : r < a.R ? page_of(r) : -1, holders = base == 0 ? holders0 : holders_of(entry);
     const bool wants = holders > 0;
     const bool copies = wants && !(now_in(asks + entry) == holders + 1 && now_in(last + entry) == r + 1);
     unsigned need[1] = {copies ? 1u : 0u};
-    block_scan<16>(need, sums);
-    if (tid == 1023) total = need[0];
+    block_scan<WAVES>(need, sums);
+    if (tid == THREADS - 1) total = need[0];
     const unsigned needs = min(before + need[0], kFull);
     const bool granted = !wants || needs <= count;
     int2 move = {entry, -1};
@@ -259,7 +266,7 @@ __global__ __launch_bounds__(1024) void cache_own_kernel(PagesArgs a) {
     before = min(before + total, kFull);
     __syncthreads();
   }
-  for (int r = tid; r < a.R; r += 1024) {
+  for (int r = tid; r < a.R; r += THREADS) {
     const int2 move = r == tid ? move0 : a.moves[r];
     if (move.x < 0) continue;
     asks[move.x] = 0;
@@ -373,7 +380,7 @@ __global__ __launch_bounds__(1024) void cache_choose_kernel(CompactArgs c) {
 }
 __global__ __launch_bounds__(1024) void cache_count_and_choose_kernel(CompactArgs c) {
   __shared__ CompactScratch s;
-  each_entry(c.p, [&](int r, int at) { count_columns<1>(c.p, r, at, 0); });
+  each_entry<1024>(c.p, [&](int r, int at) { count_columns<1>(c.p, r, at, 0); });
   __threadfence_block();
   __syncthreads();
   choose_moves(c, s);

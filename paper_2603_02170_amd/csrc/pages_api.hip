@@ -10,6 +10,9 @@ using namespace sage;
 // Entries of the table up to which a call is one launch of one workgroup.
 constexpr int64_t kSmallEntries = 2048;
 bool small(int R, int columns) { return (int64_t)R * columns <= kSmallEntries; }
+// Entries, pages and requests up to which that has four waves and not sixteen (eight requests of 18 pages, free, fork and own 16.2 -> 15.2 us).
+bool smallest(int R, int columns, int pages) { return (int64_t)R * columns <= 512 && pages <= 16384; }
+constexpr int kFewRequests = 256;
 // Workgroups of a launch that has kColumns columns of a row each.
 unsigned row_chunks(int R, int columns) { return (unsigned)(R * (int64_t)((columns + kColumns - 1) / kColumns)); }
 
@@ -69,7 +72,8 @@ int sagebwd_cache_free(const int32_t* keep, int32_t* lengths, int32_t* block_tab
   a.pages = pages;
   hipStream_t st = (hipStream_t)stream;
   if (small(R, columns)) {
-    cache_free_kernel<<<1, 1024, 0, st>>>(a);
+    if (smallest(R, columns, pages)) cache_free_kernel<4><<<1, 256, 0, st>>>(a);
+    else cache_free_kernel<16><<<1, 1024, 0, st>>>(a);
   } else {
     cache_free_rows_kernel<<<row_chunks(R, columns), 256, 0, st>>>(a);
     SERVE_LAUNCH_CHECK();
@@ -110,7 +114,8 @@ int sagebwd_cache_fork(const int32_t* parents, int32_t* lengths, int32_t* block_
   a.pages = pages;
   hipStream_t st = (hipStream_t)stream;
   if (small(R, columns)) {
-    cache_fork_kernel<<<1, 1024, 0, st>>>(a);
+    if (smallest(R, columns, pages)) cache_fork_kernel<4><<<1, 256, 0, st>>>(a);
+    else cache_fork_kernel<16><<<1, 1024, 0, st>>>(a);
   } else {
     cache_fork_rows_kernel<<<row_chunks(R, columns), 256, 0, st>>>(a);
     SERVE_LAUNCH_CHECK();
@@ -147,7 +152,8 @@ int sagebwd_cache_own(const int32_t* added, const int32_t* lengths, int32_t* blo
   a.capacity = capacity;
   a.pages = params->pages;
   hipStream_t st = (hipStream_t)stream;
-  cache_own_kernel<<<1, 1024, 0, st>>>(a);
+  if (R <= kFewRequests) cache_own_kernel<4><<<1, 256, 0, st>>>(a);
+  else cache_own_kernel<16><<<1, 1024, 0, st>>>(a);
   SERVE_LAUNCH_CHECK();
   cache_copy_pages_kernel<<<dim3(R, pieces_of(page_bytes)), 256, 0, st>>>(a.moves, (unsigned char*)pool, page_bytes);
   SERVE_LAUNCH_CHECK();
