@@ -95,6 +95,9 @@ inline int check_call(const sagebwd_cache_params* p, const sagebwd_cache_call* c
 // Keys of a request up to this many units are not divided (four requests of 500 tokens 11.0 -> 9.3 us, 256 of 650 56.4 -> 52.0: the joining
 // launch is 4 to 5 us, a unit 0.6 where the machine is empty).
 constexpr int kWholeUnits = 8;
+// Held in 8 bits, where undivided items fill half of the machine, they may be this long (keys of 1500: 16 requests of 8 heads 16.7 -> 14.8
+// us, 64 42.9 -> 39.0; 64 of 16 heads, d = 64, 46.5 -> 38.5; with fewer items division is the faster: one request 11.4 -> 14.0 undivided).
+constexpr int kWholeUnits8 = 12;
 // Held in 8 bits, items of so many keys have a wave each, whatever their number.
 constexpr int kShortLength = 128;
 // Keys and values are unpacked beforehand where a request's meet so many row tiles (us, unpacked by every tile -> beforehand: one request of 512 new
@@ -161,7 +164,7 @@ inline AttendPlan attend_plan(const sagebwd_cache_params& p, const sagebwd_cache
     l.rows_to = here > 32 ? few_rows : 16 * l.nq;
     l.join_rows = (int)(here < 16 * l.nq ? here : 16 * l.nq);
     const int most_units = (w.max_length + kUnit - 1) / kUnit;
-    l.split = most_units > kWholeUnits;
+    l.split = most_units > (p.block > 0 && (int64_t)c.R * p.H * tiles >= kCus / 2 ? kWholeUnits8 : kWholeUnits);
     const int64_t units = (int64_t)c.R * p.H * tiles * (l.split ? most_units + kItemCost : 1);
     // (Held in 8 bits the keys alone bound a call of one tile, and a workgroup a CU has enough of them under way: 32 requests of 4096 tokens, 16 rows
     // 59.4 -> 55.1 us, 32 rows 63.2 -> 57.0, one of 131000 57.4 -> 55.2.  Of several tiles two: heads of 64, up to 100 rows 19.6 -> 18.4.)

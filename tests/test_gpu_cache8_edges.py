@@ -121,3 +121,32 @@ def test_prompts_and_decoding_in_one_captured_graph_with_other_work_between_repl
         got = [t.clone() for t in out]
         want = work()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+@pytest.mark.parametrize("R,n,G,H,d,block", [(16, 1, 4, 8, 128, 64), (9, 16, 1, 16, 64, 32), (48, 2, 3, 24, 64, 64), (5, 30, 2, 14, 128, 32), (2, 100, 1, 16, 64, 64)])
+def test_many_undivided_requests(R, n, G, H, d, block):
+    """Up to 1536 tokens are walked in one go where requests and heads fill half of the machine, by a workgroup an item or a wave an item; requests
+    of one token, and one without new ones, in between."""
+    g, rng = torch.Generator().manual_seed(R * n), np.random.default_rng(R)
+    p = CacheParams(H=H, d=d, page=64, block=block)
+    base = Filled([1536], p, g, spare_columns=0)       # (its pages are every request's)
+    lens = [1536 - int(x) for x in rng.integers(0, 1536 - n, R)]
+    news = [int(x) for x in rng.integers(1, n + 1, R)]
+    lens[0], news[0], lens[-1] = 1536, n, news[-1]
+    lens[R // 2] = 1 if news[R // 2] == 1 else lens[R // 2]
+    if R > 8:
+        news[3] = 0
+    q = _randn((sum(news), H * G, d), g)
+    cu = np.concatenate([[0], np.cumsum(news)]).astype(int).tolist()
+    for causal in (True, False):
+        O, lse = cache.sagebwd_cache_attention(q.cuda(), base.pool, base.table.expand(R, -1).contiguous(), _i32(lens), _i32(cu), p, n, causal=causal)
+        again = cache.sagebwd_cache_attention(q.cuda(), base.pool, base.table.expand(R, -1).contiguous(), _i32(lens), _i32(cu), p, n, causal=causal)
+        assert torch.equal(O, again[0]) and torch.equal(lse, again[1])
+        for r in sorted({0, R // 2, R - 1, int(rng.integers(0, R))}):
+            a, b = cu[r], cu[r + 1]
+            for h in (0, H - 1):
+                if a == b:
+                    continue
+                one = type("One", (), dict(p=p, lens=[lens[r]], k=base.k[:lens[r], h:h + 1], v=base.v[:lens[r], h:h + 1], at=[0, lens[r]]))
+                heads = slice(h * G, h * G + G)
+                _check(one, q[a:b, heads], [0, b - a], O[a:b, heads], lse[heads, a:b], causal)
