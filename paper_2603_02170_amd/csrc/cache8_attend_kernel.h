@@ -246,7 +246,8 @@ __global__ __launch_bounds__(256, 2) void cache8_short_kernel(AttendArgs a) {
 // ---- many rows ---------------------------------------------------------------------------------------------------------
 // V's scale of a half goes into its exponents (log2 of it), so that they give the probabilities times it, and out of their sum.  (Of a scale of zero, whose
 // codes are zeros, any other will do, and for one that is no number poison() stands in.)  It saves 32 products of a lane and tile: 2048 new tokens of
-// 4 heads of a group against 10000 313 -> 304 us.
+// 4 heads of a group against 10000 313 -> 304 us.  Only of a magnitude that the quantiser may have stored, zero or 2^-100 and more: where nothing was stored any
+// bits may be, and the logarithm of a number so small that its scale flushes to zero would make the sum of a half of which no row sees a token 0 times infinity.
 struct ByteKnown {
   int flags[2];           // bit 0: the half's page exists; bit 1: and its values are not numbers; bit 2: and its keys
   float k[2], log_v[2];
@@ -254,7 +255,7 @@ struct ByteKnown {
     const auto number = [](float x) { return x >= 0.f && x < INFINITY; };      // (where nothing was stored any bits may be)
     flags[half] = is_page ? 1 | (number(va) ? 0 : 2) | (number(ka) ? 0 : 4) : 0;
     k[half] = number(ka) ? ka * kBy127 : 0.f;
-    log_v[half] = number(va) && va > 0.f ? __builtin_amdgcn_logf(va * kBy127) : 0.f;
+    log_v[half] = is_page && number(va) && va >= kLeast8 ? __builtin_amdgcn_logf(va * kBy127) : 0.f;
   }
   // Of all lanes the same: to scalar registers.
   __device__ __forceinline__ ByteKnown uniform(int lane) const {

@@ -19,6 +19,7 @@ struct Bytes8 {
   }
 };
 
+constexpr float kLeast8 = 0x1p-100f;      // of magnitudes stored, but for zero
 // The largest magnitude of a block as it is stored, from its bits (of an infinity and a NaN the largest).
 __device__ __forceinline__ float magnitude8(unsigned top) {
   return __uint_as_float(top < 0x0D800000u ? 0u : top >= 0x7F000000u ? 0x7FC00000u : top);
