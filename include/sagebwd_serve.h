@@ -203,6 +203,8 @@ typedef struct sagebwd_cache_call {
  * Range: with |Q| < 2^117 (held in 8 bits 2^112, as codes are whole numbers up to 127), and V's largest magnitude (less its mean) times the request's length < 2^117, no sum overflows where the result does
  * not.  (Logits: nibbles are read as 16 .. 31 and 24 sum(Q) taken off.  Values: a row's sum is formed before it is divided, of probabilities
  * relative to a reference up to 2^8 below the largest, times nibbles of 31.)  Beyond it rows may be infinite or NaN.
+ * Held in 8 bits, of a key whose weight (relative to that reference) times V's scale is below 2^-126 the value may count as zero in O; its weight counts in
+ * the softmax's sum and in LSE, which do not depend on V.
  * The workspace depends on the host's sizes alone; its contents before the call do not matter, and calls in flight at a time (on two
  * streams, in two graphs) need one each.
  * Bounds: R <= 2^20, columns * page < 2^30, R * H * (columns * page / 128 + 3) <= 2^29, T * Hq / H < 2^30; with more than 32 rows a request

@@ -248,14 +248,20 @@ __global__ __launch_bounds__(256, 2) void cache8_short_kernel(AttendArgs a) {
 // codes are zeros, any other will do, and for one that is no number poison() stands in.)  It saves 32 products of a lane and tile: 2048 new tokens of
 // 4 heads of a group against 10000 313 -> 304 us.  Only of a magnitude that the quantiser may have stored, zero or 2^-100 and more: where nothing was stored any
 // bits may be, and the logarithm of a number so small that its scale flushes to zero would make the sum of a half of which no row sees a token 0 times infinity.
+// What is folded in is at most 2^64 either way: exp2 flushes what is below 2^-126, so that the sum loses weights of less than 2^-62 of the reference (2^30 keys
+// of them are 2^-32; of a magnitude of 2^-100 it would lose those of 2^-19, and LSE depend on V).  The few magnitudes beyond leave a power of two to be
+// multiplied into the probabilities behind the sum, in the branch of blocks that are not numbers.  (In the softmax that took 12 to 17 registers more and 308 -> 319
+// us; into V's fragments where they are stored, four of 5000 tokens with 300 new ones 136 -> 142; so 134 -> 132.)
 struct ByteKnown {
-  int flags[2];           // bit 0: the half's page exists; bit 1: and its values are not numbers; bit 2: and its keys
+  int flags[2];           // bit 0: the half's page exists; bit 1: and its values are not numbers; bit 2: and its keys; from bit 8 on, signed: the power of two
   float k[2], log_v[2];
   __device__ __forceinline__ void set(int half, bool is_page, float ka, float va) {
     const auto number = [](float x) { return x >= 0.f && x < INFINITY; };      // (where nothing was stored any bits may be)
-    flags[half] = is_page ? 1 | (number(va) ? 0 : 2) | (number(ka) ? 0 : 4) : 0;
+    const bool stored = is_page && number(va) && va >= kLeast8;
+    const int e = (int)(__float_as_uint(va) >> 23) - 127, left = stored && (e < -57 || e > 70) ? e - 7 : 0;
+    flags[half] = (is_page ? 1 | (number(va) ? 0 : 2) | (number(ka) ? 0 : 4) : 0) | left * 256;
     k[half] = number(ka) ? ka * kBy127 : 0.f;
-    log_v[half] = is_page && number(va) && va >= kLeast8 ? __builtin_amdgcn_logf(va * kBy127) : 0.f;
+    log_v[half] = stored ? __builtin_amdgcn_logf(__builtin_ldexpf(va * kBy127, -left)) : 0.f;
   }
   // Of all lanes the same: to scalar registers.
   __device__ __forceinline__ ByteKnown uniform(int lane) const {
@@ -371,6 +377,17 @@ struct ByteChunkRows : ChunkRows<D> {
                                    pack_bf16(s[b][8 * k + 4], s[b][8 * k + 5]), pack_bf16(s[b][8 * k + 6], s[b][8 * k + 7])});
     }
   }
+  // What the probabilities are still to be multiplied by.
+  static __device__ __forceinline__ void scale(v8bf (&p)[4], const ByteKnown& known) {
+#pragma unroll
+    for (int b = 0; b < 2; b++) {
+      const float by = __builtin_ldexpf(1.f, known.flags[b] >> 8);
+#pragma unroll
+      for (int k = 0; k < 2; k++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) p[2 * b + k][i] = (__bf16)((float)p[2 * b + k][i] * by);
+    }
+  }
   // A block whose keys or values are not numbers, to the rows that see some of it.
   __device__ __forceinline__ void poison(const ByteKnown& known, int t0) {
 #pragma unroll
@@ -389,9 +406,13 @@ struct ByteChunks {
   typedef ByteChunk<D> Tile;
   typedef ByteChunkRows<D> Rows;
   typedef ByteKnown Known;
-  static __device__ __forceinline__ void poison(Rows& rows, bool, const unsigned char*, const Known& known, int t0) {
-    if (__builtin_expect(__builtin_amdgcn_readfirstlane(known.flags[0] | known.flags[1]) & 6, 0)) rows.poison(known, t0);
+  static __device__ __forceinline__ void before_values(Rows& rows, v8bf (&p)[4], const Known& known, int t0) {
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(known.flags[0] | known.flags[1]) & ~1, 0)) {
+      Rows::scale(p, known);
+      rows.poison(known, t0);
+    }
   }
+  static __device__ __forceinline__ void poison(Rows&, bool, const unsigned char*, const Known&, int) {}      // (before_values has)
   static constexpr bool WORDS_IN_RING = true;      // (six registers of them are more than the kernel for heads of 64 has)
   typedef ByteKnown Word;
   static __device__ __forceinline__ Word word(const Known& known, bool) { return known; }

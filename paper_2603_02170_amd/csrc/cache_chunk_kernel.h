@@ -409,6 +409,8 @@ struct NibbleChunks {
   typedef ChunkTile<D, GROUP> Tile;
   typedef ChunkRows<D> Rows;
   typedef ChunkKnown Known;
+  // What is to be done in front of the product of 64 tokens' probabilities and values.
+  static __device__ __forceinline__ void before_values(Rows&, v8bf (&)[4], const Known&, int) {}
   // Of 64 tokens: `bad` has those that are not numbers, if there are any.
   static __device__ __forceinline__ void poison(Rows& rows, bool any, const unsigned char* bad, const Known& known, int t0) {
     if (any) rows.poison(bad, GROUP, t0, known);
@@ -484,6 +486,7 @@ __device__ __forceinline__ void chunk_items(AttendArgs a) {
     for (int k = 0, v = 2; k <= count; k++, v = v == 2 ? 0 : v + 1) {      // v = (k + 2) % 3
       if (late && k > 0) probabilities(k - 1);
       if (k > 0 && (j0 + k - 1) * kChunkUnit < rows.wave_sees) {
+        Form::before_values(rows, p, known[k - 1 & 3], (j0 + k - 1) * kChunkUnit);
         rows.values(Vs[v], p);
         Form::poison(rows, poisoned[k - 1 & 3] == tag + k - 1, poison[k - 1 & 3], known[k - 1 & 3], (j0 + k - 1) * kChunkUnit);
       }
@@ -564,6 +567,7 @@ __device__ __forceinline__ void span_items(AttendArgs a) {
       v8bf p[4];
       rows.logits(lds[set][kg], s);
       rows.softmax(s, p, t0, of, a.scale_log2);
+      Form::before_values(rows, p, of, t0);
       rows.values(lds[set][kg] + HALF, p);
       Form::poison(rows, poisoned[set][kg] == tag + k, poison[set][kg], of, t0);
     };
@@ -754,6 +758,7 @@ __device__ __forceinline__ void wide_items(AttendArgs a) {
       else word = words.of(k % 64);
       if (late && k > 0) probabilities(k - 1, word_before);
       if (k > 0 && (j0 + k - 1) * kChunkUnit < rows.wave_sees) {
+        Form::before_values(rows, p, Form::known(word_before), (j0 + k - 1) * kChunkUnit);
         rows.values(ring[(k - 1) % kWideStages] + TILE / 2, p);
         Form::poison(rows, Form::any_bad(word_before), a.poison + (tile0 + k - 1) * (Form::Tile::NG * 64), Form::known(word_before), (j0 + k - 1) * kChunkUnit);
       }
