@@ -77,3 +77,11 @@ def test_only_the_rings_copies_use_m0(assembly):
             assert inside, (kernel, line)
             rings.add(kernel)
     assert len(rings) == 2 and all("cache8_wide_kernel" in k for k in rings), rings
+
+
+def test_what_is_spilled_does_not_grow(kernels):
+    """Of heads of 64 the kernel whose keys are unpacked beforehand holds 128 registers for two workgroups a CU, and 29 words of a lane in scratch."""
+    for k in _pick(kernels, "cache8_wide_kernel", "ILi64E"):
+        assert k["scratch"] <= 116, k
+    for k in _pick(kernels, "cache8_short_kernel"):
+        assert k["scratch"] == 0 and k["vgpr"] <= 256 and 2 * k["lds"] <= 160 * 1024, k
