@@ -66,6 +66,8 @@
 extern "C" {
 #endif
 
+/* (Set it to zeros before filling it in, and compile against the header of the library that is called: `block` came behind the other fields, and a
+ * program that fills those one by one or was built without it leaves it undefined.  Zero is the format of 4 bits.) */
 typedef struct sagebwd_cache_params {
   int32_t H;      /* key/value heads */
   int32_t d;      /* 64 or 128 */
@@ -130,7 +132,8 @@ int sagebwd_cache_trim(const int32_t* keep, int32_t* lengths, int32_t* block_tab
  * own: before tokens are added (before plan).  A request with added[r] > 0 whose last page is not full and has other holders gets a page of
  * its own with the same bytes, from the stack, and the table names that; if all holders of a page are such requests the last of them
  * keeps it.  Requests are served in order: behind one for which no page is left none gets one.  added_out int32 [R] (may be `added`): added[r], or 0
- * where a page was wanted and not got: that request must not add tokens, and plan then grants it none.
+ * where a page was wanted and not got, and behind such a request also for the last holder that would have kept its page: a request
+ * with 0 must not add tokens, and plan then grants it none.
  *
  * compact: moves the pages in use (those that a request's row names for its length) to 0 .. used - 1: pages from used on are copied to
  * unused ones below, in the order of their numbers, the others stay.  Out: table_out (may be `block_table`; entries behind a
@@ -195,7 +198,8 @@ typedef struct sagebwd_cache_call {
  * Where max_new tokens are up to 32 query rows (new tokens x Hq / H) all requests go to a kernel for few rows, else to one for many; but where
  * T is less than R * max_new and Hq / H at most 32 the call launches both, and requests of up to 16 rows (32, where Hq / H is more than 16) go
  * to the former.  Held in 8 bits the kernel for few rows takes up to 128, in tiles of 16 to 64 rows with a pass over the keys each (32 where R * H *
- * (max_length / 128 + 3) passes 2^27), beside requests of more rows too; short requests have a wave each.  A tile of tokens on a page that does not exist is passed over by the kernel for few rows and masked by the others.
+ * (max_length / 128 + 3) passes 2^27), beside requests of more rows too, unless the call is small (R * H * max_length / 64 up to 512: all of its
+ * requests go to the kernel for many then); short requests have a wave each.  A tile of tokens on a page that does not exist is passed over by the kernel for few rows and masked by the others.
  * Where a call has few items for the machine their keys are divided over it and the parts joined by a further launch; from 2048 rows a request on, keys and values are
  * unpacked to bf16 in the workspace first (256 d bytes for 64 tokens and head; at most 4 GiB, else each tile unpacks its own).  How
  * work is divided depends on all requests of the call, so that O agrees between calls of different batches to its rounding, and bit

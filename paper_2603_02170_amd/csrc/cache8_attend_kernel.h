@@ -328,6 +328,9 @@ struct ByteChunk {
   }
 };
 
+// The probabilities are rounded to bf16, once: the matrix pipe bounds these calls, and a product of what that leaves, as tiles of few rows have, takes a
+// third and more (2048 new tokens against 10000 307 -> 415 us, heads of 64 210 -> 317; four of 5000 with 300 130 -> 163) for an error of O of 0.0017 in
+// place of 0.0024.
 template <int D>
 struct ByteChunkRows : ChunkRows<D> {
   typedef ChunkRows<D> Base;

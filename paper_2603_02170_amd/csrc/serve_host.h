@@ -45,12 +45,9 @@ constexpr int kCus = 256;
 // Query rows of a request and head that cache_attend_kernel takes (32 requests of 4096 tokens, 32 rows: 59 us, the kernel for many rows 135; 64 rows in
 // four tiles a wave, which its registers do not hold at d = 128, 206).
 constexpr int kFewRows = 32;
-// Query rows of a request and head at most, keys of a request at most, and the rows of a workgroup of the kernel for many.  cache_span_kernel has 64 or
-// 128 and unpacks 256 or 128 tokens at a time (tiles of 256 rows -> these, us: 32 requests of 4096 tokens, 64 rows 123 -> 87, 128 rows 126 ->
-// 107; 64 of 40 rows, 1000 tokens, 60 -> 46; four requests of 64 tokens 15 -> 19; 65 to 128 rows as two tiles of 64 188, 256 as two of 128, 3000
-// tokens, 79 -> 93).
 // Of a cache held in 8 bits: rows in several tiles of 32, each a pass over the keys, while the line that they are dealt out on holds them.
 constexpr int kTiledRows = 128;
+// Query rows of a request and head at most, and its keys.
 inline int64_t most_rows(const sagebwd_cache_params& p, const sagebwd_cache_call& c) { return (int64_t)(c.max_new < c.T ? c.max_new : c.T) * (c.Hq / p.H); }
 inline int most_length(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
   const int64_t all = (int64_t)c.columns * p.page;
@@ -68,6 +65,9 @@ inline int few_rows_of(const sagebwd_cache_params& p, const sagebwd_cache_call& 
   const int64_t line = (int64_t)c.R * p.H * (kTiledRows / 32) * ((most_length(p, c) + kUnit - 1) / kUnit + kItemCost);
   return p.block > 0 && line <= 1 << 29 ? kTiledRows : kFewRows;
 }
+// The rows of a workgroup of the kernel for many.  Of a cache held in 4 bits cache_span_kernel has 64 or 128 and unpacks 256 or 128 tokens at a time (tiles of
+// 256 rows -> these, us: 32 requests of 4096 tokens, 64 rows 123 -> 87, 128 rows 126 -> 107; 64 of 40 rows, 1000 tokens, 60 -> 46; four requests of 64
+// tokens 15 -> 19; 65 to 128 rows as two tiles of 64 188, 256 as two of 128, 3000 tokens, 79 -> 93).
 inline int tile_rows_of(const sagebwd_cache_params& p, const sagebwd_cache_call& c) {
   const int64_t most = most_rows(p, c);
   return p.block > 0 || most > 128 || most_length(p, c) <= 256 ? kChunkRows : most > 64 ? 128 : 64;
